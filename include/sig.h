@@ -356,6 +356,102 @@ int sig_backward_windows(const sig_wordset* ws, const float* path, const float* 
 int sig_leadlag_transform(const float* path, int64_t B, int64_t n_points, int d, float* out, void* stream);
 int sig_leadlag_backward(const float* grad_out, int64_t B, int64_t n_points, int d, float* grad_path, void* stream);
 
+/* ---- sequence operators -----------------------------------------------------------------------------------
+ * What a model over a sequence of signature tokens (e.g. the windows of a path, [B, K, |W|], projected to D channels) is made of: a short
+ * causal convolution over time, a selective state space scan, their gradients and their single-token forms for streams, and the
+ * clipping of a model's gradients by their global norm.
+ *
+ * Conventions beyond those at the top: tokens are channels last.  `dtype` is the type of tokens and of their gradients, SIG_F32 or
+ * SIG_BF16; parameters, recurrent states and their gradients are float32, and so is all arithmetic.  Inputs with strides give them in
+ * elements for batch and time (0 is allowed: a broadcast input); their channels are contiguous.  Outputs are contiguous, and no output
+ * overlaps an input unless stated.  Nothing has to be aligned beyond its type; rows whose addresses are multiples of 16 bytes get
+ * the widest accesses.  lengths: device int32 [B] or NULL (all L); clamped to [0, L].  Tokens from lengths[b] on are not read: they give
+ * outputs and gradients of zero and leave states as they are.  Calls only enqueue kernels on `stream`; two calls on the same inputs give
+ * the same bits.  B == 0 is a no-op (gradients of parameters are set to zero), L == 0 is allowed: a final state is the initial one. */
+#define SIG_F32  0
+#define SIG_BF16 1
+
+#define SIG_MAX_CONV_WIDTH  8
+#define SIG_MAX_SCAN_STATES 64
+
+/* Causal depthwise convolution: y_t = f(bias + sum_k weight[., k] x_(t - W + 1 + k)), k = 0 .. W - 1 <= SIG_MAX_CONV_WIDTH - 1,
+ * f(s) = s sigmoid(s) (silu = 1) or s (silu = 0).  Tokens before the first are those of initial_state, oldest first (NULL: zeros). */
+typedef struct sig_conv_args {
+    int64_t dtype, B, L, D, W, silu;
+    int64_t x_stride_b, x_stride_t;
+    const void* x;                  /* device dtype [B, L, D] */
+    const float* weight;            /* device [D, W] */
+    const float* bias;              /* device [D] or NULL */
+    const void* initial_state;      /* device dtype [B, W - 1, D] or NULL */
+    const int32_t* lengths;         /* device [B] or NULL */
+} sig_conv_args;
+/* final_state: dtype [B, W - 1, D] or NULL, receives the last W - 1 tokens before lengths[b] (those of initial_state among them). */
+int    sig_conv_forward(const sig_conv_args* args, void* y, void* final_state, void* stream);
+/* grad_y [B, L, D] with strides of its own, grad_final_state or NULL -> grad_x [B, L, D], grad_weight [D, W], grad_bias [D] or NULL,
+ * grad_initial_state [B, W - 1, D] or NULL; all overwritten. */
+size_t sig_conv_backward_workspace_bytes(const sig_conv_args* args);
+int    sig_conv_backward(const sig_conv_args* args, const void* grad_y, int64_t gy_stride_b, int64_t gy_stride_t,
+                         const void* grad_final_state, void* grad_x, float* grad_weight, float* grad_bias,
+                         void* grad_initial_state, void* workspace, size_t workspace_bytes, void* stream);
+/* One token of every stream: x [B, D] (x_stride_b; L, x_stride_t, initial_state and lengths are not looked at), state dtype
+ * [B, W - 1, D] is shifted by it in place. */
+int    sig_conv_step(const sig_conv_args* args, void* state, void* y, void* stream);
+
+/* Selective state space scan over N <= SIG_MAX_SCAN_STATES states a channel, channel d using B and C of group d / (D / G):
+ *   delta_t = softplus(dt_t + dt_bias) (softplus = 1) or dt_t + dt_bias (softplus = 0),
+ *   h_t = exp(delta_t A) h_(t-1) + delta_t x_t b_t,   y_t = (sum_n c_t h_t + skip x_t) f_t,   f_t = gate_t sigmoid(gate_t), or 1 without gate. */
+typedef struct sig_scan_args {
+    int64_t dtype, B, L, D, G, N, softplus;
+    int64_t x_stride_b, x_stride_t, dt_stride_b, dt_stride_t, gate_stride_b, gate_stride_t;
+    int64_t b_stride_b, b_stride_t, b_stride_g, c_stride_b, c_stride_t, c_stride_g;
+    const void* x;                  /* device dtype [B, L, D] */
+    const void* dt;                 /* device dtype [B, L, D] */
+    const void* gate;               /* device dtype [B, L, D] or NULL */
+    const void* b;                  /* device dtype [B, L, G, N], states contiguous */
+    const void* c;                  /* device dtype [B, L, G, N], states contiguous */
+    const float* A;                 /* device [D, N] */
+    const float* skip;              /* device [D] or NULL */
+    const float* dt_bias;           /* device [D] or NULL */
+    const float* initial_state;     /* device [B, D, N] or NULL (zeros) */
+    const int32_t* lengths;         /* device [B] or NULL */
+} sig_scan_args;
+/* y dtype [B, L, D]; final_state [B, D, N] or NULL; checkpoint: NULL, or sig_scan_checkpoint_bytes bytes for sig_scan_backward (states
+ * every 16 tokens), the caller's to keep until then. */
+size_t sig_scan_checkpoint_bytes(const sig_scan_args* args);
+size_t sig_scan_forward_workspace_bytes(const sig_scan_args* args);
+int    sig_scan_forward(const sig_scan_args* args, void* y, float* final_state, void* checkpoint, size_t checkpoint_bytes,
+                        void* workspace, size_t workspace_bytes, void* stream);
+/* Gradients of the inputs of the same name; those of tokens in dtype and contiguous.  grad_gate, grad_skip and grad_dt_bias may be NULL
+ * where the input is, grad_initial_state always. */
+typedef struct sig_scan_grads {
+    int64_t gy_stride_b, gy_stride_t;
+    const void* grad_y;             /* device dtype [B, L, D] */
+    const float* grad_final_state;  /* device [B, D, N] or NULL */
+    void* grad_x;
+    void* grad_dt;
+    void* grad_gate;
+    void* grad_b;
+    void* grad_c;
+    float* grad_A;
+    float* grad_skip;
+    float* grad_dt_bias;
+    float* grad_initial_state;
+} sig_scan_grads;
+size_t sig_scan_backward_workspace_bytes(const sig_scan_args* args);
+int    sig_scan_backward(const sig_scan_args* args, const sig_scan_grads* grads, const void* checkpoint, size_t checkpoint_bytes,
+                         void* workspace, size_t workspace_bytes, void* stream);
+/* One token of every stream: x, dt, gate [B, D], b, c [B, G, N], y [B, D]; state float32 [B, D, N] is updated in place (L, time strides,
+ * initial_state and lengths are not looked at). */
+int    sig_scan_step(const sig_scan_args* args, float* state, void* y, void* stream);
+
+/* Global 2-norm over n_tensors tensors and their products with min(1, max_norm / (norm + 1e-6)).  in, out, sizes, in_dtypes, out_dtypes:
+ * host arrays of n_tensors entries (device pointers, elements, SIG_F32 / SIG_BF16), read before the call returns; tensors are
+ * contiguous, out[k] may be in[k] (the same type then) and overlaps nothing else.  norm: device float32.  Squares are summed in float64.
+ * A NaN among the inputs makes norm and all outputs NaN; an infinity makes the norm infinite, the infinite entries NaN and the others 0. */
+size_t sig_grad_clip_workspace_bytes(int64_t n_tensors, const int64_t* sizes);
+int    sig_grad_clip(int64_t n_tensors, const void* const* in, void* const* out, const int64_t* sizes, const int64_t* in_dtypes,
+                     const int64_t* out_dtypes, float max_norm, float* norm, void* workspace, size_t workspace_bytes, void* stream);
+
 /* ---- kernel timer ----------------------------------------------------------------------------------------
  * For benchmarks: while enabled, sig_forward / sig_backward record two HIP event pairs on the caller's stream:
  * one around their main kernel (the hot loop over segments) and one around everything the call enqueues (with

@@ -9,3 +9,5 @@ from .binding import (SigError, WindowPlan, WordSet, lib_path, load_library, sig
                       sig_leadlag_backward, sig_leadlag_transform, sig_logsig_backward, sig_logsig_forward,
                       sig_wordset_build_logsig, sig_wordset_build, sig_wordset_build_anisotropic,
                       sig_wordset_build_graph, sig_wordset_build_leadlag_sparse, sig_wordset_build_truncated)
+from .sequence import (sig_conv_backward, sig_conv_forward, sig_conv_step, sig_grad_clip, sig_scan_backward, sig_scan_forward,  # noqa: F401
+                       sig_scan_step)

@@ -112,6 +112,18 @@ def load_library():
     sig("sig_probe_fma", c_int, [c_p, c_sz, c_int, c_int, c_p])
     sig("sig_probe_issue", c_int, [c_p, c_sz, c_int, c_int, c_int, c_p])
     sig("sig_jit_launch_shape_ok", c_int, [c_int, c_int, c_int, c_int])
+    sig("sig_conv_forward", c_int, [c_p, c_p, c_p, c_p])
+    sig("sig_conv_backward_workspace_bytes", c_sz, [c_p])
+    sig("sig_conv_backward", c_int, [c_p, c_p, c_i64, c_i64, c_p, c_p, c_p, c_p, c_p, c_p, c_sz, c_p])
+    sig("sig_conv_step", c_int, [c_p, c_p, c_p, c_p])
+    sig("sig_scan_checkpoint_bytes", c_sz, [c_p])
+    sig("sig_scan_forward_workspace_bytes", c_sz, [c_p])
+    sig("sig_scan_forward", c_int, [c_p, c_p, c_p, c_p, c_sz, c_p, c_sz, c_p])
+    sig("sig_scan_backward_workspace_bytes", c_sz, [c_p])
+    sig("sig_scan_backward", c_int, [c_p, c_p, c_p, c_sz, c_p, c_sz, c_p])
+    sig("sig_scan_step", c_int, [c_p, c_p, c_p, c_p])
+    sig("sig_grad_clip_workspace_bytes", c_sz, [c_i64, c_p])
+    sig("sig_grad_clip", c_int, [c_i64, c_p, c_p, c_p, c_p, c_p, ctypes.c_float, c_p, c_p, c_sz, c_p])
     _lib = lib
     return lib
 

@@ -13,6 +13,7 @@
 #include "../../include/sig.h"
 #include "jit.hpp"
 #include "kernels.hpp"
+#include "seq.hpp"
 #include "wordset.hpp"
 
 struct sig_wordset : public sig::WordSet {};
@@ -25,6 +26,9 @@ int hip_fail(hipError_t e)
     g_last_hip = (int)e;
     return SIG_EHIP;
 }
+}  // namespace
+int sig::record_hip_error(hipError_t e) { return hip_fail(e); }
+namespace {
 
 const sig::WordSet* W(const sig_wordset* ws) { return ws; }
 

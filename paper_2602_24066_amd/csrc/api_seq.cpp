@@ -1,0 +1,180 @@
+// C ABI of the sequence operators: checks of arguments, then the launches (see include/sig.h for the contracts).
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+
+#include "seq.hpp"
+
+namespace {
+
+constexpr int64_t kMost = (int64_t)1 << 40;       // bound of sizes and of their products: more than any memory holds, and no overflow below
+
+int hip_code(hipError_t e) { return e == hipSuccess ? SIG_OK : sig::record_hip_error(e); }
+
+bool bad_type(int64_t t) { return t != SIG_F32 && t != SIG_BF16; }
+
+// SIG_EINVAL for a negative size, SIG_ETOOLARGE where the product of the (non-negative) sizes passes kMost
+int check_sizes(std::initializer_list<int64_t> sizes)
+{
+    int64_t p = 1;
+    for (int64_t v : sizes)
+        if (v < 0) return SIG_EINVAL;
+    for (int64_t v : sizes) {
+        if (v > kMost || (v && p > kMost / v)) return SIG_ETOOLARGE;
+        p *= std::max<int64_t>(v, 1);
+    }
+    return SIG_OK;
+}
+
+int check_conv(const sig_conv_args* a)
+{
+    if (!a || bad_type(a->dtype) || a->D < 1 || a->W < 1) return SIG_EINVAL;
+    if (a->W > SIG_MAX_CONV_WIDTH) return SIG_EUNSUPPORTED;
+    if (a->silu != 0 && a->silu != 1) return SIG_EINVAL;
+    return check_sizes({a->B, a->L, a->D});
+}
+
+int check_scan(const sig_scan_args* a)
+{
+    if (!a || bad_type(a->dtype) || a->D < 1 || a->G < 1 || a->N < 1 || a->D % a->G != 0) return SIG_EINVAL;
+    if (a->N > SIG_MAX_SCAN_STATES) return SIG_EUNSUPPORTED;
+    if (a->softplus != 0 && a->softplus != 1) return SIG_EINVAL;
+    return check_sizes({a->B, a->L, a->D, a->N});
+}
+
+bool scan_inputs_there(const sig_scan_args& a, bool tokens)
+{
+    return a.A && (!tokens || (a.x && a.dt && a.b && a.c));
+}
+
+size_t ckpt_bytes(const sig_scan_args& a) { return (size_t)(a.B * ((a.L + sig::kScanTile - 1) / sig::kScanTile) * a.D * a.N * 4); }
+
+}  // namespace
+
+extern "C" {
+
+int sig_conv_forward(const sig_conv_args* a, void* y, void* final_state, void* stream)
+{
+    int rc = check_conv(a);
+    if (rc != SIG_OK || a->B == 0) return rc;
+    if (!a->weight || (a->L && (!a->x || !y))) return SIG_EINVAL;
+    return hip_code(sig::conv_forward(*a, y, final_state, (hipStream_t)stream));
+}
+
+size_t sig_conv_backward_workspace_bytes(const sig_conv_args* a) { return check_conv(a) == SIG_OK ? sig::conv_backward_workspace(*a) : 0; }
+
+int sig_conv_backward(const sig_conv_args* a, const void* grad_y, int64_t gy_stride_b, int64_t gy_stride_t, const void* grad_final_state,
+                      void* grad_x, float* grad_weight, float* grad_bias, void* grad_initial_state, void* workspace, size_t workspace_bytes,
+                      void* stream)
+{
+    int rc = check_conv(a);
+    if (rc != SIG_OK) return rc;
+    if (!a->weight || !grad_weight || (a->B && a->L && (!a->x || !grad_y || !grad_x))) return SIG_EINVAL;
+    if (workspace_bytes < sig::conv_backward_workspace(*a) || (!workspace && sig::conv_backward_workspace(*a))) return SIG_EWORKSPACE;
+    sig::ConvGrads g{grad_y, gy_stride_b, gy_stride_t, grad_final_state, grad_x, grad_weight, grad_bias, grad_initial_state};
+    return hip_code(sig::conv_backward(*a, g, (float*)workspace, (hipStream_t)stream));
+}
+
+int sig_conv_step(const sig_conv_args* a, void* state, void* y, void* stream)
+{
+    int rc = check_conv(a);
+    if (rc != SIG_OK || a->B == 0) return rc;
+    if (!a->weight || !a->x || !y || (a->W > 1 && !state)) return SIG_EINVAL;
+    return hip_code(sig::conv_step(*a, state, y, (hipStream_t)stream));
+}
+
+size_t sig_scan_checkpoint_bytes(const sig_scan_args* a) { return check_scan(a) == SIG_OK ? ckpt_bytes(*a) : 0; }
+size_t sig_scan_forward_workspace_bytes(const sig_scan_args* a) { return check_scan(a) == SIG_OK ? sig::scan_forward_workspace(*a) : 0; }
+size_t sig_scan_backward_workspace_bytes(const sig_scan_args* a) { return check_scan(a) == SIG_OK ? sig::scan_backward_workspace(*a) : 0; }
+
+int sig_scan_forward(const sig_scan_args* a, void* y, float* final_state, void* checkpoint, size_t checkpoint_bytes, void* workspace,
+                     size_t workspace_bytes, void* stream)
+{
+    int rc = check_scan(a);
+    if (rc != SIG_OK || a->B == 0) return rc;
+    if (!scan_inputs_there(*a, a->L > 0) || (a->L && !y)) return SIG_EINVAL;
+    if (checkpoint && checkpoint_bytes < ckpt_bytes(*a)) return SIG_EWORKSPACE;
+    size_t need = sig::scan_forward_workspace(*a);
+    if (workspace_bytes < need || (need && !workspace)) return SIG_EWORKSPACE;
+    return hip_code(sig::scan_forward(*a, y, final_state, (float*)checkpoint, (float*)workspace, (hipStream_t)stream));
+}
+
+int sig_scan_backward(const sig_scan_args* a, const sig_scan_grads* g, const void* checkpoint, size_t checkpoint_bytes, void* workspace,
+                      size_t workspace_bytes, void* stream)
+{
+    int rc = check_scan(a);
+    if (rc != SIG_OK) return rc;
+    bool tokens = a->B > 0 && a->L > 0;
+    if (!g || !g->grad_A || !scan_inputs_there(*a, tokens)) return SIG_EINVAL;
+    if ((a->skip && !g->grad_skip) || (a->dt_bias && !g->grad_dt_bias)) return SIG_EINVAL;
+    if (tokens && (!g->grad_y || !g->grad_x || !g->grad_dt || !g->grad_b || !g->grad_c || (a->gate && !g->grad_gate))) return SIG_EINVAL;
+    if (checkpoint_bytes < ckpt_bytes(*a) || (tokens && !checkpoint)) return SIG_EWORKSPACE;
+    size_t need = sig::scan_backward_workspace(*a);
+    if (workspace_bytes < need || (need && !workspace)) return SIG_EWORKSPACE;
+    return hip_code(sig::scan_backward(*a, *g, (const float*)checkpoint, (float*)workspace, (hipStream_t)stream));
+}
+
+int sig_scan_step(const sig_scan_args* a, float* state, void* y, void* stream)
+{
+    int rc = check_scan(a);
+    if (rc != SIG_OK || a->B == 0) return rc;
+    if (!scan_inputs_there(*a, true) || !state || !y) return SIG_EINVAL;
+    return hip_code(sig::scan_step(*a, state, y, (hipStream_t)stream));
+}
+
+size_t sig_grad_clip_workspace_bytes(int64_t n_tensors, const int64_t* sizes)
+{
+    if (n_tensors <= 0 || !sizes) return 0;
+    int64_t blocks = 0;
+    for (int64_t i = 0; i < n_tensors; i++) {
+        if (sizes[i] < 0 || sizes[i] > kMost) return 0;
+        blocks += (sizes[i] + sig::kClipBlock - 1) / sig::kClipBlock;
+    }
+    return (size_t)blocks * sizeof(double);
+}
+
+int sig_grad_clip(int64_t n_tensors, const void* const* in, void* const* out, const int64_t* sizes, const int64_t* in_dtypes,
+                  const int64_t* out_dtypes, float max_norm, float* norm, void* workspace, size_t workspace_bytes, void* stream)
+{
+    if (n_tensors < 0 || !norm || !(max_norm >= 0.0f)) return SIG_EINVAL;
+    if (n_tensors && (!in || !out || !sizes || !in_dtypes || !out_dtypes)) return SIG_EINVAL;
+    int64_t blocks = 0;
+    for (int64_t i = 0; i < n_tensors; i++) {
+        if (sizes[i] < 0 || bad_type(in_dtypes[i]) || bad_type(out_dtypes[i])) return SIG_EINVAL;
+        if (sizes[i] && (!in[i] || !out[i] || (in[i] == out[i] && in_dtypes[i] != out_dtypes[i]))) return SIG_EINVAL;
+        if (sizes[i] > kMost) return SIG_ETOOLARGE;
+        blocks += (sizes[i] + sig::kClipBlock - 1) / sig::kClipBlock;
+        if (blocks > (1 << 23)) return SIG_ETOOLARGE;       // what a launch can number
+    }
+    if (workspace_bytes < (size_t)blocks * sizeof(double) || (blocks && !workspace)) return SIG_EWORKSPACE;
+    hipStream_t s = (hipStream_t)stream;
+    // all tables of the norm first, then its square root, then all tables of the products
+    for (int pass = 0; pass < 2; pass++) {
+        double* part = (double*)workspace;
+        sig::ClipTable tab;
+        tab.n = 0;
+        for (int64_t i = 0; i <= n_tensors; i++) {
+            if (i < n_tensors && sizes[i]) {
+                int k = tab.n++;
+                tab.in[k] = in[i];
+                tab.out[k] = out[i];
+                tab.size[k] = sizes[i];
+                tab.kind[k] = (uint8_t)(in_dtypes[i] | out_dtypes[i] << 1);
+                tab.end[k] = (k ? tab.end[k - 1] : 0) + (uint32_t)((sizes[i] + sig::kClipBlock - 1) / sig::kClipBlock);
+            }
+            if (tab.n == 0 || (tab.n < sig::kClipTensors && i < n_tensors)) continue;
+            hipError_t e = pass == 0 ? sig::norm_parts(tab, part, s) : sig::clip_scaled(tab, norm, max_norm, s);
+            if (e != hipSuccess) return sig::record_hip_error(e);
+            part += tab.end[tab.n - 1];
+            tab.n = 0;
+        }
+        if (pass == 0) {
+            hipError_t e = sig::norm_total((const double*)workspace, blocks, norm, s);
+            if (e != hipSuccess) return sig::record_hip_error(e);
+        }
+    }
+    return SIG_OK;
+}
+
+}  // extern "C"

@@ -1,0 +1,321 @@
+// Short causal convolution over time, a filter for each channel (depthwise), with an optional SiLU:
+//   s_t = bias + sum_k w[k] x_{t - W + 1 + k},   y_t = s_t sigmoid(s_t)  or  s_t,   k = 0 .. W - 1
+// and its gradient: g_t = dL/ds_t,  dL/dx_p = sum_k w[k] g_{p + W - 1 - k},  dL/dw[k] = sum_t g_t x_{t - W + 1 + k}.
+// Both directions are bound by memory: 2 W multiply-adds stand against 4 bytes (bf16) a token and channel.
+#include <algorithm>
+
+#include "seq.hpp"
+
+namespace sig {
+namespace {
+
+constexpr int kThreads = 256;
+
+// A thread walks one time chunk of V neighbouring channels with the last W tokens in registers, so a token is read once and (at
+// chunk starts) W - 1 tokens twice.  Threads of a wavefront are neighbours in the channel axis: their accesses are contiguous.
+struct Split {
+    int64_t chunk;       // tokens of a chunk
+    int64_t chunks;
+    int64_t vecs;        // groups of V channels
+    int64_t threads;
+};
+Split split_time(int64_t B, int64_t L, int64_t D, int V)
+{
+    Split s;
+    s.vecs = (D + V - 1) / V;
+    // two wavefronts on each SIMD (2,048 of 64 threads) hide the memory's latency here; chunks shorter than 16 tokens would
+    // read a fifth and more of their input twice
+    int64_t want = (int64_t)2048 * 64 / std::max<int64_t>(1, B * s.vecs) + 1;
+    s.chunk = std::max<int64_t>(16, (L + want - 1) / want);
+    s.chunks = std::max<int64_t>(1, (L + s.chunk - 1) / s.chunk);
+    s.threads = B * s.chunks * s.vecs;
+    return s;
+}
+
+template <class T, int V> __device__ __forceinline__ void load(float (&r)[V], const T* p)
+{
+    Pack<T, V> q = *(const Pack<T, V>*)p;
+#pragma unroll
+    for (int i = 0; i < V; i++) r[i] = to_float(q.v[i]);
+}
+template <class T, int V> __device__ __forceinline__ void store(T* p, const float (&r)[V])
+{
+    Pack<T, V> q;
+#pragma unroll
+    for (int i = 0; i < V; i++) q.v[i] = from_float<T>(r[i]);
+    *(Pack<T, V>*)p = q;
+}
+
+// token p of the sequence that starts W - 1 tokens before the first: the initial state, then x
+template <class T, int V, int W> __device__ __forceinline__ void load_token(float (&r)[V], const T* x, int64_t stride_t, const T* initial, int64_t D, int64_t p)
+{
+    if (p >= 0) {
+        load<T, V>(r, x + p * stride_t);
+    } else if (initial) {
+        load<T, V>(r, initial + (W - 1 + p) * D);
+    } else {
+#pragma unroll
+        for (int i = 0; i < V; i++) r[i] = 0.0f;
+    }
+}
+
+template <int V, int W> __device__ __forceinline__ void load_filter(float (&w)[W][V], float (&bias)[V], const sig_conv_args& a, int64_t d)
+{
+#pragma unroll
+    for (int i = 0; i < V; i++) {
+#pragma unroll
+        for (int k = 0; k < W; k++) w[k][i] = a.weight[(d + i) * W + k];
+        bias[i] = a.bias ? a.bias[d + i] : 0.0f;
+    }
+}
+
+template <class T, int V, int W>
+__global__ __launch_bounds__(kThreads) void conv_fwd_kernel(sig_conv_args a, T* y, T* final_state, Split s)
+{
+    int64_t id = (int64_t)blockIdx.x * kThreads + threadIdx.x;
+    if (id >= s.threads) return;
+    int64_t d = id % s.vecs * V, row = id / s.vecs, c = row % s.chunks, b = row / s.chunks;
+    const T* x = (const T*)a.x + b * a.x_stride_b + d;
+    const T* initial = a.initial_state ? (const T*)a.initial_state + b * (W - 1) * a.D + d : nullptr;
+    int64_t t0 = c * s.chunk, t1 = min(t0 + s.chunk, a.L), len = live_length(a.lengths, b, a.L);
+    y += (b * a.L + t0) * a.D + d;
+    float w[W][V], bias[V], r[W][V];
+    load_filter<V, W>(w, bias, a, d);
+    int64_t end = min(t1, len);
+    if (t0 < end) {
+#pragma unroll
+        for (int k = 0; k < W - 1; k++) load_token<T, V, W>(r[k + 1], x, a.x_stride_t, initial, a.D, t0 - W + 1 + k);
+    }
+    int64_t t = t0;
+    for (; t < end; t++, y += a.D) {
+#pragma unroll
+        for (int k = 0; k < W - 1; k++)
+#pragma unroll
+            for (int i = 0; i < V; i++) r[k][i] = r[k + 1][i];
+        load<T, V>(r[W - 1], x + t * a.x_stride_t);
+        float o[V];
+#pragma unroll
+        for (int i = 0; i < V; i++) {
+            o[i] = bias[i];
+#pragma unroll
+            for (int k = 0; k < W; k++) o[i] = fmaf(w[k][i], r[k][i], o[i]);
+            if (a.silu) o[i] *= sigmoid(o[i]);
+        }
+        store<T, V>(y, o);
+    }
+    float zero[V] = {};
+    for (; t < t1; t++, y += a.D) store<T, V>(y, zero);
+    if (final_state && c == 0) {
+        final_state += b * (W - 1) * a.D + d;
+#pragma unroll
+        for (int k = 0; k < W - 1; k++) {
+            float v[V];
+            load_token<T, V, W>(v, x, a.x_stride_t, initial, a.D, len - W + 1 + k);
+            store<T, V>(final_state + k * a.D, v);
+        }
+    }
+}
+
+// The gradient walks forward as well: at token t it has s_t from the window of x, g_t from it and the upstream gradient, and with the
+// last W of them the gradient of token t - W + 1.  A chunk goes W - 1 tokens past its end for the gradients of its last tokens.
+template <class T, int V, int W>
+__global__ __launch_bounds__(kThreads) void conv_bwd_kernel(sig_conv_args a, ConvGrads g, float* part, Split s)
+{
+    int64_t id = (int64_t)blockIdx.x * kThreads + threadIdx.x;
+    if (id >= s.threads) return;
+    int64_t d = id % s.vecs * V, row = id / s.vecs, c = row % s.chunks, b = row / s.chunks;
+    const T* x = (const T*)a.x + b * a.x_stride_b + d;
+    const T* gy = (const T*)g.grad_y + b * g.gy_stride_b + d;
+    const T* initial = a.initial_state ? (const T*)a.initial_state + b * (W - 1) * a.D + d : nullptr;
+    const T* gf = g.grad_final ? (const T*)g.grad_final + b * (W - 1) * a.D + d : nullptr;
+    T* gi = g.grad_initial ? (T*)g.grad_initial + b * (W - 1) * a.D + d : nullptr;
+    T* gx = (T*)g.grad_x + b * a.L * a.D + d;
+    int64_t t0 = c * s.chunk, t1 = min(t0 + s.chunk, a.L), len = live_length(a.lengths, b, a.L);
+    float w[W][V], bias[V], r[W][V] = {}, h[W][V] = {}, gw[W + 1][V] = {};
+    load_filter<V, W>(w, bias, a, d);
+    if (t0 < len) {
+#pragma unroll
+        for (int k = 0; k < W - 1; k++) load_token<T, V, W>(r[k + 1], x, a.x_stride_t, initial, a.D, t0 - W + 1 + k);
+    }
+    for (int64_t t = t0; t < t1 + W - 1; t++) {
+#pragma unroll
+        for (int k = 0; k < W - 1; k++)
+#pragma unroll
+            for (int i = 0; i < V; i++) r[k][i] = r[k + 1][i], h[k][i] = h[k + 1][i];
+        if (t < len) {
+            load<T, V>(r[W - 1], x + t * a.x_stride_t);
+            load<T, V>(h[W - 1], gy + t * g.gy_stride_t);
+#pragma unroll
+            for (int i = 0; i < V; i++) {
+                if (a.silu) {
+                    float o = bias[i];
+#pragma unroll
+                    for (int k = 0; k < W; k++) o = fmaf(w[k][i], r[k][i], o);
+                    float p = sigmoid(o);
+                    h[W - 1][i] *= p * fmaf(o, 1.0f - p, 1.0f);
+                }
+                if (t < t1) {
+#pragma unroll
+                    for (int k = 0; k < W; k++) gw[k][i] = fmaf(h[W - 1][i], r[k][i], gw[k][i]);
+                    gw[W][i] += h[W - 1][i];
+                }
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < V; i++) h[W - 1][i] = 0.0f;
+        }
+        int64_t p = t - W + 1;
+        if (p < (c == 0 ? -(int64_t)(W - 1) : t0)) continue;
+        if (p < 0 && !gi) continue;
+        float o[V];
+#pragma unroll
+        for (int i = 0; i < V; i++) {
+            o[i] = 0.0f;
+#pragma unroll
+            for (int k = 0; k < W; k++) o[i] = fmaf(w[k][i], h[W - 1 - k][i], o[i]);
+        }
+        if (gf && p < len && p >= len - (W - 1)) {
+            float v[V];
+            load<T, V>(v, gf + (p - len + W - 1) * a.D);
+#pragma unroll
+            for (int i = 0; i < V; i++) o[i] += v[i];
+        }
+        store<T, V>(p >= 0 ? gx + p * a.D : gi + (W - 1 + p) * a.D, o);
+    }
+    part += row * (W + 1) * a.D + d;
+#pragma unroll
+    for (int k = 0; k <= W; k++)
+#pragma unroll
+        for (int i = 0; i < V; i++) part[k * a.D + i] = gw[k][i];
+}
+
+// sums the chunks' filter gradients part[rows][W + 1][D] in a fixed order
+template <int W> __global__ __launch_bounds__(kThreads) void conv_bwd_sum_kernel(const float* part, int64_t rows, int64_t D, float* gw, float* gb)
+{
+    int64_t id = (int64_t)blockIdx.x * kThreads + threadIdx.x;
+    if (id >= (W + 1) * D) return;
+    float v = 0.0f;
+    for (int64_t r = 0; r < rows; r++) v += part[r * (W + 1) * D + id];
+    int64_t k = id / D, d = id % D;
+    if (k < W) gw[d * W + k] = v;
+    else if (gb) gb[d] = v;
+}
+
+template <class T, int V, int W> __global__ __launch_bounds__(kThreads) void conv_step_kernel(sig_conv_args a, T* state, T* y, int64_t vecs)
+{
+    int64_t id = (int64_t)blockIdx.x * kThreads + threadIdx.x;
+    if (id >= a.B * vecs) return;
+    int64_t d = id % vecs * V, b = id / vecs;
+    state += b * (W - 1) * a.D + d;
+    float w[W][V], bias[V], r[W][V], o[V];
+    load_filter<V, W>(w, bias, a, d);
+#pragma unroll
+    for (int k = 0; k < W - 1; k++) load<T, V>(r[k], state + k * a.D);
+    load<T, V>(r[W - 1], (const T*)a.x + b * a.x_stride_b + d);
+#pragma unroll
+    for (int k = 0; k < W - 1; k++) store<T, V>(state + k * a.D, r[k + 1]);
+#pragma unroll
+    for (int i = 0; i < V; i++) {
+        o[i] = bias[i];
+#pragma unroll
+        for (int k = 0; k < W; k++) o[i] = fmaf(w[k][i], r[k][i], o[i]);
+        if (a.silu) o[i] *= sigmoid(o[i]);
+    }
+    store<T, V>(y + b * a.D + d, o);
+}
+
+// V channels in one access need rows that start at multiples of its size
+bool aligned_rows(const void* p, int64_t stride_b, int64_t stride_t, int64_t D, int V, int bytes)
+{
+    return ((uintptr_t)p % (V * bytes)) == 0 && stride_b % V == 0 && stride_t % V == 0 && D % V == 0;
+}
+
+unsigned blocks_for(int64_t threads) { return (unsigned)((threads + kThreads - 1) / kThreads); }
+
+template <class F> hipError_t with_width(int64_t W, F f)
+{
+    switch (W) {
+        case 1: return f(std::integral_constant<int, 1>());
+        case 2: return f(std::integral_constant<int, 2>());
+        case 3: return f(std::integral_constant<int, 3>());
+        case 4: return f(std::integral_constant<int, 4>());
+        case 5: return f(std::integral_constant<int, 5>());
+        case 6: return f(std::integral_constant<int, 6>());
+        case 7: return f(std::integral_constant<int, 7>());
+        default: return f(std::integral_constant<int, 8>());
+    }
+}
+
+constexpr int wide(const float*) { return 4; }
+constexpr int wide(const bf16*) { return 8; }
+
+template <class T> hipError_t forward(const sig_conv_args& a, T* y, T* fin, hipStream_t stream)
+{
+    constexpr int V = wide((T*)nullptr);
+    bool vec = aligned_rows(a.x, a.x_stride_b, a.x_stride_t, a.D, V, sizeof(T)) && aligned_rows(y, 0, 0, a.D, V, sizeof(T)) &&
+               aligned_rows(a.initial_state, 0, 0, a.D, V, sizeof(T)) && aligned_rows(fin, 0, 0, a.D, V, sizeof(T));
+    Split s = split_time(a.B, a.L, a.D, vec ? V : 1);
+    return with_width(a.W, [&](auto w) {
+        constexpr int W = decltype(w)::value;
+        if (vec) conv_fwd_kernel<T, V, W><<<blocks_for(s.threads), kThreads, 0, stream>>>(a, y, fin, s);
+        else conv_fwd_kernel<T, 1, W><<<blocks_for(s.threads), kThreads, 0, stream>>>(a, y, fin, s);
+        return hipGetLastError();
+    });
+}
+
+template <class T> hipError_t backward(const sig_conv_args& a, const ConvGrads& g, float* part, hipStream_t stream)
+{
+    constexpr int V = wide((T*)nullptr) / 2;     // 8 bytes: the two windows and the filter's sums of more channels would not fit the registers
+    bool vec = aligned_rows(a.x, a.x_stride_b, a.x_stride_t, a.D, V, sizeof(T)) && aligned_rows(g.grad_y, g.gy_stride_b, g.gy_stride_t, a.D, V, sizeof(T)) &&
+               aligned_rows(g.grad_x, 0, 0, a.D, V, sizeof(T)) && aligned_rows(a.initial_state, 0, 0, a.D, V, sizeof(T)) &&
+               aligned_rows(g.grad_final, 0, 0, a.D, V, sizeof(T)) && aligned_rows(g.grad_initial, 0, 0, a.D, V, sizeof(T));
+    Split s = split_time(a.B, a.L, a.D, vec ? V : 1);
+    return with_width(a.W, [&](auto w) {
+        constexpr int W = decltype(w)::value;
+        if (a.B == 0) {}     // the sums below are zero
+        else if (vec) conv_bwd_kernel<T, V, W><<<blocks_for(s.threads), kThreads, 0, stream>>>(a, g, part, s);
+        else conv_bwd_kernel<T, 1, W><<<blocks_for(s.threads), kThreads, 0, stream>>>(a, g, part, s);
+        conv_bwd_sum_kernel<W><<<blocks_for((W + 1) * a.D), kThreads, 0, stream>>>(part, a.B * s.chunks, a.D, g.grad_weight, g.grad_bias);
+        return hipGetLastError();
+    });
+}
+
+template <class T> hipError_t step(const sig_conv_args& a, T* state, T* y, hipStream_t stream)
+{
+    constexpr int V = wide((T*)nullptr) / 4;
+    bool vec = aligned_rows(a.x, a.x_stride_b, 0, a.D, V, sizeof(T)) && aligned_rows(state, 0, 0, a.D, V, sizeof(T)) && aligned_rows(y, 0, 0, a.D, V, sizeof(T));
+    int64_t vecs = vec ? a.D / V : a.D;
+    return with_width(a.W, [&](auto w) {
+        constexpr int W = decltype(w)::value;
+        if (vec) conv_step_kernel<T, V, W><<<blocks_for(a.B * vecs), kThreads, 0, stream>>>(a, state, y, vecs);
+        else conv_step_kernel<T, 1, W><<<blocks_for(a.B * vecs), kThreads, 0, stream>>>(a, state, y, vecs);
+        return hipGetLastError();
+    });
+}
+
+}  // namespace
+
+hipError_t conv_forward(const sig_conv_args& a, void* y, void* final_state, hipStream_t stream)
+{
+    return a.dtype == SIG_BF16 ? forward<bf16>(a, (bf16*)y, (bf16*)final_state, stream) : forward<float>(a, (float*)y, (float*)final_state, stream);
+}
+
+size_t conv_backward_workspace(const sig_conv_args& a)
+{
+    // either split of the channels into accesses may be taken, the addresses decide
+    int V = a.dtype == SIG_BF16 ? 4 : 2;
+    int64_t rows = a.B * std::max(split_time(a.B, a.L, a.D, V).chunks, split_time(a.B, a.L, a.D, 1).chunks);
+    return (size_t)(rows * (a.W + 1) * a.D * 4);
+}
+
+hipError_t conv_backward(const sig_conv_args& a, const ConvGrads& g, float* workspace, hipStream_t stream)
+{
+    return a.dtype == SIG_BF16 ? backward<bf16>(a, g, workspace, stream) : backward<float>(a, g, workspace, stream);
+}
+
+hipError_t conv_step(const sig_conv_args& a, void* state, void* y, hipStream_t stream)
+{
+    return a.dtype == SIG_BF16 ? step<bf16>(a, (bf16*)state, (bf16*)y, stream) : step<float>(a, (float*)state, (float*)y, stream);
+}
+
+}  // namespace sig
