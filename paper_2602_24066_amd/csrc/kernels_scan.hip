@@ -8,6 +8,9 @@
 //   dA = sum_{b,t} l_t a_t h_{t-1} D_t,             dgate_t = dL/dy_t s_t silu'(gate_t),          dh_0 = a_1 l_1.
 // States, sums and gradients in registers are float32; y and the tokens' gradients are rounded once, when they are stored.
 #include <algorithm>
+#include <climits>
+#include <type_traits>
+#include <utility>
 
 #include "seq.hpp"
 
@@ -89,43 +92,200 @@ template <class T, int S> __device__ __forceinline__ void load_row(float (&h)[S]
     for (int s = 0; s < S; s++) h[s] = s < n ? to_float(p[s]) : 0.0f;
 }
 
-template <class T, class Sh>
-__global__ __launch_bounds__(kThreads) void scan_fwd_kernel(sig_scan_args a, Rows r, T* y, float* final_state, float* checkpoint, int64_t tiles)
+// ---- forward
+// A workgroup takes 64 neighbouring channels of one stream and group, a channel a lane; its W wavefronts share out the states, S each, so
+// that sums over states meet in LDS once a token while loads and stores of tokens are whole lines.  Tiles of 16 tokens: the wavefronts
+// prepare D_t and D_t x_t of the tile's tokens in turn (LDS), all run the recurrence of their states over the tile, and each adds
+// up and stores the outputs of the tokens that it prepared.  B and C of a tile lie across the 16 lanes of a row, 16 / S tokens in a
+// register, and reach the multiply-adds as row broadcasts of the instruction itself.
+// What bounds it: the exponentials (3.9 ns for 64 states on a SIMD) and the four other vector instructions a state and token.
+template <int S_, int W_> struct Group { static constexpr int S = S_, W = W_; };
+
+template <int I, int N, class F> __device__ __forceinline__ void unrolled(F f)
 {
-    int64_t row = (int64_t)blockIdx.x * (kThreads / 64) + threadIdx.x / 64;
-    if (row >= r.total) return;
-    Lane<T, Sh> l(a, r, row);
-    int n = (int)min((int64_t)Sh::S, a.N - l.q * Sh::S);
-    float h[Sh::S];
-    load_states(h, a.initial_state ? a.initial_state + l.state(a) : nullptr, n);
-    y += l.b * a.L * a.D + l.d;
-    for (int64_t t = 0; t < l.len; t++) {
-        if (checkpoint && t % kTile == 0 && l.on) {
-            float* ck = checkpoint + ((l.b * tiles + t / kTile) * a.D + l.d) * a.N + l.q * Sh::S;
-            for (int s = 0; s < n; s++) ck[s] = h[s];
-        }
-        float x = to_float(l.x[t * a.x_stride_t]), D = to_float(l.dt[t * a.dt_stride_t]) + l.bias, B[Sh::S], C[Sh::S];
-        if (a.softplus) D = softplus(D);
-        load_row(B, l.B + t * a.b_stride_t, n);
-        load_row(C, l.C + t * a.c_stride_t, n);
-        float o = 0.0f, u = D * x;
-#pragma unroll
-        for (int s = 0; s < Sh::S; s++) {
-            h[s] = fmaf(fast_exp(D * l.A[s]), h[s], u * B[s]);
-            o = fmaf(C[s], h[s], o);
-        }
-        o = fmaf(l.skip, x, sum_states<Sh::Q>(o));
-        if (l.gate) {
-            float z = to_float(l.gate[t * a.gate_stride_t]);
-            o *= z * sigmoid(z);
-        }
-        if (l.on && l.q == 0) y[t * a.D] = from_float<T>(o);
+    if constexpr (I < N) {
+        f(std::integral_constant<int, I>());
+        unrolled<I + 1, N>(f);
     }
-    if (!l.on) return;
-    if (l.q == 0)
-        for (int64_t t = l.len; t < a.L; t++) y[t * a.D] = from_float<T>(0.0f);
-    if (final_state)
-        for (int s = 0; s < n; s++) final_state[l.state(a) + s] = h[s];
+}
+// v times what lane K of each row of 16 lanes holds in r: one instruction
+template <int K> __device__ __forceinline__ float times_broadcast(float r, float v)
+{
+    return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(r), 0x150 + K, 0xf, 0xf, true)) * v;
+}
+// o + sum_s r[K + s] h[s], r[k] the value of lane k of each row.  The compiler does not merge the broadcast into a multiply-add; s_nop
+// keeps the two wait states between a write of r and its first use across lanes, which it does not look for in here.
+template <int K, int S> __device__ __forceinline__ float add_broadcast(float o, float r, const float (&h)[S])
+{
+    static_assert(S % 2 == 0, "states come in pairs");
+#pragma unroll
+    for (int s = 0; s < S; s += 2)
+        asm("s_nop 1\n\tv_fmac_f32_dpp %0, %1, %2 row_newbcast:%4 row_mask:0xf bank_mask:0xf\n\tv_fmac_f32_dpp %0, %1, %3 row_newbcast:%5 row_mask:0xf bank_mask:0xf"
+            : "+v"(o) : "v"(r), "v"(h[s]), "v"(h[s + 1]), "n"(K + s), "n"(K + s + 1));
+    return o;
+}
+
+// Element at a lane's byte offset from a row that is the same for the wavefront: the row stays in scalar registers.
+template <class T> __device__ __forceinline__ T& lane_at(T* row, unsigned bytes) { return *(T*)((char*)row + bytes); }
+template <class T> __device__ __forceinline__ const T& lane_at(const T* row, unsigned bytes) { return *(const T*)((const char*)row + bytes); }
+
+// The workgroups of a launch: 64 channels of a group of one stream, one time chunk.
+struct Blocks {
+    int64_t per_group;   // channels of a group
+    unsigned runs;       // workgroups for the channels of a group
+    unsigned chunks;
+    int64_t chunk;       // tokens of a time chunk, a multiple of kTile
+    unsigned total;
+};
+
+// Time chunks: where a launch has few workgroups, a first kernel runs every chunk from a state of zero and leaves its last state and the sum
+// of its step sizes; exp(A sum D) is the chunk's decay, so the state before any chunk is a short recurrence over the chunks before it.
+struct ChunkStates {
+    float* last;         // [B, chunks, N, D]
+    float* steps;        // [B, chunks, D]
+};
+
+template <class T, class Gr, bool kOutputs>
+__global__ __launch_bounds__(Gr::W * 64, Gr::W > 2 && Gr::S == 4 ? 4 : 2) void scan_fwd_kernel(sig_scan_args a, Blocks bl, ChunkStates cs, T* y, float* final_state, float* checkpoint)
+{
+    constexpr int S = Gr::S, W = Gr::W, PT = kTile / W, RT = 16 / S, KB = kTile / RT;
+    __shared__ float2 steps[kTile][64];
+    __shared__ float sums[kOutputs ? W : 1][kTile][64];
+    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+    const unsigned c = blockIdx.x % bl.chunks, rest = blockIdx.x / bl.chunks, run = rest % bl.runs, bg = rest / bl.runs;
+    const int64_t g = bg % (unsigned)a.G, b = bg / (unsigned)a.G;
+    const int64_t d0 = g * bl.per_group + run * 64;       // the workgroup's first channel
+    const bool on = run * 64 + lane < bl.per_group;
+    const unsigned e = on ? lane : 0;                     // lanes without a channel read the first one's and store nothing
+    const int64_t d = d0 + e;
+    const int64_t len = live_length(a.lengths, b, a.L), t_first = c * bl.chunk, t_end = min(t_first + bl.chunk, a.L);
+    int64_t left = min(t_end, len) - t_first;             // tokens from the tile's first to the last of the chunk that counts
+    const float bias = a.dt_bias ? a.dt_bias[d] : 0.0f, skip = a.skip ? a.skip[d] : 0.0f;
+    // rows of the wavefront's first token in the tile
+    const int64_t t1 = t_first + w;
+    const T *px = (const T*)a.x + b * a.x_stride_b + t1 * a.x_stride_t + d0, *pdt = (const T*)a.dt + b * a.dt_stride_b + t1 * a.dt_stride_t + d0;
+    const T* pz = a.gate ? (const T*)a.gate + b * a.gate_stride_b + t1 * a.gate_stride_t + d0 : nullptr;
+    T* py = kOutputs ? y + (b * a.L + t1) * a.D + d0 : nullptr;
+    const int n0 = w * S, nb = n0 + lane % S;             // first state of the wavefront; the state whose B and C this lane loads
+    const int tb = nb < a.N ? lane % 16 / S : INT_MAX / 2;    // and the first of their tokens in the tile
+    const int64_t tbc = t_first + lane % 16 / S;
+    const T *pb = (const T*)a.b + b * a.b_stride_b + g * a.b_stride_g + tbc * a.b_stride_t + nb;
+    const T *pc = (const T*)a.c + b * a.c_stride_b + g * a.c_stride_g + tbc * a.c_stride_t + nb;
+    if (checkpoint) checkpoint += ((b * ((a.L + kTile - 1) / kTile) + t_first / kTile) * a.N + n0) * a.D + d0;
+    float A[S], h[S];
+#pragma unroll
+    for (int s = 0; s < S; s++) {
+        A[s] = n0 + s < a.N ? a.A[d * a.N + n0 + s] * kLog2e : 0.0f;
+        h[s] = kOutputs && a.initial_state && n0 + s < a.N ? a.initial_state[(b * a.D + d) * a.N + n0 + s] : 0.0f;
+    }
+    if constexpr (kOutputs) {
+        const float *last = cs.last + (b * bl.chunks * a.N + n0) * a.D + d0, *sums_of = cs.steps + b * bl.chunks * a.D + d0;
+        for (unsigned j = 0; j < c && j * bl.chunk < len; j++, last += a.N * a.D, sums_of += a.D) {
+            float sum = sums_of[e];
+#pragma unroll
+            for (int s = 0; s < S; s++)
+                if (n0 + s < a.N) h[s] = fmaf(__builtin_amdgcn_exp2f(A[s] * sum), h[s], (last + s * a.D)[e]);
+        }
+    }
+    T x[PT], dt[PT], z[PT], bv[KB], cv[KB];
+    float total = 0.0f;
+    auto fetch = [&](int64_t left) {       // the tile at the pointers; they go on to the next
+        unsigned et = e * sizeof(T);
+        asm("" : "+v"(et));                // or the compiler carries a vector address for every row
+#pragma unroll
+        for (int i = 0; i < PT; i++) {
+            if (i * W + w < left) {
+                x[i] = lane_at(px, et);
+                dt[i] = lane_at(pdt, et);
+                if (kOutputs && pz) z[i] = lane_at(pz, et);
+            }
+            px += W * a.x_stride_t, pdt += W * a.dt_stride_t;
+            if (kOutputs && pz) pz += W * a.gate_stride_t;
+        }
+#pragma unroll
+        for (int j = 0; j < KB; j++) {
+            bv[j] = cv[j] = from_float<T>(0.0f);
+            if (j * RT + tb < left) {
+                bv[j] = *pb;
+                if (kOutputs) cv[j] = *pc;
+            }
+            pb += RT * a.b_stride_t;
+            if (kOutputs) pc += RT * a.c_stride_t;
+        }
+    };
+    fetch(left);
+    int64_t room = t_end - t_first;        // tokens of the chunk from the tile's first
+    for (; left > 0; left -= kTile, room -= kTile) {
+        float keep[PT], f[PT], B[KB], C[KB];
+        const int m = (int)min((int64_t)kTile, left), m_out = (int)min((int64_t)kTile, room);
+#pragma unroll
+        for (int i = 0; i < PT; i++) {
+            int k = i * W + w;
+            float D = 0.0f, u = 0.0f;
+            f[i] = 0.0f, keep[i] = 0.0f;
+            if (k < m) {
+                float v = to_float(x[i]);
+                D = to_float(dt[i]) + bias;
+                if (a.softplus) D = softplus(D);
+                u = D * v;
+                keep[i] = skip * v;
+                f[i] = 1.0f;
+                if (kOutputs && pz) {
+                    f[i] = to_float(z[i]);
+                    f[i] *= sigmoid(f[i]);
+                }
+            }
+            steps[k][lane] = make_float2(D, u);
+        }
+#pragma unroll
+        for (int j = 0; j < KB; j++) B[j] = to_float(bv[j]), C[j] = to_float(cv[j]);
+        if (kOutputs && checkpoint) {
+            unsigned ef = e * 4;
+            asm("" : "+v"(ef));
+#pragma unroll
+            for (int s = 0; s < S; s++)
+                if (on && n0 + s < a.N) lane_at(checkpoint + s * a.D, ef) = h[s];
+            checkpoint += a.N * a.D;
+        }
+        fetch(left - kTile);
+        __syncthreads();
+        unrolled<0, kTile>([&](auto it) {
+            constexpr int i = decltype(it)::value, k = i % RT * S;
+            float2 q = steps[i][lane];
+            if (!kOutputs) total += q.x;
+            unrolled<0, S>([&](auto is) {
+                constexpr int s = decltype(is)::value;
+                h[s] = fmaf(__builtin_amdgcn_exp2f(q.x * A[s]), h[s], times_broadcast<k + s>(B[i / RT], q.y));
+            });
+            if constexpr (kOutputs) sums[w][i][lane] = add_broadcast<k>(0.0f, C[i / RT], h);
+        });
+        __syncthreads();
+        if constexpr (kOutputs) {
+#pragma unroll
+            for (int i = 0; i < PT; i++, py += W * a.D) {
+                unsigned et = e * sizeof(T);
+                asm("" : "+v"(et));
+                int k = i * W + w;
+                float o = keep[i];
+#pragma unroll
+                for (int v = 0; v < W; v++) o += sums[v][k][lane];
+                if (on && k < m_out) lane_at(py, et) = from_float<T>(k < m ? o * f[i] : 0.0f);
+            }
+        }
+    }
+    if (!on) return;
+    if constexpr (kOutputs) {
+        for (int64_t k = w; k < room; k += W, py += W * a.D) py[e] = from_float<T>(0.0f);
+        if (final_state && c == (unsigned)(len > 0 ? (len - 1) / bl.chunk : 0))
+#pragma unroll
+            for (int s = 0; s < S; s++)
+                if (n0 + s < a.N) final_state[(b * a.D + d) * a.N + n0 + s] = h[s];
+    } else {
+#pragma unroll
+        for (int s = 0; s < S; s++)
+            if (n0 + s < a.N) (cs.last + ((b * bl.chunks + c) * a.N + n0 + s) * a.D + d0)[e] = h[s];
+        if (w == 0) cs.steps[(b * bl.chunks + c) * a.D + d] = total;
+    }
 }
 
 // Tiles of kTile tokens from the last to the first: the states inside a tile are computed again from the checkpoint before it and stay
@@ -153,7 +313,8 @@ __global__ __launch_bounds__(kThreads) void scan_bwd_kernel(sig_scan_args a, sig
         int64_t t0 = tile * kTile;
         int m = (int)min((int64_t)kTile, l.len - t0);
         float h0[S], h[kTile][S], e[kTile][S], x[kTile], D[kTile], raw[kTile];
-        load_states(h0, checkpoint + ((l.b * tiles + tile) * a.D + l.d) * a.N + l.q * S, n);
+#pragma unroll
+        for (int s = 0; s < S; s++) h0[s] = s < n ? checkpoint[((l.b * tiles + tile) * a.N + l.q * S + s) * a.D + l.d] : 0.0f;
 #pragma unroll
         for (int i = 0; i < kTile; i++) {
             int64_t t = t0 + (i < m ? i : 0);
@@ -290,6 +451,30 @@ template <class F> auto with_shape(int64_t N, F f)
 }
 template <class F> auto with_type(int64_t dtype, F f) { return dtype == SIG_BF16 ? f(bf16()) : f(float()); }
 
+// wavefronts of a workgroup by the number of states, four states each, eight beyond 32 (the sums of sixteen would not fit 64 KB of LDS)
+template <class F> auto with_group(int64_t N, F f)
+{
+    if (N <= 4) return f(Group<4, 1>());
+    if (N <= 8) return f(Group<4, 2>());
+    if (N <= 16) return f(Group<4, 4>());
+    if (N <= 32) return f(Group<4, 8>());
+    return f(Group<8, 8>());
+}
+
+Blocks forward_blocks(const sig_scan_args& a)
+{
+    Blocks bl;
+    bl.per_group = a.D / a.G;
+    bl.runs = (unsigned)((bl.per_group + 63) / 64);
+    int64_t rows = a.B * a.G * bl.runs, waves = rows * with_group(a.N, [](auto gr) { return decltype(gr)::W; });
+    int64_t want = std::max<int64_t>(1, std::min<int64_t>(64, 2048 / std::max<int64_t>(1, waves)));
+    int64_t tiles = std::max<int64_t>(1, tiles_of(a)), per = std::max<int64_t>(2, (tiles + want - 1) / want);
+    bl.chunk = per * kTile;
+    bl.chunks = (unsigned)((tiles + per - 1) / per);
+    bl.total = (unsigned)(rows * bl.chunks);
+    return bl;
+}
+
 struct BackwardParts { size_t bc, a, d; };
 BackwardParts backward_parts(const sig_scan_args& a)
 {
@@ -299,21 +484,27 @@ BackwardParts backward_parts(const sig_scan_args& a)
 
 }  // namespace
 
-size_t scan_forward_workspace(const sig_scan_args&) { return 0; }
+size_t scan_forward_workspace(const sig_scan_args& a)
+{
+    Blocks bl = forward_blocks(a);
+    return bl.chunks > 1 ? (size_t)(a.B * bl.chunks * a.D * (a.N + 1) * 4) : 0;
+}
 size_t scan_backward_workspace(const sig_scan_args& a)
 {
     BackwardParts p = backward_parts(a);
     return (p.bc + p.a + p.d) * 4;
 }
 
-hipError_t scan_forward(const sig_scan_args& a, void* y, float* final_state, float* checkpoint, float*, hipStream_t stream)
+hipError_t scan_forward(const sig_scan_args& a, void* y, float* final_state, float* checkpoint, float* workspace, hipStream_t stream)
 {
+    Blocks bl = forward_blocks(a);
+    ChunkStates cs{workspace, workspace ? workspace + a.B * bl.chunks * a.N * a.D : nullptr};
     return with_type(a.dtype, [&](auto t) {
-        return with_shape(a.N, [&](auto sh) {
+        return with_group(a.N, [&](auto gr) {
             using T = decltype(t);
-            using Sh = decltype(sh);
-            Rows r = rows_of<Sh>(a);
-            scan_fwd_kernel<T, Sh><<<blocks_for(r.total * 64), kThreads, 0, stream>>>(a, r, (T*)y, final_state, checkpoint, tiles_of(a));
+            using Gr = decltype(gr);
+            if (bl.chunks > 1) scan_fwd_kernel<T, Gr, false><<<(unsigned)bl.total, Gr::W * 64, 0, stream>>>(a, bl, cs, nullptr, nullptr, nullptr);
+            scan_fwd_kernel<T, Gr, true><<<(unsigned)bl.total, Gr::W * 64, 0, stream>>>(a, bl, cs, (T*)y, final_state, checkpoint);
             return hipGetLastError();
         });
     });
