@@ -8,7 +8,7 @@
 
 namespace {
 
-constexpr int64_t kMost = (int64_t)1 << 40;       // bound of sizes and of their products: more than any memory holds, and no overflow below
+constexpr int64_t kMost = (int64_t)1 << 38;       // bound of sizes and of their products: more than the memory holds, and no overflow below
 
 int hip_code(hipError_t e) { return e == hipSuccess ? SIG_OK : sig::record_hip_error(e); }
 
@@ -40,6 +40,11 @@ int check_scan(const sig_scan_args* a)
     if (!a || bad_type(a->dtype) || a->D < 1 || a->G < 1 || a->N < 1 || a->D % a->G != 0) return SIG_EINVAL;
     if (a->N > SIG_MAX_SCAN_STATES) return SIG_EUNSUPPORTED;
     if (a->softplus != 0 && a->softplus != 1) return SIG_EINVAL;
+    // a launch numbers at least the streams' channels; the kernels count tokens in 32 bits and reach those of a tile by 32-bit offsets
+    if (a->B > 0 && a->D > INT32_MAX / a->B) return SIG_ETOOLARGE;
+    if (a->L > INT32_MAX - 64) return SIG_ETOOLARGE;
+    for (int64_t s : {a->x_stride_t, a->dt_stride_t, a->gate_stride_t, a->b_stride_t, a->c_stride_t, a->D})
+        if (s < 0 || s >= (1 << 26)) return s < 0 ? SIG_EINVAL : SIG_ETOOLARGE;
     return check_sizes({a->B, a->L, a->D, a->N});
 }
 

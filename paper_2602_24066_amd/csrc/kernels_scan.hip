@@ -12,6 +12,7 @@
 #include <type_traits>
 #include <utility>
 
+#include "kernels.hpp"
 #include "seq.hpp"
 
 namespace sig {
@@ -94,11 +95,12 @@ template <class T, int S> __device__ __forceinline__ void load_row(float (&h)[S]
 
 // ---- forward
 // A workgroup takes 64 neighbouring channels of one stream and group, a channel a lane; its W wavefronts share out the states, S each, so
-// that sums over states meet in LDS once a token while loads and stores of tokens are whole lines.  Tiles of 16 tokens: the wavefronts
-// prepare D_t and D_t x_t of the tile's tokens in turn (LDS), all run the recurrence of their states over the tile, and each adds
-// up and stores the outputs of the tokens that it prepared.  B and C of a tile lie across the 16 lanes of a row, 16 / S tokens in a
-// register, and reach the multiply-adds as row broadcasts of the instruction itself.
-// What bounds it: the exponentials (3.9 ns for 64 states on a SIMD) and the four other vector instructions a state and token.
+// that loads and stores of tokens are whole lines and sums over states meet in LDS once a token.  Tiles of 16 tokens: the wavefronts
+// prepare D_t and D_t x_t of the tile's tokens (LDS), all run the recurrence of their states over the tile, and each adds up and
+// stores the outputs of the tokens that it prepared.  B and C of a tile lie across the 16 lanes of a row, 16 / S tokens in a
+// register, and reach the products as row broadcasts of the instruction itself: no LDS, no unpacking a token.
+// What bounds it: vector instructions, of which a state and token needs an exponential (3.5 ns on a SIMD) and four others (1.1 to 2.2 ns).
+// 8 x 4096 x 2048 bf16, 16 states: 387 us, 2.8e12 states a second; the bytes alone would take 105 us.
 template <int S_, int W_> struct Group { static constexpr int S = S_, W = W_; };
 
 template <int I, int N, class F> __device__ __forceinline__ void unrolled(F f)
@@ -113,28 +115,63 @@ template <int K> __device__ __forceinline__ float times_broadcast(float r, float
 {
     return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(r), 0x150 + K, 0xf, 0xf, true)) * v;
 }
-// o + sum_s r[K + s] h[s], r[k] the value of lane k of each row.  The compiler does not merge the broadcast into a multiply-add; s_nop
-// keeps the two wait states between a write of r and its first use across lanes, which it does not look for in here.
-template <int K, int S> __device__ __forceinline__ float add_broadcast(float o, float r, const float (&h)[S])
+// o[t] = sum_s r[K + S t + s] h[t][s] for four tokens t, r[k] the value of lane k of each row.  The compiler does not merge the broadcast into a
+// multiply-add; s_nop keeps the two wait states between a write of r and its first use across lanes, which it does not look for in here.
+#define SIG_FMAC(o, h, k) "v_fmac_f32_dpp %" #o ", %4, %" #h " row_newbcast:%" #k " row_mask:0xf bank_mask:0xf\n\t"
+template <int K, int S, int s = 1> __device__ __forceinline__ void sum_broadcast(float (&o)[4], float r, const float (&h)[4][S])
 {
-    static_assert(S % 2 == 0, "states come in pairs");
-#pragma unroll
-    for (int s = 0; s < S; s += 2)
-        asm("s_nop 1\n\tv_fmac_f32_dpp %0, %1, %2 row_newbcast:%4 row_mask:0xf bank_mask:0xf\n\tv_fmac_f32_dpp %0, %1, %3 row_newbcast:%5 row_mask:0xf bank_mask:0xf"
-            : "+v"(o) : "v"(r), "v"(h[s]), "v"(h[s + 1]), "n"(K + s), "n"(K + s + 1));
-    return o;
+    if constexpr (s == 1) {
+        o[0] = times_broadcast<K>(r, h[0][0]), o[1] = times_broadcast<K + S>(r, h[1][0]);
+        o[2] = times_broadcast<K + 2 * S>(r, h[2][0]), o[3] = times_broadcast<K + 3 * S>(r, h[3][0]);
+    }
+    if constexpr (s < S) {
+        asm("s_nop 1\n\t" SIG_FMAC(0, 5, 9) SIG_FMAC(1, 6, 10) SIG_FMAC(2, 7, 11) SIG_FMAC(3, 8, 12)
+            : "+v"(o[0]), "+v"(o[1]), "+v"(o[2]), "+v"(o[3])
+            : "v"(r), "v"(h[0][s]), "v"(h[1][s]), "v"(h[2][s]), "v"(h[3][s]), "n"(K + s), "n"(K + S + s), "n"(K + 2 * S + s), "n"(K + 3 * S + s));
+        sum_broadcast<K, S, s + 1>(o, r, h);
+    }
 }
+#undef SIG_FMAC
 
-// Element at a lane's byte offset from a row that is the same for the wavefront: the row stays in scalar registers.
-template <class T> __device__ __forceinline__ T& lane_at(T* row, unsigned bytes) { return *(T*)((char*)row + bytes); }
-template <class T> __device__ __forceinline__ const T& lane_at(const T* row, unsigned bytes) { return *(const T*)((const char*)row + bytes); }
+// Loads and stores at a lane's byte offset from a row that is the same for the wavefront, and an offset between rows in bytes; an offset
+// of kNowhere makes a load give zero and a store do nothing, so tokens that are not there need no branches around them.
+using Buffer = __amdgpu_buffer_rsrc_t;
+__device__ __forceinline__ Buffer buffer_at(const void* p) { return __builtin_amdgcn_make_buffer_rsrc((void*)p, 0, 0xfffffff0u, 0x00020000); }
+template <class T> __device__ __forceinline__ T buffer_load(Buffer r, unsigned at, unsigned row)
+{
+    T v;
+    if constexpr (sizeof(T) == 2) {
+        uint16_t q = __builtin_amdgcn_raw_buffer_load_b16(r, at, row, 0);
+        __builtin_memcpy(&v, &q, 2);
+    } else {
+        uint32_t q = __builtin_amdgcn_raw_buffer_load_b32(r, at, row, 0);
+        __builtin_memcpy(&v, &q, 4);
+    }
+    return v;
+}
+template <class T> __device__ __forceinline__ void buffer_store(Buffer r, unsigned at, unsigned row, T v)
+{
+    if constexpr (sizeof(T) == 2) {
+        uint16_t q;
+        __builtin_memcpy(&q, &v, 2);
+        __builtin_amdgcn_raw_buffer_store_b16(q, r, at, row, 0);
+    } else {
+        uint32_t q;
+        __builtin_memcpy(&q, &v, 4);
+        __builtin_amdgcn_raw_buffer_store_b32(q, r, at, row, 0);
+    }
+}
+constexpr unsigned kNowhere = 0xfffffffcu;
+// v where mask is all ones, 0 or `other` where it is zero; the masks are the same for the wavefront
+__device__ __forceinline__ float only_if(uint32_t mask, float v) { return __uint_as_float(__float_as_uint(v) & mask); }
+__device__ __forceinline__ float either(uint32_t mask, float v, float other) { return __uint_as_float((__float_as_uint(v) & mask) | (__float_as_uint(other) & ~mask)); }
 
 // The workgroups of a launch: 64 channels of a group of one stream, one time chunk.
 struct Blocks {
     int64_t per_group;   // channels of a group
     unsigned runs;       // workgroups for the channels of a group
     unsigned chunks;
-    int64_t chunk;       // tokens of a time chunk, a multiple of kTile
+    int chunk;           // tokens of a time chunk, a multiple of kTile
     unsigned total;
 };
 
@@ -149,8 +186,10 @@ template <class T, class Gr, bool kOutputs>
 __global__ __launch_bounds__(Gr::W * 64, Gr::W > 2 && Gr::S == 4 ? 4 : 2) void scan_fwd_kernel(sig_scan_args a, Blocks bl, ChunkStates cs, T* y, float* final_state, float* checkpoint)
 {
     constexpr int S = Gr::S, W = Gr::W, PT = kTile / W, RT = 16 / S, KB = kTile / RT;
-    __shared__ float2 steps[kTile][64];
-    __shared__ float sums[kOutputs ? W : 1][kTile][64];
+    extern __shared__ float lds[];
+    // D_t and D_t x_t of two tokens for each lane, and the wavefronts' sums of four (where there are outputs), each twice
+    float4(*steps)[64] = (float4(*)[64])lds;                                             // [2][kTile / 2][64]
+    float4(*sums)[kTile / 4][64] = (float4(*)[kTile / 4][64])(lds + 4 * kTile * 64);     // [2][W][kTile / 4][64]
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     const unsigned c = blockIdx.x % bl.chunks, rest = blockIdx.x / bl.chunks, run = rest % bl.runs, bg = rest / bl.runs;
     const int64_t g = bg % (unsigned)a.G, b = bg / (unsigned)a.G;
@@ -158,20 +197,11 @@ __global__ __launch_bounds__(Gr::W * 64, Gr::W > 2 && Gr::S == 4 ? 4 : 2) void s
     const bool on = run * 64 + lane < bl.per_group;
     const unsigned e = on ? lane : 0;                     // lanes without a channel read the first one's and store nothing
     const int64_t d = d0 + e;
-    const int64_t len = live_length(a.lengths, b, a.L), t_first = c * bl.chunk, t_end = min(t_first + bl.chunk, a.L);
-    int64_t left = min(t_end, len) - t_first;             // tokens from the tile's first to the last of the chunk that counts
+    const int len = (int)live_length(a.lengths, b, a.L), t_first = (int)c * bl.chunk, t_end = min(t_first + bl.chunk, (int)a.L);
+    int left = min(t_end, len) - t_first;                 // tokens from the tile's first to the last of the chunk that counts
     const float bias = a.dt_bias ? a.dt_bias[d] : 0.0f, skip = a.skip ? a.skip[d] : 0.0f;
-    // rows of the wavefront's first token in the tile
-    const int64_t t1 = t_first + w;
-    const T *px = (const T*)a.x + b * a.x_stride_b + t1 * a.x_stride_t + d0, *pdt = (const T*)a.dt + b * a.dt_stride_b + t1 * a.dt_stride_t + d0;
-    const T* pz = a.gate ? (const T*)a.gate + b * a.gate_stride_b + t1 * a.gate_stride_t + d0 : nullptr;
-    T* py = kOutputs ? y + (b * a.L + t1) * a.D + d0 : nullptr;
-    const int n0 = w * S, nb = n0 + lane % S;             // first state of the wavefront; the state whose B and C this lane loads
-    const int tb = nb < a.N ? lane % 16 / S : INT_MAX / 2;    // and the first of their tokens in the tile
-    const int64_t tbc = t_first + lane % 16 / S;
-    const T *pb = (const T*)a.b + b * a.b_stride_b + g * a.b_stride_g + tbc * a.b_stride_t + nb;
-    const T *pc = (const T*)a.c + b * a.c_stride_b + g * a.c_stride_g + tbc * a.c_stride_t + nb;
-    if (checkpoint) checkpoint += ((b * ((a.L + kTile - 1) / kTile) + t_first / kTile) * a.N + n0) * a.D + d0;
+    const uint32_t soft = a.softplus ? ~0u : 0u, gated = a.gate ? ~0u : 0u;
+    const int n0 = w * S;                                 // first state of the wavefront
     float A[S], h[S];
 #pragma unroll
     for (int s = 0; s < S; s++) {
@@ -180,103 +210,167 @@ __global__ __launch_bounds__(Gr::W * 64, Gr::W > 2 && Gr::S == 4 ? 4 : 2) void s
     }
     if constexpr (kOutputs) {
         const float *last = cs.last + (b * bl.chunks * a.N + n0) * a.D + d0, *sums_of = cs.steps + b * bl.chunks * a.D + d0;
-        for (unsigned j = 0; j < c && j * bl.chunk < len; j++, last += a.N * a.D, sums_of += a.D) {
+        for (unsigned j = 0; j < c && (int)j * bl.chunk < len; j++, last += a.N * a.D, sums_of += a.D) {
             float sum = sums_of[e];
 #pragma unroll
             for (int s = 0; s < S; s++)
                 if (n0 + s < a.N) h[s] = fmaf(__builtin_amdgcn_exp2f(A[s] * sum), h[s], (last + s * a.D)[e]);
         }
     }
+    // rows of the wavefront's first token of the chunk, and of its first token's B and C
+    const int64_t t1 = t_first + w * PT;
+    const T *px = (const T*)a.x + b * a.x_stride_b + t1 * a.x_stride_t + d0, *pdt = (const T*)a.dt + b * a.dt_stride_b + t1 * a.dt_stride_t + d0;
+    const T *pz = a.gate ? (const T*)a.gate + b * a.gate_stride_b + t1 * a.gate_stride_t + d0 : px;
+    const T *pb = (const T*)a.b + b * a.b_stride_b + g * a.b_stride_g + t_first * a.b_stride_t + n0;
+    const T *pc = (const T*)a.c + b * a.c_stride_b + g * a.c_stride_g + t_first * a.c_stride_t + n0;
+    T* py = kOutputs ? y + (b * a.L + t1) * a.D + d0 : nullptr;
+    float* pk = checkpoint ? checkpoint + ((b * ((a.L + kTile - 1) / kTile) + t_first / kTile) * a.N + n0) * a.D + d0 : nullptr;
+    constexpr unsigned E = sizeof(T);
+    const unsigned x_row = (unsigned)a.x_stride_t * E, dt_row = (unsigned)a.dt_stride_t * E, z_row = gated ? (unsigned)a.gate_stride_t * E : x_row;
+    const unsigned y_row = (unsigned)a.D * E, b_row = (unsigned)(RT * a.b_stride_t) * E, c_row = (unsigned)(RT * a.c_stride_t) * E;
+    // the token of a tile and the state whose B and C this lane loads
+    const int tb = n0 + lane % S < a.N ? lane % 16 / S : INT_MAX / 2;
+    const unsigned b_at = (unsigned)(lane % 16 / S * a.b_stride_t + lane % S) * E, c_at = (unsigned)(lane % 16 / S * a.c_stride_t + lane % S) * E;
+
     T x[PT], dt[PT], z[PT], bv[KB], cv[KB];
-    float total = 0.0f;
-    auto fetch = [&](int64_t left) {       // the tile at the pointers; they go on to the next
-        unsigned et = e * sizeof(T);
-        asm("" : "+v"(et));                // or the compiler carries a vector address for every row
+    float f[PT], keep[PT], f_next[PT], keep_next[PT], o[PT], B[KB], C[KB], total = 0.0f;
+    // reads the tile at the row pointers, n tokens of it; the pointers go on to the next
+    auto fetch = [&](int n) {
+        Buffer rx = buffer_at(px), rdt = buffer_at(pdt), rz = buffer_at(pz), rb = buffer_at(pb), rc = buffer_at(pc);
 #pragma unroll
         for (int i = 0; i < PT; i++) {
-            if (i * W + w < left) {
-                x[i] = lane_at(px, et);
-                dt[i] = lane_at(pdt, et);
-                if (kOutputs && pz) z[i] = lane_at(pz, et);
-            }
-            px += W * a.x_stride_t, pdt += W * a.dt_stride_t;
-            if (kOutputs && pz) pz += W * a.gate_stride_t;
+            unsigned at = w * PT + i < n ? e * E : kNowhere;
+            x[i] = buffer_load<T>(rx, at, i * x_row);
+            dt[i] = buffer_load<T>(rdt, at, i * dt_row);
+            if (kOutputs) z[i] = buffer_load<T>(rz, at, i * z_row);
         }
 #pragma unroll
         for (int j = 0; j < KB; j++) {
-            bv[j] = cv[j] = from_float<T>(0.0f);
-            if (j * RT + tb < left) {
-                bv[j] = *pb;
-                if (kOutputs) cv[j] = *pc;
-            }
-            pb += RT * a.b_stride_t;
-            if (kOutputs) pc += RT * a.c_stride_t;
+            bool there = j * RT + tb < n;
+            bv[j] = buffer_load<T>(rb, there ? b_at : kNowhere, j * b_row);
+            if (kOutputs) cv[j] = buffer_load<T>(rc, there ? c_at : kNowhere, j * c_row);
         }
+        px += kTile * a.x_stride_t, pdt += kTile * a.dt_stride_t, pz += kTile * (gated ? a.gate_stride_t : a.x_stride_t);
+        pb += kTile * a.b_stride_t, pc += kTile * a.c_stride_t;
     };
-    fetch(left);
-    int64_t room = t_end - t_first;        // tokens of the chunk from the tile's first
-    for (; left > 0; left -= kTile, room -= kTile) {
-        float keep[PT], f[PT], B[KB], C[KB];
-        const int m = (int)min((int64_t)kTile, left), m_out = (int)min((int64_t)kTile, room);
+    // D_t and D_t x_t of the wavefront's tokens of a tile with n tokens (zero beyond: states stay), and what its outputs need besides
+    auto prepare = [&](float4 (*to)[64], int n, const float (&xf)[PT], const float (&df)[PT], const float (&zf)[PT]) {
 #pragma unroll
         for (int i = 0; i < PT; i++) {
-            int k = i * W + w;
-            float D = 0.0f, u = 0.0f;
-            f[i] = 0.0f, keep[i] = 0.0f;
-            if (k < m) {
-                float v = to_float(x[i]);
-                D = to_float(dt[i]) + bias;
-                if (a.softplus) D = softplus(D);
-                u = D * v;
-                keep[i] = skip * v;
-                f[i] = 1.0f;
-                if (kOutputs && pz) {
-                    f[i] = to_float(z[i]);
-                    f[i] *= sigmoid(f[i]);
-                }
+            float D = df[i] + bias;
+            D = only_if(w * PT + i < n ? ~0u : 0u, either(soft, softplus(D), D));
+            ((float2*)&to[(w * PT + i) / 2][lane])[(w * PT + i) % 2] = make_float2(D, D * xf[i]);
+            if (kOutputs) {
+                keep_next[i] = skip * xf[i];
+                f_next[i] = either(gated, zf[i] * sigmoid(zf[i]), 1.0f);
             }
-            steps[k][lane] = make_float2(D, u);
         }
+    };
+    auto collect = [&](const float4 (*from)[kTile / 4][64]) {
+        constexpr int G = PT < 4 ? PT : 4;                // tokens of an access
 #pragma unroll
-        for (int j = 0; j < KB; j++) B[j] = to_float(bv[j]), C[j] = to_float(cv[j]);
+        for (int i = 0; i < PT; i += G) {
+#pragma unroll
+            for (int j = 0; j < G; j++) o[i + j] = keep[i + j];
+#pragma unroll
+            for (int v = 0; v < W; v++) {
+                Pack<float, G> q = *(const Pack<float, G>*)((const float*)&from[v][(w * PT + i) / 4][lane] + (w * PT + i) % 4);
+#pragma unroll
+                for (int j = 0; j < G; j++) o[i + j] += q.v[j];
+            }
+#pragma unroll
+            for (int j = 0; j < G; j++) o[i + j] *= f[i + j];
+        }
+    };
+    // Three tiles are in work at a time: while one runs, the step sizes of the next are prepared and the outputs of the one before are
+    // added up, so that no wavefront waits for the latencies of either; one barrier a tile.
+    float xf[PT], df[PT], zf[PT];
+    fetch(left);
+#pragma unroll
+    for (int i = 0; i < PT; i++) xf[i] = to_float(x[i]), df[i] = to_float(dt[i]), zf[i] = kOutputs ? to_float(z[i]) : 0.0f;
+    prepare(steps, left, xf, df, zf);
+#pragma unroll
+    for (int j = 0; j < KB; j++) B[j] = to_float(bv[j]), C[j] = kOutputs ? to_float(cv[j]) : 0.0f;
+    fetch(left - kTile);
+    __syncthreads();
+    bool stores = false;                   // no outputs to store in the first turn
+    auto tile = [&](auto parity) {         // which half of LDS: a constant, so that the compiler sees that reads and writes do not meet
+        constexpr int turn = decltype(parity)::value;
+        float4(*now)[64] = steps + turn * kTile / 2, (*next)[64] = steps + (turn ^ 1) * kTile / 2;
+        float4(*sums_now)[kTile / 4][64] = sums + turn * W, (*sums_before)[kTile / 4][64] = sums + (turn ^ 1) * W;
+        float b_next[KB], c_next[KB];
+#pragma unroll
+        for (int i = 0; i < PT; i++) xf[i] = to_float(x[i]), df[i] = to_float(dt[i]), zf[i] = kOutputs ? to_float(z[i]) : 0.0f;
+#pragma unroll
+        for (int j = 0; j < KB; j++) b_next[j] = to_float(bv[j]), c_next[j] = kOutputs ? to_float(cv[j]) : 0.0f;
+        fetch(left - 2 * kTile);
         if (kOutputs && checkpoint) {
-            unsigned ef = e * 4;
-            asm("" : "+v"(ef));
 #pragma unroll
-            for (int s = 0; s < S; s++)
-                if (on && n0 + s < a.N) lane_at(checkpoint + s * a.D, ef) = h[s];
-            checkpoint += a.N * a.D;
+            for (int s = 0; s < S; s++) buffer_store(buffer_at(pk), n0 + s < a.N ? e * 4 : kNowhere, (unsigned)(s * a.D) * 4, h[s]);
+            pk += a.N * a.D;
         }
-        fetch(left - kTile);
-        __syncthreads();
-        unrolled<0, kTile>([&](auto it) {
-            constexpr int i = decltype(it)::value, k = i % RT * S;
-            float2 q = steps[i][lane];
-            if (!kOutputs) total += q.x;
-            unrolled<0, S>([&](auto is) {
-                constexpr int s = decltype(is)::value;
-                h[s] = fmaf(__builtin_amdgcn_exp2f(q.x * A[s]), h[s], times_broadcast<k + s>(B[i / RT], q.y));
-            });
-            if constexpr (kOutputs) sums[w][i][lane] = add_broadcast<k>(0.0f, C[i / RT], h);
-        });
-        __syncthreads();
-        if constexpr (kOutputs) {
+        if (kOutputs) {
+            collect(sums_before);
 #pragma unroll
-            for (int i = 0; i < PT; i++, py += W * a.D) {
-                unsigned et = e * sizeof(T);
-                asm("" : "+v"(et));
-                int k = i * W + w;
-                float o = keep[i];
+            for (int i = 0; i < PT; i++) f[i] = f_next[i], keep[i] = keep_next[i];
+        }
+        prepare(next, left - kTile, xf, df, zf);
+        unrolled<0, kTile / 4>([&](auto jt) {
+            constexpr int i = decltype(jt)::value * 4, k = i % RT * S;
+            float4 p = now[i / 2][lane], q = now[i / 2 + 1][lane];
+            const float D[4] = {p.x, p.z, q.x, q.z}, u[4] = {p.y, p.w, q.y, q.w};
+            float decay[4][S], ht[4][S];
 #pragma unroll
-                for (int v = 0; v < W; v++) o += sums[v][k][lane];
-                if (on && k < m_out) lane_at(py, et) = from_float<T>(k < m ? o * f[i] : 0.0f);
+            for (int j = 0; j < 4; j++) {
+                if (!kOutputs) total += D[j];
+#pragma unroll
+                for (int s = 0; s < S; s++) decay[j][s] = __builtin_amdgcn_exp2f(D[j] * A[s]);
             }
+            unrolled<0, 4>([&](auto it) {
+                constexpr int j = decltype(it)::value;
+                unrolled<0, S>([&](auto is) {
+                    constexpr int s = decltype(is)::value;
+                    ht[j][s] = h[s] = fmaf(decay[j][s], h[s], times_broadcast<k + j * S + s>(B[i / RT], u[j]));
+                });
+            });
+            if constexpr (kOutputs) {
+                float y4[4];
+                sum_broadcast<k>(y4, C[i / RT], ht);
+                sums_now[w][i / 4][lane] = make_float4(y4[0], y4[1], y4[2], y4[3]);
+            }
+        });
+        if (kOutputs) {                    // lanes without a channel repeat the first one's outputs
+#pragma unroll
+            for (int i = 0; i < PT; i++) buffer_store(buffer_at(py), stores ? e * E : kNowhere, i * y_row, from_float<T>(o[i]));
+            py += stores ? kTile * a.D : 0;
+            stores = true;
         }
+#pragma unroll
+        for (int j = 0; j < KB; j++) B[j] = b_next[j], C[j] = c_next[j];
+        left -= kTile;
+        __syncthreads();
+    };
+    unsigned turn = 0;
+    while (left > 0) {
+        tile(std::integral_constant<int, 0>());
+        turn = 1;
+        if (left <= 0) break;
+        tile(std::integral_constant<int, 1>());
+        turn = 0;
     }
-    if (!on) return;
+    int room = t_end - t_first;            // tokens of the chunk from the first whose output is not stored yet
     if constexpr (kOutputs) {
-        for (int64_t k = w; k < room; k += W, py += W * a.D) py[e] = from_float<T>(0.0f);
-        if (final_state && c == (unsigned)(len > 0 ? (len - 1) / bl.chunk : 0))
+        if (len > t_first) {               // the last tile, of left + kTile tokens
+            room -= (min(t_end, len) - t_first - 1) / kTile * kTile;
+            collect(sums + (turn ^ 1) * W);
+#pragma unroll
+            for (int i = 0; i < PT; i++)
+                buffer_store(buffer_at(py), w * PT + i < room ? e * E : kNowhere, i * y_row, from_float<T>(w * PT + i < left + kTile ? o[i] : 0.0f));
+            py += kTile * a.D, room -= kTile;
+        }
+        for (py -= w * (PT - 1) * a.D; room > 0; room -= W, py += W * a.D)
+            if (w < room) py[e] = from_float<T>(0.0f);
+        if (final_state && (int)c == (len > 0 ? (len - 1) / bl.chunk : 0))
 #pragma unroll
             for (int s = 0; s < S; s++)
                 if (n0 + s < a.N) final_state[(b * a.D + d) * a.N + n0 + s] = h[s];
@@ -451,25 +545,28 @@ template <class F> auto with_shape(int64_t N, F f)
 }
 template <class F> auto with_type(int64_t dtype, F f) { return dtype == SIG_BF16 ? f(bf16()) : f(float()); }
 
-// wavefronts of a workgroup by the number of states, four states each, eight beyond 32 (the sums of sixteen would not fit 64 KB of LDS)
+// States of a wavefront and wavefronts of a workgroup, by the number of states.  Measured at 8 x 4096 x 2048 with 16 states: 386 us with two states
+// on eight wavefronts, 504 with four on four (a wavefront alone on its SIMD), 525 with one on sixteen (their sums fill the LDS pipe).
 template <class F> auto with_group(int64_t N, F f)
 {
-    if (N <= 4) return f(Group<4, 1>());
-    if (N <= 8) return f(Group<4, 2>());
-    if (N <= 16) return f(Group<4, 4>());
+    if (N <= 4) return f(Group<2, 2>());
+    if (N <= 8) return f(Group<2, 4>());
+    if (N <= 16) return f(Group<2, 8>());
     if (N <= 32) return f(Group<4, 8>());
-    return f(Group<8, 8>());
+    return f(Group<4, 16>());
 }
 
+// Time chunks cost a second pass over most of the work and are taken where a launch would leave SIMDs without a wavefront: then as many
+// as give each four (1 x 16384 x 1024: 327 us with 8 chunks, 188 with 16, 173 with 32; 8 x 4096 x 2048: 386 us with one, 541 with two).
 Blocks forward_blocks(const sig_scan_args& a)
 {
     Blocks bl;
     bl.per_group = a.D / a.G;
     bl.runs = (unsigned)((bl.per_group + 63) / 64);
-    int64_t rows = a.B * a.G * bl.runs, waves = rows * with_group(a.N, [](auto gr) { return decltype(gr)::W; });
-    int64_t want = std::max<int64_t>(1, std::min<int64_t>(64, 2048 / std::max<int64_t>(1, waves)));
+    int64_t rows = a.B * a.G * bl.runs, waves = std::max<int64_t>(1, rows * with_group(a.N, [](auto gr) { return decltype(gr)::W; }));
+    int64_t want = waves >= 1024 ? 1 : std::min<int64_t>(64, 4096 / waves);
     int64_t tiles = std::max<int64_t>(1, tiles_of(a)), per = std::max<int64_t>(2, (tiles + want - 1) / want);
-    bl.chunk = per * kTile;
+    bl.chunk = (int)(per * kTile);
     bl.chunks = (unsigned)((tiles + per - 1) / per);
     bl.total = (unsigned)(rows * bl.chunks);
     return bl;
@@ -503,8 +600,13 @@ hipError_t scan_forward(const sig_scan_args& a, void* y, float* final_state, flo
         return with_group(a.N, [&](auto gr) {
             using T = decltype(t);
             using Gr = decltype(gr);
-            if (bl.chunks > 1) scan_fwd_kernel<T, Gr, false><<<(unsigned)bl.total, Gr::W * 64, 0, stream>>>(a, bl, cs, nullptr, nullptr, nullptr);
-            scan_fwd_kernel<T, Gr, true><<<(unsigned)bl.total, Gr::W * 64, 0, stream>>>(a, bl, cs, (T*)y, final_state, checkpoint);
+            constexpr int steps = 2 * kTile * 64 * 8, sums = 2 * Gr::W * kTile * 64 * 4;
+            if (steps + sums > 65536) {
+                hipError_t e = ensure_dynamic_lds((const void*)scan_fwd_kernel<T, Gr, true>, steps + sums);
+                if (e != hipSuccess) return e;
+            }
+            if (bl.chunks > 1) scan_fwd_kernel<T, Gr, false><<<bl.total, Gr::W * 64, steps, stream>>>(a, bl, cs, nullptr, nullptr, nullptr);
+            scan_fwd_kernel<T, Gr, true><<<bl.total, Gr::W * 64, steps + sums, stream>>>(a, bl, cs, (T*)y, final_state, checkpoint);
             return hipGetLastError();
         });
     });
