@@ -112,6 +112,8 @@ int sig_scan_backward(const sig_scan_args* a, const sig_scan_grads* g, const voi
     if (rc != SIG_OK) return rc;
     bool tokens = a->B > 0 && a->L > 0;
     if (!g || !g->grad_A || !scan_inputs_there(*a, tokens)) return SIG_EINVAL;
+    if (tokens && g->gy_stride_t < 0) return SIG_EINVAL;
+    if (tokens && g->gy_stride_t >= (1 << 26)) return SIG_ETOOLARGE;
     if ((a->skip && !g->grad_skip) || (a->dt_bias && !g->grad_dt_bias)) return SIG_EINVAL;
     if (tokens && (!g->grad_y || !g->grad_x || !g->grad_dt || !g->grad_b || !g->grad_c || (a->gate && !g->grad_gate))) return SIG_EINVAL;
     if (checkpoint_bytes < ckpt_bytes(*a) || (tokens && !checkpoint)) return SIG_EWORKSPACE;

@@ -45,12 +45,6 @@ template <int Q> __device__ __forceinline__ float sum_states(float v)     // ove
     for (int m = 1; m < Q; m *= 2) v += __shfl_xor(v, m);
     return v;
 }
-template <int Q> __device__ __forceinline__ float sum_channels(float v)   // over the channels of the wavefront
-{
-#pragma unroll
-    for (int m = Q; m < 64; m *= 2) v += __shfl_xor(v, m);
-    return v;
-}
 
 // what a lane knows of its channel
 template <class T, class Sh> struct Lane {
@@ -382,124 +376,373 @@ __global__ __launch_bounds__(Gr::W * 64, Gr::W > 2 && Gr::S == 4 ? 4 : 2) void s
     }
 }
 
-// Tiles of kTile tokens from the last to the first: the states inside a tile are computed again from the checkpoint before it and stay
-// in registers with their decays; the adjoint states walk back over them.
-template <class T, class Sh>
-__global__ __launch_bounds__(kThreads) void scan_bwd_kernel(sig_scan_args a, sig_scan_grads g, Rows r, const float* checkpoint, int64_t tiles,
-                                                            float* part_bc, float* part_a, float* part_d)
+// ---- backward
+// The same workgroups, tiles from the last to the first.  The states of a tile are computed again from the checkpoint before it and stay in
+// registers with their decays (with four states a wavefront the decays are computed twice instead: the registers hold one of the two);
+// the adjoint states walk back over them.  Three sums over states a token (for dx, dD and, for the gate, y) meet in LDS by half tiles, two
+// barriers a tile.  dB and dC are sums over channels, that is over lanes: a reduction that halves the number of values at each of its
+// six steps leaves the 64 sums of 16 tokens (2 states, dB and dC) one to a lane in 129 instructions, where a sum to all lanes would take six for
+// each; the workgroups' sums are added by a second kernel in their order, no atomics.
+template <int K, int S> __device__ __forceinline__ void add_broadcast(float (&o)[S], float r, float v)      // o[s] += r[K + s] v
 {
-    constexpr int S = Sh::S;
-    int64_t row = (int64_t)blockIdx.x * (kThreads / 64) + threadIdx.x / 64;
-    if (row >= r.total) return;
-    Lane<T, Sh> l(a, r, row);
-    int n = (int)min((int64_t)S, a.N - l.q * S);
-    float adj[S], gA[S] = {}, gskip = 0.0f, gbias = 0.0f;     // adj: a_{t+1} l_{t+1}
-    load_states(adj, g.grad_final_state ? g.grad_final_state + l.state(a) : nullptr, n);
-    const T* gy = (const T*)g.grad_y + l.b * g.gy_stride_b + l.d;
-    int64_t out = l.b * a.L * a.D + l.d;
-    T *gx = (T*)g.grad_x + out, *gdt = (T*)g.grad_dt + out, *gz = l.gate ? (T*)g.grad_gate + out : nullptr;
-    if (l.on && l.q == 0)
-        for (int64_t t = l.len; t < a.L; t++) {
-            gx[t * a.D] = gdt[t * a.D] = from_float<T>(0.0f);
-            if (gz) gz[t * a.D] = from_float<T>(0.0f);
+    static_assert(S == 2 || S == 4, "states of a wavefront");
+    if constexpr (S == 2)
+        asm("s_nop 1\n\tv_fmac_f32_dpp %0, %2, %3 row_newbcast:%4 row_mask:0xf bank_mask:0xf\n\tv_fmac_f32_dpp %1, %2, %3 row_newbcast:%5 row_mask:0xf bank_mask:0xf"
+            : "+v"(o[0]), "+v"(o[1]) : "v"(r), "v"(v), "n"(K), "n"(K + 1));
+    else
+        asm("s_nop 1\n\tv_fmac_f32_dpp %0, %4, %5 row_newbcast:%6 row_mask:0xf bank_mask:0xf\n\tv_fmac_f32_dpp %1, %4, %5 row_newbcast:%7 row_mask:0xf bank_mask:0xf\n\t"
+            "v_fmac_f32_dpp %2, %4, %5 row_newbcast:%8 row_mask:0xf bank_mask:0xf\n\tv_fmac_f32_dpp %3, %4, %5 row_newbcast:%9 row_mask:0xf bank_mask:0xf"
+            : "+v"(o[0]), "+v"(o[1]), "+v"(o[2]), "+v"(o[3]) : "v"(r), "v"(v), "n"(K), "n"(K + 1), "n"(K + 2), "n"(K + 3));
+}
+// Steps of the reduction over lanes: from a and b one register that holds, where the lane's bit is clear, a's sum over the two lanes that
+// differ in that bit, and b's where it is set.
+__device__ __forceinline__ float fold5(float a, float b)
+{
+    auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(a), __float_as_uint(b), false, false);
+    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+__device__ __forceinline__ float fold4(float a, float b)
+{
+    auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(a), __float_as_uint(b), false, false);
+    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+__device__ __forceinline__ float fold3(float a, float b)       // banks of four lanes: 0, 1 take a, 2, 3 take b
+{
+    float r;
+    asm("s_nop 1\n\tv_add_f32_dpp %0, %1, %1 row_ror:8 row_mask:0xf bank_mask:0x3\n\tv_add_f32_dpp %0, %2, %2 row_ror:8 row_mask:0xf bank_mask:0xc" : "=&v"(r) : "v"(a), "v"(b));
+    return r;
+}
+__device__ __forceinline__ float fold2(float a, float b)       // 0, 2 take a, 1, 3 take b
+{
+    float r;
+    asm("s_nop 1\n\tv_add_f32_dpp %0, %1, %1 row_ror:12 row_mask:0xf bank_mask:0x5\n\tv_add_f32_dpp %0, %2, %2 row_ror:4 row_mask:0xf bank_mask:0xa" : "=&v"(r) : "v"(a), "v"(b));
+    return r;
+}
+template <int Bit> __device__ __forceinline__ float fold_quad(float a, float b, int lane)      // bits 1 and 0, within four lanes
+{
+    float keep = lane & (1 << Bit) ? b : a, send = lane & (1 << Bit) ? a : b;
+    return keep + __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(send), Bit ? 0x4e : 0xb1, 0xf, 0xf, true));
+}
+// the token of a tile whose sums a lane has in the end: its four lower bits, reversed
+__device__ __forceinline__ int token_of(int lane) { return (lane & 1) << 3 | (lane & 2) << 1 | (lane & 4) >> 1 | (lane & 8) >> 3; }
+
+// float32 arrays of a backward launch
+struct Parts {
+    float* bc;           // [B, tiles, G, runs, W, S / 2, 64] sums of a workgroup's channels
+    float* A;            // [B, chunks, N, D]
+    float* rest;         // [B, chunks, W, 2, D] dskip, ddt_bias
+};
+
+// kFull = false: the adjoint states of a time chunk alone, from zero at its end (see ChunkStates).
+template <class T, class Gr, bool kFull>
+__global__ __launch_bounds__(Gr::W * 64, Gr::W > 8 ? 4 : 2) void scan_bwd_kernel(sig_scan_args a, sig_scan_grads g, Blocks bl, ChunkStates cs, const float* checkpoint, Parts parts)
+{
+    constexpr int S = Gr::S, W = Gr::W, PT = kTile / W, PH = PT > 1 ? PT / 2 : 1, RT = 16 / S, KB = kTile / RT, kHalf = kTile / 2, Q = S / 2;
+    constexpr bool kDecays = S == 2, kTwice = W <= 8;      // decays stay in registers; the sums' LDS is there for either half of a tile
+    constexpr unsigned E = sizeof(T);
+    extern __shared__ float lds[];
+    float4(*in)[kTile / 4][64] = (float4(*)[kTile / 4][64])lds;                                          // [2][3: D, D x, dL/ds][kTile / 4][64]
+    float4(*sums)[3][kHalf / 4][64] = (float4(*)[3][kHalf / 4][64])(lds + 2 * 3 * kTile * 64);           // [2 or 1][W][3][kHalf / 4][64]
+    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+    const unsigned c = blockIdx.x % bl.chunks, rest = blockIdx.x / bl.chunks, run = rest % bl.runs, bg = rest / bl.runs;
+    const int64_t grp = bg % (unsigned)a.G, b = bg / (unsigned)a.G;
+    const int64_t d0 = grp * bl.per_group + run * 64;
+    const bool on = run * 64 + lane < bl.per_group;
+    const unsigned e = on ? lane : 0;                      // lanes without a channel read the first one's, add nothing and store nothing
+    const int64_t d = d0 + e;
+    const int len = (int)live_length(a.lengths, b, a.L), t_first = (int)c * bl.chunk, t_end = min(t_first + bl.chunk, (int)a.L), live = min(t_end, len) - t_first;
+    const float bias = a.dt_bias ? a.dt_bias[d] : 0.0f, skip = a.skip ? a.skip[d] : 0.0f;
+    const uint32_t soft = a.softplus ? ~0u : 0u, gated = a.gate ? ~0u : 0u;
+    const int n0 = w * S;
+    const int64_t tiles = (a.L + kTile - 1) / kTile;
+    float A[S], A2[S], adj[S], gA[S] = {}, gskip = 0.0f, gbias = 0.0f, total = 0.0f;       // adj: a_{t+1} l_{t+1}
+#pragma unroll
+    for (int s = 0; s < S; s++) {
+        A[s] = n0 + s < a.N ? a.A[d * a.N + n0 + s] : 0.0f;
+        A2[s] = A[s] * kLog2e;
+        adj[s] = kFull && g.grad_final_state && n0 + s < a.N ? g.grad_final_state[(b * a.D + d) * a.N + n0 + s] : 0.0f;
+    }
+    if constexpr (kFull) {
+        const int after = (len - 1) / bl.chunk;            // the last chunk with tokens (len > 0)
+        for (int j = len > 0 ? after : 0; j > (int)c; j--) {
+            const int64_t row = b * bl.chunks + j;
+            float sum = cs.steps[row * a.D + d];
+#pragma unroll
+            for (int s = 0; s < S; s++)
+                if (n0 + s < a.N) adj[s] = fmaf(__builtin_amdgcn_exp2f(A2[s] * sum), adj[s], cs.last[(row * a.N + n0 + s) * a.D + d]);
         }
-    for (int64_t tile = (l.len + kTile - 1) / kTile - 1; tile >= 0; tile--) {
-        int64_t t0 = tile * kTile;
-        int m = (int)min((int64_t)kTile, l.len - t0);
-        float h0[S], h[kTile][S], e[kTile][S], x[kTile], D[kTile], raw[kTile];
+    }
+    // tiles with tokens that count, and the tokens of the last one: none for a chunk beyond the stream's length
+    const int n_tiles = live > 0 ? (live + kTile - 1) / kTile : 0, n_last = n_tiles > 0 ? live - (n_tiles - 1) * kTile : 0;
+    // rows of the last tile's first token; they go back a tile at a time
+    const int64_t t1 = t_first + (int64_t)(n_tiles - 1) * kTile;
+    const T *px = (const T*)a.x + b * a.x_stride_b + t1 * a.x_stride_t + d0, *pdt = (const T*)a.dt + b * a.dt_stride_b + t1 * a.dt_stride_t + d0;
+    const T *pz = a.gate ? (const T*)a.gate + b * a.gate_stride_b + t1 * a.gate_stride_t + d0 : px, *pg = (const T*)g.grad_y + b * g.gy_stride_b + t1 * g.gy_stride_t + d0;
+    const T *pb = (const T*)a.b + b * a.b_stride_b + grp * a.b_stride_g + t1 * a.b_stride_t + n0, *pc = (const T*)a.c + b * a.c_stride_b + grp * a.c_stride_g + t1 * a.c_stride_t + n0;
+    const float* ph = kFull ? checkpoint + ((b * tiles + t1 / kTile) * a.N + n0) * a.D + d0 : nullptr;
+    const int64_t out = (b * a.L + t1) * a.D + d0;
+    T *qx = (T*)g.grad_x + out, *qdt = (T*)g.grad_dt + out, *qz = (T*)g.grad_gate + out;
+    const unsigned x_row = (unsigned)a.x_stride_t * E, dt_row = (unsigned)a.dt_stride_t * E, z_row = gated ? (unsigned)a.gate_stride_t * E : x_row, g_row = (unsigned)g.gy_stride_t * E;
+    const unsigned y_row = (unsigned)a.D * E, b_row = (unsigned)(RT * a.b_stride_t) * E, c_row = (unsigned)(RT * a.c_stride_t) * E;
+    const int tb = n0 + lane % S < a.N ? lane % 16 / S : INT_MAX / 2;
+    const unsigned b_at = (unsigned)(lane % 16 / S * a.b_stride_t + lane % S) * E, c_at = (unsigned)(lane % 16 / S * a.c_stride_t + lane % S) * E;
+    auto own = [&](int half, int i) { return PT > 1 ? half * kHalf + w * PH + i : w; };       // the tokens that the wavefront prepares and stores
+
+    T x[PT], dt[PT], z[PT], up[PT], bv[KB], cv[KB];
+    float hv[S];
+    auto fetch = [&](int n) {              // the tile at the row pointers, n tokens of it
+        Buffer rx = buffer_at(px), rdt = buffer_at(pdt), rz = buffer_at(pz), rg = buffer_at(pg), rb = buffer_at(pb), rc = buffer_at(pc), rh = buffer_at(ph);
 #pragma unroll
-        for (int s = 0; s < S; s++) h0[s] = s < n ? checkpoint[((l.b * tiles + tile) * a.N + l.q * S + s) * a.D + l.d] : 0.0f;
-#pragma unroll
-        for (int i = 0; i < kTile; i++) {
-            int64_t t = t0 + (i < m ? i : 0);
-            float B[S];
-            x[i] = to_float(l.x[t * a.x_stride_t]);
-            raw[i] = to_float(l.dt[t * a.dt_stride_t]) + l.bias;
-            D[i] = a.softplus ? softplus(raw[i]) : raw[i];
-            load_row(B, l.B + t * a.b_stride_t, n);
-#pragma unroll
-            for (int s = 0; s < S; s++) {
-                e[i][s] = fast_exp(D[i] * l.A[s]);
-                h[i][s] = fmaf(e[i][s], i ? h[i - 1][s] : h0[s], D[i] * x[i] * B[s]);
-            }
+        for (int i = 0; i < PT; i++) {
+            int k = own(i / PH, i % PH);
+            unsigned at = k < n ? e * E : kNowhere;
+            if (kFull) x[i] = buffer_load<T>(rx, at, k * x_row);
+            dt[i] = buffer_load<T>(rdt, at, k * dt_row);
+            z[i] = buffer_load<T>(rz, at, k * z_row);
+            up[i] = buffer_load<T>(rg, at, k * g_row);
         }
 #pragma unroll
-        for (int i = kTile - 1; i >= 0; i--) {
-            if (i >= m) continue;
-            int64_t t = t0 + i;
-            float B[S], C[S], up = to_float(gy[t * g.gy_stride_t]), o = 0.0f, gB[S], gC[S], dx = 0.0f, dD = 0.0f;
-            load_row(B, l.B + t * a.b_stride_t, n);
-            load_row(C, l.C + t * a.c_stride_t, n);
-            if (l.gate) {
-                float z = to_float(l.gate[t * a.gate_stride_t]), p = sigmoid(z);
+        for (int j = 0; j < KB; j++) {
+            bool there = j * RT + tb < n;
+            if (kFull) bv[j] = buffer_load<T>(rb, there ? b_at : kNowhere, j * b_row);
+            cv[j] = buffer_load<T>(rc, there ? c_at : kNowhere, j * c_row);
+        }
+        if (kFull)
 #pragma unroll
-                for (int s = 0; s < S; s++) o = fmaf(C[s], h[i][s], o);
-                o = fmaf(l.skip, x[i], sum_states<Sh::Q>(o));
-                if (l.on && l.q == 0) gz[t * a.D] = from_float<T>(up * o * p * fmaf(z, 1.0f - p, 1.0f));
-                up *= z * p;
-            }
+            for (int s = 0; s < S; s++) hv[s] = buffer_load<float>(rh, n > 0 && n0 + s < a.N ? e * 4 : kNowhere, (unsigned)(s * a.D) * 4);
+        px -= kTile * a.x_stride_t, pdt -= kTile * a.dt_stride_t, pz -= kTile * (gated ? a.gate_stride_t : a.x_stride_t), pg -= kTile * g.gy_stride_t;
+        pb -= kTile * a.b_stride_t, pc -= kTile * a.c_stride_t, ph -= a.N * a.D;
+    };
+    // of each of the wavefront's tokens: x, D, dL/ds, dD/d(dt + bias), dL/dy times the gate's slope; of the tile at work and the one after it
+    float xs[2][PT], Ds[2][PT], us[2][PT], sl[2][PT], gs[2][PT];
+    int counts[2] = {0, 0}, rooms[2] = {kTile, kTile};     // tokens of the tile that count, and that the chunk has
+    auto prepare = [&](int slot, float4 (*to)[kTile / 4][64], int n, int room) {
+        counts[slot] = n, rooms[slot] = room;
 #pragma unroll
-            for (int s = 0; s < S; s++) {
-                float lam = fmaf(C[s], up, adj[s]), keep;
-                adj[s] = lam * e[i][s];
-                keep = adj[s] * (i ? h[i - 1][s] : h0[s]);
-                gC[s] = sum_channels<Sh::Q>(l.on ? up * h[i][s] : 0.0f);
-                gB[s] = sum_channels<Sh::Q>(l.on ? lam * D[i] * x[i] : 0.0f);
-                gA[s] = fmaf(keep, D[i], gA[s]);
-                dx = fmaf(lam, B[s], dx);
-                dD = fmaf(keep, l.A[s], dD);
-            }
-            dx = sum_states<Sh::Q>(dx), dD = sum_states<Sh::Q>(dD);
-            dD = fmaf(dx, x[i], dD);
-            if (a.softplus) dD *= sigmoid(raw[i]);
-            gskip = fmaf(up, x[i], gskip);
+        for (int i = 0; i < PT; i++) {
+            int k = own(i / PH, i % PH);
+            uint32_t there = k < n ? ~0u : 0u;
+            float raw = to_float(dt[i]) + bias, zf = to_float(z[i]), gy = to_float(up[i]), p = sigmoid(zf), v = kFull ? to_float(x[i]) : 0.0f;
+            float D = only_if(there, either(soft, softplus(raw), raw)), u = gy * either(gated, zf * p, 1.0f);
+            xs[slot][i] = v, Ds[slot][i] = D, us[slot][i] = u;
+            sl[slot][i] = either(soft, sigmoid(raw), 1.0f);
+            gs[slot][i] = gy * p * fmaf(zf, 1.0f - p, 1.0f);
+            ((float*)&to[0][k / 4][lane])[k % 4] = D;
+            if (kFull) ((float*)&to[1][k / 4][lane])[k % 4] = on ? D * v : 0.0f;
+            ((float*)&to[2][k / 4][lane])[k % 4] = !kFull || on ? u : 0.0f;
+        }
+    };
+    // the gradients of a half's tokens; from: the wavefronts' sums
+    auto put = [&](int half, int slot, const float4 (*from)[3][kHalf / 4][64]) {
+        const int n = counts[slot], room = rooms[slot];
+        Buffer rx = buffer_at(qx), rdt = buffer_at(qdt), rz = buffer_at(qz);
+#pragma unroll
+        for (int i = 0; i < PH; i++) {
+            if (PT == 1 && w / kHalf != half) continue;
+            const int k = own(half, i), kh = k % kHalf, m = PT > 1 ? half * PH + i : 0;
+            float r[3] = {0.0f, 0.0f, skip * xs[slot][m]};
+#pragma unroll
+            for (int v = 0; v < W; v++)
+#pragma unroll
+                for (int q = 0; q < 3; q++) r[q] += ((const float*)&from[v][q][kh / 4][lane])[kh % 4];
+            const bool there = k < n;
+            const float D = Ds[slot][m], u = us[slot][m], v = xs[slot][m];
+            float dx = there ? fmaf(r[0], D, skip * u) : 0.0f, dD = there ? fmaf(r[0], v, r[1]) * sl[slot][m] : 0.0f, dz = there ? gs[slot][m] * r[2] : 0.0f;
+            gskip = fmaf(there ? u : 0.0f, v, gskip);
             gbias += dD;
-            if (l.on && l.q == 0) {
-                gx[t * a.D] = from_float<T>(fmaf(dx, D[i], l.skip * up));
-                gdt[t * a.D] = from_float<T>(dD);
-            }
-            if ((threadIdx.x & 63) < Sh::Q) {
-                int64_t at = (((l.b * a.L + t) * a.G + l.g) * r.runs + row % r.runs) * 2 * a.N + l.q * S;
-                for (int s = 0; s < n; s++) part_bc[at + s] = gB[s], part_bc[at + a.N + s] = gC[s];
-            }
+            const unsigned at = on && k < room ? e * E : kNowhere;
+            buffer_store(rx, at, k * y_row, from_float<T>(dx));
+            buffer_store(rdt, at, k * y_row, from_float<T>(dD));
+            buffer_store(rz, gated ? at : kNowhere, k * y_row, from_float<T>(dz));
         }
+    };
+    fetch(n_last);
+    float B[KB], C[KB], h0[S];
+    auto take = [&](float (&Bn)[KB], float (&Cn)[KB], float (&hn)[S]) {
+#pragma unroll
+        for (int j = 0; j < KB; j++) Bn[j] = kFull ? to_float(bv[j]) : 0.0f, Cn[j] = to_float(cv[j]);
+#pragma unroll
+        for (int s = 0; s < S; s++) hn[s] = kFull ? hv[s] : 0.0f;
+    };
+    take(B, C, h0);
+    prepare(0, in, n_last, t_end - t_first - (n_tiles - 1) * kTile);
+    fetch(n_tiles > 1 ? kTile : 0);
+    __syncthreads();
+    int tile = n_tiles - 1;
+    auto work = [&](auto parity) {
+        constexpr int slot = decltype(parity)::value;
+        const float4(*now)[kTile / 4][64] = in + slot * 3;
+        float4(*upper)[3][kHalf / 4][64] = sums, (*lower)[3][kHalf / 4][64] = sums + (kTwice ? W : 0);
+        const bool first = tile == n_tiles - 1;
+        float Bn[KB], Cn[KB], hn[S], group[4][Q];
+        take(Bn, Cn, hn);
+        if (kFull && !first) {             // what is left of the tile before
+            put(0, slot ^ 1, lower);
+            qx -= kTile * a.D, qdt -= kTile * a.D, qz -= kTile * a.D;
+            if (!kTwice) __syncthreads();
+        }
+        prepare(slot ^ 1, in + (slot ^ 1) * 3, tile > 0 ? kTile : 0, kTile);
+        fetch(tile > 1 ? kTile : 0);
+        // D[t], D[t] x[t] and dL/ds[t] of four tokens from LDS
+        auto four = [&](int q, int i, float (&v)[4]) {
+            float4 r = now[q][i / 4][lane];
+            v[0] = r.x, v[1] = r.y, v[2] = r.z, v[3] = r.w;
+        };
+        float h[kFull ? kTile + 1 : 1][S], decay[kDecays && kFull ? kTile : 1][S];       // h[t + 1]: after token t
+        if constexpr (kFull) {
+#pragma unroll
+            for (int s = 0; s < S; s++) h[0][s] = h0[s];
+            unrolled<0, kTile / 4>([&](auto jt) {
+                constexpr int i = decltype(jt)::value * 4, k = i % RT * S;
+                float D[4], u[4];
+                four(0, i, D), four(1, i, u);
+                unrolled<0, 4>([&](auto it) {
+                    constexpr int j = decltype(it)::value;
+                    unrolled<0, S>([&](auto is) {
+                        constexpr int s = decltype(is)::value;
+                        float f = __builtin_amdgcn_exp2f(D[j] * A2[s]);
+                        if constexpr (kDecays) decay[i + j][s] = f;
+                        h[i + j + 1][s] = fmaf(f, h[i + j][s], times_broadcast<k + j * S + s>(B[i / RT], u[j]));
+                    });
+                });
+            });
+        }
+        auto back = [&](auto half_) {
+            constexpr int half = decltype(half_)::value;
+            unrolled<0, kHalf / 4>([&](auto jt) {
+                constexpr int q = kHalf / 4 - 1 - decltype(jt)::value, i = half * kHalf + q * 4, k = i % RT * S;
+                float D[4], u[4], v[4], lam[4][S], ht[4][S], dD[4] = {}, o[4], fold[4][Q];
+                four(0, i, D), four(2, i, v);
+                if (kFull) four(1, i, u);
+                unrolled<0, 4>([&](auto it) {
+                    constexpr int j = 3 - decltype(it)::value;
+                    add_broadcast<k + j * S, S>(adj, C[i / RT], v[j]);
+#pragma unroll
+                    for (int s = 0; s < S; s++) {
+                        lam[j][s] = adj[s];
+                        float f;
+                        if constexpr (kDecays && kFull) f = decay[i + j][s];
+                        else f = __builtin_amdgcn_exp2f(D[j] * A2[s]);
+                        adj[s] = lam[j][s] * f;
+                        if constexpr (kFull) {
+                            ht[j][s] = h[i + j + 1][s];
+                            float keep = adj[s] * h[i + j][s];
+                            gA[s] = fmaf(keep, D[j], gA[s]);
+                            dD[j] = fmaf(keep, A[s], dD[j]);
+                        }
+                    }
+                    if constexpr (kFull) {
+#pragma unroll
+                        for (int m = 0; m < Q; m++)
+                            fold[j][m] = fold4(fold5(lam[j][2 * m] * u[j], v[j] * ht[j][2 * m]), fold5(lam[j][2 * m + 1] * u[j], v[j] * ht[j][2 * m + 1]));
+                    } else {
+                        total += D[j];
+                    }
+                });
+                if constexpr (kFull) {
+#pragma unroll
+                    for (int m = 0; m < Q; m++) group[i / 4][m] = fold2(fold3(fold[0][m], fold[1][m]), fold3(fold[2][m], fold[3][m]));
+                    float4(*to)[3][kHalf / 4][64] = half ? upper : lower;
+                    sum_broadcast<k>(o, B[i / RT], lam);
+                    to[w][0][q][lane] = make_float4(o[0], o[1], o[2], o[3]);
+                    to[w][1][q][lane] = make_float4(dD[0], dD[1], dD[2], dD[3]);
+                    sum_broadcast<k>(o, C[i / RT], ht);
+                    to[w][2][q][lane] = make_float4(o[0], o[1], o[2], o[3]);
+                }
+            });
+        };
+        back(std::integral_constant<int, 1>());
+        if constexpr (kFull) {
+            __syncthreads();
+            put(1, slot, upper);
+            if (!kTwice) __syncthreads();
+        }
+        back(std::integral_constant<int, 0>());
+        if constexpr (kFull) {
+            float* to = parts.bc + ((((b * tiles + t_first / kTile + tile) * a.G + grp) * bl.runs + run) * W + w) * Q * 64;
+#pragma unroll
+            for (int m = 0; m < Q; m++)
+                (to + m * 64)[lane] = fold_quad<0>(fold_quad<1>(group[0][m], group[1][m], lane), fold_quad<1>(group[2][m], group[3][m], lane), lane);
+        }
+#pragma unroll
+        for (int j = 0; j < KB; j++) B[j] = Bn[j], C[j] = Cn[j];
+#pragma unroll
+        for (int s = 0; s < S; s++) h0[s] = hn[s];
+        tile--;
+        __syncthreads();
+    };
+    unsigned turn = 0;
+    while (tile >= 0) {
+        work(std::integral_constant<int, 0>());
+        turn = 0;
+        if (tile < 0) break;
+        work(std::integral_constant<int, 1>());
+        turn = 1;
     }
-    if (!l.on) return;
-    for (int s = 0; s < n; s++) {
-        part_a[l.state(a) + s] = gA[s];
-        if (g.grad_initial_state) g.grad_initial_state[l.state(a) + s] = adj[s];
-    }
-    if (l.q == 0) {
-        part_d[(l.b * 2 + 0) * a.D + l.d] = gskip;
-        part_d[(l.b * 2 + 1) * a.D + l.d] = gbias;
+    if constexpr (kFull) {
+        if (n_tiles > 0) {
+            float4(*lower)[3][kHalf / 4][64] = sums + (kTwice ? W : 0);
+            if (turn) put(0, 1, lower);
+            else put(0, 0, lower);
+        }
+        // tokens that do not count
+        T *rx = (T*)g.grad_x + (b * a.L + t_first) * a.D + d0, *rdt = (T*)g.grad_dt + (b * a.L + t_first) * a.D + d0, *rz = (T*)g.grad_gate + (b * a.L + t_first) * a.D + d0;
+        for (int64_t t = n_tiles * kTile + w; t < t_end - t_first; t += W)
+            if (on) {
+                rx[t * a.D + e] = rdt[t * a.D + e] = from_float<T>(0.0f);
+                if (gated) rz[t * a.D + e] = from_float<T>(0.0f);
+            }
+        if (!on) return;
+        const int64_t row = b * bl.chunks + c;
+#pragma unroll
+        for (int s = 0; s < S; s++)
+            if (n0 + s < a.N) {
+                parts.A[(row * a.N + n0 + s) * a.D + d] = gA[s];
+                if (g.grad_initial_state && c == 0) g.grad_initial_state[(b * a.D + d) * a.N + n0 + s] = adj[s];
+            }
+        parts.rest[((row * W + w) * 2 + 0) * a.D + d] = gskip;
+        parts.rest[((row * W + w) * 2 + 1) * a.D + d] = gbias;
+    } else {
+        if (!on) return;
+        const int64_t row = b * bl.chunks + c;
+#pragma unroll
+        for (int s = 0; s < S; s++)
+            if (n0 + s < a.N) cs.last[(row * a.N + n0 + s) * a.D + d] = adj[s];
+        if (w == 0) cs.steps[row * a.D + d] = total;
     }
 }
 
-// dB and dC of a token: the sums over the runs of its group's channels, in their order
-template <class T> __global__ __launch_bounds__(kThreads) void scan_bwd_bc_kernel(sig_scan_args a, Rows r, const float* part, T* gB, T* gC)
+// dB and dC of a tile: the sums over the workgroups of its group's channels, in their order
+template <class T, class Gr> __global__ __launch_bounds__(kThreads) void scan_bwd_bc_kernel(sig_scan_args a, Blocks bl, const float* part, T* gB, T* gC)
 {
-    int64_t id = (int64_t)blockIdx.x * kThreads + threadIdx.x, N2 = 2 * a.N;
-    if (id >= a.B * a.L * a.G * N2) return;
-    int64_t k = id % N2, tok = id / N2, t = tok / a.G % a.L, b = tok / a.G / a.L;
+    constexpr int Q = Gr::S / 2, R = Gr::W * Q;
+    const int64_t id = (int64_t)blockIdx.x * (kThreads / 64) + threadIdx.x / 64, tiles = (a.L + kTile - 1) / kTile;      // a wavefront for each [.., W, Q]
+    if (id >= a.B * tiles * a.G * R) return;
+    const int lane = threadIdx.x & 63, r = (int)(id % R);
+    const int64_t grp = id / R % a.G, tile = id / R / a.G % tiles, b = id / R / a.G / tiles, t = tile * kTile + token_of(lane);
+    const int n = r / Q * Gr::S + r % Q * 2 + (lane >> 4 & 1);
+    const int64_t len = live_length(a.lengths, b, a.L);
     float v = 0.0f;
-    if (t < live_length(a.lengths, b, a.L))
-        for (int64_t j = 0; j < r.runs; j++) v += part[(tok * r.runs + j) * N2 + k];
-    (k < a.N ? gB : gC)[tok * a.N + k % a.N] = from_float<T>(v);
+    if (tile * kTile < len) {
+        const float* p = part + (((b * tiles + tile) * a.G + grp) * bl.runs * R + r) * 64 + lane;
+        for (unsigned j = 0; j < bl.runs; j++, p += R * 64) v += *p;
+    }
+    if (t < a.L && n < a.N) (lane & 32 ? gC : gB)[((b * a.L + t) * a.G + grp) * a.N + n] = from_float<T>(t < len ? v : 0.0f);
 }
 
-// dA, dskip and ddt_bias: the sums over the streams, in their order
-__global__ __launch_bounds__(kThreads) void scan_bwd_params_kernel(sig_scan_args a, const float* part_a, const float* part_d, float* gA, float* gskip, float* gbias)
+// dA, dskip and ddt_bias: the sums over streams, time chunks and wavefronts, in their order
+__global__ __launch_bounds__(kThreads) void scan_bwd_params_kernel(sig_scan_args a, int64_t rows, int64_t waves, Parts parts, float* gA, float* gskip, float* gbias)
 {
-    int64_t id = (int64_t)blockIdx.x * kThreads + threadIdx.x, DN = a.D * a.N;
+    const int64_t id = (int64_t)blockIdx.x * kThreads + threadIdx.x, DN = a.D * a.N;
     float v = 0.0f;
     if (id < DN) {
-        for (int64_t b = 0; b < a.B; b++) v += part_a[b * DN + id];
-        gA[id] = v;
+        for (int64_t r = 0; r < rows; r++) v += parts.A[r * DN + id];
+        gA[id % a.D * a.N + id / a.D] = v;
     } else if (id < DN + 2 * a.D) {
-        int64_t k = (id - DN) / a.D, d = (id - DN) % a.D;
+        const int64_t k = (id - DN) / a.D, d = (id - DN) % a.D;
         float* to = k ? gbias : gskip;
         if (!to) return;
-        for (int64_t b = 0; b < a.B; b++) v += part_d[(b * 2 + k) * a.D + d];
+        for (int64_t r = 0; r < rows * waves; r++) v += parts.rest[(r * 2 + k) * a.D + d];
         to[d] = v;
     }
 }
@@ -558,7 +801,7 @@ template <class F> auto with_group(int64_t N, F f)
 
 // Time chunks cost a second pass over most of the work and are taken where a launch would leave SIMDs without a wavefront: then as many
 // as give each four (1 x 16384 x 1024: 327 us with 8 chunks, 188 with 16, 173 with 32; 8 x 4096 x 2048: 386 us with one, 541 with two).
-Blocks forward_blocks(const sig_scan_args& a)
+Blocks blocks_of(const sig_scan_args& a)
 {
     Blocks bl;
     bl.per_group = a.D / a.G;
@@ -572,29 +815,29 @@ Blocks forward_blocks(const sig_scan_args& a)
     return bl;
 }
 
-struct BackwardParts { size_t bc, a, d; };
-BackwardParts backward_parts(const sig_scan_args& a)
+// floats of the chunks' states, and of a backward launch's sums
+size_t chunk_floats(const sig_scan_args& a, const Blocks& bl) { return bl.chunks > 1 ? (size_t)(a.B * bl.chunks * a.D * (a.N + 1)) : 0; }
+struct PartFloats { size_t bc, A, rest; };
+PartFloats part_floats(const sig_scan_args& a, const Blocks& bl)
 {
-    int64_t runs = with_shape(a.N, [&](auto sh) { return rows_of<decltype(sh)>(a).runs; });
-    return {(size_t)(a.B * a.L * a.G * runs * 2 * a.N), (size_t)(a.B * a.D * a.N), (size_t)(a.B * 2 * a.D)};
+    int64_t W = 0, Q = 0;
+    with_group(a.N, [&](auto gr) { W = decltype(gr)::W, Q = decltype(gr)::S / 2; return 0; });
+    return {(size_t)(a.B * tiles_of(a) * a.G * bl.runs * W * Q * 64), (size_t)(a.B * bl.chunks * a.N * a.D), (size_t)(a.B * bl.chunks * W * 2 * a.D)};
 }
 
 }  // namespace
 
-size_t scan_forward_workspace(const sig_scan_args& a)
-{
-    Blocks bl = forward_blocks(a);
-    return bl.chunks > 1 ? (size_t)(a.B * bl.chunks * a.D * (a.N + 1) * 4) : 0;
-}
+size_t scan_forward_workspace(const sig_scan_args& a) { return chunk_floats(a, blocks_of(a)) * 4; }
 size_t scan_backward_workspace(const sig_scan_args& a)
 {
-    BackwardParts p = backward_parts(a);
-    return (p.bc + p.a + p.d) * 4;
+    Blocks bl = blocks_of(a);
+    PartFloats p = part_floats(a, bl);
+    return (p.bc + p.A + p.rest + chunk_floats(a, bl)) * 4;
 }
 
 hipError_t scan_forward(const sig_scan_args& a, void* y, float* final_state, float* checkpoint, float* workspace, hipStream_t stream)
 {
-    Blocks bl = forward_blocks(a);
+    Blocks bl = blocks_of(a);
     ChunkStates cs{workspace, workspace ? workspace + a.B * bl.chunks * a.N * a.D : nullptr};
     return with_type(a.dtype, [&](auto t) {
         return with_group(a.N, [&](auto gr) {
@@ -614,17 +857,26 @@ hipError_t scan_forward(const sig_scan_args& a, void* y, float* final_state, flo
 
 hipError_t scan_backward(const sig_scan_args& a, const sig_scan_grads& g, const float* checkpoint, float* workspace, hipStream_t stream)
 {
-    BackwardParts p = backward_parts(a);
-    float *bc = workspace, *pa = bc + p.bc, *pd = pa + p.a;
+    Blocks bl = blocks_of(a);
+    PartFloats p = part_floats(a, bl);
+    Parts parts{workspace, workspace + p.bc, workspace + p.bc + p.A};
+    float* states = parts.rest + p.rest;
+    ChunkStates cs{states, states + a.B * bl.chunks * a.N * a.D};
     return with_type(a.dtype, [&](auto t) {
-        return with_shape(a.N, [&](auto sh) {
+        return with_group(a.N, [&](auto gr) {
             using T = decltype(t);
-            using Sh = decltype(sh);
-            Rows r = rows_of<Sh>(a);
-            if (a.B > 0) scan_bwd_kernel<T, Sh><<<blocks_for(r.total * 64), kThreads, 0, stream>>>(a, g, r, checkpoint, tiles_of(a), bc, pa, pd);
-            if (a.B > 0 && a.L > 0)
-                scan_bwd_bc_kernel<T><<<blocks_for(a.B * a.L * a.G * 2 * a.N), kThreads, 0, stream>>>(a, r, bc, (T*)g.grad_b, (T*)g.grad_c);
-            scan_bwd_params_kernel<<<blocks_for(a.D * (a.N + 2)), kThreads, 0, stream>>>(a, pa, pd, g.grad_A, g.grad_skip, g.grad_dt_bias);
+            using Gr = decltype(gr);
+            constexpr int in = 2 * 3 * kTile * 64 * 4, sums = (Gr::W <= 8 ? 2 : 1) * Gr::W * 3 * kTile / 2 * 64 * 4;
+            if (in + sums > 65536) {
+                hipError_t e = ensure_dynamic_lds((const void*)scan_bwd_kernel<T, Gr, true>, in + sums);
+                if (e != hipSuccess) return e;
+            }
+            if (a.B > 0) {
+                if (bl.chunks > 1) scan_bwd_kernel<T, Gr, false><<<bl.total, Gr::W * 64, in, stream>>>(a, g, bl, cs, nullptr, parts);
+                scan_bwd_kernel<T, Gr, true><<<bl.total, Gr::W * 64, in + sums, stream>>>(a, g, bl, cs, checkpoint, parts);
+                if (a.L > 0) scan_bwd_bc_kernel<T, Gr><<<blocks_for(p.bc / bl.runs), kThreads, 0, stream>>>(a, bl, parts.bc, (T*)g.grad_b, (T*)g.grad_c);
+            }
+            scan_bwd_params_kernel<<<blocks_for(a.D * (a.N + 2)), kThreads, 0, stream>>>(a, a.B * bl.chunks, Gr::W, parts, g.grad_A, g.grad_skip, g.grad_dt_bias);
             return hipGetLastError();
         });
     });
