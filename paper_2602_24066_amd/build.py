@@ -16,9 +16,13 @@ HIPCC_FLAGS = ["-O3", "-std=c++17", "-fPIC", "--offload-arch=gfx950", "-Xclang",
                # matrix-instruction results stay in ordinary vector registers: the vector ALU reads them without
                # v_accvgpr_read copies (a quarter of the instructions of the backward kernels otherwise)
                "-mllvm", "-amdgpu-mfma-vgpr-form",
+               # (see NO_MAX_ILP for the exceptions)
                # instruction scheduling for latency hiding inside a wavefront rather than for occupancy, which launch
                # bounds fix anyway (two wavefronts per SIMD at most in the main kernels): measured 3-7 % on them
                "-mllvm", "-amdgpu-sched-strategy=max-ilp"]
+# kernels bound by memory, which need wavefronts more than instructions in order: the option doubles the registers of the
+# convolution (98 -> 196 at eight channels a thread)
+NO_MAX_ILP = ("kernels_conv.hip", "kernels_clip.hip")
 
 
 def hipcc() -> str:
@@ -35,7 +39,8 @@ def build(verbose: bool = False) -> str:
     procs = []
     for src in SOURCES:
         obj = os.path.join(bdir, src + ".o")
-        cmd = [hipcc(), *HIPCC_FLAGS, "-c", os.path.join(CSRC, src), "-o", obj]
+        flags = HIPCC_FLAGS[:-2] if src in NO_MAX_ILP else HIPCC_FLAGS
+        cmd = [hipcc(), *flags, "-c", os.path.join(CSRC, src), "-o", obj]
         if verbose:
             print(" ".join(cmd), flush=True)
         procs.append((src, subprocess.Popen(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)))

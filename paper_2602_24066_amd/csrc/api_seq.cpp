@@ -53,6 +53,15 @@ bool scan_inputs_there(const sig_scan_args& a, bool tokens)
     return a.A && (!tokens || (a.x && a.dt && a.b && a.c));
 }
 
+// Elements of a workgroup of the clipping kernels: 4,096 until the chip is full, then twice as many as often as it takes to keep the sums that
+// one workgroup adds up in the end few.
+int64_t clip_block(int64_t total)
+{
+    int64_t block = sig::kClipBlock;
+    while (total / block > sig::kClipBlocks && block < (1 << 30)) block *= 2;
+    return block;
+}
+
 size_t ckpt_bytes(const sig_scan_args& a) { return (size_t)(a.B * ((a.L + sig::kScanTile - 1) / sig::kScanTile) * a.D * a.N * 4); }
 
 }  // namespace
@@ -133,11 +142,12 @@ int sig_scan_step(const sig_scan_args* a, float* state, void* y, void* stream)
 size_t sig_grad_clip_workspace_bytes(int64_t n_tensors, const int64_t* sizes)
 {
     if (n_tensors <= 0 || !sizes) return 0;
-    int64_t blocks = 0;
+    int64_t total = 0, blocks = 0;
     for (int64_t i = 0; i < n_tensors; i++) {
-        if (sizes[i] < 0 || sizes[i] > kMost) return 0;
-        blocks += (sizes[i] + sig::kClipBlock - 1) / sig::kClipBlock;
+        if (sizes[i] < 0 || sizes[i] > kMost || (total += sizes[i]) > kMost) return 0;
     }
+    const int64_t block = clip_block(total);
+    for (int64_t i = 0; i < n_tensors; i++) blocks += (sizes[i] + block - 1) / block;
     return (size_t)blocks * sizeof(double);
 }
 
@@ -146,14 +156,14 @@ int sig_grad_clip(int64_t n_tensors, const void* const* in, void* const* out, co
 {
     if (n_tensors < 0 || !norm || !(max_norm >= 0.0f)) return SIG_EINVAL;
     if (n_tensors && (!in || !out || !sizes || !in_dtypes || !out_dtypes)) return SIG_EINVAL;
-    int64_t blocks = 0;
+    int64_t total = 0, blocks = 0;
     for (int64_t i = 0; i < n_tensors; i++) {
         if (sizes[i] < 0 || bad_type(in_dtypes[i]) || bad_type(out_dtypes[i])) return SIG_EINVAL;
         if (sizes[i] && (!in[i] || !out[i] || (in[i] == out[i] && in_dtypes[i] != out_dtypes[i]))) return SIG_EINVAL;
-        if (sizes[i] > kMost) return SIG_ETOOLARGE;
-        blocks += (sizes[i] + sig::kClipBlock - 1) / sig::kClipBlock;
-        if (blocks > (1 << 23)) return SIG_ETOOLARGE;       // what a launch can number
+        if (sizes[i] > kMost || (total += sizes[i]) > kMost) return SIG_ETOOLARGE;
     }
+    const int64_t block = clip_block(total);
+    for (int64_t i = 0; i < n_tensors; i++) blocks += (sizes[i] + block - 1) / block;
     if (workspace_bytes < (size_t)blocks * sizeof(double) || (blocks && !workspace)) return SIG_EWORKSPACE;
     hipStream_t s = (hipStream_t)stream;
     // all tables of the norm first, then its square root, then all tables of the products
@@ -161,6 +171,7 @@ int sig_grad_clip(int64_t n_tensors, const void* const* in, void* const* out, co
         double* part = (double*)workspace;
         sig::ClipTable tab;
         tab.n = 0;
+        tab.block = (uint32_t)block;
         for (int64_t i = 0; i <= n_tensors; i++) {
             if (i < n_tensors && sizes[i]) {
                 int k = tab.n++;
@@ -168,7 +179,7 @@ int sig_grad_clip(int64_t n_tensors, const void* const* in, void* const* out, co
                 tab.out[k] = out[i];
                 tab.size[k] = sizes[i];
                 tab.kind[k] = (uint8_t)(in_dtypes[i] | out_dtypes[i] << 1);
-                tab.end[k] = (k ? tab.end[k - 1] : 0) + (uint32_t)((sizes[i] + sig::kClipBlock - 1) / sig::kClipBlock);
+                tab.end[k] = (k ? tab.end[k - 1] : 0) + (uint32_t)((sizes[i] + block - 1) / block);
             }
             if (tab.n == 0 || (tab.n < sig::kClipTensors && i < n_tensors)) continue;
             hipError_t e = pass == 0 ? sig::norm_parts(tab, part, s) : sig::clip_scaled(tab, norm, max_norm, s);

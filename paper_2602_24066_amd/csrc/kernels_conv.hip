@@ -23,9 +23,9 @@ Split split_time(int64_t B, int64_t L, int64_t D, int V)
 {
     Split s;
     s.vecs = (D + V - 1) / V;
-    // two wavefronts on each SIMD (2,048 of 64 threads) hide the memory's latency here; chunks shorter than 16 tokens would
-    // read a fifth and more of their input twice
-    int64_t want = (int64_t)2048 * 64 / std::max<int64_t>(1, B * s.vecs) + 1;
+    // four wavefronts on each SIMD (4,096 of 64 threads), each with two groups of loads under way, hide the memory's latency; chunks
+    // shorter than 16 tokens would read a fifth and more of their input twice
+    int64_t want = (int64_t)4096 * 64 / std::max<int64_t>(1, B * s.vecs) + 1;
     s.chunk = std::max<int64_t>(16, (L + want - 1) / want);
     s.chunks = std::max<int64_t>(1, (L + s.chunk - 1) / s.chunk);
     s.threads = B * s.chunks * s.vecs;
@@ -86,23 +86,48 @@ __global__ __launch_bounds__(kThreads) void conv_fwd_kernel(sig_conv_args a, T* 
 #pragma unroll
         for (int k = 0; k < W - 1; k++) load_token<T, V, W>(r[k + 1], x, a.x_stride_t, initial, a.D, t0 - W + 1 + k);
     }
-    int64_t t = t0;
-    for (; t < end; t++, y += a.D) {
-#pragma unroll
-        for (int k = 0; k < W - 1; k++)
-#pragma unroll
-            for (int i = 0; i < V; i++) r[k][i] = r[k + 1][i];
-        load<T, V>(r[W - 1], x + t * a.x_stride_t);
+    auto token = [&](const float (&in)[V]) {
         float o[V];
 #pragma unroll
         for (int i = 0; i < V; i++) {
             o[i] = bias[i];
 #pragma unroll
-            for (int k = 0; k < W; k++) o[i] = fmaf(w[k][i], r[k][i], o[i]);
+            for (int k = 0; k < W - 1; k++) r[k][i] = r[k + 1][i], o[i] = fmaf(w[k][i], r[k][i], o[i]);
+            r[W - 1][i] = in[i];
+            o[i] = fmaf(w[W - 1][i], in[i], o[i]);
             if (a.silu) o[i] *= sigmoid(o[i]);
         }
         store<T, V>(y, o);
+        y += a.D;
+    };
+    // groups of U tokens, the next one's loads under way while one is worked on
+    constexpr int U = V >= 4 ? 4 : 8;
+    int64_t t = t0;
+    x += t0 * a.x_stride_t;
+    Pack<T, V> now[U], next[U];
+    auto fetch = [&](Pack<T, V> (&to)[U]) {
+#pragma unroll
+        for (int u = 0; u < U; u++, x += a.x_stride_t) to[u] = *(const Pack<T, V>*)x;
+    };
+    if (t + U <= end) fetch(now);
+    for (; t + U <= end; t += U) {
+        if (t + 2 * U <= end) fetch(next);
+#pragma unroll
+        for (int u = 0; u < U; u++) {
+            float in[V];
+#pragma unroll
+            for (int i = 0; i < V; i++) in[i] = to_float(now[u].v[i]);
+            token(in);
+        }
+#pragma unroll
+        for (int u = 0; u < U; u++) now[u] = next[u];
     }
+    for (; t < end; t++, x += a.x_stride_t) {
+        float in[V];
+        load<T, V>(in, x);
+        token(in);
+    }
+    x = (const T*)a.x + b * a.x_stride_b + d;
     float zero[V] = {};
     for (; t < t1; t++, y += a.D) store<T, V>(y, zero);
     if (final_state && c == 0) {
@@ -137,36 +162,30 @@ __global__ __launch_bounds__(kThreads) void conv_bwd_kernel(sig_conv_args a, Con
 #pragma unroll
         for (int k = 0; k < W - 1; k++) load_token<T, V, W>(r[k + 1], x, a.x_stride_t, initial, a.D, t0 - W + 1 + k);
     }
-    for (int64_t t = t0; t < t1 + W - 1; t++) {
+    // takes token t (in: x, up: the upstream gradient, whether it counts) and stores the gradient of token t - W + 1
+    auto token = [&](int64_t t, const float (&in)[V], const float (&up)[V], bool counts) {
 #pragma unroll
-        for (int k = 0; k < W - 1; k++)
+        for (int i = 0; i < V; i++) {
 #pragma unroll
-            for (int i = 0; i < V; i++) r[k][i] = r[k + 1][i], h[k][i] = h[k + 1][i];
-        if (t < len) {
-            load<T, V>(r[W - 1], x + t * a.x_stride_t);
-            load<T, V>(h[W - 1], gy + t * g.gy_stride_t);
+            for (int k = 0; k < W - 1; k++) r[k][i] = r[k + 1][i], h[k][i] = h[k + 1][i];
+            r[W - 1][i] = in[i];
+            float g = up[i];
+            if (a.silu) {
+                float o = bias[i];
 #pragma unroll
-            for (int i = 0; i < V; i++) {
-                if (a.silu) {
-                    float o = bias[i];
-#pragma unroll
-                    for (int k = 0; k < W; k++) o = fmaf(w[k][i], r[k][i], o);
-                    float p = sigmoid(o);
-                    h[W - 1][i] *= p * fmaf(o, 1.0f - p, 1.0f);
-                }
-                if (t < t1) {
-#pragma unroll
-                    for (int k = 0; k < W; k++) gw[k][i] = fmaf(h[W - 1][i], r[k][i], gw[k][i]);
-                    gw[W][i] += h[W - 1][i];
-                }
+                for (int k = 0; k < W; k++) o = fmaf(w[k][i], r[k][i], o);
+                float p = sigmoid(o);
+                g *= p * fmaf(o, 1.0f - p, 1.0f);
             }
-        } else {
+            h[W - 1][i] = counts ? g : 0.0f;
+            if (counts && t < t1) {
 #pragma unroll
-            for (int i = 0; i < V; i++) h[W - 1][i] = 0.0f;
+                for (int k = 0; k < W; k++) gw[k][i] = fmaf(g, r[k][i], gw[k][i]);
+                gw[W][i] += g;
+            }
         }
         int64_t p = t - W + 1;
-        if (p < (c == 0 ? -(int64_t)(W - 1) : t0)) continue;
-        if (p < 0 && !gi) continue;
+        if (p < (c == 0 ? (gi ? -(int64_t)(W - 1) : 0) : t0)) return;
         float o[V];
 #pragma unroll
         for (int i = 0; i < V; i++) {
@@ -181,6 +200,37 @@ __global__ __launch_bounds__(kThreads) void conv_bwd_kernel(sig_conv_args a, Con
             for (int i = 0; i < V; i++) o[i] += v[i];
         }
         store<T, V>(p >= 0 ? gx + p * a.D : gi + (W - 1 + p) * a.D, o);
+    };
+    // groups of U tokens, the next one's loads under way while one is worked on
+    constexpr int U = V >= 4 ? 4 : 8;
+    const int64_t end = min(t1, len);
+    int64_t t = t0;
+    const T *qx = x + t0 * a.x_stride_t, *qg = gy + t0 * g.gy_stride_t;
+    Pack<T, V> nx[U], ng[U], mx[U], mg[U];
+    auto fetch = [&](Pack<T, V> (&tx)[U], Pack<T, V> (&tg)[U]) {
+#pragma unroll
+        for (int u = 0; u < U; u++, qx += a.x_stride_t, qg += g.gy_stride_t) tx[u] = *(const Pack<T, V>*)qx, tg[u] = *(const Pack<T, V>*)qg;
+    };
+    if (t + U <= end) fetch(nx, ng);
+    for (; t + U <= end; t += U) {
+        if (t + 2 * U <= end) fetch(mx, mg);
+#pragma unroll
+        for (int u = 0; u < U; u++) {
+            float in[V], up[V];
+#pragma unroll
+            for (int i = 0; i < V; i++) in[i] = to_float(nx[u].v[i]), up[i] = to_float(ng[u].v[i]);
+            token(t + u, in, up, true);
+        }
+#pragma unroll
+        for (int u = 0; u < U; u++) nx[u] = mx[u], ng[u] = mg[u];
+    }
+    for (; t < t1 + W - 1; t++) {
+        float in[V] = {}, up[V] = {};
+        if (t < len) {
+            load<T, V>(in, x + t * a.x_stride_t);
+            load<T, V>(up, gy + t * g.gy_stride_t);
+        }
+        token(t, in, up, t < len);
     }
     part += row * (W + 1) * a.D + d;
 #pragma unroll
@@ -189,14 +239,13 @@ __global__ __launch_bounds__(kThreads) void conv_bwd_kernel(sig_conv_args a, Con
         for (int i = 0; i < V; i++) part[k * a.D + i] = gw[k][i];
 }
 
-// sums the chunks' filter gradients part[rows][W + 1][D] in a fixed order
-template <int W> __global__ __launch_bounds__(kThreads) void conv_bwd_sum_kernel(const float* part, int64_t rows, int64_t D, float* gw, float* gb)
+// sums the chunks' filter gradients part[rows][W + 1][D] in a fixed order, 64 sums a workgroup
+template <int W> __global__ __launch_bounds__(1024) void conv_bwd_sum_kernel(const float* part, int64_t rows, int64_t D, float* gw, float* gb)
 {
-    int64_t id = (int64_t)blockIdx.x * kThreads + threadIdx.x;
-    if (id >= (W + 1) * D) return;
-    float v = 0.0f;
-    for (int64_t r = 0; r < rows; r++) v += part[r * (W + 1) * D + id];
-    int64_t k = id / D, d = id % D;
+    const int64_t id = (int64_t)blockIdx.x * 64 + (threadIdx.x & 63), n = (W + 1) * D;
+    const float v = sum_rows(part + id, id < n ? rows : 0, n);
+    if (threadIdx.x >= 64 || id >= n) return;
+    const int64_t k = id / D, d = id % D;
     if (k < W) gw[d * W + k] = v;
     else if (gb) gb[d] = v;
 }
@@ -275,7 +324,7 @@ template <class T> hipError_t backward(const sig_conv_args& a, const ConvGrads& 
         if (a.B == 0) {}     // the sums below are zero
         else if (vec) conv_bwd_kernel<T, V, W><<<blocks_for(s.threads), kThreads, 0, stream>>>(a, g, part, s);
         else conv_bwd_kernel<T, 1, W><<<blocks_for(s.threads), kThreads, 0, stream>>>(a, g, part, s);
-        conv_bwd_sum_kernel<W><<<blocks_for((W + 1) * a.D), kThreads, 0, stream>>>(part, a.B * s.chunks, a.D, g.grad_weight, g.grad_bias);
+        conv_bwd_sum_kernel<W><<<(unsigned)(((W + 1) * a.D + 63) / 64), 1024, 0, stream>>>(part, a.B * s.chunks, a.D, g.grad_weight, g.grad_bias);
         return hipGetLastError();
     });
 }

@@ -430,7 +430,7 @@ __device__ __forceinline__ int token_of(int lane) { return (lane & 1) << 3 | (la
 struct Parts {
     float* bc;           // [B, tiles, G, runs, W, S / 2, 64] sums of a workgroup's channels
     float* A;            // [B, chunks, N, D]
-    float* rest;         // [B, chunks, W, 2, D] dskip, ddt_bias
+    float* rest;         // [B, chunks, 2, D] dskip, ddt_bias
 };
 
 // kFull = false: the adjoint states of a time chunk alone, from zero at its end (see ChunkStates).
@@ -480,7 +480,7 @@ __global__ __launch_bounds__(Gr::W * 64, Gr::W > 8 ? 4 : 2) void scan_bwd_kernel
     const T *pz = a.gate ? (const T*)a.gate + b * a.gate_stride_b + t1 * a.gate_stride_t + d0 : px, *pg = (const T*)g.grad_y + b * g.gy_stride_b + t1 * g.gy_stride_t + d0;
     const T *pb = (const T*)a.b + b * a.b_stride_b + grp * a.b_stride_g + t1 * a.b_stride_t + n0, *pc = (const T*)a.c + b * a.c_stride_b + grp * a.c_stride_g + t1 * a.c_stride_t + n0;
     const float* ph = kFull ? checkpoint + ((b * tiles + t1 / kTile) * a.N + n0) * a.D + d0 : nullptr;
-    const int64_t out = (b * a.L + t1) * a.D + d0;
+    const int64_t out = (b * a.L + t1 + kTile) * a.D + d0;       // one tile on: every turn begins with the lower half of the tile before
     T *qx = (T*)g.grad_x + out, *qdt = (T*)g.grad_dt + out, *qz = (T*)g.grad_gate + out;
     const unsigned x_row = (unsigned)a.x_stride_t * E, dt_row = (unsigned)a.dt_stride_t * E, z_row = gated ? (unsigned)a.gate_stride_t * E : x_row, g_row = (unsigned)g.gy_stride_t * E;
     const unsigned y_row = (unsigned)a.D * E, b_row = (unsigned)(RT * a.b_stride_t) * E, c_row = (unsigned)(RT * a.c_stride_t) * E;
@@ -515,7 +515,7 @@ __global__ __launch_bounds__(Gr::W * 64, Gr::W > 8 ? 4 : 2) void scan_bwd_kernel
     };
     // of each of the wavefront's tokens: x, D, dL/ds, dD/d(dt + bias), dL/dy times the gate's slope; of the tile at work and the one after it
     float xs[2][PT], Ds[2][PT], us[2][PT], sl[2][PT], gs[2][PT];
-    int counts[2] = {0, 0}, rooms[2] = {kTile, kTile};     // tokens of the tile that count, and that the chunk has
+    int counts[2] = {0, 0}, rooms[2] = {0, 0};             // tokens of the tile that count, and that the chunk has
     auto prepare = [&](int slot, float4 (*to)[kTile / 4][64], int n, int room) {
         counts[slot] = n, rooms[slot] = room;
 #pragma unroll
@@ -548,7 +548,7 @@ __global__ __launch_bounds__(Gr::W * 64, Gr::W > 8 ? 4 : 2) void scan_bwd_kernel
             const bool there = k < n;
             const float D = Ds[slot][m], u = us[slot][m], v = xs[slot][m];
             float dx = there ? fmaf(r[0], D, skip * u) : 0.0f, dD = there ? fmaf(r[0], v, r[1]) * sl[slot][m] : 0.0f, dz = there ? gs[slot][m] * r[2] : 0.0f;
-            gskip = fmaf(there ? u : 0.0f, v, gskip);
+            gskip += there ? u * v : 0.0f;
             gbias += dD;
             const unsigned at = on && k < room ? e * E : kNowhere;
             buffer_store(rx, at, k * y_row, from_float<T>(dx));
@@ -573,10 +573,9 @@ __global__ __launch_bounds__(Gr::W * 64, Gr::W > 8 ? 4 : 2) void scan_bwd_kernel
         constexpr int slot = decltype(parity)::value;
         const float4(*now)[kTile / 4][64] = in + slot * 3;
         float4(*upper)[3][kHalf / 4][64] = sums, (*lower)[3][kHalf / 4][64] = sums + (kTwice ? W : 0);
-        const bool first = tile == n_tiles - 1;
         float Bn[KB], Cn[KB], hn[S], group[4][Q];
         take(Bn, Cn, hn);
-        if (kFull && !first) {             // what is left of the tile before
+        if (kFull) {                       // what is left of the tile before (in the first turn nothing, whatever LDS holds)
             put(0, slot ^ 1, lower);
             qx -= kTile * a.D, qdt -= kTile * a.D, qz -= kTile * a.D;
             if (!kTwice) __syncthreads();
@@ -692,6 +691,9 @@ __global__ __launch_bounds__(Gr::W * 64, Gr::W > 8 ? 4 : 2) void scan_bwd_kernel
                 rx[t * a.D + e] = rdt[t * a.D + e] = from_float<T>(0.0f);
                 if (gated) rz[t * a.D + e] = from_float<T>(0.0f);
             }
+        __syncthreads();
+        lds[(w * 2 + 0) * 64 + lane] = gskip, lds[(w * 2 + 1) * 64 + lane] = gbias;
+        __syncthreads();
         if (!on) return;
         const int64_t row = b * bl.chunks + c;
 #pragma unroll
@@ -700,8 +702,13 @@ __global__ __launch_bounds__(Gr::W * 64, Gr::W > 8 ? 4 : 2) void scan_bwd_kernel
                 parts.A[(row * a.N + n0 + s) * a.D + d] = gA[s];
                 if (g.grad_initial_state && c == 0) g.grad_initial_state[(b * a.D + d) * a.N + n0 + s] = adj[s];
             }
-        parts.rest[((row * W + w) * 2 + 0) * a.D + d] = gskip;
-        parts.rest[((row * W + w) * 2 + 1) * a.D + d] = gbias;
+        if (w == 0) {
+            float r[2] = {0.0f, 0.0f};
+#pragma unroll
+            for (int v = 0; v < W; v++) r[0] += lds[(v * 2 + 0) * 64 + lane], r[1] += lds[(v * 2 + 1) * 64 + lane];
+            parts.rest[(row * 2 + 0) * a.D + d] = r[0];
+            parts.rest[(row * 2 + 1) * a.D + d] = r[1];
+        }
     } else {
         if (!on) return;
         const int64_t row = b * bl.chunks + c;
@@ -730,20 +737,20 @@ template <class T, class Gr> __global__ __launch_bounds__(kThreads) void scan_bw
     if (t < a.L && n < a.N) (lane & 32 ? gC : gB)[((b * a.L + t) * a.G + grp) * a.N + n] = from_float<T>(t < len ? v : 0.0f);
 }
 
-// dA, dskip and ddt_bias: the sums over streams, time chunks and wavefronts, in their order
-__global__ __launch_bounds__(kThreads) void scan_bwd_params_kernel(sig_scan_args a, int64_t rows, int64_t waves, Parts parts, float* gA, float* gskip, float* gbias)
+// dA, dskip and ddt_bias: the sums over streams and time chunks, in a fixed order.  64 sums a workgroup; each of its sixteen wavefronts takes
+// every sixteenth row, so that few columns with many rows wait for memory a sixteenth as often.
+__global__ __launch_bounds__(1024) void scan_bwd_params_kernel(sig_scan_args a, int64_t rows, Parts parts, float* gA, float* gskip, float* gbias)
 {
-    const int64_t id = (int64_t)blockIdx.x * kThreads + threadIdx.x, DN = a.D * a.N;
-    float v = 0.0f;
-    if (id < DN) {
-        for (int64_t r = 0; r < rows; r++) v += parts.A[r * DN + id];
-        gA[id % a.D * a.N + id / a.D] = v;
-    } else if (id < DN + 2 * a.D) {
-        const int64_t k = (id - DN) / a.D, d = (id - DN) % a.D;
-        float* to = k ? gbias : gskip;
-        if (!to) return;
-        for (int64_t r = 0; r < rows * waves; r++) v += parts.rest[(r * 2 + k) * a.D + d];
-        to[d] = v;
+    const int64_t id = (int64_t)blockIdx.x * 64 + (threadIdx.x & 63), DN = a.D * a.N;
+    const bool of_A = id < DN, of_rest = !of_A && id < DN + 2 * a.D;
+    const float* from = of_A ? parts.A + id : parts.rest + (id - DN);
+    const int64_t step = of_A ? DN : 2 * a.D;
+    const float v = sum_rows(from, of_A || of_rest ? rows : 0, step);
+    if (threadIdx.x >= 64) return;
+    if (of_A) gA[id % a.D * a.N + id / a.D] = v;
+    if (of_rest) {
+        float* to = id - DN < a.D ? gskip : gbias;
+        if (to) to[(id - DN) % a.D] = v;
     }
 }
 
@@ -822,7 +829,7 @@ PartFloats part_floats(const sig_scan_args& a, const Blocks& bl)
 {
     int64_t W = 0, Q = 0;
     with_group(a.N, [&](auto gr) { W = decltype(gr)::W, Q = decltype(gr)::S / 2; return 0; });
-    return {(size_t)(a.B * tiles_of(a) * a.G * bl.runs * W * Q * 64), (size_t)(a.B * bl.chunks * a.N * a.D), (size_t)(a.B * bl.chunks * W * 2 * a.D)};
+    return {(size_t)(a.B * tiles_of(a) * a.G * bl.runs * W * Q * 64), (size_t)(a.B * bl.chunks * a.N * a.D), (size_t)(a.B * bl.chunks * 2 * a.D)};
 }
 
 }  // namespace
@@ -876,7 +883,7 @@ hipError_t scan_backward(const sig_scan_args& a, const sig_scan_grads& g, const 
                 scan_bwd_kernel<T, Gr, true><<<bl.total, Gr::W * 64, in + sums, stream>>>(a, g, bl, cs, checkpoint, parts);
                 if (a.L > 0) scan_bwd_bc_kernel<T, Gr><<<blocks_for(p.bc / bl.runs), kThreads, 0, stream>>>(a, bl, parts.bc, (T*)g.grad_b, (T*)g.grad_c);
             }
-            scan_bwd_params_kernel<<<blocks_for(a.D * (a.N + 2)), kThreads, 0, stream>>>(a, a.B * bl.chunks, Gr::W, parts, g.grad_A, g.grad_skip, g.grad_dt_bias);
+            scan_bwd_params_kernel<<<(unsigned)((a.D * (a.N + 2) + 63) / 64), 1024, 0, stream>>>(a, a.B * bl.chunks, parts, g.grad_A, g.grad_skip, g.grad_dt_bias);
             return hipGetLastError();
         });
     });

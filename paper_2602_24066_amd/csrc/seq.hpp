@@ -36,7 +36,8 @@ hipError_t scan_step(const sig_scan_args& a, float* state, void* y, hipStream_t 
 
 // ---- gradient norm and clipping (kernels_clip.hip)
 constexpr int kClipTensors = 128;       // tensors that one launch takes: their table is a kernel argument (of at most 4 KB)
-constexpr int kClipBlock = 16384;       // elements of a workgroup
+constexpr int kClipBlock = 4096;        // elements of a workgroup, at least
+constexpr int kClipBlocks = 4096;       // workgroups that all tensors are spread over, about
 struct ClipTable {
     const void* in[kClipTensors];
     void* out[kClipTensors];
@@ -44,6 +45,7 @@ struct ClipTable {
     uint32_t end[kClipTensors];         // workgroups up to and with this tensor
     uint8_t kind[kClipTensors];         // bit 0: in is bf16, bit 1: out is bf16
     int n;
+    uint32_t block;                     // elements of a workgroup
 };
 hipError_t norm_parts(const ClipTable& tab, double* part, hipStream_t stream);     // part: one sum of squares for each workgroup
 hipError_t norm_total(const double* part, int64_t n, float* norm, hipStream_t stream);
@@ -87,6 +89,27 @@ __device__ __forceinline__ float softplus(float v)
     p = fmaf(p, q, 1.0f / 3.0f);
     p = fmaf(p, q, 1.0f);
     return fmaxf(v, 0.0f) + 2.0f * s * p;
+}
+
+// The sum over rows of a column, p[r step], by a workgroup of sixteen wavefronts whose lanes have a column each: wavefront w adds up rows
+// w, w + 16, .., the first one their sums in order.  Returned to the first wavefront.
+__device__ __forceinline__ float sum_rows(const float* p, int64_t rows, int64_t step)
+{
+    __shared__ float part[16][64];
+    const int lane = threadIdx.x & 63, w = threadIdx.x / 64;
+    float v[4] = {};
+    int64_t r = w;
+    for (; r + 48 < rows; r += 64)
+#pragma unroll
+        for (int i = 0; i < 4; i++) v[i] += p[(r + 16 * i) * step];
+    for (; r < rows; r += 16) v[0] += p[r * step];
+    part[w][lane] = (v[0] + v[1]) + (v[2] + v[3]);
+    __syncthreads();
+    float s = 0.0f;
+    if (w == 0)
+#pragma unroll
+        for (int i = 0; i < 16; i++) s += part[i][lane];
+    return s;
 }
 
 __device__ __forceinline__ int64_t live_length(const int32_t* lengths, int64_t b, int64_t L)
