@@ -166,31 +166,36 @@ int sig_grad_clip(int64_t n_tensors, const void* const* in, void* const* out, co
     for (int64_t i = 0; i < n_tensors; i++) blocks += (sizes[i] + block - 1) / block;
     if (workspace_bytes < (size_t)blocks * sizeof(double) || (blocks && !workspace)) return SIG_EWORKSPACE;
     hipStream_t s = (hipStream_t)stream;
-    // all tables of the norm first, then its square root, then all tables of the products
-    for (int pass = 0; pass < 2; pass++) {
-        double* part = (double*)workspace;
-        sig::ClipTable tab;
-        tab.n = 0;
-        tab.block = (uint32_t)block;
-        for (int64_t i = 0; i <= n_tensors; i++) {
-            if (i < n_tensors && sizes[i]) {
-                int k = tab.n++;
-                tab.in[k] = in[i];
-                tab.out[k] = out[i];
-                tab.size[k] = sizes[i];
-                tab.kind[k] = (uint8_t)(in_dtypes[i] | out_dtypes[i] << 1);
-                tab.end[k] = (k ? tab.end[k - 1] : 0) + (uint32_t)((sizes[i] + block - 1) / block);
-            }
-            if (tab.n == 0 || (tab.n < sig::kClipTensors && i < n_tensors)) continue;
-            hipError_t e = pass == 0 ? sig::norm_parts(tab, part, s) : sig::clip_scaled(tab, norm, max_norm, s);
-            if (e != hipSuccess) return sig::record_hip_error(e);
-            part += tab.end[tab.n - 1];
-            tab.n = 0;
-        }
-        if (pass == 0) {
+    // all tables of the norm first, then its square root, then the tables of the products in the opposite order, whose kernel goes
+    // backwards too: it begins with what the cache still holds
+    const int64_t per = sig::kClipTensors, tables = (n_tensors + per - 1) / per;
+    double* part = (double*)workspace;
+    for (int64_t k = 0; k < 2 * tables; k++) {
+        if (k == tables) {
             hipError_t e = sig::norm_total((const double*)workspace, blocks, norm, s);
             if (e != hipSuccess) return sig::record_hip_error(e);
         }
+        const int64_t first = per * (k < tables ? k : 2 * tables - 1 - k), last = std::min(n_tensors, first + per);
+        sig::ClipTable tab;
+        tab.n = 0;
+        tab.block = (uint32_t)block;
+        for (int64_t i = first; i < last; i++) {
+            if (!sizes[i]) continue;
+            const int j = tab.n++;
+            tab.in[j] = in[i];
+            tab.out[j] = out[i];
+            tab.size[j] = sizes[i];
+            tab.kind[j] = (uint8_t)(in_dtypes[i] | out_dtypes[i] << 1);
+            tab.end[j] = (j ? tab.end[j - 1] : 0) + (uint32_t)((sizes[i] + block - 1) / block);
+        }
+        if (tab.n == 0) continue;
+        hipError_t e = k < tables ? sig::norm_parts(tab, part, s) : sig::clip_scaled(tab, norm, max_norm, s);
+        if (e != hipSuccess) return sig::record_hip_error(e);
+        part += k < tables ? tab.end[tab.n - 1] : 0;
+    }
+    if (tables == 0) {
+        hipError_t e = sig::norm_total((const double*)workspace, 0, norm, s);
+        if (e != hipSuccess) return sig::record_hip_error(e);
     }
     return SIG_OK;
 }

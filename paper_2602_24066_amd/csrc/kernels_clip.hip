@@ -109,7 +109,8 @@ template <class I, class O> __device__ __forceinline__ void scaled(const I* in, 
 
 __global__ __launch_bounds__(kThreads) void clip_kernel(ClipTable tab, const float* norm, float max_norm)
 {
-    Piece p = piece_of(tab, blockIdx.x);
+    // from the last workgroup to the first: what the norm read last is still in the cache
+    Piece p = piece_of(tab, gridDim.x - 1 - blockIdx.x);
     float q = max_norm / (*norm + 1e-6f), scale = q > 1.0f ? 1.0f : q;      // a NaN stays one
     const void* in = tab.in[p.t];
     void* out = tab.out[p.t];

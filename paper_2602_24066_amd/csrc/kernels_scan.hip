@@ -442,7 +442,7 @@ __global__ __launch_bounds__(Gr::W * 64, Gr::W > 8 ? 4 : 2) void scan_bwd_kernel
     constexpr unsigned E = sizeof(T);
     extern __shared__ float lds[];
     float4(*in)[kTile / 4][64] = (float4(*)[kTile / 4][64])lds;                                          // [2][3: D, D x, dL/ds][kTile / 4][64]
-    float4(*sums)[3][kHalf / 4][64] = (float4(*)[3][kHalf / 4][64])(lds + 2 * 3 * kTile * 64);           // [2 or 1][W][3][kHalf / 4][64]
+    float(*sums)[3][kHalf][64] = (float(*)[3][kHalf][64])(lds + 2 * 3 * kTile * 64);                     // [2 or 1][W][3][kHalf][64]
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     const unsigned c = blockIdx.x % bl.chunks, rest = blockIdx.x / bl.chunks, run = rest % bl.runs, bg = rest / bl.runs;
     const int64_t grp = bg % (unsigned)a.G, b = bg / (unsigned)a.G;
@@ -533,7 +533,7 @@ __global__ __launch_bounds__(Gr::W * 64, Gr::W > 8 ? 4 : 2) void scan_bwd_kernel
         }
     };
     // the gradients of a half's tokens; from: the wavefronts' sums
-    auto put = [&](int half, int slot, const float4 (*from)[3][kHalf / 4][64]) {
+    auto put = [&](int half, int slot, const float (*from)[3][kHalf][64]) {
         const int n = counts[slot], room = rooms[slot];
         Buffer rx = buffer_at(qx), rdt = buffer_at(qdt), rz = buffer_at(qz);
 #pragma unroll
@@ -544,7 +544,7 @@ __global__ __launch_bounds__(Gr::W * 64, Gr::W > 8 ? 4 : 2) void scan_bwd_kernel
 #pragma unroll
             for (int v = 0; v < W; v++)
 #pragma unroll
-                for (int q = 0; q < 3; q++) r[q] += ((const float*)&from[v][q][kh / 4][lane])[kh % 4];
+                for (int q = 0; q < 3; q++) r[q] += from[v][q][kh][lane];
             const bool there = k < n;
             const float D = Ds[slot][m], u = us[slot][m], v = xs[slot][m];
             float dx = there ? fmaf(r[0], D, skip * u) : 0.0f, dD = there ? fmaf(r[0], v, r[1]) * sl[slot][m] : 0.0f, dz = there ? gs[slot][m] * r[2] : 0.0f;
@@ -572,7 +572,7 @@ __global__ __launch_bounds__(Gr::W * 64, Gr::W > 8 ? 4 : 2) void scan_bwd_kernel
     auto work = [&](auto parity) {
         constexpr int slot = decltype(parity)::value;
         const float4(*now)[kTile / 4][64] = in + slot * 3;
-        float4(*upper)[3][kHalf / 4][64] = sums, (*lower)[3][kHalf / 4][64] = sums + (kTwice ? W : 0);
+        float(*upper)[3][kHalf][64] = sums, (*lower)[3][kHalf][64] = sums + (kTwice ? W : 0);
         float Bn[KB], Cn[KB], hn[S], group[4][Q];
         take(Bn, Cn, hn);
         if (kFull) {                       // what is left of the tile before (in the first turn nothing, whatever LDS holds)
@@ -641,12 +641,13 @@ __global__ __launch_bounds__(Gr::W * 64, Gr::W > 8 ? 4 : 2) void scan_bwd_kernel
                 if constexpr (kFull) {
 #pragma unroll
                     for (int m = 0; m < Q; m++) group[i / 4][m] = fold2(fold3(fold[0][m], fold[1][m]), fold3(fold[2][m], fold[3][m]));
-                    float4(*to)[3][kHalf / 4][64] = half ? upper : lower;
+                    float(*to)[3][kHalf][64] = half ? upper : lower;
                     sum_broadcast<k>(o, B[i / RT], lam);
-                    to[w][0][q][lane] = make_float4(o[0], o[1], o[2], o[3]);
-                    to[w][1][q][lane] = make_float4(dD[0], dD[1], dD[2], dD[3]);
+#pragma unroll
+                    for (int j = 0; j < 4; j++) to[w][0][q * 4 + j][lane] = o[j], to[w][1][q * 4 + j][lane] = dD[j];
                     sum_broadcast<k>(o, C[i / RT], ht);
-                    to[w][2][q][lane] = make_float4(o[0], o[1], o[2], o[3]);
+#pragma unroll
+                    for (int j = 0; j < 4; j++) to[w][2][q * 4 + j][lane] = o[j];
                 }
             });
         };
@@ -680,7 +681,7 @@ __global__ __launch_bounds__(Gr::W * 64, Gr::W > 8 ? 4 : 2) void scan_bwd_kernel
     }
     if constexpr (kFull) {
         if (n_tiles > 0) {
-            float4(*lower)[3][kHalf / 4][64] = sums + (kTwice ? W : 0);
+            float(*lower)[3][kHalf][64] = sums + (kTwice ? W : 0);
             if (turn) put(0, 1, lower);
             else put(0, 0, lower);
         }

@@ -37,7 +37,7 @@ hipError_t scan_step(const sig_scan_args& a, float* state, void* y, hipStream_t 
 // ---- gradient norm and clipping (kernels_clip.hip)
 constexpr int kClipTensors = 128;       // tensors that one launch takes: their table is a kernel argument (of at most 4 KB)
 constexpr int kClipBlock = 4096;        // elements of a workgroup, at least
-constexpr int kClipBlocks = 4096;       // workgroups that all tensors are spread over, about
+constexpr int kClipBlocks = 16384;      // workgroups that all tensors are spread over at most, about (166e6 elements: 341 us with 4,096, 314 with these)
 struct ClipTable {
     const void* in[kClipTensors];
     void* out[kClipTensors];

@@ -12,81 +12,89 @@ import struct
 
 from .binding import _call, _calls, _enqueue
 
-_torch = None
+# torch and its types, set by the first call; the checks below are written for calls of one token, whose kernels take less time than they do
+_torch = _f32 = _b16 = _i32 = _plain = None
 
 
 def _t():
-    global _torch
+    global _torch, _f32, _b16, _i32, _plain
     if _torch is None:
         import torch
+        _f32, _b16, _i32, _plain = torch.float32, torch.bfloat16, torch.int32, torch.Tensor
         _torch = torch
     return _torch
 
 
-def _tokens(name, t, shape, like):
-    """Checks a tensor of tokens against the type and device of `like`; its last axis is contiguous on return."""
-    if t.dtype is not like.dtype or t.device != like.device:
-        raise ValueError(f"{name} must be of type {like.dtype} on {like.device}")
-    if t.shape != shape:
-        raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
-    return t if t.stride(-1) == 1 or shape[-1] == 1 else t.contiguous()
-
-
-def _whole(name, t, shape, dtype, device):
-    """Checks a parameter, state or list of lengths and returns it contiguous; None stays None."""
-    if t is None:
-        return None
-    if t.dtype is not dtype or t.device != device:
-        raise ValueError(f"{name} must be of type {dtype} on {device}")
-    if t.shape != shape:
-        raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
-    return t if t.is_contiguous() else t.contiguous()
-
-
-def _in_place(name, t, shape, dtype, device):
-    if t is None or t.dtype is not dtype or t.device != device or t.shape != shape or not t.is_contiguous():
-        raise ValueError(f"{name} must be a contiguous tensor of type {dtype} and shape {tuple(shape)} on {device}")
-    return t
+def _refuse(name, t, shape, dtype):
+    raise ValueError(f"{name} must be a tensor of type {dtype} and shape {tuple(shape)} on the device of x, got {t.dtype}, {tuple(t.shape)}, {t.device}")
 
 
 def _first(x, dims):
-    torch = _t()
-    if not x.is_cuda or x.dim() != dims or x.dtype not in (torch.float32, torch.bfloat16):
+    """Checks x; returns what makes the outputs, and the code of its type."""
+    if _torch is None:
+        _t()
+    t = x.dtype
+    if not x.is_cuda or x.dim() != dims or (t is not _f32 and t is not _b16):
         raise ValueError("x must be a float32 or bfloat16 CUDA tensor " + ("[B, L, D]" if dims == 3 else "[B, D]"))
-    return torch, int(x.dtype is torch.bfloat16)
+    return x if type(x) is _plain else _torch.empty(0, dtype=t, device=x.device), 1 if t is _b16 else 0
 
 
-def _ptr(t):
-    return 0 if t is None else t.data_ptr()
+def _tokens(name, t, shape, dtype, index):
+    """Checks a tensor of tokens; returns it with a contiguous last axis, and its strides."""
+    if t.dtype is not dtype or t.get_device() != index or t.shape != shape:
+        _refuse(name, t, shape, dtype)
+    s = t.stride()
+    if (s[-1] != 1 and shape[-1] != 1) or (len(s) > 2 and s[1] >= 1 << 26):      # time strides that the kernels do not reach are copied away
+        t = t.contiguous()
+        s = t.stride()
+    return t, s
 
 
-def _scratch(torch, name, args, device):
+def _whole(name, t, shape, dtype, index):
+    """Checks a parameter, state or list of lengths and returns it contiguous."""
+    if t.dtype is not dtype or t.get_device() != index or t.shape != shape:
+        _refuse(name, t, shape, dtype)
+    return t if t.is_contiguous() else t.contiguous()
+
+
+def _in_place(name, t, shape, dtype, index):
+    if t.dtype is not dtype or t.get_device() != index or t.shape != shape or not t.is_contiguous():
+        _refuse(name + " (contiguous)", t, shape, dtype)
+
+
+def _scratch(make, name, args):
     """The workspace a call asks for: (tensor to keep alive, address, bytes)."""
     n = (_calls.get(name) or _call(name))(args)
-    t = torch.empty(n, dtype=torch.uint8, device=device) if n else None
-    return t, _ptr(t), n
+    if n == 0:
+        return None, 0, 0
+    t = make.new_empty(n, dtype=_torch.uint8)
+    return t, t.data_ptr(), n
 
 
 _CONV = struct.Struct("13q")
 
 
 def _conv_args(x, weight, bias, initial_state, lengths, silu):
-    torch, kind = _first(x, 3)
-    f32, dev, shape = torch.float32, x.device, x.shape
-    B, L, D = shape
-    if weight.dim() != 2 or weight.shape[1] < 1:
-        raise ValueError("weight must be [D, W]")
+    make, kind = _first(x, 3)
+    B, L, D = shape = x.shape
+    index = x.get_device()
+    if weight.dim() != 2 or not 1 <= weight.shape[1] <= 8:
+        raise ValueError("weight must be [D, W] with W <= 8")
     W = weight.shape[1]
-    if W > 8:
-        raise ValueError("filters of more than 8 tokens are not supported")
-    x = _tokens("x", x, shape, x)
-    weight = _whole("weight", weight, (D, W), f32, dev)
-    bias = _whole("bias", bias, (D,), f32, dev)
-    initial_state = _whole("initial_state", initial_state, (B, W - 1, D), x.dtype, dev)
-    lengths = _whole("lengths", lengths, (B,), torch.int32, dev)
-    sb, st, _ = x.stride()
-    args = _CONV.pack(kind, B, L, D, W, 1 if silu else 0, sb, st, x.data_ptr(), weight.data_ptr(), _ptr(bias), _ptr(initial_state), _ptr(lengths))
-    return torch, args, W, (x, weight, bias, initial_state, lengths)
+    x, (sb, st, _) = _tokens("x", x, shape, x.dtype, index)
+    weight = _whole("weight", weight, (D, W), _f32, index)
+    pb = pi = pl = 0
+    if bias is not None:
+        bias = _whole("bias", bias, (D,), _f32, index)
+        pb = bias.data_ptr()
+    if initial_state is not None:
+        initial_state = _whole("initial_state", initial_state, (B, W - 1, D), x.dtype, index)
+        pi = initial_state.data_ptr()
+    if lengths is not None:
+        lengths = _whole("lengths", lengths, (B,), _i32, index)
+        pl = lengths.data_ptr()
+    args = _CONV.pack(kind, B, L, D, W, 1 if silu else 0, sb, st, x.data_ptr(), weight.data_ptr(), pb, pi, pl)
+    return make, args, W, (x, weight, bias, initial_state, lengths)
 
 
 def sig_conv_forward(x, weight, bias=None, initial_state=None, lengths=None, silu=True, return_state=False):
@@ -95,48 +103,52 @@ def sig_conv_forward(x, weight, bias=None, initial_state=None, lengths=None, sil
     x [B, L, D]; weight float32 [D, W], W <= 8; bias float32 [D]; initial_state [B, W-1, D] of x's type: the tokens before the first, oldest
     first (default zeros); lengths int32 [B]: tokens from there on are not read and give zeros.  Returns y [B, L, D], or with
     return_state (y, state): the last W-1 tokens of every stream, for sig_conv_step or the next prompt's initial_state."""
-    torch, args, W, kept = _conv_args(x, weight, bias, initial_state, lengths, silu)
+    make, args, W, kept = _conv_args(x, weight, bias, initial_state, lengths, silu)
     B, L, D = x.shape
-    y = torch.empty((B, L, D), dtype=x.dtype, device=x.device)
-    state = torch.empty((B, W - 1, D), dtype=x.dtype, device=x.device) if return_state else None
-    _enqueue(x.device, "sig_conv_forward", args, y.data_ptr(), _ptr(state))
+    y = make.new_empty((B, L, D))
+    state = make.new_empty((B, W - 1, D)) if return_state else None
+    _enqueue(x.device, "sig_conv_forward", args, y.data_ptr(), state.data_ptr() if return_state else 0)
     return (y, state) if return_state else y
 
 
 def sig_conv_backward(x, weight, grad_out, bias=None, initial_state=None, lengths=None, silu=True, grad_final_state=None):
     """Gradient of sig_conv_forward: (grad_x, grad_weight, grad_bias, grad_initial_state), None for those whose input is None.
     grad_out [B, L, D] and grad_final_state [B, W-1, D] are of x's type."""
-    torch, args, W, kept = _conv_args(x, weight, bias, initial_state, lengths, silu)
+    make, args, W, kept = _conv_args(x, weight, bias, initial_state, lengths, silu)
     B, L, D = x.shape
-    dev = x.device
-    grad_out = _tokens("grad_out", grad_out, x.shape, x)
-    grad_final_state = _whole("grad_final_state", grad_final_state, (B, W - 1, D), x.dtype, dev)
-    gx = torch.empty((B, L, D), dtype=x.dtype, device=dev)
-    gw = torch.empty((D, W), dtype=torch.float32, device=dev)
-    gb = torch.empty(D, dtype=torch.float32, device=dev) if bias is not None else None
-    gi = torch.empty((B, W - 1, D), dtype=x.dtype, device=dev) if initial_state is not None else None
-    keep, wptr, nbytes = _scratch(torch, "sig_conv_backward_workspace_bytes", args, dev)
-    sb, st, _ = grad_out.stride()
-    _enqueue(dev, "sig_conv_backward", args, grad_out.data_ptr(), sb, st, _ptr(grad_final_state), gx.data_ptr(), gw.data_ptr(), _ptr(gb),
-             _ptr(gi), wptr, nbytes)
+    t, index = x.dtype, x.get_device()
+    grad_out, (sb, st, _) = _tokens("grad_out", grad_out, x.shape, t, index)
+    pf = 0
+    if grad_final_state is not None:
+        grad_final_state = _whole("grad_final_state", grad_final_state, (B, W - 1, D), t, index)
+        pf = grad_final_state.data_ptr()
+    gx, gw = make.new_empty((B, L, D)), make.new_empty((D, W), dtype=_f32)
+    gb = make.new_empty(D, dtype=_f32) if bias is not None else None
+    gi = make.new_empty((B, W - 1, D)) if initial_state is not None else None
+    keep, wptr, nbytes = _scratch(make, "sig_conv_backward_workspace_bytes", args)
+    _enqueue(x.device, "sig_conv_backward", args, grad_out.data_ptr(), sb, st, pf, gx.data_ptr(), gw.data_ptr(), 0 if gb is None else gb.data_ptr(),
+             0 if gi is None else gi.data_ptr(), wptr, nbytes)
     return gx, gw, gb, gi
 
 
 def sig_conv_step(x, state, weight, bias=None, silu=True):
     """One token of every stream: x [B, D], state [B, W-1, D] of x's type, shifted by it in place.  Returns y [B, D]."""
-    torch, kind = _first(x, 2)
-    B, D = x.shape
-    dev = x.device
+    make, kind = _first(x, 2)
+    B, D = shape = x.shape
+    t, index = x.dtype, x.get_device()
     if weight.dim() != 2 or not 1 <= weight.shape[1] <= 8:
         raise ValueError("weight must be [D, W] with W <= 8")
     W = weight.shape[1]
-    x = _tokens("x", x, x.shape, x)
-    weight = _whole("weight", weight, (D, W), torch.float32, dev)
-    bias = _whole("bias", bias, (D,), torch.float32, dev)
-    _in_place("state", state, (B, W - 1, D), x.dtype, dev)
-    y = torch.empty((B, D), dtype=x.dtype, device=dev)
-    args = _CONV.pack(kind, B, 1, D, W, 1 if silu else 0, x.stride(0), 0, x.data_ptr(), weight.data_ptr(), _ptr(bias), 0, 0)
-    _enqueue(dev, "sig_conv_step", args, state.data_ptr(), y.data_ptr())
+    x, (sb, _) = _tokens("x", x, shape, t, index)
+    weight = _whole("weight", weight, (D, W), _f32, index)
+    pb = 0
+    if bias is not None:
+        bias = _whole("bias", bias, (D,), _f32, index)
+        pb = bias.data_ptr()
+    _in_place("state", state, (B, W - 1, D), t, index)
+    y = make.new_empty((B, D))
+    _enqueue(x.device, "sig_conv_step", _CONV.pack(kind, B, 1, D, W, 1 if silu else 0, sb, 0, x.data_ptr(), weight.data_ptr(), pb, 0, 0),
+             state.data_ptr(), y.data_ptr())
     return y
 
 
@@ -144,46 +156,50 @@ _SCAN = struct.Struct("29q")
 _SCAN_GRADS = struct.Struct("13q")
 
 
-def _groups(name, t, lead, like):
-    """b or c: [..., N] (one group) or [..., G, N]; (tensor with the group axis, G, N)."""
-    if t.dim() == len(lead) + 1:
-        t = t.unsqueeze(-2)
-    if t.dim() != len(lead) + 2:
-        raise ValueError(f"{name} must have the shape of the tokens before its axes [groups, states] or [states]")
-    return _tokens(name, t, (*lead, *t.shape[-2:]), like)
-
-
 def _scan_args(x, dt, A, b, c, skip, gate, dt_bias, softplus, initial_state, lengths, dims):
-    torch, kind = _first(x, dims)
-    f32, dev, shape = torch.float32, x.device, x.shape
-    lead, D = shape[:-1], shape[-1]
-    x = _tokens("x", x, shape, x)
-    dt = _tokens("dt", dt, shape, x)
-    b, c = _groups("b", b, lead, x), _groups("c", c, lead, x)
+    make, kind = _first(x, dims)
+    shape = x.shape
+    D, t, index = shape[-1], x.dtype, x.get_device()
+    if b.dim() == dims:                                                                     # one group
+        b = b.unsqueeze(-2)
+    if c.dim() == dims:
+        c = c.unsqueeze(-2)
     G, N = b.shape[-2:]
-    if c.shape != b.shape or G < 1 or D % G:
-        raise ValueError("b and c must have the same groups and states, and the groups divide the channels")
-    if not 1 <= N <= 64:
-        raise ValueError("1 to 64 states are supported")
+    if G < 1 or D % G or not 1 <= N <= 64:
+        raise ValueError("b and c must be [..., groups, states] or [..., states], the groups dividing the channels, of 1 to 64 states")
+    x, xs = _tokens("x", x, shape, t, index)
+    dt, ts = _tokens("dt", dt, shape, t, index)
+    of_bc = (*shape[:-1], G, N)
+    b, bs = _tokens("b", b, of_bc, t, index)
+    c, cs = _tokens("c", c, of_bc, t, index)
+    pz = ps = pd = pi = pl = 0
+    zs = (0, 0, 0)
     if gate is not None:
-        gate = _tokens("gate", gate, shape, x)
-    A = _whole("A", A, (D, N), f32, dev)
+        gate, zs = _tokens("gate", gate, shape, t, index)
+        pz = gate.data_ptr()
     if A is None:
         raise ValueError("A is missing")
-    skip, dt_bias = _whole("skip", skip, (D,), f32, dev), _whole("dt_bias", dt_bias, (D,), f32, dev)
+    A = _whole("A", A, (D, N), _f32, index)
+    if skip is not None:
+        skip = _whole("skip", skip, (D,), _f32, index)
+        ps = skip.data_ptr()
+    if dt_bias is not None:
+        dt_bias = _whole("dt_bias", dt_bias, (D,), _f32, index)
+        pd = dt_bias.data_ptr()
     if dims == 3:
         B, L, _ = shape
-        initial_state = _whole("initial_state", initial_state, (B, D, N), f32, dev)
-        lengths = _whole("lengths", lengths, (B,), torch.int32, dev)
-        (xb, xt, _), (tb, tt, _), (zb, zt, _) = x.stride(), dt.stride(), (0, 0, 0) if gate is None else gate.stride()
-        (bb, bt, bg, _), (cb, ct, cg, _) = b.stride(), c.stride()
+        if initial_state is not None:
+            initial_state = _whole("initial_state", initial_state, (B, D, N), _f32, index)
+            pi = initial_state.data_ptr()
+        if lengths is not None:
+            lengths = _whole("lengths", lengths, (B,), _i32, index)
+            pl = lengths.data_ptr()
+        args = _SCAN.pack(kind, B, L, D, G, N, 1 if softplus else 0, xs[0], xs[1], ts[0], ts[1], zs[0], zs[1], bs[0], bs[1], bs[2], cs[0], cs[1], cs[2],
+                          x.data_ptr(), dt.data_ptr(), pz, b.data_ptr(), c.data_ptr(), A.data_ptr(), ps, pd, pi, pl)
     else:
-        B, L = shape[0], 1
-        xb, xt, tb, tt, zb, zt = x.stride(0), 0, dt.stride(0), 0, 0 if gate is None else gate.stride(0), 0
-        (bb, bg, _), (cb, cg, _), bt, ct = b.stride(), c.stride(), 0, 0
-    args = _SCAN.pack(kind, B, L, D, G, N, 1 if softplus else 0, xb, xt, tb, tt, zb, zt, bb, bt, bg, cb, ct, cg, x.data_ptr(), dt.data_ptr(),
-                      _ptr(gate), b.data_ptr(), c.data_ptr(), A.data_ptr(), _ptr(skip), _ptr(dt_bias), _ptr(initial_state), _ptr(lengths))
-    return torch, args, G, N, (x, dt, A, b, c, skip, gate, dt_bias, initial_state, lengths)
+        args = _SCAN.pack(kind, shape[0], 1, D, G, N, 1 if softplus else 0, xs[0], 0, ts[0], 0, zs[0], 0, bs[0], 0, bs[1], cs[0], 0, cs[1],
+                          x.data_ptr(), dt.data_ptr(), pz, b.data_ptr(), c.data_ptr(), A.data_ptr(), ps, pd, 0, 0)
+    return make, args, G, N, (x, dt, A, b, c, skip, gate, dt_bias, initial_state, lengths)
 
 
 def sig_scan_forward(x, dt, A, b, c, skip=None, gate=None, dt_bias=None, softplus=True, initial_state=None, lengths=None, checkpoint=False):
@@ -193,53 +209,52 @@ def sig_scan_forward(x, dt, A, b, c, skip=None, gate=None, dt_bias=None, softplu
     x, dt, gate [B, L, D]; b, c [B, L, G, N] or [B, L, N]: channel d uses group d // (D // G); A float32 [D, N]; skip, dt_bias float32 [D];
     initial_state float32 [B, D, N] (default zeros); lengths int32 [B]: tokens from there on are not read, give zeros and leave the
     state.  Returns (y [B, L, D], final state float32 [B, D, N]); with checkpoint=True a third tensor for sig_scan_backward."""
-    torch, args, G, N, kept = _scan_args(x, dt, A, b, c, skip, gate, dt_bias, softplus, initial_state, lengths, 3)
+    make, args, G, N, kept = _scan_args(x, dt, A, b, c, skip, gate, dt_bias, softplus, initial_state, lengths, 3)
     B, L, D = x.shape
-    dev = x.device
-    y = torch.empty((B, L, D), dtype=x.dtype, device=dev)
-    state = torch.empty((B, D, N), dtype=torch.float32, device=dev)
-    ck, cptr, cbytes = _scratch(torch, "sig_scan_checkpoint_bytes", args, dev) if checkpoint else (None, 0, 0)
-    keep, wptr, nbytes = _scratch(torch, "sig_scan_forward_workspace_bytes", args, dev)
-    _enqueue(dev, "sig_scan_forward", args, y.data_ptr(), state.data_ptr(), cptr, cbytes, wptr, nbytes)
+    y = make.new_empty((B, L, D))
+    state = make.new_empty((B, D, N), dtype=_f32)
+    ck, cptr, cbytes = _scratch(make, "sig_scan_checkpoint_bytes", args) if checkpoint else (None, 0, 0)
+    keep, wptr, nbytes = _scratch(make, "sig_scan_forward_workspace_bytes", args)
+    _enqueue(x.device, "sig_scan_forward", args, y.data_ptr(), state.data_ptr(), cptr, cbytes, wptr, nbytes)
     if not checkpoint:
         return y, state
-    return y, state, ck if ck is not None else torch.empty(0, dtype=torch.uint8, device=dev)
+    return y, state, ck if ck is not None else make.new_empty(0, dtype=_torch.uint8)
 
 
 def sig_scan_backward(x, dt, A, b, c, grad_out, checkpoint, skip=None, gate=None, dt_bias=None, softplus=True, initial_state=None, lengths=None,
                       grad_final_state=None):
     """Gradient of sig_scan_forward, whose `checkpoint` it reads: a dict of the gradients "x", "dt", "A", "B", "C", "skip", "gate", "dt_bias"
     and "initial_state", None for those whose input is None.  grad_out [B, L, D] of x's type, grad_final_state float32 [B, D, N] or None."""
-    torch, args, G, N, kept = _scan_args(x, dt, A, b, c, skip, gate, dt_bias, softplus, initial_state, lengths, 3)
+    make, args, G, N, kept = _scan_args(x, dt, A, b, c, skip, gate, dt_bias, softplus, initial_state, lengths, 3)
     B, L, D = x.shape
-    t, dev, f32 = x.dtype, x.device, torch.float32
-    grad_out = _tokens("grad_out", grad_out, x.shape, x)
-    grad_final_state = _whole("grad_final_state", grad_final_state, (B, D, N), f32, dev)
-    if not checkpoint.is_cuda or checkpoint.device != dev or not checkpoint.is_contiguous():
+    t, index = x.dtype, x.get_device()
+    grad_out, (sb, st, _) = _tokens("grad_out", grad_out, x.shape, t, index)
+    pf = 0
+    if grad_final_state is not None:
+        grad_final_state = _whole("grad_final_state", grad_final_state, (B, D, N), _f32, index)
+        pf = grad_final_state.data_ptr()
+    if checkpoint.get_device() != index or not checkpoint.is_contiguous():
         raise ValueError("checkpoint must be the tensor that sig_scan_forward returned")
-    gx, gdt = torch.empty((B, L, D), dtype=t, device=dev), torch.empty((B, L, D), dtype=t, device=dev)
-    gz = torch.empty((B, L, D), dtype=t, device=dev) if gate is not None else None
-    gb, gc = torch.empty((B, L, G, N), dtype=t, device=dev), torch.empty((B, L, G, N), dtype=t, device=dev)
-    gA = torch.empty((D, N), dtype=f32, device=dev)
-    gskip = torch.empty(D, dtype=f32, device=dev) if skip is not None else None
-    gbias = torch.empty(D, dtype=f32, device=dev) if dt_bias is not None else None
-    gi = torch.empty((B, D, N), dtype=f32, device=dev) if initial_state is not None else None
-    sb, st, _ = grad_out.stride()
-    grads = _SCAN_GRADS.pack(sb, st, grad_out.data_ptr(), _ptr(grad_final_state), gx.data_ptr(), gdt.data_ptr(), _ptr(gz), gb.data_ptr(),
-                             gc.data_ptr(), gA.data_ptr(), _ptr(gskip), _ptr(gbias), _ptr(gi))
-    keep, wptr, nbytes = _scratch(torch, "sig_scan_backward_workspace_bytes", args, dev)
-    _enqueue(dev, "sig_scan_backward", args, grads, checkpoint.data_ptr(), checkpoint.numel() * checkpoint.element_size(), wptr, nbytes)
-    if b.dim() == 3:
-        gb, gc = gb.view(B, L, N), gc.view(B, L, N)
-    return {"x": gx, "dt": gdt, "A": gA, "B": gb, "C": gc, "skip": gskip, "gate": gz, "dt_bias": gbias, "initial_state": gi}
+    tokens = lambda: make.new_empty((B, L, D))                                              # noqa: E731
+    params = lambda *shape: make.new_empty(shape, dtype=_f32)                               # noqa: E731
+    of_bc = (B, L, N) if b.dim() == 3 else (B, L, G, N)
+    g = {"x": tokens(), "dt": tokens(), "A": params(D, N), "B": make.new_empty(of_bc), "C": make.new_empty(of_bc),
+         "skip": params(D) if skip is not None else None, "gate": tokens() if gate is not None else None,
+         "dt_bias": params(D) if dt_bias is not None else None, "initial_state": params(B, D, N) if initial_state is not None else None}
+    ptr = lambda v: 0 if v is None else v.data_ptr()                                        # noqa: E731
+    grads = _SCAN_GRADS.pack(sb, st, grad_out.data_ptr(), pf, ptr(g["x"]), ptr(g["dt"]), ptr(g["gate"]), ptr(g["B"]), ptr(g["C"]), ptr(g["A"]),
+                             ptr(g["skip"]), ptr(g["dt_bias"]), ptr(g["initial_state"]))
+    keep, wptr, nbytes = _scratch(make, "sig_scan_backward_workspace_bytes", args)
+    _enqueue(x.device, "sig_scan_backward", args, grads, checkpoint.data_ptr(), checkpoint.numel() * checkpoint.element_size(), wptr, nbytes)
+    return g
 
 
 def sig_scan_step(x, dt, A, b, c, state, skip=None, gate=None, dt_bias=None, softplus=True):
     """One token of every stream: x, dt, gate [B, D], b, c [B, G, N] or [B, N]; state float32 [B, D, N] is updated in place.  Returns y [B, D]."""
-    torch, args, G, N, kept = _scan_args(x, dt, A, b, c, skip, gate, dt_bias, softplus, None, None, 2)
-    B, D = x.shape
-    _in_place("state", state, (B, D, N), torch.float32, x.device)
-    y = torch.empty((B, D), dtype=x.dtype, device=x.device)
+    make, args, G, N, kept = _scan_args(x, dt, A, b, c, skip, gate, dt_bias, softplus, None, None, 2)
+    B, D = shape = x.shape
+    _in_place("state", state, (B, D, N), _f32, x.get_device())
+    y = make.new_empty(shape)
     _enqueue(x.device, "sig_scan_step", args, state.data_ptr(), y.data_ptr())
     return y
 
@@ -249,31 +264,36 @@ def sig_grad_clip(grads, max_norm, out=None):
     writes the products into the tensors `out` (of the same sizes, either type).  Returns norm, a float32 tensor of no axes on the
     device.  Tensors may have any order of axes as long as they fill their memory; those of `out` have that of their input."""
     torch = _t()
-    f32, b16 = torch.float32, torch.bfloat16
     grads = list(grads)
     outs = grads if out is None else list(out)
-    if len(outs) != len(grads):
+    n = len(grads)
+    if len(outs) != n:
         raise ValueError("out must have a tensor for each of grads")
     if not max_norm >= 0:
         raise ValueError("max_norm must not be negative")
-    dev = grads[0].device if grads else torch.device("cuda", torch.cuda.current_device())
+    dev = grads[0].device if n else torch.device("cuda", torch.cuda.current_device())
     if dev.type != "cuda":
         raise ValueError("grads must be CUDA tensors")
+    index, kinds = dev.index, {_f32: 0, _b16: 1}
+    into, to, sizes, from_kinds, to_kinds = [], [], [], [], []
     for g, o in zip(grads, outs):
-        if g.device != dev or o.device != dev or g.dtype not in (f32, b16) or o.dtype not in (f32, b16):
-            raise ValueError("grads and out must be float32 or bfloat16 tensors on one device")
-        if g.shape != o.shape or not (g.is_contiguous() and o.is_contiguous()) and (
-                g.stride() != o.stride() or not torch.ops.aten.is_non_overlapping_and_dense(g)):
-            raise ValueError("every tensor must fill its memory, and out must have the shape and the order of axes of grads")
-    n = len(grads)
-    tab = array.array("q", [g.data_ptr() for g in grads])
-    tab.extend(o.data_ptr() for o in outs)
-    tab.extend(g.numel() for g in grads)
-    tab.extend(int(g.dtype is b16) for g in grads)
-    tab.extend(int(o.dtype is b16) for o in outs)
-    at, _ = tab.buffer_info()
-    norm = torch.empty((), dtype=f32, device=dev)
+        k = kinds.get(g.dtype)
+        if k is None or g.get_device() != index:
+            raise ValueError("grads must be float32 or bfloat16 tensors on one device")
+        p = q = g.data_ptr()
+        m = k
+        if o is not g:
+            m, q = kinds.get(o.dtype), o.data_ptr()
+            if m is None or o.get_device() != index or o.shape != g.shape:
+                raise ValueError("out must have float32 or bfloat16 tensors of the shapes of grads on their device")
+        if not g.is_contiguous() or not o.is_contiguous():
+            if g.stride() != o.stride() or not torch.ops.aten.is_non_overlapping_and_dense(g):
+                raise ValueError("every tensor must fill its memory, and out must have the order of axes of grads")
+        into.append(p), to.append(q), sizes.append(g.numel()), from_kinds.append(k), to_kinds.append(m)
+    tab = array.array("q", into + to + sizes + from_kinds + to_kinds)
+    at = tab.buffer_info()[0]
+    norm = torch.empty((), dtype=_f32, device=dev)
     nbytes = (_calls.get("sig_grad_clip_workspace_bytes") or _call("sig_grad_clip_workspace_bytes"))(n, at + 16 * n)
-    keep = torch.empty(nbytes, dtype=torch.uint8, device=dev)
-    _enqueue(dev, "sig_grad_clip", n, at, at + 8 * n, at + 16 * n, at + 24 * n, at + 32 * n, float(max_norm), norm.data_ptr(), _ptr(keep), nbytes)
+    keep = norm.new_empty(nbytes, dtype=torch.uint8)
+    _enqueue(dev, "sig_grad_clip", n, at, at + 8 * n, at + 16 * n, at + 24 * n, at + 32 * n, float(max_norm), norm.data_ptr(), keep.data_ptr(), nbytes)
     return norm
