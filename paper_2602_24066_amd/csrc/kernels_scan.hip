@@ -21,72 +21,6 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kTile = kScanTile;
 
-// Q lanes hold the states of a channel, S each (state n = lane * S + s; N <= Q S, the rest are zero): a wavefront has 64 / Q channels.
-template <int Q_, int S_> struct Shape { static constexpr int Q = Q_, S = S_, channels = 64 / Q_; };
-
-// The waves of a launch, one for each stream, group and run of channels of that group.
-struct Rows {
-    int64_t per_group;   // channels of a group
-    int64_t runs;        // wavefronts for the channels of a group
-    int64_t total;
-};
-template <class Sh> Rows rows_of(const sig_scan_args& a)
-{
-    Rows r;
-    r.per_group = a.D / a.G;
-    r.runs = (r.per_group + Sh::channels - 1) / Sh::channels;
-    r.total = a.B * a.G * r.runs;
-    return r;
-}
-
-template <int Q> __device__ __forceinline__ float sum_states(float v)     // over the Q lanes of a channel
-{
-#pragma unroll
-    for (int m = 1; m < Q; m *= 2) v += __shfl_xor(v, m);
-    return v;
-}
-
-// what a lane knows of its channel
-template <class T, class Sh> struct Lane {
-    int64_t b, g, d, len;
-    int q;
-    bool on;             // the channel exists
-    float A[Sh::S], skip, bias;
-    const T *x, *dt, *gate, *B, *C;
-    __device__ __forceinline__ Lane(const sig_scan_args& a, const Rows& r, int64_t row)
-    {
-        int lane = threadIdx.x & 63;
-        int64_t run = row % r.runs, bg = row / r.runs;
-        g = bg % a.G, b = bg / a.G;
-        int64_t c = run * Sh::channels + lane / Sh::Q;
-        q = lane % Sh::Q;
-        on = c < r.per_group;
-        d = g * r.per_group + (on ? c : 0);
-        len = live_length(a.lengths, b, a.L);
-#pragma unroll
-        for (int s = 0; s < Sh::S; s++) A[s] = q * Sh::S + s < a.N ? a.A[d * a.N + q * Sh::S + s] : 0.0f;
-        skip = a.skip ? a.skip[d] : 0.0f;
-        bias = a.dt_bias ? a.dt_bias[d] : 0.0f;
-        x = (const T*)a.x + b * a.x_stride_b + d;
-        dt = (const T*)a.dt + b * a.dt_stride_b + d;
-        gate = a.gate ? (const T*)a.gate + b * a.gate_stride_b + d : nullptr;
-        B = (const T*)a.b + b * a.b_stride_b + g * a.b_stride_g + q * Sh::S;
-        C = (const T*)a.c + b * a.c_stride_b + g * a.c_stride_g + q * Sh::S;
-    }
-    __device__ __forceinline__ int64_t state(const sig_scan_args& a) const { return (b * a.D + d) * a.N + q * Sh::S; }
-};
-
-template <int S> __device__ __forceinline__ void load_states(float (&h)[S], const float* p, int n)
-{
-#pragma unroll
-    for (int s = 0; s < S; s++) h[s] = p && s < n ? p[s] : 0.0f;
-}
-template <class T, int S> __device__ __forceinline__ void load_row(float (&h)[S], const T* p, int n)
-{
-#pragma unroll
-    for (int s = 0; s < S; s++) h[s] = s < n ? to_float(p[s]) : 0.0f;
-}
-
 // ---- forward
 // A workgroup takes 64 neighbouring channels of one stream and group, a channel a lane; its W wavefronts share out the states, S each, so
 // that loads and stores of tokens are whole lines and sums over states meet in LDS once a token.  Tiles of 16 tokens: the wavefronts
@@ -175,6 +109,28 @@ struct ChunkStates {
     float* last;         // [B, chunks, N, D]
     float* steps;        // [B, chunks, D]
 };
+// h over the chunks from `from` to `to` (without it, in either direction): h = exp(A2 steps) h + last, eight chunks' loads under way at a
+// time.  last, steps: the lane's channel and the wavefront's first state in the stream's first chunk; n: states there are.
+template <int S> __device__ __forceinline__ void join_chunks(float (&h)[S], const float (&A2)[S], int from, int to, const float* last, const float* steps, int64_t N, int64_t D, int n)
+{
+    constexpr int U = 8;
+    const int way = to >= from ? 1 : -1, count = (to - from) * way;
+    for (int j0 = 0; j0 < count; j0 += U) {
+        float sum[U], l[U][S];
+#pragma unroll
+        for (int u = 0; u < U; u++) {
+            const bool there = j0 + u < count;
+            const int64_t row = there ? from + way * (j0 + u) : from;
+            sum[u] = there ? steps[row * D] : 0.0f;
+#pragma unroll
+            for (int s = 0; s < S; s++) l[u][s] = there && s < n ? last[(row * N + s) * D] : 0.0f;
+        }
+#pragma unroll
+        for (int u = 0; u < U; u++)
+#pragma unroll
+            for (int s = 0; s < S; s++) h[s] = fmaf(__builtin_amdgcn_exp2f(A2[s] * sum[u]), h[s], l[u][s]);
+    }
+}
 
 template <class T, class Gr, bool kOutputs>
 __global__ __launch_bounds__(Gr::W * 64, Gr::W > 2 && Gr::S == 4 ? 4 : 2) void scan_fwd_kernel(sig_scan_args a, Blocks bl, ChunkStates cs, T* y, float* final_state, float* checkpoint)
@@ -203,13 +159,8 @@ __global__ __launch_bounds__(Gr::W * 64, Gr::W > 2 && Gr::S == 4 ? 4 : 2) void s
         h[s] = kOutputs && a.initial_state && n0 + s < a.N ? a.initial_state[(b * a.D + d) * a.N + n0 + s] : 0.0f;
     }
     if constexpr (kOutputs) {
-        const float *last = cs.last + (b * bl.chunks * a.N + n0) * a.D + d0, *sums_of = cs.steps + b * bl.chunks * a.D + d0;
-        for (unsigned j = 0; j < c && (int)j * bl.chunk < len; j++, last += a.N * a.D, sums_of += a.D) {
-            float sum = sums_of[e];
-#pragma unroll
-            for (int s = 0; s < S; s++)
-                if (n0 + s < a.N) h[s] = fmaf(__builtin_amdgcn_exp2f(A[s] * sum), h[s], (last + s * a.D)[e]);
-        }
+        const int before = len > 0 ? min((int)c, (len - 1) / bl.chunk + 1) : 0;          // chunks with tokens before this one
+        join_chunks(h, A, 0, before, cs.last + (b * bl.chunks * a.N + n0) * a.D + d, cs.steps + b * bl.chunks * a.D + d, a.N, a.D, (int)a.N - n0);
     }
     // rows of the wavefront's first token of the chunk, and of its first token's B and C
     const int64_t t1 = t_first + w * PT;
@@ -463,14 +414,9 @@ __global__ __launch_bounds__(Gr::W * 64, Gr::W > 8 ? 4 : 2) void scan_bwd_kernel
         adj[s] = kFull && g.grad_final_state && n0 + s < a.N ? g.grad_final_state[(b * a.D + d) * a.N + n0 + s] : 0.0f;
     }
     if constexpr (kFull) {
-        const int after = (len - 1) / bl.chunk;            // the last chunk with tokens (len > 0)
-        for (int j = len > 0 ? after : 0; j > (int)c; j--) {
-            const int64_t row = b * bl.chunks + j;
-            float sum = cs.steps[row * a.D + d];
-#pragma unroll
-            for (int s = 0; s < S; s++)
-                if (n0 + s < a.N) adj[s] = fmaf(__builtin_amdgcn_exp2f(A2[s] * sum), adj[s], cs.last[(row * a.N + n0 + s) * a.D + d]);
-        }
+        const int after = len > 0 ? (len - 1) / bl.chunk : 0;      // the last chunk with tokens
+        if (after > (int)c)
+            join_chunks(adj, A2, after, (int)c, cs.last + (b * bl.chunks * a.N + n0) * a.D + d, cs.steps + b * bl.chunks * a.D + d, a.N, a.D, (int)a.N - n0);
     }
     // tiles with tokens that count, and the tokens of the last one: none for a chunk beyond the stream's length
     const int n_tiles = live > 0 ? (live + kTile - 1) / kTile : 0, n_last = n_tiles > 0 ? live - (n_tiles - 1) * kTile : 0;
@@ -755,31 +701,60 @@ __global__ __launch_bounds__(1024) void scan_bwd_params_kernel(sig_scan_args a, 
     }
 }
 
-template <class T, class Sh> __global__ __launch_bounds__(kThreads) void scan_step_kernel(sig_scan_args a, Rows r, float* state, T* y)
+// ---- one token
+// Q lanes hold the states of a channel, S each (state n = lane * S + s; N <= Q S, the rest are zero): reads and writes of the states, which are
+// nearly all there is, are contiguous over the wavefront, 16 bytes a lane where they are aligned (kWide).
+template <int Q_, int S_> struct Shape { static constexpr int Q = Q_, S = S_, channels = 64 / Q_; };
+
+template <class T, int S, bool kWide> __device__ __forceinline__ void load_states(float (&h)[S], const T* p, int n)
 {
-    int64_t row = (int64_t)blockIdx.x * (kThreads / 64) + threadIdx.x / 64;
-    if (row >= r.total) return;
-    Lane<T, Sh> l(a, r, row);
-    int n = (int)min((int64_t)Sh::S, a.N - l.q * Sh::S);
-    float h[Sh::S], B[Sh::S], C[Sh::S];
-    load_states(h, state + l.state(a), n);
-    float x = to_float(l.x[0]), D = to_float(l.dt[0]) + l.bias, o = 0.0f;
-    if (a.softplus) D = softplus(D);
-    load_row(B, l.B, n);
-    load_row(C, l.C, n);
+    if constexpr (kWide) {
+        Pack<T, S> r = *(const Pack<T, S>*)p;
 #pragma unroll
-    for (int s = 0; s < Sh::S; s++) {
-        h[s] = fmaf(fast_exp(D * l.A[s]), h[s], D * x * B[s]);
+        for (int s = 0; s < S; s++) h[s] = to_float(r.v[s]);
+    } else {
+#pragma unroll
+        for (int s = 0; s < S; s++) h[s] = s < n ? to_float(p[s]) : 0.0f;
+    }
+}
+
+template <class T, class Sh, bool kWide> __global__ __launch_bounds__(kThreads) void scan_step_kernel(sig_scan_args a, float* state, T* y)
+{
+    constexpr int S = Sh::S, Q = Sh::Q;
+    const unsigned D = (unsigned)a.D, id = blockIdx.x * (kThreads / Q) + threadIdx.x / Q, q = threadIdx.x % Q;      // the channel, over all streams
+    const bool on = id < (unsigned)a.B * D;
+    const unsigned at = on ? id : 0, b = at / D, d = at % D, g = d / (D / (unsigned)a.G);
+    const int n = min(S, (int)a.N - (int)q * S);
+    float A[S], h[S], B[S], C[S];
+    float* to = state + (int64_t)at * a.N + q * S;
+    load_states<float, S, kWide>(h, to, n);
+    load_states<float, S, kWide>(A, a.A + (int64_t)d * a.N + q * S, n);
+    load_states<T, S, false>(B, (const T*)a.b + b * a.b_stride_b + g * a.b_stride_g + q * S, n);
+    load_states<T, S, false>(C, (const T*)a.c + b * a.c_stride_b + g * a.c_stride_g + q * S, n);
+    const float x = to_float(((const T*)a.x)[b * a.x_stride_b + d]), z = a.gate ? to_float(((const T*)a.gate)[b * a.gate_stride_b + d]) : 0.0f;
+    float step = to_float(((const T*)a.dt)[b * a.dt_stride_b + d]) + (a.dt_bias ? a.dt_bias[d] : 0.0f), o = 0.0f;
+    if (a.softplus) step = softplus(step);
+#pragma unroll
+    for (int s = 0; s < S; s++) {
+        h[s] = fmaf(fast_exp(step * A[s]), h[s], step * x * B[s]);
         o = fmaf(C[s], h[s], o);
     }
-    o = fmaf(l.skip, x, sum_states<Sh::Q>(o));
-    if (l.gate) {
-        float z = to_float(l.gate[0]);
-        o *= z * sigmoid(z);
+#pragma unroll
+    for (int m = 1; m < Q; m *= 2) o += __shfl_xor(o, m);
+    if (a.skip) o = fmaf(a.skip[d], x, o);
+    if (a.gate) o *= z * sigmoid(z);
+    if (!on) return;
+    if constexpr (kWide) {
+        Pack<float, S> r;
+#pragma unroll
+        for (int s = 0; s < S; s++) r.v[s] = h[s];
+        *(Pack<float, S>*)to = r;
+    } else {
+#pragma unroll
+        for (int s = 0; s < S; s++)
+            if (s < n) to[s] = h[s];
     }
-    if (!l.on) return;
-    for (int s = 0; s < n; s++) state[l.state(a) + s] = h[s];
-    if (l.q == 0) y[l.b * a.D + l.d] = from_float<T>(o);
+    if (q == 0) y[at] = from_float<T>(o);
 }
 
 unsigned blocks_for(int64_t threads) { return (unsigned)((threads + kThreads - 1) / kThreads); }
@@ -896,8 +871,10 @@ hipError_t scan_step(const sig_scan_args& a, float* state, void* y, hipStream_t 
         return with_shape(a.N, [&](auto sh) {
             using T = decltype(t);
             using Sh = decltype(sh);
-            Rows r = rows_of<Sh>(a);
-            scan_step_kernel<T, Sh><<<blocks_for(r.total * 64), kThreads, 0, stream>>>(a, r, state, (T*)y);
+            const bool wide = a.N == Sh::Q * Sh::S && (((uintptr_t)state | (uintptr_t)a.A) & (Sh::S * 4 - 1)) == 0;
+            const unsigned blocks = blocks_for(a.B * a.D * Sh::Q);
+            if (wide) scan_step_kernel<T, Sh, true><<<blocks, kThreads, 0, stream>>>(a, state, (T*)y);
+            else scan_step_kernel<T, Sh, false><<<blocks, kThreads, 0, stream>>>(a, state, (T*)y);
             return hipGetLastError();
         });
     });
