@@ -122,10 +122,20 @@ __global__ __launch_bounds__(kThreads) void conv_fwd_kernel(sig_conv_args a, T* 
 #pragma unroll
         for (int u = 0; u < U; u++) now[u] = next[u];
     }
-    for (; t < end; t++, x += a.x_stride_t) {
-        float in[V];
-        load<T, V>(in, x);
-        token(in);
+    if (t < end) {                      // the last, incomplete group
+        Pack<T, V> some[U] = {};
+#pragma unroll
+        for (int u = 0; u < U; u++)
+            if (t + u < end) some[u] = *(const Pack<T, V>*)(x + u * a.x_stride_t);
+#pragma unroll
+        for (int u = 0; u < U; u++) {
+            if (t + u >= end) break;
+            float in[V];
+#pragma unroll
+            for (int i = 0; i < V; i++) in[i] = to_float(some[u].v[i]);
+            token(in);
+        }
+        t = end;
     }
     x = (const T*)a.x + b * a.x_stride_b + d;
     float zero[V] = {};
@@ -224,13 +234,19 @@ __global__ __launch_bounds__(kThreads) void conv_bwd_kernel(sig_conv_args a, Con
 #pragma unroll
         for (int u = 0; u < U; u++) nx[u] = mx[u], ng[u] = mg[u];
     }
-    for (; t < t1 + W - 1; t++) {
-        float in[V] = {}, up[V] = {};
-        if (t < len) {
-            load<T, V>(in, x + t * a.x_stride_t);
-            load<T, V>(up, gy + t * g.gy_stride_t);
+    for (; t < t1 + W - 1; t += U) {    // incomplete groups, the W - 1 tokens after the chunk and what does not count among them
+        Pack<T, V> sx[U] = {}, sg[U] = {};
+#pragma unroll
+        for (int u = 0; u < U; u++)
+            if (t + u < len && t + u < t1 + W - 1) sx[u] = *(const Pack<T, V>*)(x + (t + u) * a.x_stride_t), sg[u] = *(const Pack<T, V>*)(gy + (t + u) * g.gy_stride_t);
+#pragma unroll
+        for (int u = 0; u < U; u++) {
+            if (t + u >= t1 + W - 1) break;
+            float in[V], up[V];
+#pragma unroll
+            for (int i = 0; i < V; i++) in[i] = to_float(sx[u].v[i]), up[i] = to_float(sg[u].v[i]);
+            token(t + u, in, up, t + u < len);
         }
-        token(t, in, up, t < len);
     }
     part += row * (W + 1) * a.D + d;
 #pragma unroll

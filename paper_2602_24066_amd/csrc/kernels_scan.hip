@@ -775,7 +775,6 @@ template <class F> auto with_type(int64_t dtype, F f) { return dtype == SIG_BF16
 // on eight wavefronts, 504 with four on four (a wavefront alone on its SIMD), 525 with one on sixteen (their sums fill the LDS pipe).
 template <class F> auto with_group(int64_t N, F f)
 {
-    if (N <= 4) return f(Group<2, 2>());
     if (N <= 8) return f(Group<2, 4>());
     if (N <= 16) return f(Group<2, 8>());
     if (N <= 32) return f(Group<4, 8>());

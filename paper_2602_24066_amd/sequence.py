@@ -261,7 +261,7 @@ def sig_scan_step(x, dt, A, b, c, state, skip=None, gate=None, dt_bias=None, sof
 
 def sig_grad_clip(grads, max_norm, out=None):
     """Scales the tensors `grads` (float32 or bfloat16, one device) in place by min(1, max_norm / (norm + 1e-6)), norm their global 2-norm, or
-    writes the products into the tensors `out` (of the same sizes, either type).  Returns norm, a float32 tensor of no axes on the
+    writes the products into the tensors `out` (of as many elements, either type).  Returns norm, a float32 tensor of no axes on the
     device.  Tensors may have any order of axes as long as they fill their memory; those of `out` have that of their input."""
     torch = _t()
     grads = list(grads)
@@ -274,22 +274,18 @@ def sig_grad_clip(grads, max_norm, out=None):
     dev = grads[0].device if n else torch.device("cuda", torch.cuda.current_device())
     if dev.type != "cuda":
         raise ValueError("grads must be CUDA tensors")
-    index, kinds = dev.index, {_f32: 0, _b16: 1}
-    into, to, sizes, from_kinds, to_kinds = [], [], [], [], []
+    index, kind = dev.index, {_f32: 0, _b16: 1}.get
+    into, sizes, from_kinds = [g.data_ptr() for g in grads], [g.numel() for g in grads], [kind(g.dtype) for g in grads]
+    to, to_kinds = into, from_kinds
+    if out is not None:
+        to, to_kinds = [o.data_ptr() for o in outs], [kind(o.dtype) for o in outs]
+        if [o.numel() for o in outs] != sizes:
+            raise ValueError("out must have tensors of the sizes of grads")
+    if None in from_kinds or None in to_kinds or any(t.get_device() != index for t in (grads if out is None else grads + outs)):
+        raise ValueError("grads and out must be float32 or bfloat16 tensors on one device")
     for g, o in zip(grads, outs):
-        k = kinds.get(g.dtype)
-        if k is None or g.get_device() != index:
-            raise ValueError("grads must be float32 or bfloat16 tensors on one device")
-        p = q = g.data_ptr()
-        m = k
-        if o is not g:
-            m, q = kinds.get(o.dtype), o.data_ptr()
-            if m is None or o.get_device() != index or o.shape != g.shape:
-                raise ValueError("out must have float32 or bfloat16 tensors of the shapes of grads on their device")
-        if not g.is_contiguous() or not o.is_contiguous():
-            if g.stride() != o.stride() or not torch.ops.aten.is_non_overlapping_and_dense(g):
-                raise ValueError("every tensor must fill its memory, and out must have the order of axes of grads")
-        into.append(p), to.append(q), sizes.append(g.numel()), from_kinds.append(k), to_kinds.append(m)
+        if not (g.is_contiguous() and o.is_contiguous()) and (g.shape != o.shape or g.stride() != o.stride() or not torch.ops.aten.is_non_overlapping_and_dense(g)):
+            raise ValueError("every tensor must fill its memory, and out must have the order of axes of grads")
     tab = array.array("q", into + to + sizes + from_kinds + to_kinds)
     at = tab.buffer_info()[0]
     norm = torch.empty((), dtype=_f32, device=dev)
