@@ -142,6 +142,7 @@ __global__ __launch_bounds__(Gr::W * 64, Gr::W > 2 && Gr::S == 4 ? 4 : 2) void s
     float4(*sums)[kTile / 4][64] = (float4(*)[kTile / 4][64])(lds + 4 * kTile * 64);     // [2][W][kTile / 4][64]
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     const unsigned c = blockIdx.x % bl.chunks, rest = blockIdx.x / bl.chunks, run = rest % bl.runs, bg = rest / bl.runs;
+    if (!kOutputs && c + 1 == bl.chunks) return;          // nothing comes after the last chunk's state
     const int64_t g = bg % (unsigned)a.G, b = bg / (unsigned)a.G;
     const int64_t d0 = g * bl.per_group + run * 64;       // the workgroup's first channel
     const bool on = run * 64 + lane < bl.per_group;
@@ -396,6 +397,7 @@ __global__ __launch_bounds__(Gr::W * 64, Gr::W > 8 ? 4 : 2) void scan_bwd_kernel
     float(*sums)[3][kHalf][64] = (float(*)[3][kHalf][64])(lds + 2 * 3 * kTile * 64);                     // [2 or 1][W][3][kHalf][64]
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     const unsigned c = blockIdx.x % bl.chunks, rest = blockIdx.x / bl.chunks, run = rest % bl.runs, bg = rest / bl.runs;
+    if (!kFull && c == 0) return;                          // nothing comes before the first chunk's adjoint state
     const int64_t grp = bg % (unsigned)a.G, b = bg / (unsigned)a.G;
     const int64_t d0 = grp * bl.per_group + run * 64;
     const bool on = run * 64 + lane < bl.per_group;
@@ -781,20 +783,56 @@ template <class F> auto with_group(int64_t N, F f)
     return f(Group<4, 16>());
 }
 
-// Time chunks cost a second pass over most of the work and are taken where a launch would leave SIMDs without a wavefront: then as many
-// as give each four (1 x 16384 x 1024: 327 us with 8 chunks, 188 with 16, 173 with 32; 8 x 4096 x 2048: 386 us with one, 541 with two).
-Blocks blocks_of(const sig_scan_args& a)
+// Time chunks give a launch of few workgroups more of them, for a second pass over a part of the work (`second` of the first one's time).  The chunks are those
+// with the least time by a model: a compute unit runs `resident` workgroups at once (what LDS allows), W wavefronts each, whose SIMDs
+// issue at kRate of their rate with one to four wavefronts; workgroups beyond what the chip holds wait for a round of their own.
+// Unit: a wavefront's work on a token, 104 of them a microsecond.  Measured, forward of 16 states in bf16 over 2,048 channels: 8 streams of 4,096
+// tokens 389 us with one chunk, 541 with two; 16 of 2,048 316 us; a stream of 16,384 over 1,024 channels 327 us with 8 chunks, 188 with
+// 16, 169 with 32.
+constexpr double kRate[] = {0.45, 0.8, 0.93, 1.0};
+constexpr int kUnits = 256;
+double launch_time(int64_t workgroups, int W, int resident, double tokens)
+{
+    auto round = [&](int64_t n) {        // n workgroups on a compute unit
+        const int waves = std::min<int64_t>(4, (n * W + 3) / 4);
+        return n ? (double)(n * W) / kRate[waves - 1] : 0.0;
+    };
+    const int64_t most = (int64_t)kUnits * resident, left = workgroups % most;
+    return tokens * ((double)(workgroups / most) * round(resident) + round((left + kUnits - 1) / kUnits));
+}
+
+Blocks blocks_of(const sig_scan_args& a, int resident, double second)
 {
     Blocks bl;
     bl.per_group = a.D / a.G;
     bl.runs = (unsigned)((bl.per_group + 63) / 64);
-    int64_t rows = a.B * a.G * bl.runs, waves = std::max<int64_t>(1, rows * with_group(a.N, [](auto gr) { return decltype(gr)::W; }));
-    int64_t want = waves >= 1024 ? 1 : std::min<int64_t>(64, 4096 / waves);
-    int64_t tiles = std::max<int64_t>(1, tiles_of(a)), per = std::max<int64_t>(2, (tiles + want - 1) / want);
-    bl.chunk = (int)(per * kTile);
-    bl.chunks = (unsigned)((tiles + per - 1) / per);
+    const int64_t rows = a.B * a.G * bl.runs, tiles = std::max<int64_t>(1, tiles_of(a));
+    const int W = with_group(a.N, [](auto gr) { return decltype(gr)::W; });
+    int64_t best = tiles;
+    double least = launch_time(rows, W, resident, (double)tiles * kTile);
+    for (int64_t c = 2; c <= 64 && 2 * c <= tiles; c++) {
+        const int64_t per = (tiles + c - 1) / c, chunks = (tiles + per - 1) / per;
+        // a launch more and, for every chunk before a workgroup's own, an eighth of a memory access' latency
+        const double t = launch_time(rows * chunks, W, resident, (double)per * kTile) * (1.0 + second * (double)(chunks - 1) / (double)chunks) + 800.0 + 20.0 * (double)chunks;
+        if (t < least) least = t, best = per;
+    }
+    bl.chunk = (int)(best * kTile);
+    bl.chunks = (unsigned)((tiles + best - 1) / best);
     bl.total = (unsigned)(rows * bl.chunks);
     return bl;
+}
+
+// dynamic LDS of the kernels in bytes, and the workgroups of a compute unit that it leaves room for
+constexpr int kLds = 160 * 1024;
+constexpr int forward_lds(int W) { return 2 * kTile * 64 * 8 + 2 * W * kTile * 64 * 4; }
+constexpr int backward_lds(int W) { return 2 * 3 * kTile * 64 * 4 + (W <= 8 ? 2 : 1) * W * 3 * kTile / 2 * 64 * 4; }
+Blocks forward_blocks(const sig_scan_args& a)
+{
+    return blocks_of(a, with_group(a.N, [](auto gr) { return kLds / forward_lds(decltype(gr)::W); }), 0.7);
+}
+Blocks backward_blocks(const sig_scan_args& a)
+{
+    return blocks_of(a, with_group(a.N, [](auto gr) { return kLds / backward_lds(decltype(gr)::W); }), 0.25);
 }
 
 // floats of the chunks' states, and of a backward launch's sums
@@ -809,29 +847,29 @@ PartFloats part_floats(const sig_scan_args& a, const Blocks& bl)
 
 }  // namespace
 
-size_t scan_forward_workspace(const sig_scan_args& a) { return chunk_floats(a, blocks_of(a)) * 4; }
+size_t scan_forward_workspace(const sig_scan_args& a) { return chunk_floats(a, forward_blocks(a)) * 4; }
 size_t scan_backward_workspace(const sig_scan_args& a)
 {
-    Blocks bl = blocks_of(a);
+    Blocks bl = backward_blocks(a);
     PartFloats p = part_floats(a, bl);
     return (p.bc + p.A + p.rest + chunk_floats(a, bl)) * 4;
 }
 
 hipError_t scan_forward(const sig_scan_args& a, void* y, float* final_state, float* checkpoint, float* workspace, hipStream_t stream)
 {
-    Blocks bl = blocks_of(a);
+    Blocks bl = forward_blocks(a);
     ChunkStates cs{workspace, workspace ? workspace + a.B * bl.chunks * a.N * a.D : nullptr};
     return with_type(a.dtype, [&](auto t) {
         return with_group(a.N, [&](auto gr) {
             using T = decltype(t);
             using Gr = decltype(gr);
-            constexpr int steps = 2 * kTile * 64 * 8, sums = 2 * Gr::W * kTile * 64 * 4;
-            if (steps + sums > 65536) {
-                hipError_t e = ensure_dynamic_lds((const void*)scan_fwd_kernel<T, Gr, true>, steps + sums);
+            constexpr int lds = forward_lds(Gr::W);
+            if (lds > 65536) {
+                hipError_t e = ensure_dynamic_lds((const void*)scan_fwd_kernel<T, Gr, true>, lds);
                 if (e != hipSuccess) return e;
             }
-            if (bl.chunks > 1) scan_fwd_kernel<T, Gr, false><<<bl.total, Gr::W * 64, steps, stream>>>(a, bl, cs, nullptr, nullptr, nullptr);
-            scan_fwd_kernel<T, Gr, true><<<bl.total, Gr::W * 64, steps + sums, stream>>>(a, bl, cs, (T*)y, final_state, checkpoint);
+            if (bl.chunks > 1) scan_fwd_kernel<T, Gr, false><<<bl.total, Gr::W * 64, forward_lds(0), stream>>>(a, bl, cs, nullptr, nullptr, nullptr);
+            scan_fwd_kernel<T, Gr, true><<<bl.total, Gr::W * 64, lds, stream>>>(a, bl, cs, (T*)y, final_state, checkpoint);
             return hipGetLastError();
         });
     });
@@ -839,7 +877,7 @@ hipError_t scan_forward(const sig_scan_args& a, void* y, float* final_state, flo
 
 hipError_t scan_backward(const sig_scan_args& a, const sig_scan_grads& g, const float* checkpoint, float* workspace, hipStream_t stream)
 {
-    Blocks bl = blocks_of(a);
+    Blocks bl = backward_blocks(a);
     PartFloats p = part_floats(a, bl);
     Parts parts{workspace, workspace + p.bc, workspace + p.bc + p.A};
     float* states = parts.rest + p.rest;
@@ -848,14 +886,14 @@ hipError_t scan_backward(const sig_scan_args& a, const sig_scan_grads& g, const 
         return with_group(a.N, [&](auto gr) {
             using T = decltype(t);
             using Gr = decltype(gr);
-            constexpr int in = 2 * 3 * kTile * 64 * 4, sums = (Gr::W <= 8 ? 2 : 1) * Gr::W * 3 * kTile / 2 * 64 * 4;
-            if (in + sums > 65536) {
-                hipError_t e = ensure_dynamic_lds((const void*)scan_bwd_kernel<T, Gr, true>, in + sums);
+            constexpr int lds = backward_lds(Gr::W);
+            if (lds > 65536) {
+                hipError_t e = ensure_dynamic_lds((const void*)scan_bwd_kernel<T, Gr, true>, lds);
                 if (e != hipSuccess) return e;
             }
             if (a.B > 0) {
-                if (bl.chunks > 1) scan_bwd_kernel<T, Gr, false><<<bl.total, Gr::W * 64, in, stream>>>(a, g, bl, cs, nullptr, parts);
-                scan_bwd_kernel<T, Gr, true><<<bl.total, Gr::W * 64, in + sums, stream>>>(a, g, bl, cs, checkpoint, parts);
+                if (bl.chunks > 1) scan_bwd_kernel<T, Gr, false><<<bl.total, Gr::W * 64, backward_lds(0), stream>>>(a, g, bl, cs, nullptr, parts);
+                scan_bwd_kernel<T, Gr, true><<<bl.total, Gr::W * 64, lds, stream>>>(a, g, bl, cs, checkpoint, parts);
                 if (a.L > 0) scan_bwd_bc_kernel<T, Gr><<<blocks_for(p.bc / bl.runs), kThreads, 0, stream>>>(a, bl, parts.bc, (T*)g.grad_b, (T*)g.grad_c);
             }
             scan_bwd_params_kernel<<<(unsigned)((a.D * (a.N + 2) + 63) / 64), 1024, 0, stream>>>(a, a.B * bl.chunks, parts, g.grad_A, g.grad_skip, g.grad_dt_bias);
