@@ -99,9 +99,13 @@ __device__ __forceinline__ float sum_rows(const float* p, int64_t rows, int64_t 
     const int lane = threadIdx.x & 63, w = threadIdx.x / 64;
     float v[4] = {};
     int64_t r = w;
-    for (; r + 48 < rows; r += 64)
+    for (; r + 112 < rows; r += 128) {
+        float q[8];
 #pragma unroll
-        for (int i = 0; i < 4; i++) v[i] += p[(r + 16 * i) * step];
+        for (int i = 0; i < 8; i++) q[i] = p[(r + 16 * i) * step];
+#pragma unroll
+        for (int i = 0; i < 8; i++) v[i % 4] += q[i];
+    }
     for (; r < rows; r += 16) v[0] += p[r * step];
     part[w][lane] = (v[0] + v[1]) + (v[2] + v[3]);
     __syncthreads();
