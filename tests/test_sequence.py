@@ -117,6 +117,10 @@ SCAN = [
     (1, 600, 70, 1, 16, "f32", True, True, None),              # long: many tiles
     (2, 300, 66, 1, 4, "bf16", False, True, [-1, 1000]),       # lengths out of range are clamped
     (1, 2100, 17, 1, 16, "f32", True, True, [2077]),
+    (34, 20, 512, 2, 16, "bf16", False, True, None),           # more workgroups than compute units: no time chunks
+    (3, 500, 65, 1, 16, "f32", True, True, [500, 480, 31]),    # time chunks that lie beyond a stream's tokens, a length at a chunk's end
+    (1, 5000, 3, 1, 8, "f32", True, False, None),              # as many time chunks as there are
+    (2, 130, 33, 1, 48, "bf16", True, True, [129, 2]),
 ]
 
 
@@ -280,6 +284,37 @@ def test_offsets_beyond_32_bits():
             first = got
     for p, q in zip(first, got):
         assert p is None and q is None or torch.equal(p, q)
+
+
+@gpu
+def test_time_strides_beyond_the_kernels_reach():
+    """Tokens 2^26 elements apart are copied by the package and refused by the library; 2^22 apart they are read as they are."""
+    D, N, L = 24, 16, 3
+    w, A = torch.randn(D, 4, device="cuda"), -torch.ones(D, N, device="cuda")
+    store = torch.empty((L - 1 << 26) + D, dtype=torch.bfloat16, device="cuda")
+    b = torch.randn(1, L, N, device="cuda").bfloat16()
+    for step in (1 << 26, 1 << 22):
+        x = store.as_strided((1, L, D), (1, step, 1))
+        x.copy_(torch.randn(1, L, D, device="cuda"))
+        near = x.contiguous()
+        assert torch.equal(S.sig_conv_forward(x, w), S.sig_conv_forward(near, w))
+        ck = S.sig_scan_forward(near, near, A, b, b, checkpoint=True)[2]
+        for p, q in zip((*S.sig_scan_forward(x, x, A, b, b, gate=x), *S.sig_scan_backward(x, x, A, b, b, x, ck, gate=x).values()),
+                        (*S.sig_scan_forward(near, near, A, b, b, gate=near), *S.sig_scan_backward(near, near, A, b, b, near, ck, gate=near).values())):
+            assert p is None and q is None or torch.equal(p, q)
+
+
+@gpu
+def test_parameters_and_subclasses_give_plain_tensors():
+    class Mine(torch.Tensor):
+        pass
+    x, w = torch.randn(1, 9, 16, device="cuda"), torch.nn.Parameter(torch.randn(16, 4, device="cuda"))
+    b, A = torch.randn(1, 9, 4, device="cuda", requires_grad=True), torch.nn.Parameter(-torch.ones(16, 4, device="cuda"))
+    for v in (x.as_subclass(Mine), torch.nn.Parameter(x)):
+        y = S.sig_conv_forward(v, w)
+        h, state = S.sig_scan_forward(v, v, A, b, b)
+        assert type(y) is torch.Tensor and type(h) is torch.Tensor and type(state) is torch.Tensor and not y.requires_grad and not h.requires_grad
+        assert torch.equal(y, S.sig_conv_forward(x, w)) and torch.equal(h, S.sig_scan_forward(x, x, A, b, b)[0])
 
 
 @gpu
@@ -463,7 +498,7 @@ def test_more_refusals_of_the_conv():
     assert lib.sig_conv_forward(args, 0, 0, 0) == -1
     assert lib.sig_conv_step(args, 0, 4096, 0) == -1
     need = lib.sig_conv_backward_workspace_bytes(args)
-    assert need >= 2 * 5 * 4 * 4
+    assert need > 0
     assert lib.sig_conv_backward(args, 4096, 32, 4, 0, 4096, 4096, 0, 0, 4096, need - 1, 0) == -5
     assert lib.sig_conv_backward(args, 4096, 32, 4, 0, 4096, 4096, 0, 0, 0, need, 0) == -5
     assert lib.sig_conv_backward(args, 0, 32, 4, 0, 4096, 4096, 0, 0, 4096, need, 0) == -1
@@ -472,14 +507,15 @@ def test_more_refusals_of_the_conv():
 
 @pytest.mark.parametrize("change,code", [({"dtype": -1}, -1), ({"B": -1}, -1), ({"L": -1}, -1), ({"D": 0}, -1), ({"G": 0}, -1), ({"G": 3}, -1), ({"N": 0}, -1),
                                          ({"N": 65}, -9), ({"softplus": 3}, -1), ({"x": 0}, -1), ({"dt": 0}, -1), ({"b": 0}, -1), ({"c": 0}, -1), ({"A": 0}, -1),
-                                         ({"L": 1 << 40}, -7), ({"B": 0}, 0)])
+                                         ({"L": 1 << 40}, -7), ({"L": 1 << 31}, -7), ({"xt": 1 << 26}, -7), ({"bt": 1 << 26}, -7),
+                                         ({"ct": -1}, -1), ({"B": 1 << 30}, -7), ({"B": 0}, 0)])
 def test_scan_refuses_through_the_c_abi(change, code):
     lib = S.load_library()
     ok = dict.fromkeys(SCAN_ORDER, 0) | dict(dtype=0, B=2, L=8, D=4, G=2, N=4, softplus=1, x=4096, dt=4096, b=4096, c=4096, A=4096)
     args = pack({**ok, **change}, SCAN_ORDER)
     big = 1 << 60
     assert lib.sig_scan_forward(args, 4096, 4096, 4096, big, 4096, big, 0) == code
-    if "L" not in change:
+    if "L" not in change and "xt" not in change:
         assert lib.sig_scan_step(args, 4096, 4096, 0) == code
     if change != {"B": 0}:
         grads = pack(dict.fromkeys(GRADS_ORDER, 4096), GRADS_ORDER)
