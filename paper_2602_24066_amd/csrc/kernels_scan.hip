@@ -54,7 +54,7 @@ template <int K, int S, int s = 1> __device__ __forceinline__ void sum_broadcast
     }
     if constexpr (s < S) {
         asm("s_nop 1\n\t" SIG_FMAC(0, 5, 9) SIG_FMAC(1, 6, 10) SIG_FMAC(2, 7, 11) SIG_FMAC(3, 8, 12)
-            : "+v"(o[0]), "+v"(o[1]), "+v"(o[2]), "+v"(o[3])
+            : "+&v"(o[0]), "+&v"(o[1]), "+&v"(o[2]), "+&v"(o[3])
             : "v"(r), "v"(h[0][s]), "v"(h[1][s]), "v"(h[2][s]), "v"(h[3][s]), "n"(K + s), "n"(K + S + s), "n"(K + 2 * S + s), "n"(K + 3 * S + s));
         sum_broadcast<K, S, s + 1>(o, r, h);
     }
@@ -340,11 +340,11 @@ template <int K, int S> __device__ __forceinline__ void add_broadcast(float (&o)
     static_assert(S == 2 || S == 4, "states of a wavefront");
     if constexpr (S == 2)
         asm("s_nop 1\n\tv_fmac_f32_dpp %0, %2, %3 row_newbcast:%4 row_mask:0xf bank_mask:0xf\n\tv_fmac_f32_dpp %1, %2, %3 row_newbcast:%5 row_mask:0xf bank_mask:0xf"
-            : "+v"(o[0]), "+v"(o[1]) : "v"(r), "v"(v), "n"(K), "n"(K + 1));
+            : "+&v"(o[0]), "+&v"(o[1]) : "v"(r), "v"(v), "n"(K), "n"(K + 1));
     else
         asm("s_nop 1\n\tv_fmac_f32_dpp %0, %4, %5 row_newbcast:%6 row_mask:0xf bank_mask:0xf\n\tv_fmac_f32_dpp %1, %4, %5 row_newbcast:%7 row_mask:0xf bank_mask:0xf\n\t"
             "v_fmac_f32_dpp %2, %4, %5 row_newbcast:%8 row_mask:0xf bank_mask:0xf\n\tv_fmac_f32_dpp %3, %4, %5 row_newbcast:%9 row_mask:0xf bank_mask:0xf"
-            : "+v"(o[0]), "+v"(o[1]), "+v"(o[2]), "+v"(o[3]) : "v"(r), "v"(v), "n"(K), "n"(K + 1), "n"(K + 2), "n"(K + 3));
+            : "+&v"(o[0]), "+&v"(o[1]), "+&v"(o[2]), "+&v"(o[3]) : "v"(r), "v"(v), "n"(K), "n"(K + 1), "n"(K + 2), "n"(K + 3));
 }
 // Steps of the reduction over lanes: from a and b one register that holds, where the lane's bit is clear, a's sum over the two lanes that
 // differ in that bit, and b's where it is set.
