@@ -90,6 +90,14 @@ template <class T> __device__ __forceinline__ void buffer_store(Buffer r, unsign
     }
 }
 constexpr unsigned kNowhere = 0xfffffffcu;
+// at, or kNowhere: a selection that the compiler does not turn into branches around two accesses (worth 1 % of the backward pass; in the
+// forward pass the straight code takes more registers and a tenth longer over time chunks)
+__device__ __forceinline__ unsigned offset_if(bool there, unsigned at)
+{
+    unsigned r = there ? at : kNowhere;
+    asm("" : "+v"(r));
+    return r;
+}
 // v where mask is all ones, 0 or `other` where it is zero; the masks are the same for the wavefront
 __device__ __forceinline__ float only_if(uint32_t mask, float v) { return __uint_as_float(__float_as_uint(v) & mask); }
 __device__ __forceinline__ float either(uint32_t mask, float v, float other) { return __uint_as_float((__float_as_uint(v) & mask) | (__float_as_uint(other) & ~mask)); }
@@ -192,7 +200,7 @@ __global__ __launch_bounds__(Gr::W * 64, Gr::W > 2 && Gr::S == 4 ? 4 : 2) void s
         }
 #pragma unroll
         for (int j = 0; j < KB; j++) {
-            bool there = j * RT + tb < n;
+            const bool there = j * RT + tb < n;
             bv[j] = buffer_load<T>(rb, there ? b_at : kNowhere, j * b_row);
             if (kOutputs) cv[j] = buffer_load<T>(rc, there ? c_at : kNowhere, j * c_row);
         }
@@ -201,31 +209,38 @@ __global__ __launch_bounds__(Gr::W * 64, Gr::W > 2 && Gr::S == 4 ? 4 : 2) void s
     };
     // D_t and D_t x_t of the wavefront's tokens of a tile with n tokens (zero beyond: states stay), and what its outputs need besides
     auto prepare = [&](float4 (*to)[64], int n, const float (&xf)[PT], const float (&df)[PT], const float (&zf)[PT]) {
+        float2 step[PT];
 #pragma unroll
         for (int i = 0; i < PT; i++) {
             float D = df[i] + bias;
             D = only_if(w * PT + i < n ? ~0u : 0u, either(soft, softplus(D), D));
-            ((float2*)&to[(w * PT + i) / 2][lane])[(w * PT + i) % 2] = make_float2(D, D * xf[i]);
+            step[i] = make_float2(D, D * xf[i]);
             if (kOutputs) {
                 keep_next[i] = skip * xf[i];
                 f_next[i] = either(gated, zf[i] * sigmoid(zf[i]), 1.0f);
             }
         }
+        if constexpr (PT == 1) {
+            ((float2*)&to[w / 2][lane])[w % 2] = step[0];
+        } else {
+#pragma unroll
+            for (int i = 0; i < PT; i += 2) to[(w * PT + i) / 2][lane] = make_float4(step[i].x, step[i].y, step[i + 1].x, step[i + 1].y);
+        }
     };
     auto collect = [&](const float4 (*from)[kTile / 4][64]) {
-        constexpr int G = PT < 4 ? PT : 4;                // tokens of an access
+        constexpr int P = PT < 4 ? PT : 4;                // tokens of an access
 #pragma unroll
-        for (int i = 0; i < PT; i += G) {
+        for (int i = 0; i < PT; i += P) {
 #pragma unroll
-            for (int j = 0; j < G; j++) o[i + j] = keep[i + j];
+            for (int j = 0; j < P; j++) o[i + j] = keep[i + j];
 #pragma unroll
             for (int v = 0; v < W; v++) {
-                Pack<float, G> q = *(const Pack<float, G>*)((const float*)&from[v][(w * PT + i) / 4][lane] + (w * PT + i) % 4);
+                const Pack<float, P> q = *(const Pack<float, P>*)((const float*)&from[v][(w * PT + i) / 4][lane] + (w * PT + i) % 4);
 #pragma unroll
-                for (int j = 0; j < G; j++) o[i + j] += q.v[j];
+                for (int j = 0; j < P; j++) o[i + j] += q.v[j];
             }
 #pragma unroll
-            for (int j = 0; j < G; j++) o[i + j] *= f[i + j];
+            for (int j = 0; j < P; j++) o[i + j] *= f[i + j];
         }
     };
     // Three tiles are in work at a time: while one runs, the step sizes of the next are prepared and the outputs of the one before are
@@ -451,9 +466,9 @@ __global__ __launch_bounds__(Gr::W * 64, Gr::W > 8 ? 4 : 2) void scan_bwd_kernel
         }
 #pragma unroll
         for (int j = 0; j < KB; j++) {
-            bool there = j * RT + tb < n;
-            if (kFull) bv[j] = buffer_load<T>(rb, there ? b_at : kNowhere, j * b_row);
-            cv[j] = buffer_load<T>(rc, there ? c_at : kNowhere, j * c_row);
+            const bool there = j * RT + tb < n;
+            if (kFull) bv[j] = buffer_load<T>(rb, offset_if(there, b_at), j * b_row);
+            cv[j] = buffer_load<T>(rc, offset_if(there, c_at), j * c_row);
         }
         if (kFull)
 #pragma unroll
@@ -498,7 +513,7 @@ __global__ __launch_bounds__(Gr::W * 64, Gr::W > 8 ? 4 : 2) void scan_bwd_kernel
             float dx = there ? fmaf(r[0], D, skip * u) : 0.0f, dD = there ? fmaf(r[0], v, r[1]) * sl[slot][m] : 0.0f, dz = there ? gs[slot][m] * r[2] : 0.0f;
             gskip += there ? u * v : 0.0f;
             gbias += dD;
-            const unsigned at = on && k < room ? e * E : kNowhere;
+            const unsigned at = offset_if(on && k < room, e * E);
             buffer_store(rx, at, k * y_row, from_float<T>(dx));
             buffer_store(rdt, at, k * y_row, from_float<T>(dD));
             buffer_store(rz, gated ? at : kNowhere, k * y_row, from_float<T>(dz));
