@@ -44,7 +44,7 @@ int check_scan(const sig_scan_args* a)
     if (a->B > 0 && a->D > INT32_MAX / a->B) return SIG_ETOOLARGE;
     if (a->L > INT32_MAX - 64) return SIG_ETOOLARGE;
     for (int64_t s : {a->x_stride_t, a->dt_stride_t, a->gate_stride_t, a->b_stride_t, a->c_stride_t, a->D})
-        if (s < 0 || s >= (1 << 26)) return s < 0 ? SIG_EINVAL : SIG_ETOOLARGE;
+        if (s < 0 || s >= (1 << 24)) return s < 0 ? SIG_EINVAL : SIG_ETOOLARGE;
     return check_sizes({a->B, a->L, a->D, a->N});
 }
 
@@ -122,7 +122,7 @@ int sig_scan_backward(const sig_scan_args* a, const sig_scan_grads* g, const voi
     bool tokens = a->B > 0 && a->L > 0;
     if (!g || !g->grad_A || !scan_inputs_there(*a, tokens)) return SIG_EINVAL;
     if (tokens && g->gy_stride_t < 0) return SIG_EINVAL;
-    if (tokens && g->gy_stride_t >= (1 << 26)) return SIG_ETOOLARGE;
+    if (tokens && g->gy_stride_t >= (1 << 24)) return SIG_ETOOLARGE;
     if ((a->skip && !g->grad_skip) || (a->dt_bias && !g->grad_dt_bias)) return SIG_EINVAL;
     if (tokens && (!g->grad_y || !g->grad_x || !g->grad_dt || !g->grad_b || !g->grad_c || (a->gate && !g->grad_gate))) return SIG_EINVAL;
     if (checkpoint_bytes < ckpt_bytes(*a) || (tokens && !checkpoint)) return SIG_EWORKSPACE;

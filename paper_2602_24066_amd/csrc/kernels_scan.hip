@@ -89,6 +89,8 @@ template <class T> __device__ __forceinline__ void buffer_store(Buffer r, unsign
         __builtin_amdgcn_raw_buffer_store_b32(q, r, at, row, 0);
     }
 }
+// p some bytes on (32 bits: a tile's rows, see the limits of strides in api_seq.cpp; scalar registers are few)
+template <class T> __device__ __forceinline__ void forth(T*& p, unsigned bytes) { p = (T*)((const char*)p + bytes); }
 constexpr unsigned kNowhere = 0xfffffffcu;
 // at, or kNowhere: a selection that the compiler does not turn into branches around two accesses (worth 1 % of the backward pass; in the
 // forward pass the straight code takes more registers and a tenth longer over time chunks)
@@ -204,8 +206,7 @@ __global__ __launch_bounds__(Gr::W * 64, Gr::W > 2 && Gr::S == 4 ? 4 : 2) void s
             bv[j] = buffer_load<T>(rb, there ? b_at : kNowhere, j * b_row);
             if (kOutputs) cv[j] = buffer_load<T>(rc, there ? c_at : kNowhere, j * c_row);
         }
-        px += kTile * a.x_stride_t, pdt += kTile * a.dt_stride_t, pz += kTile * (gated ? a.gate_stride_t : a.x_stride_t);
-        pb += kTile * a.b_stride_t, pc += kTile * a.c_stride_t;
+        forth(px, kTile * x_row), forth(pdt, kTile * dt_row), forth(pz, kTile * z_row), forth(pb, KB * b_row), forth(pc, KB * c_row);
     };
     // D_t and D_t x_t of the wavefront's tokens of a tile with n tokens (zero beyond: states stay), and what its outputs need besides
     auto prepare = [&](float4 (*to)[64], int n, const float (&xf)[PT], const float (&df)[PT], const float (&zf)[PT]) {
@@ -569,7 +570,7 @@ __global__ __launch_bounds__(Gr::W * 64, Gr::W > 8 ? 4 : 2) void scan_bwd_kernel
                 });
             });
         }
-        auto back = [&](auto half_) {
+        auto half_back = [&](auto half_) {
             constexpr int half = decltype(half_)::value;
             unrolled<0, kHalf / 4>([&](auto jt) {
                 constexpr int q = kHalf / 4 - 1 - decltype(jt)::value, i = half * kHalf + q * 4, k = i % RT * S;
@@ -614,13 +615,13 @@ __global__ __launch_bounds__(Gr::W * 64, Gr::W > 8 ? 4 : 2) void scan_bwd_kernel
                 }
             });
         };
-        back(std::integral_constant<int, 1>());
+        half_back(std::integral_constant<int, 1>());
         if constexpr (kFull) {
             __syncthreads();
             put(1, slot, upper);
             if (!kTwice) __syncthreads();
         }
-        back(std::integral_constant<int, 0>());
+        half_back(std::integral_constant<int, 0>());
         if constexpr (kFull) {
             float* to = parts.bc + ((((b * tiles + t_first / kTile + tile) * a.G + grp) * bl.runs + run) * W + w) * Q * 64;
 #pragma unroll

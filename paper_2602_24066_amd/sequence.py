@@ -44,7 +44,7 @@ def _tokens(name, t, shape, dtype, index):
     if t.dtype is not dtype or t.get_device() != index or t.shape != shape:
         _refuse(name, t, shape, dtype)
     s = t.stride()
-    if (s[-1] != 1 and shape[-1] != 1) or (len(s) > 2 and s[1] >= 1 << 26):      # time strides that the kernels do not reach are copied away
+    if (s[-1] != 1 and shape[-1] != 1) or (len(s) > 2 and s[1] >= 1 << 24):      # time strides that the kernels do not reach are copied away
         t = t.contiguous()
         s = t.stride()
     return t, s
