@@ -368,7 +368,7 @@ int sig_leadlag_backward(const float* grad_out, int64_t B, int64_t n_points, int
  * the widest accesses.  lengths: device int32 [B] or NULL (all L); clamped to [0, L].  Tokens from lengths[b] on are not read: they give
  * outputs and gradients of zero and leave states as they are.  Calls only enqueue kernels on `stream`; two calls on the same inputs give
  * the same bits.  B == 0 is a no-op (gradients of parameters are set to zero), L == 0 is allowed: a final state is the initial one.
- * SIG_ETOOLARGE: sizes whose product passes 2^38; for the scan L >= 2^31 - 64, B * D >= 2^31, D or a time stride of 2^24 and more (time strides
+ * SIG_ETOOLARGE: sizes whose product passes 2^38; for the scan L >= 2^30, B * D >= 2^31, D or a time stride of 2^24 and more (time strides
  * of the scan are not negative).  SIG_EUNSUPPORTED: more filter taps or states than the limits below. */
 #define SIG_F32  0
 #define SIG_BF16 1
@@ -411,7 +411,7 @@ typedef struct sig_scan_args {
     const void* gate;               /* device dtype [B, L, D] or NULL */
     const void* b;                  /* device dtype [B, L, G, N], states contiguous */
     const void* c;                  /* device dtype [B, L, G, N], states contiguous */
-    const float* A;                 /* device [D, N] */
+    const float* A;                 /* device [D, N], finite */
     const float* skip;              /* device [D] or NULL */
     const float* dt_bias;           /* device [D] or NULL */
     const float* initial_state;     /* device [B, D, N] or NULL (zeros) */

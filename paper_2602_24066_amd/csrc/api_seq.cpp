@@ -42,7 +42,7 @@ int check_scan(const sig_scan_args* a)
     if (a->softplus != 0 && a->softplus != 1) return SIG_EINVAL;
     // a launch numbers at least the streams' channels; the kernels count tokens in 32 bits and reach those of a tile by 32-bit offsets
     if (a->B > 0 && a->D > INT32_MAX / a->B) return SIG_ETOOLARGE;
-    if (a->L > INT32_MAX - 64) return SIG_ETOOLARGE;
+    if (a->L >= (1 << 30)) return SIG_ETOOLARGE;        // a chunk's end is at most L rounded up to tiles, times two at the most
     for (int64_t s : {a->x_stride_t, a->dt_stride_t, a->gate_stride_t, a->b_stride_t, a->c_stride_t, a->D})
         if (s < 0 || s >= (1 << 24)) return s < 0 ? SIG_EINVAL : SIG_ETOOLARGE;
     return check_sizes({a->B, a->L, a->D, a->N});

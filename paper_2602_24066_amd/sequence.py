@@ -58,6 +58,8 @@ def _whole(name, t, shape, dtype, index):
 
 
 def _in_place(name, t, shape, dtype, index):
+    if t is None:
+        raise ValueError(f"{name} is missing")
     if t.dtype is not dtype or t.get_device() != index or t.shape != shape or not t.is_contiguous():
         _refuse(name + " (contiguous)", t, shape, dtype)
 
@@ -233,7 +235,7 @@ def sig_scan_backward(x, dt, A, b, c, grad_out, checkpoint, skip=None, gate=None
     if grad_final_state is not None:
         grad_final_state = _whole("grad_final_state", grad_final_state, (B, D, N), _f32, index)
         pf = grad_final_state.data_ptr()
-    if checkpoint.get_device() != index or not checkpoint.is_contiguous():
+    if checkpoint is None or checkpoint.get_device() != index or not checkpoint.is_contiguous():
         raise ValueError("checkpoint must be the tensor that sig_scan_forward returned")
     tokens = lambda: make.new_empty((B, L, D))                                              # noqa: E731
     params = lambda *shape: make.new_empty(shape, dtype=_f32)                               # noqa: E731

@@ -522,6 +522,16 @@ def test_scan_refuses_through_the_c_abi(change, code):
         assert lib.sig_scan_backward(args, grads, 4096, big, 4096, big, 0) == code
 
 
+def test_the_longest_scan():
+    lib = S.load_library()
+    args = lambda L: pack(dict.fromkeys(SCAN_ORDER, 0) | dict(dtype=0, B=1, L=L, D=1, G=1, N=1, softplus=1, x=4096, dt=4096, b=4096, c=4096, A=4096), SCAN_ORDER)   # noqa: E731
+    big = 1 << 60
+    assert lib.sig_scan_checkpoint_bytes(args((1 << 30) - 1)) == 1 << 28          # 2^26 tiles, a float each
+    assert lib.sig_scan_forward(args((1 << 30) - 1), 0, 0, 0, 0, 4096, big, 0) == -1
+    assert lib.sig_scan_forward(args(1 << 30), 4096, 0, 0, 0, 4096, big, 0) == -7
+    assert lib.sig_scan_checkpoint_bytes(args(1 << 30)) == 0
+
+
 def test_more_refusals_of_the_scan():
     lib = S.load_library()
     ok = dict.fromkeys(SCAN_ORDER, 0) | dict(dtype=0, B=2, L=40, D=4, G=2, N=4, softplus=1, x=4096, dt=4096, b=4096, c=4096, A=4096, gate=4096, skip=4096, bias=4096)
@@ -564,6 +574,15 @@ def test_host_tensors_are_refused():
     for f in (lambda: S.sig_conv_forward(x, w), lambda: S.sig_conv_step(x[:, 0], x[:, :3], w), lambda: S.sig_conv_backward(x, w, x),
               lambda: S.sig_scan_forward(x, x, A, b, b), lambda: S.sig_scan_step(x[:, 0], x[:, 0], A, b[:, 0], b[:, 0], torch.zeros(2, 8, 16)),
               lambda: S.sig_grad_clip([x], 1.0), lambda: S.sig_grad_clip([x], -1.0), lambda: S.sig_grad_clip([x], 1.0, out=[])):
+        with pytest.raises(ValueError):
+            f()
+
+
+@gpu
+def test_missing_states_are_refused():
+    x, w, b, A = torch.zeros(2, 5, 8, device="cuda"), torch.zeros(8, 4, device="cuda"), torch.zeros(2, 5, 16, device="cuda"), torch.zeros(8, 16, device="cuda")
+    for f in (lambda: S.sig_conv_step(x[:, 0], None, w), lambda: S.sig_scan_step(x[:, 0], x[:, 0], A, b[:, 0], b[:, 0], None),
+              lambda: S.sig_scan_backward(x, x, A, b, b, x, None)):
         with pytest.raises(ValueError):
             f()
 
