@@ -688,18 +688,21 @@ __global__ __launch_bounds__(Gr::W * 64, Gr::W > 8 ? 4 : 2) void scan_bwd_kernel
 template <class T, class Gr> __global__ __launch_bounds__(kThreads) void scan_bwd_bc_kernel(sig_scan_args a, Blocks bl, const float* part, T* gB, T* gC)
 {
     constexpr int Q = Gr::S / 2, R = Gr::W * Q;
-    const int64_t id = (int64_t)blockIdx.x * (kThreads / 64) + threadIdx.x / 64, tiles = (a.L + kTile - 1) / kTile;      // a wavefront for each [.., W, Q]
-    if (id >= a.B * tiles * a.G * R) return;
-    const int lane = threadIdx.x & 63, r = (int)(id % R);
-    const int64_t grp = id / R % a.G, tile = id / R / a.G % tiles, b = id / R / a.G / tiles, t = tile * kTile + token_of(lane);
-    const int n = r / Q * Gr::S + r % Q * 2 + (lane >> 4 & 1);
-    const int64_t len = live_length(a.lengths, b, a.L);
-    float v = 0.0f;
-    if (tile * kTile < len) {
-        const float* p = part + (((b * tiles + tile) * a.G + grp) * bl.runs * R + r) * 64 + lane;
-        for (unsigned j = 0; j < bl.runs; j++, p += R * 64) v += *p;
+    const int64_t tiles = (a.L + kTile - 1) / kTile, all = a.B * tiles * a.G * R;
+    const int lane = threadIdx.x & 63;
+    // a wavefront for each [.., W, Q]
+    for (int64_t id = (int64_t)blockIdx.x * (kThreads / 64) + threadIdx.x / 64; id < all; id += (int64_t)gridDim.x * (kThreads / 64)) {
+        const int r = (int)(id % R);
+        const int64_t grp = id / R % a.G, tile = id / R / a.G % tiles, b = id / R / a.G / tiles, t = tile * kTile + token_of(lane);
+        const int n = r / Q * Gr::S + r % Q * 2 + (lane >> 4 & 1);
+        const int64_t len = live_length(a.lengths, b, a.L);
+        float v = 0.0f;
+        if (tile * kTile < len) {
+            const float* p = part + (((b * tiles + tile) * a.G + grp) * bl.runs * R + r) * 64 + lane;
+            for (unsigned j = 0; j < bl.runs; j++, p += R * 64) v += *p;
+        }
+        if (t < a.L && n < a.N) (lane & 32 ? gC : gB)[((b * a.L + t) * a.G + grp) * a.N + n] = from_float<T>(t < len ? v : 0.0f);
     }
-    if (t < a.L && n < a.N) (lane & 32 ? gC : gB)[((b * a.L + t) * a.G + grp) * a.N + n] = from_float<T>(t < len ? v : 0.0f);
 }
 
 // dA, dskip and ddt_bias: the sums over streams and time chunks, in a fixed order.  64 sums a workgroup; each of its sixteen wavefronts takes
@@ -910,7 +913,7 @@ hipError_t scan_backward(const sig_scan_args& a, const sig_scan_grads& g, const 
             if (a.B > 0) {
                 if (bl.chunks > 1) scan_bwd_kernel<T, Gr, false><<<bl.total, Gr::W * 64, backward_lds(0), stream>>>(a, g, bl, cs, nullptr, parts);
                 scan_bwd_kernel<T, Gr, true><<<bl.total, Gr::W * 64, lds, stream>>>(a, g, bl, cs, checkpoint, parts);
-                if (a.L > 0) scan_bwd_bc_kernel<T, Gr><<<blocks_for(p.bc / bl.runs), kThreads, 0, stream>>>(a, bl, parts.bc, (T*)g.grad_b, (T*)g.grad_c);
+                if (a.L > 0) scan_bwd_bc_kernel<T, Gr><<<std::min(1u << 22, blocks_for(p.bc / bl.runs)), kThreads, 0, stream>>>(a, bl, parts.bc, (T*)g.grad_b, (T*)g.grad_c);
             }
             scan_bwd_params_kernel<<<(unsigned)((a.D * (a.N + 2) + 63) / 64), 1024, 0, stream>>>(a, a.B * bl.chunks, parts, g.grad_A, g.grad_skip, g.grad_dt_bias);
             return hipGetLastError();

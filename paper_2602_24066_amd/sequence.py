@@ -13,14 +13,15 @@ import struct
 from .binding import _call, _calls, _enqueue
 
 # torch and its types, set by the first call; the checks below are written for calls of one token, whose kernels take less time than they do
-_torch = _f32 = _b16 = _i32 = _plain = None
+_torch = _f32 = _b16 = _i32 = _plain = _KINDS = None
 
 
 def _t():
-    global _torch, _f32, _b16, _i32, _plain
+    global _torch, _f32, _b16, _i32, _plain, _KINDS
     if _torch is None:
         import torch
         _f32, _b16, _i32, _plain = torch.float32, torch.bfloat16, torch.int32, torch.Tensor
+        _KINDS = {_f32: 0, _b16: 1}
         _torch = torch
     return _torch
 
@@ -276,19 +277,19 @@ def sig_grad_clip(grads, max_norm, out=None):
     dev = grads[0].device if n else torch.device("cuda", torch.cuda.current_device())
     if dev.type != "cuda":
         raise ValueError("grads must be CUDA tensors")
-    index, kind = dev.index, {_f32: 0, _b16: 1}.get
-    into, sizes, from_kinds = [g.data_ptr() for g in grads], [g.numel() for g in grads], [kind(g.dtype) for g in grads]
-    to, to_kinds = into, from_kinds
-    if out is not None:
-        to, to_kinds = [o.data_ptr() for o in outs], [kind(o.dtype) for o in outs]
-        if [o.numel() for o in outs] != sizes:
-            raise ValueError("out must have tensors of the sizes of grads")
-    if None in from_kinds or None in to_kinds or any(t.get_device() != index for t in (grads if out is None else grads + outs)):
+    # by calls mapped over the lists: with a few dozen small tensors these checks take longer than the kernels
+    T, every = torch.Tensor, grads if out is None else grads + outs
+    kinds = [_KINDS.get(t.dtype) for t in every]
+    if None in kinds or not set(map(T.get_device, every)) <= {dev.index}:
         raise ValueError("grads and out must be float32 or bfloat16 tensors on one device")
-    for g, o in zip(grads, outs):
-        if not (g.is_contiguous() and o.is_contiguous()) and (g.shape != o.shape or g.stride() != o.stride() or not torch.ops.aten.is_non_overlapping_and_dense(g)):
-            raise ValueError("every tensor must fill its memory, and out must have the order of axes of grads")
-    tab = array.array("q", into + to + sizes + from_kinds + to_kinds)
+    into, sizes = list(map(T.data_ptr, every)), list(map(T.numel, every))
+    if out is not None and sizes[:n] != sizes[n:]:
+        raise ValueError("out must have tensors of the sizes of grads")
+    if not all(map(T.is_contiguous, every)):
+        for g, o in zip(grads, outs):
+            if not (g.is_contiguous() and o.is_contiguous()) and (g.shape != o.shape or g.stride() != o.stride() or not torch.ops.aten.is_non_overlapping_and_dense(g)):
+                raise ValueError("every tensor must fill its memory, and out must have the order of axes of grads")
+    tab = array.array("q", into + sizes[:n] + kinds if out is not None else into + into + sizes + kinds + kinds)
     at = tab.buffer_info()[0]
     norm = torch.empty((), dtype=_f32, device=dev)
     nbytes = (_calls.get("sig_grad_clip_workspace_bytes") or _call("sig_grad_clip_workspace_bytes"))(n, at + 16 * n)
