@@ -26,7 +26,7 @@ Split split_time(int64_t B, int64_t L, int64_t D, int V)
     // four wavefronts on each SIMD (4,096 of 64 threads), each with two groups of loads under way, hide the memory's latency; chunks
     // shorter than 16 tokens would read a fifth and more of their input twice
     int64_t want = (int64_t)4096 * 64 / std::max<int64_t>(1, B * s.vecs) + 1;
-    s.chunk = std::max<int64_t>(16, (L + want - 1) / want);
+    s.chunk = std::min<int64_t>(1 << 30, std::max<int64_t>(16, (L + want - 1) / want));      // the kernels count a chunk's tokens in 32 bits
     s.chunks = std::max<int64_t>(1, (L + s.chunk - 1) / s.chunk);
     s.threads = B * s.chunks * s.vecs;
     return s;
@@ -69,6 +69,53 @@ template <int V, int W> __device__ __forceinline__ void load_filter(float (&w)[W
     }
 }
 
+// The W - 1 tokens before token t0 >= 0 of a stream, of which x holds token t0: no branches, so that nothing waits for the loads here.
+template <class T, int V, int W>
+__device__ __forceinline__ void load_window(float (&r)[W][V], const T* x, int64_t stride_t, const T* initial, int64_t D, int64_t t0)
+{
+#pragma unroll
+    for (int k = 0; k < W - 1; k++) {
+        const int64_t p = t0 - W + 1 + k;
+        const T* q = p >= 0 || !initial ? x + (p >= 0 ? p : t0) * stride_t : initial + (W - 1 + p) * D;
+        load<T, V>(r[k + 1], q);
+#pragma unroll
+        for (int i = 0; i < V; i++) r[k + 1][i] = p >= 0 || initial ? r[k + 1][i] : 0.0f;
+    }
+}
+
+// V elements as whole words: the compiler takes a load of an array of halves apart
+template <int kBytes> struct Words { typedef uint32_t type __attribute__((ext_vector_type(kBytes / 4))); };
+template <> struct Words<4> { typedef uint32_t type; };
+template <> struct Words<2> { typedef uint16_t type; };
+template <class T, int V> using Raw = typename Words<sizeof(T) * V>::type;
+template <class T, int V> __device__ __forceinline__ float element(const Raw<T, V>& r, int i)
+{
+    if constexpr (sizeof(T) * V == 2) return to_float(bf16{r});
+    else if constexpr (sizeof(T) * V == 4) return sizeof(T) == 4 ? __uint_as_float(r) : __uint_as_float(i ? r & 0xffff0000u : r << 16);
+    else if constexpr (sizeof(T) == 4) return __uint_as_float(r[i]);
+    else return __uint_as_float(i % 2 ? r[i / 2] & 0xffff0000u : r[i / 2] << 16);
+}
+
+// keeps the compiler from unpacking a group as soon as its loads are made, which would wait for them and take twice the registers
+template <class R> __device__ __forceinline__ R here(R r)
+{
+    asm volatile("" : "+v"(r));
+    return r;
+}
+
+// U tokens from p on, of which there are `left` (at least one, at first): after the last one it is read again.  A load that is always made
+// lets the compiler count how many are under way; behind a condition it waits for all of them and for the stores among them.
+template <class T, int V, int U> __device__ __forceinline__ void load_group(Raw<T, V> (&to)[U], const T*& p, int64_t stride, int& left)
+{
+#pragma unroll
+    for (int u = 0; u < U; u++, left--) {
+        to[u] = *(const Raw<T, V>*)p;
+        p += left > 1 ? stride : 0;
+    }
+}
+
+__device__ __forceinline__ float either(uint32_t mask, float v, float other) { return __uint_as_float((__float_as_uint(v) & mask) | (__float_as_uint(other) & ~mask)); }
+
 template <class T, int V, int W>
 __global__ __launch_bounds__(kThreads) void conv_fwd_kernel(sig_conv_args a, T* y, T* final_state, Split s)
 {
@@ -77,69 +124,52 @@ __global__ __launch_bounds__(kThreads) void conv_fwd_kernel(sig_conv_args a, T* 
     int64_t d = id % s.vecs * V, row = id / s.vecs, c = row % s.chunks, b = row / s.chunks;
     const T* x = (const T*)a.x + b * a.x_stride_b + d;
     const T* initial = a.initial_state ? (const T*)a.initial_state + b * (W - 1) * a.D + d : nullptr;
-    int64_t t0 = c * s.chunk, t1 = min(t0 + s.chunk, a.L), len = live_length(a.lengths, b, a.L);
+    const int64_t t0 = c * s.chunk, len = live_length(a.lengths, b, a.L);
+    const int n = (int)(min(t0 + s.chunk, a.L) - t0), live = (int)max((int64_t)0, min((int64_t)n, len - t0));
+    const uint32_t silu = a.silu ? ~0u : 0u;
     y += (b * a.L + t0) * a.D + d;
-    float w[W][V], bias[V], r[W][V];
-    load_filter<V, W>(w, bias, a, d);
-    int64_t end = min(t1, len);
-    if (t0 < end) {
+    int t = 0;
+    if (live > 0) {
+        float w[W][V], bias[V], r[W][V];
+        load_filter<V, W>(w, bias, a, d);
+        load_window<T, V, W>(r, x, a.x_stride_t, initial, a.D, t0);
+        auto token = [&](const Raw<T, V>& packed) {
+            const Raw<T, V> in = here(packed);
+            float o[V];
 #pragma unroll
-        for (int k = 0; k < W - 1; k++) load_token<T, V, W>(r[k + 1], x, a.x_stride_t, initial, a.D, t0 - W + 1 + k);
-    }
-    auto token = [&](const float (&in)[V]) {
-        float o[V];
+            for (int i = 0; i < V; i++) {
+                o[i] = bias[i];
 #pragma unroll
-        for (int i = 0; i < V; i++) {
-            o[i] = bias[i];
+                for (int k = 0; k < W - 1; k++) r[k][i] = r[k + 1][i], o[i] = fmaf(w[k][i], r[k][i], o[i]);
+                r[W - 1][i] = element<T, V>(in, i);
+                o[i] = fmaf(w[W - 1][i], r[W - 1][i], o[i]);
+                o[i] *= either(silu, sigmoid(o[i]), 1.0f);
+            }
+            store<T, V>(y, o);
+            y += a.D;
+        };
+        // groups of U tokens, the next one's loads under way while one is worked on
+        constexpr int U = V >= 4 ? 4 : 8;
+        Raw<T, V> now[U], next[U];
+        const T* p = x + t0 * a.x_stride_t;
+        int left = live;
+        load_group<T, V, U>(now, p, a.x_stride_t, left);
+        for (; t + U <= live; t += U) {
+            load_group<T, V, U>(next, p, a.x_stride_t, left);
 #pragma unroll
-            for (int k = 0; k < W - 1; k++) r[k][i] = r[k + 1][i], o[i] = fmaf(w[k][i], r[k][i], o[i]);
-            r[W - 1][i] = in[i];
-            o[i] = fmaf(w[W - 1][i], in[i], o[i]);
-            if (a.silu) o[i] *= sigmoid(o[i]);
-        }
-        store<T, V>(y, o);
-        y += a.D;
-    };
-    // groups of U tokens, the next one's loads under way while one is worked on
-    constexpr int U = V >= 4 ? 4 : 8;
-    int64_t t = t0;
-    x += t0 * a.x_stride_t;
-    Pack<T, V> now[U], next[U];
-    auto fetch = [&](Pack<T, V> (&to)[U]) {
+            for (int u = 0; u < U; u++) token(now[u]);
 #pragma unroll
-        for (int u = 0; u < U; u++, x += a.x_stride_t) to[u] = *(const Pack<T, V>*)x;
-    };
-    if (t + U <= end) fetch(now);
-    for (; t + U <= end; t += U) {
-        if (t + 2 * U <= end) fetch(next);
-#pragma unroll
-        for (int u = 0; u < U; u++) {
-            float in[V];
-#pragma unroll
-            for (int i = 0; i < V; i++) in[i] = to_float(now[u].v[i]);
-            token(in);
+            for (int u = 0; u < U; u++) now[u] = next[u];
         }
 #pragma unroll
-        for (int u = 0; u < U; u++) now[u] = next[u];
-    }
-    if (t < end) {                      // the last, incomplete group
-        Pack<T, V> some[U] = {};
-#pragma unroll
-        for (int u = 0; u < U; u++)
-            if (t + u < end) some[u] = *(const Pack<T, V>*)(x + u * a.x_stride_t);
-#pragma unroll
-        for (int u = 0; u < U; u++) {
-            if (t + u >= end) break;
-            float in[V];
-#pragma unroll
-            for (int i = 0; i < V; i++) in[i] = to_float(some[u].v[i]);
-            token(in);
+        for (int u = 0; u < U - 1; u++) {
+            if (t >= live) break;
+            token(now[u]);
+            t++;
         }
-        t = end;
     }
-    x = (const T*)a.x + b * a.x_stride_b + d;
     float zero[V] = {};
-    for (; t < t1; t++, y += a.D) store<T, V>(y, zero);
+    for (; t < n; t++, y += a.D) store<T, V>(y, zero);
     if (final_state && c == 0) {
         final_state += b * (W - 1) * a.D + d;
 #pragma unroll
@@ -156,96 +186,92 @@ __global__ __launch_bounds__(kThreads) void conv_fwd_kernel(sig_conv_args a, T* 
 template <class T, int V, int W>
 __global__ __launch_bounds__(kThreads) void conv_bwd_kernel(sig_conv_args a, ConvGrads g, float* part, Split s)
 {
-    const bool there = (int64_t)blockIdx.x * kThreads + threadIdx.x < s.threads;       // the others repeat the first and store nothing
-    int64_t id = there ? (int64_t)blockIdx.x * kThreads + threadIdx.x : 0;
-    int64_t d = id % s.vecs * V, row = id / s.vecs, c = row % s.chunks, b = row / s.chunks;
-    const T* x = (const T*)a.x + b * a.x_stride_b + d;
-    const T* gy = (const T*)g.grad_y + b * g.gy_stride_b + d;
-    const T* initial = a.initial_state ? (const T*)a.initial_state + b * (W - 1) * a.D + d : nullptr;
+    const bool there = (int64_t)blockIdx.x * kThreads + threadIdx.x < s.threads;
+    const int64_t id = there ? (int64_t)blockIdx.x * kThreads + threadIdx.x : 0;
+    const int64_t d = id % s.vecs * V, row = id / s.vecs, c = row % s.chunks, b = row / s.chunks;
+    T* gi = g.grad_initial && c == 0 ? (T*)g.grad_initial + b * (W - 1) * a.D + d : nullptr;
     const T* gf = g.grad_final ? (const T*)g.grad_final + b * (W - 1) * a.D + d : nullptr;
-    T* gi = g.grad_initial ? (T*)g.grad_initial + b * (W - 1) * a.D + d : nullptr;
-    T* gx = (T*)g.grad_x + b * a.L * a.D + d;
-    int64_t t0 = c * s.chunk, t1 = there ? min(t0 + s.chunk, a.L) : t0 - W + 1, len = live_length(a.lengths, b, a.L);
-    float w[W][V], bias[V], r[W][V] = {}, h[W][V] = {}, gw[W + 1][V] = {};
-    load_filter<V, W>(w, bias, a, d);
-    if (t0 < len) {
+    const int64_t t0 = c * s.chunk, len = live_length(a.lengths, b, a.L);
+    const int n = (int)(min(t0 + s.chunk, a.L) - t0);
+    T* gx = (T*)g.grad_x + (b * a.L + t0) * a.D + d;
+    float gw[W + 1][V] = {};
+    if (there && t0 < len) {
+        const T* x = (const T*)a.x + b * a.x_stride_b + d;
+        const T* initial = a.initial_state ? (const T*)a.initial_state + b * (W - 1) * a.D + d : nullptr;
+        const int live = (int)min((int64_t)n + W - 1, len - t0), lowest = gi ? 1 - W : 0;      // tokens that count, from t0 on
+        const uint32_t silu = a.silu ? ~0u : 0u;
+        float w[W][V], bias[V], r[W][V], h[W][V] = {};
+        load_filter<V, W>(w, bias, a, d);
+        load_window<T, V, W>(r, x, a.x_stride_t, initial, a.D, t0);
+        // takes token t0 + t (x and upstream gradient) and stores the gradient of token t0 + t - W + 1; kWhole: it counts and is of the chunk
+        auto token = [&](auto whole, int t, const Raw<T, V>& packed_in, const Raw<T, V>& packed_up) {
+            const Raw<T, V> in = here(packed_in), up = here(packed_up);
+            constexpr bool kWhole = decltype(whole)::value;
+            const bool counts = kWhole || t < live, ours = kWhole || t < min(n, live);
 #pragma unroll
-        for (int k = 0; k < W - 1; k++) load_token<T, V, W>(r[k + 1], x, a.x_stride_t, initial, a.D, t0 - W + 1 + k);
-    }
-    // takes token t (in: x, up: the upstream gradient, whether it counts) and stores the gradient of token t - W + 1
-    auto token = [&](int64_t t, const float (&in)[V], const float (&up)[V], bool counts) {
+            for (int i = 0; i < V; i++) {
 #pragma unroll
-        for (int i = 0; i < V; i++) {
-#pragma unroll
-            for (int k = 0; k < W - 1; k++) r[k][i] = r[k + 1][i], h[k][i] = h[k + 1][i];
-            r[W - 1][i] = in[i];
-            float g = up[i];
-            if (a.silu) {
+                for (int k = 0; k < W - 1; k++) r[k][i] = r[k + 1][i], h[k][i] = h[k + 1][i];
+                r[W - 1][i] = counts ? element<T, V>(in, i) : 0.0f;
                 float o = bias[i];
 #pragma unroll
                 for (int k = 0; k < W; k++) o = fmaf(w[k][i], r[k][i], o);
-                float p = sigmoid(o);
-                g *= p * fmaf(o, 1.0f - p, 1.0f);
+                const float p = sigmoid(o), q = element<T, V>(up, i) * either(silu, p * fmaf(o, 1.0f - p, 1.0f), 1.0f);
+                h[W - 1][i] = counts ? q : 0.0f;
+                if (ours) {
+#pragma unroll
+                    for (int k = 0; k < W; k++) gw[k][i] = fmaf(q, r[k][i], gw[k][i]);
+                    gw[W][i] += q;
+                }
             }
-            h[W - 1][i] = counts ? g : 0.0f;
-            if (counts && t < t1) {
+            const int p = t - W + 1;
+            if (p < lowest) return;
+            float o[V];
 #pragma unroll
-                for (int k = 0; k < W; k++) gw[k][i] = fmaf(g, r[k][i], gw[k][i]);
-                gw[W][i] += g;
+            for (int i = 0; i < V; i++) {
+                o[i] = 0.0f;
+#pragma unroll
+                for (int k = 0; k < W; k++) o[i] = fmaf(w[k][i], h[W - 1 - k][i], o[i]);
             }
+            if (!kWhole && gf && t0 + p < len && t0 + p >= len - (W - 1)) {
+                float v[V];
+                load<T, V>(v, gf + (t0 + p - len + W - 1) * a.D);
+#pragma unroll
+                for (int i = 0; i < V; i++) o[i] += v[i];
+            }
+            store<T, V>(p >= 0 ? gx + p * a.D : gi + (W - 1 + p) * a.D, o);
+        };
+        // groups of U tokens, the next one's loads under way while one is worked on
+        constexpr int U = V >= 4 ? 4 : 8;
+        Raw<T, V> nx[U], ng[U], mx[U], mg[U];
+        const T *qx = x + t0 * a.x_stride_t, *qg = (const T*)g.grad_y + b * g.gy_stride_b + t0 * g.gy_stride_t + d;
+        int left_x = live, left_g = live, t = 0;
+        load_group<T, V, U>(nx, qx, a.x_stride_t, left_x), load_group<T, V, U>(ng, qg, g.gy_stride_t, left_g);
+        for (const int whole = min(n, live); t + U <= whole; t += U) {
+            load_group<T, V, U>(mx, qx, a.x_stride_t, left_x), load_group<T, V, U>(mg, qg, g.gy_stride_t, left_g);
+#pragma unroll
+            for (int u = 0; u < U; u++) token(std::true_type(), t + u, nx[u], ng[u]);
+#pragma unroll
+            for (int u = 0; u < U; u++) nx[u] = mx[u], ng[u] = mg[u];
         }
-        int64_t p = t - W + 1;
-        if (p < (c == 0 ? (gi ? -(int64_t)(W - 1) : 0) : t0)) return;
-        float o[V];
+        for (;;) {                      // incomplete groups, the W - 1 tokens after the chunk and what does not count among them
+            load_group<T, V, U>(mx, qx, a.x_stride_t, left_x), load_group<T, V, U>(mg, qg, g.gy_stride_t, left_g);
 #pragma unroll
-        for (int i = 0; i < V; i++) {
-            o[i] = 0.0f;
+            for (int u = 0; u < U; u++) {
+                if (t + u >= n + W - 1) break;
+                token(std::false_type(), t + u, nx[u], ng[u]);
+            }
+            if ((t += U) >= n + W - 1) break;
 #pragma unroll
-            for (int k = 0; k < W; k++) o[i] = fmaf(w[k][i], h[W - 1 - k][i], o[i]);
+            for (int u = 0; u < U; u++) nx[u] = mx[u], ng[u] = mg[u];
         }
-        if (gf && p < len && p >= len - (W - 1)) {
-            float v[V];
-            load<T, V>(v, gf + (p - len + W - 1) * a.D);
-#pragma unroll
-            for (int i = 0; i < V; i++) o[i] += v[i];
-        }
-        store<T, V>(p >= 0 ? gx + p * a.D : gi + (W - 1 + p) * a.D, o);
-    };
-    // groups of U tokens, the next one's loads under way while one is worked on
-    constexpr int U = V >= 4 ? 4 : 8;
-    const int64_t end = min(t1, len);
-    int64_t t = t0;
-    const T *qx = x + t0 * a.x_stride_t, *qg = gy + t0 * g.gy_stride_t;
-    Pack<T, V> nx[U], ng[U], mx[U], mg[U];
-    auto fetch = [&](Pack<T, V> (&tx)[U], Pack<T, V> (&tg)[U]) {
-#pragma unroll
-        for (int u = 0; u < U; u++, qx += a.x_stride_t, qg += g.gy_stride_t) tx[u] = *(const Pack<T, V>*)qx, tg[u] = *(const Pack<T, V>*)qg;
-    };
-    if (t + U <= end) fetch(nx, ng);
-    for (; t + U <= end; t += U) {
-        if (t + 2 * U <= end) fetch(mx, mg);
-#pragma unroll
-        for (int u = 0; u < U; u++) {
-            float in[V], up[V];
-#pragma unroll
-            for (int i = 0; i < V; i++) in[i] = to_float(nx[u].v[i]), up[i] = to_float(ng[u].v[i]);
-            token(t + u, in, up, true);
-        }
-#pragma unroll
-        for (int u = 0; u < U; u++) nx[u] = mx[u], ng[u] = mg[u];
-    }
-    for (; t < t1 + W - 1; t += U) {    // incomplete groups, the W - 1 tokens after the chunk and what does not count among them
-        Pack<T, V> sx[U] = {}, sg[U] = {};
-#pragma unroll
-        for (int u = 0; u < U; u++)
-            if (t + u < len && t + u < t1 + W - 1) sx[u] = *(const Pack<T, V>*)(x + (t + u) * a.x_stride_t), sg[u] = *(const Pack<T, V>*)(gy + (t + u) * g.gy_stride_t);
-#pragma unroll
-        for (int u = 0; u < U; u++) {
-            if (t + u >= t1 + W - 1) break;
-            float in[V], up[V];
-#pragma unroll
-            for (int i = 0; i < V; i++) in[i] = to_float(sx[u].v[i]), up[i] = to_float(sg[u].v[i]);
-            token(t + u, in, up, t + u < len);
+    } else if (there) {
+        float zero[V] = {};
+        for (int t = 0; t < n; t++) store<T, V>(gx + t * a.D, zero);
+        for (int k = 0; gi && k < W - 1; k++) {      // no tokens: the final state is the initial one
+            float v[V] = {};
+            if (gf) load<T, V>(v, gf + k * a.D);
+            store<T, V>(gi + k * a.D, v);
         }
     }
     // The sums of channels that several threads of the workgroup share are added up here, in their order: otherwise the second kernel would
