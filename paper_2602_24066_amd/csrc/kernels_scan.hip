@@ -684,41 +684,44 @@ __global__ __launch_bounds__(Gr::W * 64, Gr::W > 8 ? 4 : 2) void scan_bwd_kernel
     }
 }
 
-// dB and dC of a tile: the sums over the workgroups of its group's channels, in their order
-template <class T, class Gr> __global__ __launch_bounds__(kThreads) void scan_bwd_bc_kernel(sig_scan_args a, Blocks bl, const float* part, T* gB, T* gC)
+// The sums over workgroups of a backward launch, in a fixed order; the two parts in one launch (7 x 301 x 278 in float32: 4.3 us, 4.9 and 4.0 in
+// two).  Bound by memory: 8 x 2048 x 2048 in bf16 14.2 us for 70 MB, 21.7 with one load a time instead of eight.  Sixteen wavefronts a workgroup.
+// Workgroups up to `params`: dA, dskip and ddt_bias, the sums over streams and time chunks.  64 sums a workgroup; each of its
+// wavefronts takes every sixteenth row, so that few columns with many rows wait for memory a sixteenth as often.
+// The others: dB and dC, the sums over the workgroups of a group's channels, a tile and two states a wavefront.
+constexpr int kSumThreads = 1024;
+template <class T, class Gr>
+__global__ __launch_bounds__(kSumThreads) void scan_bwd_sums_kernel(sig_scan_args a, Blocks bl, Parts parts, int64_t rows, unsigned params, T* gB, T* gC, float* gA, float* gskip, float* gbias)
 {
-    constexpr int Q = Gr::S / 2, R = Gr::W * Q;
-    const int64_t tiles = (a.L + kTile - 1) / kTile, all = a.B * tiles * a.G * R;
     const int lane = threadIdx.x & 63;
-    // a wavefront for each [.., W, Q]
-    for (int64_t id = (int64_t)blockIdx.x * (kThreads / 64) + threadIdx.x / 64; id < all; id += (int64_t)gridDim.x * (kThreads / 64)) {
+    if (blockIdx.x < params) {
+        const int64_t id = (int64_t)blockIdx.x * 64 + lane, DN = a.D * a.N;
+        const bool of_A = id < DN, of_rest = !of_A && id < DN + 2 * a.D;
+        const float* from = of_A ? parts.A + id : parts.rest + (id - DN);
+        const int64_t step = of_A ? DN : 2 * a.D;
+        const float v = sum_rows(from, of_A || of_rest ? rows : 0, step);
+        if (threadIdx.x >= 64) return;
+        if (of_A) gA[id % a.D * a.N + id / a.D] = v;
+        if (of_rest) {
+            float* to = id - DN < a.D ? gskip : gbias;
+            if (to) to[(id - DN) % a.D] = v;
+        }
+        return;
+    }
+    constexpr int Q = Gr::S / 2, R = Gr::W * Q, kWaves = kSumThreads / 64;
+    const int64_t tiles = (a.L + kTile - 1) / kTile, all = a.B * tiles * a.G * R;
+    for (int64_t id = (int64_t)(blockIdx.x - params) * kWaves + threadIdx.x / 64; id < all; id += (int64_t)(gridDim.x - params) * kWaves) {
         const int r = (int)(id % R);
         const int64_t grp = id / R % a.G, tile = id / R / a.G % tiles, b = id / R / a.G / tiles, t = tile * kTile + token_of(lane);
         const int n = r / Q * Gr::S + r % Q * 2 + (lane >> 4 & 1);
         const int64_t len = live_length(a.lengths, b, a.L);
         float v = 0.0f;
         if (tile * kTile < len) {
-            const float* p = part + (((b * tiles + tile) * a.G + grp) * bl.runs * R + r) * 64 + lane;
-            for (unsigned j = 0; j < bl.runs; j++, p += R * 64) v += *p;
+            const float* p = parts.bc + (((b * tiles + tile) * a.G + grp) * bl.runs * R + r) * 64 + lane;
+#pragma unroll 8
+            for (unsigned j = 0; j < bl.runs; j++) v += p[(int64_t)j * R * 64];
         }
         if (t < a.L && n < a.N) (lane & 32 ? gC : gB)[((b * a.L + t) * a.G + grp) * a.N + n] = from_float<T>(t < len ? v : 0.0f);
-    }
-}
-
-// dA, dskip and ddt_bias: the sums over streams and time chunks, in a fixed order.  64 sums a workgroup; each of its sixteen wavefronts takes
-// every sixteenth row, so that few columns with many rows wait for memory a sixteenth as often.
-__global__ __launch_bounds__(1024) void scan_bwd_params_kernel(sig_scan_args a, int64_t rows, Parts parts, float* gA, float* gskip, float* gbias)
-{
-    const int64_t id = (int64_t)blockIdx.x * 64 + (threadIdx.x & 63), DN = a.D * a.N;
-    const bool of_A = id < DN, of_rest = !of_A && id < DN + 2 * a.D;
-    const float* from = of_A ? parts.A + id : parts.rest + (id - DN);
-    const int64_t step = of_A ? DN : 2 * a.D;
-    const float v = sum_rows(from, of_A || of_rest ? rows : 0, step);
-    if (threadIdx.x >= 64) return;
-    if (of_A) gA[id % a.D * a.N + id / a.D] = v;
-    if (of_rest) {
-        float* to = id - DN < a.D ? gskip : gbias;
-        if (to) to[(id - DN) % a.D] = v;
     }
 }
 
@@ -913,9 +916,11 @@ hipError_t scan_backward(const sig_scan_args& a, const sig_scan_grads& g, const 
             if (a.B > 0) {
                 if (bl.chunks > 1) scan_bwd_kernel<T, Gr, false><<<bl.total, Gr::W * 64, backward_lds(0), stream>>>(a, g, bl, cs, nullptr, parts);
                 scan_bwd_kernel<T, Gr, true><<<bl.total, Gr::W * 64, lds, stream>>>(a, g, bl, cs, checkpoint, parts);
-                if (a.L > 0) scan_bwd_bc_kernel<T, Gr><<<std::min(1u << 22, blocks_for(p.bc / bl.runs)), kThreads, 0, stream>>>(a, bl, parts.bc, (T*)g.grad_b, (T*)g.grad_c);
             }
-            scan_bwd_params_kernel<<<(unsigned)((a.D * (a.N + 2) + 63) / 64), 1024, 0, stream>>>(a, a.B * bl.chunks, parts, g.grad_A, g.grad_skip, g.grad_dt_bias);
+            const unsigned params = (unsigned)((a.D * (a.N + 2) + 63) / 64);
+            const int64_t sums = a.B * tiles_of(a) * a.G * Gr::W * (Gr::S / 2);        // wavefronts
+            const unsigned others = (unsigned)std::min<int64_t>(1 << 20, (sums + kSumThreads / 64 - 1) / (kSumThreads / 64));
+            scan_bwd_sums_kernel<T, Gr><<<params + others, kSumThreads, 0, stream>>>(a, bl, parts, a.B * bl.chunks, params, (T*)g.grad_b, (T*)g.grad_c, g.grad_A, g.grad_skip, g.grad_dt_bias);
             return hipGetLastError();
         });
     });
