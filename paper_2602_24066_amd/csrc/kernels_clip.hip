@@ -1,6 +1,8 @@
 // Global norm over many tensors, n = sqrt(sum g^2), and the clipped tensors min(1, max_norm / (n + 1e-6)) g.
 // Bound by memory: everything is read for the norm and once more for the product, whose input the cache between the chip and its memory
-// (256 MB) still holds in part.  Squares are summed in float64: no overflow for any finite float32, and sums whose order is fixed.
+// (256 MB) still holds in part.  166e6 elements, 340 MB (bfloat16, the small ones float32) into 662 MB of float32, call after call: 58 us for the
+// norm, 169 us for the product (5.9 TB/s each, above a large copy's 5.1 by the cache's part), 257 us with what lies between.
+// Squares are summed in float64: no overflow for any finite float32, and sums whose order is fixed.
 #include "seq.hpp"
 
 namespace sig {
@@ -78,8 +80,16 @@ __global__ __launch_bounds__(1024) void norm_kernel(const double* part, int64_t 
     if (threadIdx.x == 0) *norm = (float)sqrt(v);
 }
 
+template <class P> __device__ __forceinline__ void store_past_cache(P* to, const P& v)
+{
+    typedef uint32_t Words __attribute__((ext_vector_type(sizeof(P) / 4)));
+    Words w;
+    __builtin_memcpy(&w, &v, sizeof(P));
+    __builtin_nontemporal_store(w, (Words*)to);
+}
+
 // Accesses of 16 bytes of the narrower side where both sides allow it, of single elements otherwise (views at odd offsets)
-template <class I, class O> __device__ __forceinline__ void scaled(const I* in, O* out, int64_t n, float scale)
+template <bool kPast, class I, class O> __device__ __forceinline__ void scaled(const I* in, O* out, int64_t n, float scale)
 {
     constexpr int V = 16 / (sizeof(I) > sizeof(O) ? sizeof(I) : sizeof(O)), U = 4;
     const uintptr_t pi = (uintptr_t)in, po = (uintptr_t)out;
@@ -100,14 +110,18 @@ template <class I, class O> __device__ __forceinline__ void scaled(const I* in, 
 #pragma unroll
         for (int u = 0; u < U; u++) r[u] = q[i + u * kThreads];
 #pragma unroll
-        for (int u = 0; u < U; u++) to[i + u * kThreads] = one(r[u]);
+        for (int u = 0; u < U; u++) {
+            if constexpr (kPast) store_past_cache(to + i + u * kThreads, one(r[u]));
+            else to[i + u * kThreads] = one(r[u]);
+        }
     }
     for (; i < vecs; i += kThreads) to[i] = one(q[i]);
     for (i = threadIdx.x; i < head; i += kThreads) out[i] = from_float<O>(to_float(in[i]) * scale);
     for (i = tail + threadIdx.x; i < n; i += kThreads) out[i] = from_float<O>(to_float(in[i]) * scale);
 }
 
-__global__ __launch_bounds__(kThreads) void clip_kernel(ClipTable tab, const float* norm, float max_norm)
+// kPast: the products go past the cache, which keeps what it holds of the tensors that are still to be read
+template <bool kPast> __global__ __launch_bounds__(kThreads) void clip_kernel(ClipTable tab, const float* norm, float max_norm)
 {
     // from the last workgroup to the first: what the norm read last is still in the cache
     Piece p = piece_of(tab, gridDim.x - 1 - blockIdx.x);
@@ -115,10 +129,10 @@ __global__ __launch_bounds__(kThreads) void clip_kernel(ClipTable tab, const flo
     const void* in = tab.in[p.t];
     void* out = tab.out[p.t];
     switch (tab.kind[p.t]) {
-        case 0: scaled((const float*)in + p.first, (float*)out + p.first, p.count, scale); break;
-        case 1: scaled((const bf16*)in + p.first, (float*)out + p.first, p.count, scale); break;
-        case 2: scaled((const float*)in + p.first, (bf16*)out + p.first, p.count, scale); break;
-        default: scaled((const bf16*)in + p.first, (bf16*)out + p.first, p.count, scale); break;
+        case 0: scaled<kPast>((const float*)in + p.first, (float*)out + p.first, p.count, scale); break;
+        case 1: scaled<kPast>((const bf16*)in + p.first, (float*)out + p.first, p.count, scale); break;
+        case 2: scaled<kPast>((const float*)in + p.first, (bf16*)out + p.first, p.count, scale); break;
+        default: scaled<kPast>((const bf16*)in + p.first, (bf16*)out + p.first, p.count, scale); break;
     }
 }
 
@@ -134,9 +148,10 @@ hipError_t norm_total(const double* part, int64_t n, float* norm, hipStream_t st
     norm_kernel<<<1, 1024, 0, stream>>>(part, n, norm);
     return hipGetLastError();
 }
-hipError_t clip_scaled(const ClipTable& tab, const float* norm, float max_norm, hipStream_t stream)
+hipError_t clip_scaled(const ClipTable& tab, const float* norm, float max_norm, bool past_cache, hipStream_t stream)
 {
-    clip_kernel<<<tab.end[tab.n - 1], kThreads, 0, stream>>>(tab, norm, max_norm);
+    if (past_cache) clip_kernel<true><<<tab.end[tab.n - 1], kThreads, 0, stream>>>(tab, norm, max_norm);
+    else clip_kernel<false><<<tab.end[tab.n - 1], kThreads, 0, stream>>>(tab, norm, max_norm);
     return hipGetLastError();
 }
 

@@ -49,7 +49,7 @@ struct ClipTable {
 };
 hipError_t norm_parts(const ClipTable& tab, double* part, hipStream_t stream);     // part: one sum of squares for each workgroup
 hipError_t norm_total(const double* part, int64_t n, float* norm, hipStream_t stream);
-hipError_t clip_scaled(const ClipTable& tab, const float* norm, float max_norm, hipStream_t stream);
+hipError_t clip_scaled(const ClipTable& tab, const float* norm, float max_norm, bool past_cache, hipStream_t stream);
 
 #ifdef __HIPCC__
 // ---- device side
