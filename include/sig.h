@@ -369,7 +369,7 @@ int sig_leadlag_backward(const float* grad_out, int64_t B, int64_t n_points, int
  * outputs and gradients of zero and leave states as they are.  Calls only enqueue kernels on `stream`; two calls on the same inputs give
  * the same bits.  B == 0 is a no-op (gradients of parameters are set to zero), L == 0 is allowed: a final state is the initial one.
  * SIG_ETOOLARGE: sizes whose product passes 2^38; for the scan L >= 2^30, B * D >= 2^31, D or a time stride of 2^24 and more (time strides
- * of the scan are not negative).  SIG_EUNSUPPORTED: more filter taps or states than the limits below. */
+ * of the scan are not negative, those of b and c with more than one token 0 or at least N).  SIG_EUNSUPPORTED: more filter taps or states than the limits below. */
 #define SIG_F32  0
 #define SIG_BF16 1
 

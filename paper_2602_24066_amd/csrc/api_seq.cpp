@@ -45,6 +45,8 @@ int check_scan(const sig_scan_args* a)
     if (a->L >= (1 << 30)) return SIG_ETOOLARGE;        // a chunk's end is at most L rounded up to tiles, times two at the most
     for (int64_t s : {a->x_stride_t, a->dt_stride_t, a->gate_stride_t, a->b_stride_t, a->c_stride_t, a->D})
         if (s < 0 || s >= (1 << 24)) return s < 0 ? SIG_EINVAL : SIG_ETOOLARGE;
+    for (int64_t s : {a->b_stride_t, a->c_stride_t})           // the kernels tell tokens that count from others by where their rows end
+        if (a->L > 1 && s > 0 && s < a->N) return SIG_EINVAL;
     return check_sizes({a->B, a->L, a->D, a->N});
 }
 

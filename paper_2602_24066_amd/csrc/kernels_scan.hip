@@ -62,9 +62,9 @@ template <int K, int S, int s = 1> __device__ __forceinline__ void sum_broadcast
 #undef SIG_FMAC
 
 // Loads and stores at a lane's byte offset from a row that is the same for the wavefront, and an offset between rows in bytes; an offset
-// of kNowhere makes a load give zero and a store do nothing, so tokens that are not there need no branches around them.
+// of kNowhere, or one past a buffer's bytes, makes a load give zero and a store do nothing: tokens that are not there need no branches around them.
 using Buffer = __amdgpu_buffer_rsrc_t;
-__device__ __forceinline__ Buffer buffer_at(const void* p) { return __builtin_amdgcn_make_buffer_rsrc((void*)p, 0, 0xfffffff0u, 0x00020000); }
+__device__ __forceinline__ Buffer buffer_at(const void* p, unsigned bytes = 0xfffffff0u) { return __builtin_amdgcn_make_buffer_rsrc((void*)p, 0, bytes, 0x00020000); }
 template <class T> __device__ __forceinline__ T buffer_load(Buffer r, unsigned at, unsigned row)
 {
     T v;
@@ -92,8 +92,7 @@ template <class T> __device__ __forceinline__ void buffer_store(Buffer r, unsign
 // p some bytes on (32 bits: a tile's rows, see the limits of strides in api_seq.cpp; scalar registers are few)
 template <class T> __device__ __forceinline__ void forth(T*& p, unsigned bytes) { p = (T*)((const char*)p + bytes); }
 constexpr unsigned kNowhere = 0xfffffffcu;
-// at, or kNowhere: a selection that the compiler does not turn into branches around two accesses (worth 1 % of the backward pass; in the
-// forward pass the straight code takes more registers and a tenth longer over time chunks)
+// at, or kNowhere: a selection that the compiler does not turn into branches around two accesses (worth 1 % of the backward pass)
 __device__ __forceinline__ unsigned offset_if(bool there, unsigned at)
 {
     unsigned r = there ? at : kNowhere;
@@ -142,8 +141,9 @@ template <int S> __device__ __forceinline__ void join_chunks(float (&h)[S], cons
     }
 }
 
-template <class T, class Gr, bool kOutputs>
-__global__ __launch_bounds__(Gr::W * 64, Gr::W > 2 && Gr::S == 4 ? 4 : 2) void scan_fwd_kernel(sig_scan_args a, Blocks bl, ChunkStates cs, T* y, float* final_state, float* checkpoint)
+// kOutputs = false: a time chunk's last state from zero and its sum of step sizes alone.  kStates: the states before every tile go to the checkpoint.
+template <class T, class Gr, bool kOutputs, bool kStates>
+__global__ __launch_bounds__(Gr::W * 64, Gr::S == 4 ? 4 : 2) void scan_fwd_kernel(sig_scan_args a, Blocks bl, ChunkStates cs, T* y, float* final_state, float* checkpoint)
 {
     constexpr int S = Gr::S, W = Gr::W, PT = kTile / W, RT = 16 / S, KB = kTile / RT;
     extern __shared__ float lds[];
@@ -180,19 +180,32 @@ __global__ __launch_bounds__(Gr::W * 64, Gr::W > 2 && Gr::S == 4 ? 4 : 2) void s
     const T *pb = (const T*)a.b + b * a.b_stride_b + g * a.b_stride_g + t_first * a.b_stride_t + n0;
     const T *pc = (const T*)a.c + b * a.c_stride_b + g * a.c_stride_g + t_first * a.c_stride_t + n0;
     T* py = kOutputs ? y + (b * a.L + t1) * a.D + d0 : nullptr;
-    float* pk = checkpoint ? checkpoint + ((b * ((a.L + kTile - 1) / kTile) + t_first / kTile) * a.N + n0) * a.D + d0 : nullptr;
+    float* pk = kStates ? checkpoint + ((b * ((a.L + kTile - 1) / kTile) + t_first / kTile) * a.N + n0) * a.D + d0 : nullptr;
     constexpr unsigned E = sizeof(T);
     const unsigned x_row = (unsigned)a.x_stride_t * E, dt_row = (unsigned)a.dt_stride_t * E, z_row = gated ? (unsigned)a.gate_stride_t * E : x_row;
-    const unsigned y_row = (unsigned)a.D * E, b_row = (unsigned)(RT * a.b_stride_t) * E, c_row = (unsigned)(RT * a.c_stride_t) * E;
-    // the token of a tile and the state whose B and C this lane loads
-    const int tb = n0 + lane % S < a.N ? lane % 16 / S : INT_MAX / 2;
-    const unsigned b_at = (unsigned)(lane % 16 / S * a.b_stride_t + lane % S) * E, c_at = (unsigned)(lane % 16 / S * a.c_stride_t + lane % S) * E;
+    const unsigned y_row = (unsigned)a.D * E;
+    // Where the lane's state and tokens of B and C lie in a tile.  The buffers end with the row of the last token that counts (rows do not overlap, or
+    // are all the same): no selection a lane, which the compiler makes branches of.  A tile is one block of instructions then, with or without
+    // states to keep (kStates): 383 us for 414 in the large case, 378 for 433 with states.
+    unsigned b_at[KB], c_at[KB];
+#pragma unroll
+    for (int j = 0; j < KB; j++) {
+        const int k = j * RT + lane % 16 / S;
+        b_at[j] = n0 + lane % S < a.N ? (unsigned)(k * a.b_stride_t + lane % S) * E : kNowhere;
+        c_at[j] = n0 + lane % S < a.N ? (unsigned)(k * a.c_stride_t + lane % S) * E : kNowhere;
+    }
+    const unsigned b_step = (unsigned)a.b_stride_t * E, c_step = (unsigned)a.c_stride_t * E, n_bytes = (unsigned)max(0, (int)a.N - n0) * E;
+    unsigned k_at[S];
+#pragma unroll
+    for (int s = 0; s < S; s++) k_at[s] = n0 + s < a.N ? e * 4 : kNowhere;
 
     T x[PT], dt[PT], z[PT], bv[KB], cv[KB];
     float f[PT], keep[PT], f_next[PT], keep_next[PT], o[PT], B[KB], C[KB], total = 0.0f;
     // reads the tile at the row pointers, n tokens of it; the pointers go on to the next
     auto fetch = [&](int n) {
-        Buffer rx = buffer_at(px), rdt = buffer_at(pdt), rz = buffer_at(pz), rb = buffer_at(pb), rc = buffer_at(pc);
+        const unsigned before = n < kTile ? n - 1 : kTile - 1;
+        Buffer rx = buffer_at(px), rdt = buffer_at(pdt), rz = buffer_at(pz);
+        Buffer rb = buffer_at(pb, __builtin_amdgcn_readfirstlane(n > 0 ? before * b_step + n_bytes : 0)), rc = buffer_at(pc, __builtin_amdgcn_readfirstlane(n > 0 ? before * c_step + n_bytes : 0));
 #pragma unroll
         for (int i = 0; i < PT; i++) {
             unsigned at = w * PT + i < n ? e * E : kNowhere;
@@ -202,11 +215,10 @@ __global__ __launch_bounds__(Gr::W * 64, Gr::W > 2 && Gr::S == 4 ? 4 : 2) void s
         }
 #pragma unroll
         for (int j = 0; j < KB; j++) {
-            const bool there = j * RT + tb < n;
-            bv[j] = buffer_load<T>(rb, there ? b_at : kNowhere, j * b_row);
-            if (kOutputs) cv[j] = buffer_load<T>(rc, there ? c_at : kNowhere, j * c_row);
+            bv[j] = buffer_load<T>(rb, b_at[j], 0);
+            if (kOutputs) cv[j] = buffer_load<T>(rc, c_at[j], 0);
         }
-        forth(px, kTile * x_row), forth(pdt, kTile * dt_row), forth(pz, kTile * z_row), forth(pb, KB * b_row), forth(pc, KB * c_row);
+        forth(px, kTile * x_row), forth(pdt, kTile * dt_row), forth(pz, kTile * z_row), forth(pb, kTile * b_step), forth(pc, kTile * c_step);
     };
     // D_t and D_t x_t of the wavefront's tokens of a tile with n tokens (zero beyond: states stay), and what its outputs need besides
     auto prepare = [&](float4 (*to)[64], int n, const float (&xf)[PT], const float (&df)[PT], const float (&zf)[PT]) {
@@ -266,9 +278,9 @@ __global__ __launch_bounds__(Gr::W * 64, Gr::W > 2 && Gr::S == 4 ? 4 : 2) void s
 #pragma unroll
         for (int j = 0; j < KB; j++) b_next[j] = to_float(bv[j]), c_next[j] = kOutputs ? to_float(cv[j]) : 0.0f;
         fetch(left - 2 * kTile);
-        if (kOutputs && checkpoint) {
+        if (kStates) {
 #pragma unroll
-            for (int s = 0; s < S; s++) buffer_store(buffer_at(pk), n0 + s < a.N ? e * 4 : kNowhere, (unsigned)(s * a.D) * 4, h[s]);
+            for (int s = 0; s < S; s++) buffer_store(buffer_at(pk), k_at[s], (unsigned)(s * a.D) * 4, h[s]);
             pk += a.N * a.D;
         }
         if (kOutputs) {
@@ -889,13 +901,16 @@ hipError_t scan_forward(const sig_scan_args& a, void* y, float* final_state, flo
             using T = decltype(t);
             using Gr = decltype(gr);
             constexpr int lds = forward_lds(Gr::W);
-            if (lds > 65536) {
-                hipError_t e = ensure_dynamic_lds((const void*)scan_fwd_kernel<T, Gr, true>, lds);
-                if (e != hipSuccess) return e;
-            }
-            if (bl.chunks > 1) scan_fwd_kernel<T, Gr, false><<<bl.total, Gr::W * 64, forward_lds(0), stream>>>(a, bl, cs, nullptr, nullptr, nullptr);
-            scan_fwd_kernel<T, Gr, true><<<bl.total, Gr::W * 64, lds, stream>>>(a, bl, cs, (T*)y, final_state, checkpoint);
-            return hipGetLastError();
+            if (bl.chunks > 1) scan_fwd_kernel<T, Gr, false, false><<<bl.total, Gr::W * 64, forward_lds(0), stream>>>(a, bl, cs, nullptr, nullptr, nullptr);
+            auto launch = [&](auto kernel) {
+                if (lds > 65536) {
+                    hipError_t e = ensure_dynamic_lds((const void*)kernel, lds);
+                    if (e != hipSuccess) return e;
+                }
+                kernel<<<bl.total, Gr::W * 64, lds, stream>>>(a, bl, cs, (T*)y, final_state, checkpoint);
+                return hipGetLastError();
+            };
+            return checkpoint ? launch(scan_fwd_kernel<T, Gr, true, true>) : launch(scan_fwd_kernel<T, Gr, true, false>);
         });
     });
 }

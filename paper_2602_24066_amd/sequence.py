@@ -191,6 +191,12 @@ def _scan_args(x, dt, A, b, c, skip, gate, dt_bias, softplus, initial_state, len
         pd = dt_bias.data_ptr()
     if dims == 3:
         B, L, _ = shape
+        if 0 < bs[1] < N:                                                                   # windows that overlap are copied
+            b = b.contiguous()
+            bs = b.stride()
+        if 0 < cs[1] < N:
+            c = c.contiguous()
+            cs = c.stride()
         if initial_state is not None:
             initial_state = _whole("initial_state", initial_state, (B, D, N), _f32, index)
             pi = initial_state.data_ptr()

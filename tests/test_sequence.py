@@ -532,6 +532,28 @@ def test_the_longest_scan():
     assert lib.sig_scan_checkpoint_bytes(args(1 << 30)) == 0
 
 
+@pytest.mark.parametrize("change,code", [({"bt": 3}, -1), ({"ct": 1}, -1), ({"bt": 4, "ct": 4, "x": 0}, -1), ({"bt": 3, "L": 1, "B": 0}, 0)])
+def test_overlapping_rows_are_refused_by_the_c_abi(change, code):
+    lib = S.load_library()
+    ok = dict.fromkeys(SCAN_ORDER, 0) | dict(dtype=0, B=2, L=8, D=4, G=1, N=4, softplus=1, x=4096, dt=4096, b=4096, c=4096, A=4096)
+    assert lib.sig_scan_forward(pack({**ok, **change}, SCAN_ORDER), 4096, 0, 0, 0, 4096, 1 << 60, 0) == code
+
+
+@gpu
+@pytest.mark.parametrize("t", [torch.float32, torch.bfloat16])
+def test_overlapping_windows_as_b_and_c(t):
+    B, L, D, N = 3, 37, 70, 12
+    x, dt, A = torch.randn(B, L, D, device="cuda").to(t), torch.randn(B, L, D, device="cuda").to(t), -torch.rand(D, N, device="cuda")
+    b, c = (torch.randn(B, L + N - 1, device="cuda").to(t).unfold(1, N, 1) for _ in range(2))
+    lengths = torch.tensor([37, 0, 20], dtype=torch.int32, device="cuda")
+    got = S.sig_scan_forward(x, dt, A, b, c, lengths=lengths, checkpoint=True)
+    want = S.sig_scan_forward(x, dt, A, b.contiguous(), c.contiguous(), lengths=lengths, checkpoint=True)
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+    one, two = (S.sig_scan_backward(x, dt, A, bb, cc, x, got[2], lengths=lengths) for bb, cc in ((b, c), (b.contiguous(), c.contiguous())))
+    for k in ("x", "dt", "A", "B", "C"):
+        assert torch.equal(one[k], two[k]), k
+
+
 def test_more_refusals_of_the_scan():
     lib = S.load_library()
     ok = dict.fromkeys(SCAN_ORDER, 0) | dict(dtype=0, B=2, L=40, D=4, G=2, N=4, softplus=1, x=4096, dt=4096, b=4096, c=4096, A=4096, gate=4096, skip=4096, bias=4096)
