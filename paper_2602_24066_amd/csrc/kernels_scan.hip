@@ -8,7 +8,6 @@
 //   dA = sum_{b,t} l_t a_t h_{t-1} D_t,             dgate_t = dL/dy_t s_t silu'(gate_t),          dh_0 = a_1 l_1.
 // States, sums and gradients in registers are float32; y and the tokens' gradients are rounded once, when they are stored.
 #include <algorithm>
-#include <climits>
 #include <type_traits>
 #include <utility>
 
@@ -91,6 +90,10 @@ template <class T> __device__ __forceinline__ void buffer_store(Buffer r, unsign
 }
 // p some bytes on (32 bits: a tile's rows, see the limits of strides in api_seq.cpp; scalar registers are few)
 template <class T> __device__ __forceinline__ void forth(T*& p, unsigned bytes) { p = (T*)((const char*)p + bytes); }
+// Keeps a row pointer in its own two scalar registers from tile to tile: the compiler otherwise makes it the sum of a start and an offset shared with
+// others, more values than there are registers, and moves them to and from vector registers.  The backward pass of 16 states takes an eighth
+// less with it; that of more than 16 spills vector registers then, and the forward pass gains nothing (large case 379 -> 403 us).
+template <class T> __device__ __forceinline__ void held(T*& p) { asm volatile("" : "+s"(p)); }
 constexpr unsigned kNowhere = 0xfffffffcu;
 // at, or kNowhere: a selection that the compiler does not turn into branches around two accesses (worth 1 % of the backward pass)
 __device__ __forceinline__ unsigned offset_if(bool there, unsigned at)
@@ -364,7 +367,7 @@ __global__ __launch_bounds__(Gr::W * 64, Gr::S == 4 ? 4 : 2) void scan_fwd_kerne
 // six steps leaves the 64 sums of 16 tokens (2 states, dB and dC) one to a lane in 129 instructions, where a sum to all lanes would take six for
 // each; the workgroups' sums are added by a second kernel in their order, no atomics.
 // What bounds it: vector instructions, 25 a state and token (two exponentials with four states a wavefront, else one), on SIMDs that are busy
-// 70 % of the time with two wavefronts each.  8 x 2048 x 2048 bf16, 16 states: 573 us, 0.94e12 states a second; the bytes alone 105 us.
+// 70 % of the time with two wavefronts each.  8 x 2048 x 2048 bf16, 16 states: 480 us, 1.12e12 states a second; the bytes alone 105 us.
 template <int K, int S> __device__ __forceinline__ void add_broadcast(float (&o)[S], float r, float v)      // o[s] += r[K + s] v
 {
     static_assert(S == 2 || S == 4, "states of a wavefront");
@@ -420,7 +423,7 @@ template <class T, class Gr, bool kFull>
 __global__ __launch_bounds__(Gr::W * 64, Gr::W > 8 ? 4 : 2) void scan_bwd_kernel(sig_scan_args a, sig_scan_grads g, Blocks bl, ChunkStates cs, const float* checkpoint, Parts parts)
 {
     constexpr int S = Gr::S, W = Gr::W, PT = kTile / W, PH = PT > 1 ? PT / 2 : 1, RT = 16 / S, KB = kTile / RT, kHalf = kTile / 2, Q = S / 2;
-    constexpr bool kDecays = S == 2, kTwice = W <= 8;      // decays stay in registers; the sums' LDS is there for either half of a tile
+    constexpr bool kDecays = S == 2, kHeld = S == 2, kTwice = W <= 8;      // decays stay in registers; row pointers are held; the sums' LDS is there for either half of a tile
     constexpr unsigned E = sizeof(T);
     extern __shared__ float lds[];
     float4(*in)[kTile / 4][64] = (float4(*)[kTile / 4][64])lds;                                          // [2][3: D, D x, dL/ds][kTile / 4][64]
@@ -454,26 +457,35 @@ __global__ __launch_bounds__(Gr::W * 64, Gr::W > 8 ? 4 : 2) void scan_bwd_kernel
     const int n_tiles = live > 0 ? (live + kTile - 1) / kTile : 0, n_last = n_tiles > 0 ? live - (n_tiles - 1) * kTile : 0;
     // rows of the last tile's first token; they go back a tile at a time
     const int64_t t1 = t_first + (int64_t)(n_tiles - 1) * kTile;
-    const T *px = (const T*)a.x + b * a.x_stride_b + t1 * a.x_stride_t + d0, *pdt = (const T*)a.dt + b * a.dt_stride_b + t1 * a.dt_stride_t + d0;
-    const T *pz = a.gate ? (const T*)a.gate + b * a.gate_stride_b + t1 * a.gate_stride_t + d0 : px, *pg = (const T*)g.grad_y + b * g.gy_stride_b + t1 * g.gy_stride_t + d0;
+    const int64_t own1 = t1 + w * PH;                      // the wavefront's first token of it
+    const T *px = (const T*)a.x + b * a.x_stride_b + own1 * a.x_stride_t + d0, *pdt = (const T*)a.dt + b * a.dt_stride_b + own1 * a.dt_stride_t + d0;
+    const T *pz = a.gate ? (const T*)a.gate + b * a.gate_stride_b + own1 * a.gate_stride_t + d0 : px, *pg = (const T*)g.grad_y + b * g.gy_stride_b + own1 * g.gy_stride_t + d0;
     const T *pb = (const T*)a.b + b * a.b_stride_b + grp * a.b_stride_g + t1 * a.b_stride_t + n0, *pc = (const T*)a.c + b * a.c_stride_b + grp * a.c_stride_g + t1 * a.c_stride_t + n0;
     const float* ph = kFull ? checkpoint + ((b * tiles + t1 / kTile) * a.N + n0) * a.D + d0 : nullptr;
-    const int64_t out = (b * a.L + t1 + kTile) * a.D + d0;       // one tile on: every turn begins with the lower half of the tile before
+    const int64_t out = (b * a.L + own1 + kTile) * a.D + d0;       // one tile on: every turn begins with the lower half of the tile before
     T *qx = (T*)g.grad_x + out, *qdt = (T*)g.grad_dt + out, *qz = (T*)g.grad_gate + out;
     const unsigned x_row = (unsigned)a.x_stride_t * E, dt_row = (unsigned)a.dt_stride_t * E, z_row = gated ? (unsigned)a.gate_stride_t * E : x_row, g_row = (unsigned)g.gy_stride_t * E;
-    const unsigned y_row = (unsigned)a.D * E, b_row = (unsigned)(RT * a.b_stride_t) * E, c_row = (unsigned)(RT * a.c_stride_t) * E;
-    const int tb = n0 + lane % S < a.N ? lane % 16 / S : INT_MAX / 2;
-    const unsigned b_at = (unsigned)(lane % 16 / S * a.b_stride_t + lane % S) * E, c_at = (unsigned)(lane % 16 / S * a.c_stride_t + lane % S) * E;
-    auto own = [&](int half, int i) { return PT > 1 ? half * kHalf + w * PH + i : w; };       // the tokens that the wavefront prepares and stores
+    const unsigned y_row = (unsigned)a.D * E, b_step = (unsigned)a.b_stride_t * E, c_step = (unsigned)a.c_stride_t * E;
+    unsigned b_at[KB], c_at[KB];                            // as in the forward kernel
+#pragma unroll
+    for (int j = 0; j < KB; j++) {
+        const int k = j * RT + lane % 16 / S;
+        b_at[j] = n0 + lane % S < a.N ? (unsigned)(k * a.b_stride_t + lane % S) * E : kNowhere;
+        c_at[j] = n0 + lane % S < a.N ? (unsigned)(k * a.c_stride_t + lane % S) * E : kNowhere;
+    }
+    const unsigned n_bytes = (unsigned)max(0, (int)a.N - n0) * E;
+    auto from_own = [&](int half, int i) { return PT > 1 ? half * kHalf + i : 0; };        // the tokens that the wavefront prepares and stores, from its first
+    auto own = [&](int half, int i) { return w * PH + from_own(half, i); };
 
     T x[PT], dt[PT], z[PT], up[PT], bv[KB], cv[KB];
     float hv[S];
     auto fetch = [&](int n) {              // the tile at the row pointers, n tokens of it
-        Buffer rx = buffer_at(px), rdt = buffer_at(pdt), rz = buffer_at(pz), rg = buffer_at(pg), rb = buffer_at(pb), rc = buffer_at(pc), rh = buffer_at(ph);
+        Buffer rx = buffer_at(px), rdt = buffer_at(pdt), rz = buffer_at(pz), rg = buffer_at(pg), rh = buffer_at(ph);
+        Buffer rb = buffer_at(pb, __builtin_amdgcn_readfirstlane(n > 0 ? (n - 1) * b_step + n_bytes : 0)), rc = buffer_at(pc, __builtin_amdgcn_readfirstlane(n > 0 ? (n - 1) * c_step + n_bytes : 0));
 #pragma unroll
         for (int i = 0; i < PT; i++) {
-            int k = own(i / PH, i % PH);
-            unsigned at = k < n ? e * E : kNowhere;
+            const int k = from_own(i / PH, i % PH);
+            unsigned at = w * PH + k < n ? e * E : kNowhere;
             if (kFull) x[i] = buffer_load<T>(rx, at, k * x_row);
             dt[i] = buffer_load<T>(rdt, at, k * dt_row);
             z[i] = buffer_load<T>(rz, at, k * z_row);
@@ -481,15 +493,15 @@ __global__ __launch_bounds__(Gr::W * 64, Gr::W > 8 ? 4 : 2) void scan_bwd_kernel
         }
 #pragma unroll
         for (int j = 0; j < KB; j++) {
-            const bool there = j * RT + tb < n;
-            if (kFull) bv[j] = buffer_load<T>(rb, offset_if(there, b_at), j * b_row);
-            cv[j] = buffer_load<T>(rc, offset_if(there, c_at), j * c_row);
+            if (kFull) bv[j] = buffer_load<T>(rb, b_at[j], 0);
+            cv[j] = buffer_load<T>(rc, c_at[j], 0);
         }
         if (kFull)
 #pragma unroll
             for (int s = 0; s < S; s++) hv[s] = buffer_load<float>(rh, n > 0 && n0 + s < a.N ? e * 4 : kNowhere, (unsigned)(s * a.D) * 4);
         px -= kTile * a.x_stride_t, pdt -= kTile * a.dt_stride_t, pz -= kTile * (gated ? a.gate_stride_t : a.x_stride_t), pg -= kTile * g.gy_stride_t;
         pb -= kTile * a.b_stride_t, pc -= kTile * a.c_stride_t, ph -= a.N * a.D;
+        if constexpr (kHeld) held(px), held(pdt), held(pz), held(pg), held(pb), held(pc), held(ph);
     };
     // of each of the wavefront's tokens: x, D, dL/ds, dD/d(dt + bias), dL/dy times the gate's slope; of the tile at work and the one after it
     float xs[2][PT], Ds[2][PT], us[2][PT], sl[2][PT], gs[2][PT];
@@ -529,9 +541,10 @@ __global__ __launch_bounds__(Gr::W * 64, Gr::W > 8 ? 4 : 2) void scan_bwd_kernel
             gskip += there ? u * v : 0.0f;
             gbias += dD;
             const unsigned at = offset_if(on && k < room, e * E);
-            buffer_store(rx, at, k * y_row, from_float<T>(dx));
-            buffer_store(rdt, at, k * y_row, from_float<T>(dD));
-            buffer_store(rz, gated ? at : kNowhere, k * y_row, from_float<T>(dz));
+            const unsigned row = from_own(half, i) * y_row;
+            buffer_store(rx, at, row, from_float<T>(dx));
+            buffer_store(rdt, at, row, from_float<T>(dD));
+            buffer_store(rz, gated ? at : kNowhere, row, from_float<T>(dz));
         }
     };
     fetch(n_last);
@@ -547,6 +560,9 @@ __global__ __launch_bounds__(Gr::W * 64, Gr::W > 8 ? 4 : 2) void scan_bwd_kernel
     fetch(n_tiles > 1 ? kTile : 0);
     __syncthreads();
     int tile = n_tiles - 1;
+    // sums of the tile at work
+    const int64_t bc_step = a.G * bl.runs * (W * Q * 64);
+    float* bc = parts.bc + ((b * tiles + t_first / kTile + tile) * bc_step + ((grp * bl.runs + run) * W + w) * (Q * 64));
     auto work = [&](auto parity) {
         constexpr int slot = decltype(parity)::value;
         const float4(*now)[kTile / 4][64] = in + slot * 3;
@@ -556,6 +572,7 @@ __global__ __launch_bounds__(Gr::W * 64, Gr::W > 8 ? 4 : 2) void scan_bwd_kernel
         if (kFull) {                       // what is left of the tile before (in the first turn nothing, whatever LDS holds)
             put(0, slot ^ 1, lower);
             qx -= kTile * a.D, qdt -= kTile * a.D, qz -= kTile * a.D;
+            if constexpr (kHeld) held(qx), held(qdt), held(qz);
             if (!kTwice) __syncthreads();
         }
         prepare(slot ^ 1, in + (slot ^ 1) * 3, tile > 0 ? kTile : 0, kTile);
@@ -637,10 +654,10 @@ __global__ __launch_bounds__(Gr::W * 64, Gr::W > 8 ? 4 : 2) void scan_bwd_kernel
         }
         half_back(std::integral_constant<int, 0>());
         if constexpr (kFull) {
-            float* to = parts.bc + ((((b * tiles + t_first / kTile + tile) * a.G + grp) * bl.runs + run) * W + w) * Q * 64;
 #pragma unroll
             for (int m = 0; m < Q; m++)
-                (to + m * 64)[lane] = fold_quad<0>(fold_quad<1>(group[0][m], group[1][m], lane), fold_quad<1>(group[2][m], group[3][m], lane), lane);
+                (bc + m * 64)[lane] = fold_quad<0>(fold_quad<1>(group[0][m], group[1][m], lane), fold_quad<1>(group[2][m], group[3][m], lane), lane);
+            bc -= bc_step;
         }
 #pragma unroll
         for (int j = 0; j < KB; j++) B[j] = Bn[j], C[j] = Cn[j];
