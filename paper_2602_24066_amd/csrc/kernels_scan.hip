@@ -428,6 +428,9 @@ __global__ __launch_bounds__(Gr::W * 64, Gr::W > 8 ? 4 : 2) void scan_bwd_kernel
     extern __shared__ float lds[];
     float4(*in)[kTile / 4][64] = (float4(*)[kTile / 4][64])lds;                                          // [2][3: D, D x, dL/ds][kTile / 4][64]
     float(*sums)[3][kHalf][64] = (float(*)[3][kHalf][64])(lds + 2 * 3 * kTile * 64);                     // [2 or 1][W][3][kHalf][64]
+    // dA of the tiles before, each lane's own: registers hold a tile's sum, as thousands of tokens one by one cost half a digit (1.0e-6 off, 0.6e-6 so)
+    Pack<float, S>* gA_before = (Pack<float, S>*)(lds + 2 * 3 * kTile * 64 + (kTwice ? 2 : 1) * W * 3 * kHalf * 64) + threadIdx.x;
+    if (kFull) *gA_before = {};
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     const unsigned c = blockIdx.x % bl.chunks, rest = blockIdx.x / bl.chunks, run = rest % bl.runs, bg = rest / bl.runs;
     if (!kFull && c == 0) return;                          // nothing comes before the first chunk's adjoint state
@@ -663,6 +666,12 @@ __global__ __launch_bounds__(Gr::W * 64, Gr::W > 8 ? 4 : 2) void scan_bwd_kernel
         for (int j = 0; j < KB; j++) B[j] = Bn[j], C[j] = Cn[j];
 #pragma unroll
         for (int s = 0; s < S; s++) h0[s] = hn[s];
+        if constexpr (kFull) {
+            Pack<float, S> r = *gA_before;
+#pragma unroll
+            for (int s = 0; s < S; s++) r.v[s] += gA[s], gA[s] = 0.0f;
+            *gA_before = r;
+        }
         tile--;
         __syncthreads();
     };
@@ -695,7 +704,7 @@ __global__ __launch_bounds__(Gr::W * 64, Gr::W > 8 ? 4 : 2) void scan_bwd_kernel
 #pragma unroll
         for (int s = 0; s < S; s++)
             if (n0 + s < a.N) {
-                parts.A[(row * a.N + n0 + s) * a.D + d] = gA[s];
+                parts.A[(row * a.N + n0 + s) * a.D + d] = gA_before->v[s];
                 if (g.grad_initial_state && c == 0) g.grad_initial_state[(b * a.D + d) * a.N + n0 + s] = adj[s];
             }
         if (w == 0) {
@@ -879,14 +888,14 @@ Blocks blocks_of(const sig_scan_args& a, int resident, double second)
 // dynamic LDS of the kernels in bytes, and the workgroups of a compute unit that it leaves room for
 constexpr int kLds = 160 * 1024;
 constexpr int forward_lds(int W) { return 2 * kTile * 64 * 8 + 2 * W * kTile * 64 * 4; }
-constexpr int backward_lds(int W) { return 2 * 3 * kTile * 64 * 4 + (W <= 8 ? 2 : 1) * W * 3 * kTile / 2 * 64 * 4; }
+constexpr int backward_lds(int W, int S) { return 2 * 3 * kTile * 64 * 4 + (W <= 8 ? 2 : 1) * W * 3 * kTile / 2 * 64 * 4 + W * S * 64 * 4; }
 Blocks forward_blocks(const sig_scan_args& a)
 {
     return blocks_of(a, with_group(a.N, [](auto gr) { return kLds / forward_lds(decltype(gr)::W); }), 0.7);
 }
 Blocks backward_blocks(const sig_scan_args& a)
 {
-    return blocks_of(a, with_group(a.N, [](auto gr) { return kLds / backward_lds(decltype(gr)::W); }), 0.25);
+    return blocks_of(a, with_group(a.N, [](auto gr) { return kLds / backward_lds(decltype(gr)::W, decltype(gr)::S); }), 0.25);
 }
 
 // floats of the chunks' states, and of a backward launch's sums
@@ -943,13 +952,13 @@ hipError_t scan_backward(const sig_scan_args& a, const sig_scan_grads& g, const 
         return with_group(a.N, [&](auto gr) {
             using T = decltype(t);
             using Gr = decltype(gr);
-            constexpr int lds = backward_lds(Gr::W);
+            constexpr int lds = backward_lds(Gr::W, Gr::S);
             if (lds > 65536) {
                 hipError_t e = ensure_dynamic_lds((const void*)scan_bwd_kernel<T, Gr, true>, lds);
                 if (e != hipSuccess) return e;
             }
             if (a.B > 0) {
-                if (bl.chunks > 1) scan_bwd_kernel<T, Gr, false><<<bl.total, Gr::W * 64, backward_lds(0), stream>>>(a, g, bl, cs, nullptr, parts);
+                if (bl.chunks > 1) scan_bwd_kernel<T, Gr, false><<<bl.total, Gr::W * 64, backward_lds(0, 0), stream>>>(a, g, bl, cs, nullptr, parts);
                 scan_bwd_kernel<T, Gr, true><<<bl.total, Gr::W * 64, lds, stream>>>(a, g, bl, cs, checkpoint, parts);
             }
             const unsigned params = (unsigned)((a.D * (a.N + 2) + 63) / 64);
