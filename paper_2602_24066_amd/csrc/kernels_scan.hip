@@ -123,10 +123,15 @@ struct ChunkStates {
 };
 // h over the chunks from `from` to `to` (without it, in either direction): h = exp(A2 steps) h + last, eight chunks' loads under way at a
 // time.  last, steps: the lane's channel and the wavefront's first state in the stream's first chunk; n: states there are.
+// Where states grow, a chunk's factor may pass float32's range although h is zero or so small that the product does not.  What comes of it
+// is no finite number any more, so all is done again then, the factor's exponent split into one of at most 127 and a power of two.
 template <int S> __device__ __forceinline__ void join_chunks(float (&h)[S], const float (&A2)[S], int from, int to, const float* last, const float* steps, int64_t N, int64_t D, int n)
 {
     constexpr int U = 8;
     const int way = to >= from ? 1 : -1, count = (to - from) * way;
+    float first[S];
+#pragma unroll
+    for (int s = 0; s < S; s++) first[s] = h[s];
     for (int j0 = 0; j0 < count; j0 += U) {
         float sum[U], l[U][S];
 #pragma unroll
@@ -141,6 +146,22 @@ template <int S> __device__ __forceinline__ void join_chunks(float (&h)[S], cons
         for (int u = 0; u < U; u++)
 #pragma unroll
             for (int s = 0; s < S; s++) h[s] = fmaf(__builtin_amdgcn_exp2f(A2[s] * sum[u]), h[s], l[u][s]);
+    }
+    bool finite = true;
+#pragma unroll
+    for (int s = 0; s < S; s++) finite = finite && fabsf(h[s]) <= 3.4028235e38f;
+    if (finite) return;
+#pragma unroll
+    for (int s = 0; s < S; s++) h[s] = first[s];
+#pragma unroll 1
+    for (int j = 0; j < count; j++) {
+        const int64_t row = from + way * j;
+#pragma unroll
+        for (int s = 0; s < S; s++) {
+            const float x = A2[s] * steps[row * D];
+            const int k = x > 127.0f ? (int)fminf(x, 1000.0f) - 126 : 0;
+            h[s] = fmaf(__builtin_amdgcn_exp2f(x > 1000.0f ? 127.0f : x - (float)k), __builtin_amdgcn_ldexpf(h[s], k), s < n ? last[(row * N + s) * D] : 0.0f);
+        }
     }
 }
 

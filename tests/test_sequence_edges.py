@@ -1,0 +1,95 @@
+"""Sequence operators at the edges of what their contract allows, against the plain 64-bit implementations."""
+import math
+
+import pytest
+import torch
+
+import paper_2602_24066_amd as S
+from tests import seq_reference as R
+from tests.test_sequence import SCAN_ORDER, gpu, pack, up
+
+TOKENS = ("x", "dt", "b", "c", "gate")
+NAMES = dict(x="x", dt="dt", A="A", b="B", c="C", skip="skip", gate="gate", dt_bias="dt_bias", initial_state="initial_state")
+
+
+def chunk_of(which, B, L, D, G, N):
+    """Tokens of a time chunk of the forward or backward kernels (L where there is one), by the workspace that they ask for."""
+    lib = S.load_library()
+    args = pack(dict.fromkeys(SCAN_ORDER, 0) | dict(dtype=0, B=B, L=L, D=D, G=G, N=N, softplus=1), SCAN_ORDER)
+    tiles, runs = -(-L // 16), G * -(-(D // G) // 64)
+    if which == "forward":
+        count = lib.sig_scan_forward_workspace_bytes(args) // (4 * B * D * (N + 1))
+    else:
+        # sums of dB and dC, then for each chunk the parameters' gradients, and with more than one chunk their states
+        states = 8 if N <= 8 else 16 if N <= 16 else 32 if N <= 32 else 64
+        left = lib.sig_scan_backward_workspace_bytes(args) // 4 - B * tiles * runs * states * 32
+        count = left // (B * D * (N + 2))
+        if count > 1:
+            count = left // (B * D * (2 * N + 3))
+    return -(-tiles // count) * 16 if count > 1 else L
+
+
+# ------------------------------------------------------------------------------------------------ states that grow
+# A chunk's growth of 2^150: its exponent, 104 in natural units, is off by a rounding of A, of A log2(e) and of their product, 3 * 2^-24 each
+# at the most, and the factor by 104 times that, 1.9e-5; the rest as for other float32 results.
+GROWTH_TOL = 3e-5
+
+
+def near(got, want, what):
+    got, want = got.detach().double().cpu(), want.double()
+    assert torch.isfinite(got).all(), f"{what}: not finite"
+    assert float((got - want).norm()) <= GROWTH_TOL * float(want.norm()), what
+
+
+@gpu
+@pytest.mark.parametrize("by", ["A", "steps"])
+@pytest.mark.parametrize("D,N", [(70, 16), (20, 40), (33, 4)])
+def test_growth_over_chunks_leaves_zeros_alone(D, N, by):
+    """States that grow by 2^150 over a chunk and are zero until the last tokens; adjoint states that are zero from the first tokens on."""
+    L = 640
+    chunk = min(chunk_of("forward", 1, L, D, 1, N), chunk_of("backward", 1, L, D, 1, N))
+    assert 16 <= chunk <= L // 3, "the case is for several time chunks"
+    v = R.inputs("scan", 1, L, D, N=N, carry=False, full=False, seed=21)
+    gy = v.pop("grad_out")
+    v.pop("grad_final_state")
+    v["dt"].fill_(1.0 if by == "A" else -1.0)
+    v["A"].fill_(-0.05 if by == "A" else 0.05)
+    v["A"][:, 0] = 150 * math.log(2.0) / chunk * float(v["dt"][0, 0, 0])
+    v["x"][:, :-4] = 0
+    gy[:, 4:] = 0
+    y, state, grads = R.with_gradients(R.scan, v, gy, None, softplus=False)
+    d = {k: up(w) for k, w in v.items()}
+    got_y, got_state, ck = S.sig_scan_forward(**d, softplus=False, checkpoint=True)
+    near(got_y, y, "y")
+    near(got_state, state, "state")
+    got = S.sig_scan_backward(**d, softplus=False, grad_out=up(gy), checkpoint=ck)
+    for k in ("x", "dt", "A", "b", "c"):
+        near(got[NAMES[k]], grads[k], "grad " + k)
+
+
+@gpu
+@pytest.mark.parametrize("from_end", [False, True])
+def test_growth_over_a_chunk_of_small_states(from_end):
+    """A state (or, from the end, an adjoint state) of 2^-100 that grows by 2^150 over one chunk: the chunk's factor is more than float32 holds, the
+    result is not."""
+    L, D, N = 640, 70, 16
+    chunk = chunk_of("backward" if from_end else "forward", 1, L, D, 1, N)
+    assert chunk <= L // 3, "the case is for several time chunks"
+    v = R.inputs("scan", 1, L, D, N=N, carry=True, full=False, seed=22)
+    gy, gs = v.pop("grad_out"), v.pop("grad_final_state")
+    v["dt"].zero_()
+    at = slice((L - 1) // chunk * chunk, L) if from_end else slice(0, chunk)
+    v["dt"][:, at] = 1.0
+    v["A"].fill_(150 * math.log(2.0) / (L - at.start if from_end else chunk))
+    v["x"].zero_()
+    gy.zero_()
+    v["initial_state"] *= 2.0 ** (-60 if from_end else -100)
+    gs *= 2.0 ** -100
+    y, state, grads = R.with_gradients(R.scan, v, gy, gs, softplus=False)
+    d = {k: up(w) for k, w in v.items()}
+    got_y, got_state, ck = S.sig_scan_forward(**d, softplus=False, checkpoint=True)
+    near(got_y, y, "y")
+    near(got_state, state, "state")
+    got = S.sig_scan_backward(**d, softplus=False, grad_out=up(gy), checkpoint=ck, grad_final_state=up(gs))
+    for k in ("x", "A", "b", "initial_state"):
+        near(got[NAMES[k]], grads[k], "grad " + k)
