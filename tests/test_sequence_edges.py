@@ -6,7 +6,7 @@ import torch
 
 import paper_2602_24066_amd as S
 from tests import seq_reference as R
-from tests.test_sequence import SCAN_ORDER, gpu, pack, up
+from tests.test_sequence import SCAN_ORDER, close, gpu, pack, up
 
 TOKENS = ("x", "dt", "b", "c", "gate")
 NAMES = dict(x="x", dt="dt", A="A", b="B", c="C", skip="skip", gate="gate", dt_bias="dt_bias", initial_state="initial_state")
@@ -30,7 +30,7 @@ def chunk_of(which, B, L, D, G, N):
 
 
 # ------------------------------------------------------------------------------------------------ states that grow
-# A chunk's growth of 2^150: its exponent, 104 in natural units, is off by a rounding of A, of A log2(e) and of their product, 3 * 2^-24 each
+# A chunk's growth of 2^150: its exponent, 104 in natural units, is off by a rounding of A, of D log2(e) and of their product, 3 * 2^-24 each
 # at the most, and the factor by 104 times that, 1.9e-5; the rest as for other float32 results.
 GROWTH_TOL = 3e-5
 
@@ -93,3 +93,29 @@ def test_growth_over_a_chunk_of_small_states(from_end):
     got = S.sig_scan_backward(**d, softplus=False, grad_out=up(gy), checkpoint=ck, grad_final_state=up(gs))
     for k in ("x", "A", "b", "initial_state"):
         near(got[NAMES[k]], grads[k], "grad " + k)
+
+
+# ------------------------------------------------------------------------------------------------ decay rates
+@gpu
+@pytest.mark.parametrize("B,L,D,N,lengths", [(2, 39, 20, 16, [39, 17]), (1, 700, 70, 4, None), (1, 45, 33, 40, None)])
+def test_the_lowest_decay_rates(B, L, D, N, lengths):
+    """A down to float32's lowest value: a state is forgotten at once, and kept where the step size is zero."""
+    v = R.inputs("scan", B, L, D, N=N, dtype=torch.float32, lengths=lengths, seed=33)
+    gy, gs = v.pop("grad_out"), v.pop("grad_final_state")
+    v["A"][:, 0], v["A"][0, 1], v["A"][1, 1] = torch.finfo(torch.float32).min, -3e38, -2e38
+    y, state, grads = R.with_gradients(R.scan, v, gy, gs)
+    d = {k: up(w) for k, w in v.items()}
+    got_y, got_state, ck = S.sig_scan_forward(**d, checkpoint=True)
+    close(got_y, y, torch.float32, "y")
+    close(got_state, state, torch.float32, "state")
+    got = S.sig_scan_backward(**d, grad_out=up(gy), checkpoint=ck, grad_final_state=up(gs))
+    for k, name in NAMES.items():
+        close(got[name], grads[k], torch.float32, "grad " + name)
+    # steps that add nothing and decay nothing: softplus(-200) is zero in float32, and the step of one token has to agree
+    d["dt"][:, 5] = d["dt"][:, 20] = -200.0
+    first = {k: w[:, :21] if k in TOKENS else w for k, w in d.items() if k != "lengths"}
+    _, one = S.sig_scan_forward(**first)
+    _, held = S.sig_scan_forward(**{k: w[:, :4] if k in TOKENS else w for k, w in first.items()})
+    for i in range(4, 21):
+        S.sig_scan_step(state=held, **{k: w[:, i] if k in TOKENS else w for k, w in first.items() if k != "initial_state"})
+    close(one, held.cpu(), torch.float32, "state by steps")
