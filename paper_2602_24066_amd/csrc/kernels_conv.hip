@@ -230,13 +230,14 @@ __global__ __launch_bounds__(kThreads) void conv_bwd_kernel(sig_conv_args a, Con
                 }
             }
             const int p = t - W + 1;
-            if (p < lowest) return;
-            float o[V];
+            if (p < (kWhole ? 0 : lowest)) return;      // whole groups begin after the initial state's tokens
+            float o[V] = {};
 #pragma unroll
-            for (int i = 0; i < V; i++) {
-                o[i] = 0.0f;
+            for (int k = 0; k < W; k++) {
+                // tokens that are not there or do not count add nothing, whatever their weight is
+                const bool adds = kWhole || (t >= k && t - k < live);
 #pragma unroll
-                for (int k = 0; k < W; k++) o[i] = fmaf(w[k][i], h[W - 1 - k][i], o[i]);
+                for (int i = 0; i < V; i++) o[i] = adds ? fmaf(w[k][i], h[W - 1 - k][i], o[i]) : o[i];
             }
             if (!kWhole && gf && t0 + p < len && t0 + p >= len - (W - 1)) {
                 float v[V];
@@ -244,7 +245,7 @@ __global__ __launch_bounds__(kThreads) void conv_bwd_kernel(sig_conv_args a, Con
 #pragma unroll
                 for (int i = 0; i < V; i++) o[i] += v[i];
             }
-            store<T, V>(p >= 0 ? gx + p * a.D : gi + (W - 1 + p) * a.D, o);
+            store<T, V>(kWhole || p >= 0 ? gx + p * a.D : gi + (W - 1 + p) * a.D, o);
         };
         // groups of U tokens, the next one's loads under way while one is worked on
         constexpr int U = V >= 4 ? 4 : 8;
@@ -252,6 +253,22 @@ __global__ __launch_bounds__(kThreads) void conv_bwd_kernel(sig_conv_args a, Con
         const T *qx = x + t0 * a.x_stride_t, *qg = (const T*)g.grad_y + b * g.gy_stride_b + t0 * g.gy_stride_t + d;
         int left_x = live, left_g = live, t = 0;
         load_group<T, V, U>(nx, qx, a.x_stride_t, left_x), load_group<T, V, U>(ng, qg, g.gy_stride_t, left_g);
+        // incomplete groups, tokens before the first, after the chunk and such as do not count among them
+        auto guarded = [&](auto last, int until) {
+            while (t < until) {
+                load_group<T, V, U>(mx, qx, a.x_stride_t, left_x), load_group<T, V, U>(mg, qg, g.gy_stride_t, left_g);
+#pragma unroll
+                for (int u = 0; u < U; u++) {
+                    if (t + u >= n + W - 1) break;
+                    token(std::false_type(), t + u, nx[u], ng[u]);
+                }
+                t += U;
+                if (decltype(last)::value && t >= until) break;         // nothing waits for loads that nobody needs
+#pragma unroll
+                for (int u = 0; u < U; u++) nx[u] = mx[u], ng[u] = mg[u];
+            }
+        };
+        if (__any(gi != nullptr)) guarded(std::false_type(), W - 1);       // the whole wavefront, whose threads keep step
         for (const int whole = min(n, live); t + U <= whole; t += U) {
             load_group<T, V, U>(mx, qx, a.x_stride_t, left_x), load_group<T, V, U>(mg, qg, g.gy_stride_t, left_g);
 #pragma unroll
@@ -259,17 +276,7 @@ __global__ __launch_bounds__(kThreads) void conv_bwd_kernel(sig_conv_args a, Con
 #pragma unroll
             for (int u = 0; u < U; u++) nx[u] = mx[u], ng[u] = mg[u];
         }
-        for (;;) {                      // incomplete groups, the W - 1 tokens after the chunk and what does not count among them
-            load_group<T, V, U>(mx, qx, a.x_stride_t, left_x), load_group<T, V, U>(mg, qg, g.gy_stride_t, left_g);
-#pragma unroll
-            for (int u = 0; u < U; u++) {
-                if (t + u >= n + W - 1) break;
-                token(std::false_type(), t + u, nx[u], ng[u]);
-            }
-            if ((t += U) >= n + W - 1) break;
-#pragma unroll
-            for (int u = 0; u < U; u++) nx[u] = mx[u], ng[u] = mg[u];
-        }
+        guarded(std::true_type(), n + W - 1);
     } else if (there) {
         float zero[V] = {};
         for (int t = 0; t < n; t++) store<T, V>(gx + t * a.D, zero);

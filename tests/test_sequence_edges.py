@@ -119,3 +119,26 @@ def test_the_lowest_decay_rates(B, L, D, N, lengths):
     for i in range(4, 21):
         S.sig_scan_step(state=held, **{k: w[:, i] if k in TOKENS else w for k, w in first.items() if k != "initial_state"})
     close(one, held.cpu(), torch.float32, "state by steps")
+
+
+# ------------------------------------------------------------------------------------------------ filter weights that are not finite
+@gpu
+@pytest.mark.parametrize("bad", [math.inf, math.nan])
+@pytest.mark.parametrize("t,D,W", [(torch.float32, 8, 4), (torch.float32, 5, 3), (torch.bfloat16, 8, 4), (torch.bfloat16, 5, 8)])
+def test_filter_weights_that_are_not_finite(t, D, W, bad):
+    """They reach the gradients of the tokens that they are multiplied with: none that does not count, and none by way of such a token."""
+    lengths = [50, 20, 0, 3, 17]
+    v = R.inputs("conv", 5, 50, D, W=W, dtype=t, lengths=lengths, seed=31)
+    gy, gs = v.pop("grad_out"), v.pop("grad_final_state")
+    v["weight"][0, 0] = bad
+    v["weight"][D - 1, W - 1] = bad
+    _, _, grads = R.with_gradients(R.conv, v, gy, gs, silu=False)
+    d = {k: up(w) for k, w in v.items()}
+    gx, gw, gb, gi = S.sig_conv_backward(d["x"], d["weight"], up(gy), d["bias"], d["initial_state"], d["lengths"], False, up(gs))
+    for got, want, kind in ((gx, grads["x"], t), (gi, grads["initial_state"], t), (gw, grads["weight"], torch.float32), (gb, grads["bias"], torch.float32)):
+        ok = torch.isfinite(want)
+        assert torch.equal(torch.isfinite(got.cpu()), ok) and torch.equal(torch.isnan(got.cpu()), torch.isnan(want))
+        assert torch.equal(got.cpu()[~ok & ~torch.isnan(want)].double(), want[~ok & ~torch.isnan(want)])
+        close(torch.where(ok, got.cpu(), 0), torch.where(ok, want, 0), kind, "gradient")
+    for i, n in enumerate(lengths):
+        assert not gx[i, n:].any()
