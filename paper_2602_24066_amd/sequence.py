@@ -48,6 +48,8 @@ def _tokens(name, t, shape, dtype, index):
     if (s[-1] != 1 and shape[-1] != 1) or (len(s) > 2 and s[1] >= 1 << 24):      # time strides that the kernels do not reach are copied away
         t = t.contiguous()
         s = t.stride()
+        if len(s) > 2 and (shape[1] <= 1 or t.numel() == 0):                         # such an axis keeps any stride, and nothing is reached by it
+            s = (s[0], 0, *s[2:])
     return t, s
 
 

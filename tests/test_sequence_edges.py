@@ -142,3 +142,25 @@ def test_filter_weights_that_are_not_finite(t, D, W, bad):
         close(torch.where(ok, got.cpu(), 0), torch.where(ok, want, 0), kind, "gradient")
     for i, n in enumerate(lengths):
         assert not gx[i, n:].any()
+
+
+# ------------------------------------------------------------------------------------------------ strides that are not used
+@gpu
+@pytest.mark.parametrize("t", [torch.float32, torch.bfloat16])
+def test_one_token_of_a_time_major_batch(t):
+    """A time axis of length one has a stride that nothing is reached by, however large."""
+    B, D, N = 3, 24, 16
+    v = R.inputs("scan", B, 1, D, N=N, dtype=t, seed=41)
+    gy, gs = up(v.pop("grad_out")), up(v.pop("grad_final_state"))
+    d = {k: up(w) for k, w in v.items()}
+    far = lambda w: w.as_strided(w.shape, (w.stride(0), 1 << 26, *w.stride()[2:]))          # noqa: E731
+    e = {k: far(w) if k in TOKENS else w for k, w in d.items()}
+    w = torch.randn(D, 4, device="cuda")
+
+    def everything(a, g):
+        y, h, ck = S.sig_scan_forward(**a, checkpoint=True)
+        grads = S.sig_scan_backward(**a, grad_out=g, checkpoint=ck, grad_final_state=gs)
+        return [y, h, *grads.values(), *S.sig_conv_forward(a["x"], w, return_state=True), *S.sig_conv_backward(a["x"], w, g)[:2]]
+
+    for p, q in zip(everything(e, far(gy)), everything(d, gy)):
+        assert torch.equal(p, q)
