@@ -40,12 +40,13 @@ def _first(x, dims):
     return x if type(x) is _plain else _torch.empty(0, dtype=t, device=x.device), 1 if t is _b16 else 0
 
 
-def _tokens(name, t, shape, dtype, index):
-    """Checks a tensor of tokens; returns it with a contiguous last axis, and its strides."""
+def _tokens(name, t, shape, dtype, index, most=1 << 24):
+    """Checks a tensor of tokens; returns it with a contiguous last axis, and its strides.  most: time strides from there on are copied away (the scan's
+    kernels do not reach them; the convolution's reach any)."""
     if t.dtype is not dtype or t.get_device() != index or t.shape != shape:
         _refuse(name, t, shape, dtype)
     s = t.stride()
-    if (s[-1] != 1 and shape[-1] != 1) or (len(s) > 2 and s[1] >= 1 << 24):      # time strides that the kernels do not reach are copied away
+    if (s[-1] != 1 and shape[-1] != 1) or (most and len(s) > 2 and s[1] >= most):
         t = t.contiguous()
         s = t.stride()
         if len(s) > 2 and (shape[1] <= 1 or t.numel() == 0):                         # such an axis keeps any stride, and nothing is reached by it
@@ -86,7 +87,7 @@ def _conv_args(x, weight, bias, initial_state, lengths, silu):
     if weight.dim() != 2 or not 1 <= weight.shape[1] <= 8:
         raise ValueError("weight must be [D, W] with W <= 8")
     W = weight.shape[1]
-    x, (sb, st, _) = _tokens("x", x, shape, x.dtype, index)
+    x, (sb, st, _) = _tokens("x", x, shape, x.dtype, index, 0)
     weight = _whole("weight", weight, (D, W), _f32, index)
     pb = pi = pl = 0
     if bias is not None:
@@ -122,7 +123,7 @@ def sig_conv_backward(x, weight, grad_out, bias=None, initial_state=None, length
     make, args, W, kept = _conv_args(x, weight, bias, initial_state, lengths, silu)
     B, L, D = x.shape
     t, index = x.dtype, x.get_device()
-    grad_out, (sb, st, _) = _tokens("grad_out", grad_out, x.shape, t, index)
+    grad_out, (sb, st, _) = _tokens("grad_out", grad_out, x.shape, t, index, 0)
     pf = 0
     if grad_final_state is not None:
         grad_final_state = _whole("grad_final_state", grad_final_state, (B, W - 1, D), t, index)

@@ -164,3 +164,19 @@ def test_one_token_of_a_time_major_batch(t):
 
     for p, q in zip(everything(e, far(gy)), everything(d, gy)):
         assert torch.equal(p, q)
+
+
+# ------------------------------------------------------------------------------------------------ strides that need no copy
+@gpu
+def test_the_convolution_reads_far_tokens_where_they_are():
+    w = torch.randn(24, 4, device="cuda")
+    store = torch.empty((2 << 26) + 24, dtype=torch.bfloat16, device="cuda")
+    x = store.as_strided((1, 3, 24), (1, 1 << 26, 1))
+    x.copy_(torch.randn(1, 3, 24, device="cuda"))
+    near_, counts = x.contiguous(), []
+    for v in (x, near_):
+        before = torch.cuda.memory_stats()["allocation.all.allocated"]
+        y, g = S.sig_conv_forward(v, w), S.sig_conv_backward(v, w, v)
+        counts.append((torch.cuda.memory_stats()["allocation.all.allocated"] - before, y, *g[:2]))
+    assert counts[0][0] == counts[1][0], "as many tensors as for tokens side by side"
+    assert all(torch.equal(p, q) for p, q in zip(counts[0][1:], counts[1][1:]))
