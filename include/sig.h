@@ -442,8 +442,8 @@ typedef struct sig_scan_grads {
 size_t sig_scan_backward_workspace_bytes(const sig_scan_args* args);
 int    sig_scan_backward(const sig_scan_args* args, const sig_scan_grads* grads, const void* checkpoint, size_t checkpoint_bytes,
                          void* workspace, size_t workspace_bytes, void* stream);
-/* One token of every stream: x, dt, gate [B, D], b, c [B, G, N], y [B, D]; state float32 [B, D, N] is updated in place (L, time strides,
- * initial_state and lengths are not looked at). */
+/* One token of every stream: x, dt, gate [B, D], b, c [B, G, N], y [B, D]; state float32 [B, D, N] is updated in place (L, the time strides of
+ * x, dt and gate, initial_state and lengths are not looked at; those of b and c are not used, but keep to their limits). */
 int    sig_scan_step(const sig_scan_args* args, float* state, void* y, void* stream);
 
 /* Global 2-norm over n_tensors tensors and their products with min(1, max_norm / (norm + 1e-6)).  in, out, sizes, in_dtypes, out_dtypes:

@@ -27,27 +27,28 @@ int check_sizes(std::initializer_list<int64_t> sizes)
     return SIG_OK;
 }
 
-int check_conv(const sig_conv_args* a)
+// prompt = false: a call of one token, which does not look at L and at what is there for several
+int check_conv(const sig_conv_args* a, bool prompt = true)
 {
     if (!a || bad_type(a->dtype) || a->D < 1 || a->W < 1) return SIG_EINVAL;
     if (a->W > SIG_MAX_CONV_WIDTH) return SIG_EUNSUPPORTED;
     if (a->silu != 0 && a->silu != 1) return SIG_EINVAL;
-    return check_sizes({a->B, a->L, a->D});
+    return check_sizes({a->B, prompt ? a->L : 1, a->D});
 }
 
-int check_scan(const sig_scan_args* a)
+int check_scan(const sig_scan_args* a, bool prompt = true)
 {
     if (!a || bad_type(a->dtype) || a->D < 1 || a->G < 1 || a->N < 1 || a->D % a->G != 0) return SIG_EINVAL;
     if (a->N > SIG_MAX_SCAN_STATES) return SIG_EUNSUPPORTED;
     if (a->softplus != 0 && a->softplus != 1) return SIG_EINVAL;
     // a launch numbers at least the streams' channels; the kernels count tokens in 32 bits and reach those of a tile by 32-bit offsets
     if (a->B > 0 && a->D > INT32_MAX / a->B) return SIG_ETOOLARGE;
-    if (a->L >= (1 << 30)) return SIG_ETOOLARGE;        // a chunk's end is at most L rounded up to tiles, times two at the most
-    for (int64_t s : {a->x_stride_t, a->dt_stride_t, a->gate_stride_t, a->b_stride_t, a->c_stride_t, a->D})
+    if (prompt && a->L >= (1 << 30)) return SIG_ETOOLARGE;        // a chunk's end is at most L rounded up to tiles, times two at the most
+    for (int64_t s : {prompt ? a->x_stride_t : 0, prompt ? a->dt_stride_t : 0, prompt ? a->gate_stride_t : 0, a->b_stride_t, a->c_stride_t, a->D})
         if (s < 0 || s >= (1 << 24)) return s < 0 ? SIG_EINVAL : SIG_ETOOLARGE;
     for (int64_t s : {a->b_stride_t, a->c_stride_t})           // the kernels tell tokens that count from others by where their rows end
-        if (a->L > 1 && s > 0 && s < a->N) return SIG_EINVAL;
-    return check_sizes({a->B, a->L, a->D, a->N});
+        if (prompt && a->L > 1 && s > 0 && s < a->N) return SIG_EINVAL;
+    return check_sizes({a->B, prompt ? a->L : 1, a->D, a->N});
 }
 
 bool scan_inputs_there(const sig_scan_args& a, bool tokens)
@@ -98,7 +99,7 @@ int sig_conv_backward(const sig_conv_args* a, const void* grad_y, int64_t gy_str
 
 int sig_conv_step(const sig_conv_args* a, void* state, void* y, void* stream)
 {
-    int rc = check_conv(a);
+    int rc = check_conv(a, false);
     if (rc != SIG_OK || a->B == 0) return rc;
     if (!a->weight || !a->x || !y || (a->W > 1 && !state)) return SIG_EINVAL;
     return hip_code(sig::conv_step(*a, state, y, (hipStream_t)stream));
@@ -139,7 +140,7 @@ int sig_scan_backward(const sig_scan_args* a, const sig_scan_grads* g, const voi
 
 int sig_scan_step(const sig_scan_args* a, float* state, void* y, void* stream)
 {
-    int rc = check_scan(a);
+    int rc = check_scan(a, false);
     if (rc != SIG_OK || a->B == 0) return rc;
     if (!scan_inputs_there(*a, true) || !state || !y) return SIG_EINVAL;
     return hip_code(sig::scan_step(*a, state, y, (hipStream_t)stream));

@@ -6,7 +6,7 @@ import torch
 
 import paper_2602_24066_amd as S
 from tests import seq_reference as R
-from tests.test_sequence import SCAN_ORDER, close, gpu, pack, up
+from tests.test_sequence import CONV_ORDER, SCAN_ORDER, close, gpu, pack, up
 
 TOKENS = ("x", "dt", "b", "c", "gate")
 NAMES = dict(x="x", dt="dt", A="A", b="B", c="C", skip="skip", gate="gate", dt_bias="dt_bias", initial_state="initial_state")
@@ -180,3 +180,22 @@ def test_the_convolution_reads_far_tokens_where_they_are():
         counts.append((torch.cuda.memory_stats()["allocation.all.allocated"] - before, y, *g[:2]))
     assert counts[0][0] == counts[1][0], "as many tensors as for tokens side by side"
     assert all(torch.equal(p, q) for p, q in zip(counts[0][1:], counts[1][1:]))
+
+
+# ------------------------------------------------------------------------------------------------ calls of one token
+def scan_args(**change):
+    return pack(dict.fromkeys(SCAN_ORDER, 0) | dict(dtype=0, B=2, L=8, D=4, G=2, N=4, softplus=1, x=4096, dt=4096, b=4096, c=4096, A=4096) | change, SCAN_ORDER)
+
+
+def conv_args(**change):
+    return pack(dict(dtype=0, B=2, L=8, D=4, W=4, silu=1, xb=32, xt=4, x=4096, weight=4096, bias=0, initial=0, lengths=0) | change, CONV_ORDER)
+
+
+@pytest.mark.parametrize("change", [{"L": 1 << 41}, {"L": -5}, {"xt": 1 << 40}, {"xt": -3}])
+def test_calls_of_one_token_do_not_look_at_time(change):
+    lib = S.load_library()
+    assert lib.sig_conv_step(conv_args(**change), 0, 4096, 0) == -1                # for its missing state
+    assert lib.sig_conv_step(conv_args(**change, B=0), 4096, 4096, 0) == 0
+    for more in ({}, {"tt": 1 << 40, "zt": -1}):
+        assert lib.sig_scan_step(scan_args(**change, **more), 0, 4096, 0) == -1
+        assert lib.sig_scan_step(scan_args(**change, **more, B=0), 4096, 4096, 0) == 0
