@@ -44,7 +44,7 @@ extern "C" {
 #define SIG_ENOMEM       (-4)  /* host allocation failed                                                 */
 #define SIG_EWORKSPACE   (-5)  /* workspace / table buffer missing or too small                          */
 #define SIG_EHIP         (-6)  /* a HIP runtime call failed; see sig_last_hip_error()                    */
-#define SIG_ETOOLARGE    (-7)  /* word set exceeds a format limit (see SIG_MAX_*)                        */
+#define SIG_ETOOLARGE    (-7)  /* word set or size exceeds a limit (see SIG_MAX_* and the calls)           */
 #define SIG_ENOTUPLOADED (-8)  /* sig_forward/sig_backward called before sig_wordset_upload              */
 #define SIG_EUNSUPPORTED (-9)  /* word length above what the kernels handle (SIG_MAX_KERNEL_LEN)         */
 #define SIG_ENOTREADY    (-11) /* sig_backward_static: the kernel for this set and batch is not loaded yet */
@@ -369,7 +369,10 @@ int sig_leadlag_backward(const float* grad_out, int64_t B, int64_t n_points, int
  * outputs and gradients of zero and leave states as they are.  Calls only enqueue kernels on `stream`; two calls on the same inputs give
  * the same bits.  B == 0 is a no-op (gradients of parameters are set to zero), L == 0 is allowed: a final state is the initial one.
  * SIG_ETOOLARGE: sizes whose product passes 2^38; for the scan L >= 2^30, B * D >= 2^31, D or a time stride of 2^24 and more (time strides
- * of the scan are not negative, those of b and c with more than one token 0 or at least N).  SIG_EUNSUPPORTED: more filter taps or states than the limits below. */
+ * of the scan are not negative, those of b and c with more than one token 0 or at least N), and a launch of 2^32 threads or more: the scan
+ * takes 256 (up to 8 states), 512 (up to 32) or 1,024 threads for every 64 channels of a group of a stream, its gradient 16 for each of the
+ * D * (N + 2) parameters' sums, its step 4 (up to 16 states), 8 (up to 32) or 16 a channel, the convolution one for 1 to 8 channels (as
+ * aligned) of 16 tokens or more.  SIG_EUNSUPPORTED: more filter taps or states than the limits below. */
 #define SIG_F32  0
 #define SIG_BF16 1
 

@@ -2285,7 +2285,7 @@ const char* sig_strerror(int code)
         case SIG_ENOMEM: return "out of host memory";
         case SIG_EWORKSPACE: return "workspace or table buffer missing or too small";
         case SIG_EHIP: return "HIP runtime error";
-        case SIG_ETOOLARGE: return "word set exceeds a format limit";
+        case SIG_ETOOLARGE: return "word set or a size of the call exceeds a limit";
         case SIG_ENOTUPLOADED: return "word set tables not uploaded";
         case SIG_EUNSUPPORTED: return "not supported for this word set";
         case SIG_EJIT: return "run-time compilation failed";

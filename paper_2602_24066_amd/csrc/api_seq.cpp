@@ -10,7 +10,7 @@ namespace {
 
 constexpr int64_t kMost = (int64_t)1 << 38;       // bound of sizes and of their products: more than the memory holds, and no overflow below
 
-int hip_code(hipError_t e) { return e == hipSuccess ? SIG_OK : sig::record_hip_error(e); }
+int hip_code(hipError_t e) { return e == hipSuccess ? SIG_OK : e == sig::kTooManyThreads ? SIG_ETOOLARGE : sig::record_hip_error(e); }
 
 bool bad_type(int64_t t) { return t != SIG_F32 && t != SIG_BF16; }
 

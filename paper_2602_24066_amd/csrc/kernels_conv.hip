@@ -358,7 +358,7 @@ bool aligned_rows(const void* p, int64_t stride_b, int64_t stride_t, int64_t D, 
 // rows of filter gradients that the gradient's main kernel leaves
 int64_t part_rows(int64_t B, const Split& s) { return s.vecs >= kThreads ? B * s.chunks : (s.threads + kThreads - 1) / kThreads; }
 
-unsigned blocks_for(int64_t threads) { return (unsigned)((threads + kThreads - 1) / kThreads); }
+int64_t blocks_for(int64_t threads) { return (threads + kThreads - 1) / kThreads; }
 
 template <class F> hipError_t with_width(int64_t W, F f)
 {
@@ -383,10 +383,12 @@ template <class T> hipError_t forward(const sig_conv_args& a, T* y, T* fin, hipS
     bool vec = aligned_rows(a.x, a.x_stride_b, a.x_stride_t, a.D, V, sizeof(T)) && aligned_rows(y, 0, 0, a.D, V, sizeof(T)) &&
                aligned_rows(a.initial_state, 0, 0, a.D, V, sizeof(T)) && aligned_rows(fin, 0, 0, a.D, V, sizeof(T));
     Split s = split_time(a.B, a.L, a.D, vec ? V : 1);
+    const int64_t blocks = blocks_for(s.threads);
+    if (!launchable(blocks, kThreads)) return kTooManyThreads;
     return with_width(a.W, [&](auto w) {
         constexpr int W = decltype(w)::value;
-        if (vec) conv_fwd_kernel<T, V, W><<<blocks_for(s.threads), kThreads, 0, stream>>>(a, y, fin, s);
-        else conv_fwd_kernel<T, 1, W><<<blocks_for(s.threads), kThreads, 0, stream>>>(a, y, fin, s);
+        if (vec) conv_fwd_kernel<T, V, W><<<(unsigned)blocks, kThreads, 0, stream>>>(a, y, fin, s);
+        else conv_fwd_kernel<T, 1, W><<<(unsigned)blocks, kThreads, 0, stream>>>(a, y, fin, s);
         return hipGetLastError();
     });
 }
@@ -398,12 +400,14 @@ template <class T> hipError_t backward(const sig_conv_args& a, const ConvGrads& 
                aligned_rows(g.grad_x, 0, 0, a.D, V, sizeof(T)) && aligned_rows(a.initial_state, 0, 0, a.D, V, sizeof(T)) &&
                aligned_rows(g.grad_final, 0, 0, a.D, V, sizeof(T)) && aligned_rows(g.grad_initial, 0, 0, a.D, V, sizeof(T));
     Split s = split_time(a.B, a.L, a.D, vec ? V : 1);
+    const int64_t blocks = blocks_for(s.threads), sums = ((a.W + 1) * a.D + 63) / 64;
+    if (!launchable(blocks, kThreads) || !launchable(sums, 1024)) return kTooManyThreads;
     return with_width(a.W, [&](auto w) {
         constexpr int W = decltype(w)::value;
         if (a.B == 0) {}     // the sums below are zero
-        else if (vec) conv_bwd_kernel<T, V, W><<<blocks_for(s.threads), kThreads, 0, stream>>>(a, g, part, s);
-        else conv_bwd_kernel<T, 1, W><<<blocks_for(s.threads), kThreads, 0, stream>>>(a, g, part, s);
-        conv_bwd_sum_kernel<W><<<(unsigned)(((W + 1) * a.D + 63) / 64), 1024, 0, stream>>>(part, part_rows(a.B, s), a.D, g.grad_weight, g.grad_bias);
+        else if (vec) conv_bwd_kernel<T, V, W><<<(unsigned)blocks, kThreads, 0, stream>>>(a, g, part, s);
+        else conv_bwd_kernel<T, 1, W><<<(unsigned)blocks, kThreads, 0, stream>>>(a, g, part, s);
+        conv_bwd_sum_kernel<W><<<(unsigned)sums, 1024, 0, stream>>>(part, part_rows(a.B, s), a.D, g.grad_weight, g.grad_bias);
         return hipGetLastError();
     });
 }
@@ -412,11 +416,12 @@ template <class T> hipError_t step(const sig_conv_args& a, T* state, T* y, hipSt
 {
     constexpr int V = wide((T*)nullptr) / 4;
     bool vec = aligned_rows(a.x, a.x_stride_b, 0, a.D, V, sizeof(T)) && aligned_rows(state, 0, 0, a.D, V, sizeof(T)) && aligned_rows(y, 0, 0, a.D, V, sizeof(T));
-    int64_t vecs = vec ? a.D / V : a.D;
+    const int64_t vecs = vec ? a.D / V : a.D, blocks = blocks_for(a.B * vecs);
+    if (!launchable(blocks, kThreads)) return kTooManyThreads;
     return with_width(a.W, [&](auto w) {
         constexpr int W = decltype(w)::value;
-        if (vec) conv_step_kernel<T, V, W><<<blocks_for(a.B * vecs), kThreads, 0, stream>>>(a, state, y, vecs);
-        else conv_step_kernel<T, 1, W><<<blocks_for(a.B * vecs), kThreads, 0, stream>>>(a, state, y, vecs);
+        if (vec) conv_step_kernel<T, V, W><<<(unsigned)blocks, kThreads, 0, stream>>>(a, state, y, vecs);
+        else conv_step_kernel<T, 1, W><<<(unsigned)blocks, kThreads, 0, stream>>>(a, state, y, vecs);
         return hipGetLastError();
     });
 }

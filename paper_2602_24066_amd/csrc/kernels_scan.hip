@@ -112,7 +112,7 @@ struct Blocks {
     unsigned runs;       // workgroups for the channels of a group
     unsigned chunks;
     int chunk;           // tokens of a time chunk, a multiple of kTile
-    unsigned total;
+    int64_t total;
 };
 
 // Time chunks: where a launch has few workgroups, a first kernel runs every chunk from a state of zero and leaves its last state and the sum
@@ -843,7 +843,6 @@ template <class T, class Sh, bool kWide> __global__ __launch_bounds__(kThreads) 
     if (q == 0) y[at] = from_float<T>(o);
 }
 
-unsigned blocks_for(int64_t threads) { return (unsigned)((threads + kThreads - 1) / kThreads); }
 int64_t tiles_of(const sig_scan_args& a) { return (a.L + kTile - 1) / kTile; }
 
 // four lanes a channel up to 16 states, four states a lane beyond
@@ -902,7 +901,7 @@ Blocks blocks_of(const sig_scan_args& a, int resident, double second)
     }
     bl.chunk = (int)(best * kTile);
     bl.chunks = (unsigned)((tiles + best - 1) / best);
-    bl.total = (unsigned)(rows * bl.chunks);
+    bl.total = rows * bl.chunks;
     return bl;
 }
 
@@ -948,13 +947,14 @@ hipError_t scan_forward(const sig_scan_args& a, void* y, float* final_state, flo
             using T = decltype(t);
             using Gr = decltype(gr);
             constexpr int lds = forward_lds(Gr::W);
-            if (bl.chunks > 1) scan_fwd_kernel<T, Gr, false, false><<<bl.total, Gr::W * 64, forward_lds(0), stream>>>(a, bl, cs, nullptr, nullptr, nullptr);
+            if (!launchable(bl.total, Gr::W * 64)) return kTooManyThreads;
+            if (bl.chunks > 1) scan_fwd_kernel<T, Gr, false, false><<<(unsigned)bl.total, Gr::W * 64, forward_lds(0), stream>>>(a, bl, cs, nullptr, nullptr, nullptr);
             auto launch = [&](auto kernel) {
                 if (lds > 65536) {
                     hipError_t e = ensure_dynamic_lds((const void*)kernel, lds);
                     if (e != hipSuccess) return e;
                 }
-                kernel<<<bl.total, Gr::W * 64, lds, stream>>>(a, bl, cs, (T*)y, final_state, checkpoint);
+                kernel<<<(unsigned)bl.total, Gr::W * 64, lds, stream>>>(a, bl, cs, (T*)y, final_state, checkpoint);
                 return hipGetLastError();
             };
             return checkpoint ? launch(scan_fwd_kernel<T, Gr, true, true>) : launch(scan_fwd_kernel<T, Gr, true, false>);
@@ -974,17 +974,18 @@ hipError_t scan_backward(const sig_scan_args& a, const sig_scan_grads& g, const 
             using T = decltype(t);
             using Gr = decltype(gr);
             constexpr int lds = backward_lds(Gr::W, Gr::S);
+            const unsigned params = (unsigned)((a.D * (a.N + 2) + 63) / 64);
+            const int64_t sums = a.B * tiles_of(a) * a.G * Gr::W * (Gr::S / 2);        // wavefronts
+            const unsigned others = (unsigned)std::min<int64_t>(1 << 20, (sums + kSumThreads / 64 - 1) / (kSumThreads / 64));
+            if (!launchable(bl.total, Gr::W * 64) || !launchable((int64_t)params + others, kSumThreads)) return kTooManyThreads;
             if (lds > 65536) {
                 hipError_t e = ensure_dynamic_lds((const void*)scan_bwd_kernel<T, Gr, true>, lds);
                 if (e != hipSuccess) return e;
             }
             if (a.B > 0) {
-                if (bl.chunks > 1) scan_bwd_kernel<T, Gr, false><<<bl.total, Gr::W * 64, backward_lds(0, 0), stream>>>(a, g, bl, cs, nullptr, parts);
-                scan_bwd_kernel<T, Gr, true><<<bl.total, Gr::W * 64, lds, stream>>>(a, g, bl, cs, checkpoint, parts);
+                if (bl.chunks > 1) scan_bwd_kernel<T, Gr, false><<<(unsigned)bl.total, Gr::W * 64, backward_lds(0, 0), stream>>>(a, g, bl, cs, nullptr, parts);
+                scan_bwd_kernel<T, Gr, true><<<(unsigned)bl.total, Gr::W * 64, lds, stream>>>(a, g, bl, cs, checkpoint, parts);
             }
-            const unsigned params = (unsigned)((a.D * (a.N + 2) + 63) / 64);
-            const int64_t sums = a.B * tiles_of(a) * a.G * Gr::W * (Gr::S / 2);        // wavefronts
-            const unsigned others = (unsigned)std::min<int64_t>(1 << 20, (sums + kSumThreads / 64 - 1) / (kSumThreads / 64));
             scan_bwd_sums_kernel<T, Gr><<<params + others, kSumThreads, 0, stream>>>(a, bl, parts, a.B * bl.chunks, params, (T*)g.grad_b, (T*)g.grad_c, g.grad_A, g.grad_skip, g.grad_dt_bias);
             return hipGetLastError();
         });
@@ -998,9 +999,10 @@ hipError_t scan_step(const sig_scan_args& a, float* state, void* y, hipStream_t 
             using T = decltype(t);
             using Sh = decltype(sh);
             const bool wide = a.N == Sh::Q * Sh::S && (((uintptr_t)state | (uintptr_t)a.A) & (Sh::S * 4 - 1)) == 0;
-            const unsigned blocks = blocks_for(a.B * a.D * Sh::Q);
-            if (wide) scan_step_kernel<T, Sh, true><<<blocks, kThreads, 0, stream>>>(a, state, (T*)y);
-            else scan_step_kernel<T, Sh, false><<<blocks, kThreads, 0, stream>>>(a, state, (T*)y);
+            const int64_t blocks = (a.B * a.D * Sh::Q + kThreads - 1) / kThreads;
+            if (!launchable(blocks, kThreads)) return kTooManyThreads;
+            if (wide) scan_step_kernel<T, Sh, true><<<(unsigned)blocks, kThreads, 0, stream>>>(a, state, (T*)y);
+            else scan_step_kernel<T, Sh, false><<<(unsigned)blocks, kThreads, 0, stream>>>(a, state, (T*)y);
             return hipGetLastError();
         });
     });

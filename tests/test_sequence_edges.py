@@ -1,4 +1,5 @@
 """Sequence operators at the edges of what their contract allows, against the plain 64-bit implementations."""
+import ctypes
 import math
 
 import pytest
@@ -199,3 +200,36 @@ def test_calls_of_one_token_do_not_look_at_time(change):
     for more in ({}, {"tt": 1 << 40, "zt": -1}):
         assert lib.sig_scan_step(scan_args(**change, **more), 0, 4096, 0) == -1
         assert lib.sig_scan_step(scan_args(**change, **more, B=0), 4096, 4096, 0) == 0
+
+
+# ------------------------------------------------------------------------------------------------ launches beyond what the hardware numbers
+@pytest.mark.parametrize("change", [
+    dict(B=4096, D=2048, G=2048, N=16),              # 2^23 workgroups of 512 threads
+    dict(B=1 << 24, D=64, G=1, N=8),                 # 2^24 of 256
+    dict(B=1 << 22, D=16, G=1, N=64),                # 2^22 of 1,024
+    dict(B=1, D=(1 << 24) - 1, G=1, N=16, L=0),      # 2^28 sums of parameters' gradients of 16 threads (the gradient alone)
+])
+def test_scan_launches_of_too_many_threads_are_refused(change):
+    lib = S.load_library()
+    args, big = scan_args(**{"L": 1, **change}), 1 << 60
+    if "L" not in change:
+        assert lib.sig_scan_forward(args, 4096, 0, 0, 0, 4096, big, 0) == -7
+    grads = (ctypes.c_int64 * 13)(*[4096] * 13)
+    grads[0] = grads[1] = 0
+    assert lib.sig_scan_backward(args, grads, 4096, big, 4096, big, 0) == -7
+
+
+@pytest.mark.parametrize("B,D,N", [(1 << 20, 1 << 10, 1), (1 << 20, 1 << 10, 16), (1 << 15, 1 << 14, 17), (1 << 15, 1 << 13, 64)])
+def test_scan_steps_of_too_many_threads_are_refused(B, D, N):
+    assert S.load_library().sig_scan_step(scan_args(B=B, D=D, G=1, N=N), 4096, 4096, 0) == -7
+
+
+@pytest.mark.parametrize("change,aligned", [(dict(B=1 << 16, L=1, D=1 << 16), False), (dict(B=1 << 17, L=1, D=1 << 17), True), (dict(B=1, L=1, D=1 << 25, W=8), None)])
+def test_conv_launches_of_too_many_threads_are_refused(change, aligned):
+    """The third is one of the filter's sums, in the gradient alone."""
+    lib = S.load_library()
+    args = conv_args(**change, xb=0, xt=0, x=4096 if aligned else 4100)
+    if aligned is not None:
+        assert lib.sig_conv_forward(args, 4096, 0, 0) == -7
+        assert lib.sig_conv_step(args, 4096, 4096, 0) == -7
+    assert lib.sig_conv_backward(args, 4096, 0, 0, 0, 4096, 4096, 0, 0, 4096, 1 << 60, 0) == -7
