@@ -249,8 +249,8 @@ def sig_scan_backward(x, dt, A, b, c, grad_out, checkpoint, skip=None, gate=None
         raise ValueError("checkpoint must be the tensor that sig_scan_forward returned")
     tokens = lambda: make.new_empty((B, L, D))                                              # noqa: E731
     params = lambda *shape: make.new_empty(shape, dtype=_f32)                               # noqa: E731
-    of_bc = (B, L, N) if b.dim() == 3 else (B, L, G, N)
-    g = {"x": tokens(), "dt": tokens(), "A": params(D, N), "B": make.new_empty(of_bc), "C": make.new_empty(of_bc),
+    of_bc = lambda v: (B, L, N) if v.dim() == 3 else (B, L, G, N)                           # noqa: E731
+    g = {"x": tokens(), "dt": tokens(), "A": params(D, N), "B": make.new_empty(of_bc(b)), "C": make.new_empty(of_bc(c)),
          "skip": params(D) if skip is not None else None, "gate": tokens() if gate is not None else None,
          "dt_bias": params(D) if dt_bias is not None else None, "initial_state": params(B, D, N) if initial_state is not None else None}
     ptr = lambda v: 0 if v is None else v.data_ptr()                                        # noqa: E731

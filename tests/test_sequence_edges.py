@@ -233,3 +233,17 @@ def test_conv_launches_of_too_many_threads_are_refused(change, aligned):
         assert lib.sig_conv_forward(args, 4096, 0, 0) == -7
         assert lib.sig_conv_step(args, 4096, 4096, 0) == -7
     assert lib.sig_conv_backward(args, 4096, 0, 0, 0, 4096, 4096, 0, 0, 4096, 1 << 60, 0) == -7
+
+
+# ------------------------------------------------------------------------------------------------ shapes of gradients
+@gpu
+@pytest.mark.parametrize("b_group,c_group", [(False, True), (True, False)])
+def test_gradients_have_the_shapes_of_their_inputs(b_group, c_group):
+    x, A = torch.randn(2, 9, 8, device="cuda"), -torch.ones(8, 4, device="cuda")
+    b, c = torch.randn(2, 9, 4, device="cuda"), torch.randn(2, 9, 4, device="cuda")
+    ck = S.sig_scan_forward(x, x, A, b, c, checkpoint=True)[2]
+    want = S.sig_scan_backward(x, x, A, b, c, x, ck)
+    b, c = b.unsqueeze(2) if b_group else b, c.unsqueeze(2) if c_group else c
+    got = S.sig_scan_backward(x, x, A, b, c, x, ck)
+    assert got["B"].shape == b.shape and got["C"].shape == c.shape
+    assert torch.equal(got["B"].reshape(2, 9, 4), want["B"]) and torch.equal(got["C"].reshape(2, 9, 4), want["C"])
