@@ -4,6 +4,7 @@
 
 #include <cstdint>
 #include <mutex>
+#include <new>
 #include <set>
 #include <utility>
 
@@ -22,8 +23,11 @@ inline hipError_t ensure_dynamic_lds(const void* kernel, int bytes)
     std::lock_guard<std::mutex> lock(m);
     if (done.count({dev, kernel})) return hipSuccess;
     e = hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
-    if (e == hipSuccess) done.insert({dev, kernel});
-    return e;
+    if (e != hipSuccess) return e;
+    try {
+        done.insert({dev, kernel});
+    } catch (const std::bad_alloc&) { }      // not remembered: the next call sets it again
+    return hipSuccess;
 }
 
 struct GenericArgs {

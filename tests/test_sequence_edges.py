@@ -1,6 +1,9 @@
 """Sequence operators at the edges of what their contract allows, against the plain 64-bit implementations."""
 import ctypes
 import math
+import os
+import shutil
+import subprocess
 
 import pytest
 import torch
@@ -247,3 +250,37 @@ def test_gradients_have_the_shapes_of_their_inputs(b_group, c_group):
     got = S.sig_scan_backward(x, x, A, b, c, x, ck)
     assert got["B"].shape == b.shape and got["C"].shape == c.shape
     assert torch.equal(got["B"].reshape(2, 9, 4), want["B"]) and torch.equal(got["C"].reshape(2, 9, 4), want["C"])
+
+
+# ------------------------------------------------------------------------------------------------ host memory that runs out
+NO_MEMORY = r"""
+#include <cstdlib>
+#include <new>
+static bool none = false;
+void* operator new(std::size_t n) { if (none) throw std::bad_alloc(); if (void* p = std::malloc(n ? n : 1)) return p; throw std::bad_alloc(); }
+void operator delete(void* p) noexcept { std::free(p); }
+void operator delete(void* p, std::size_t) noexcept { std::free(p); }
+#include "kernels.hpp"
+static int set = 0;
+extern "C" hipError_t hipGetDevice(int* d) { *d = 0; return hipSuccess; }
+extern "C" hipError_t hipFuncSetAttribute(const void*, hipFuncAttribute, int) { set++; return hipSuccess; }
+int main()
+{
+    int k = 0;
+    none = true;
+    if (sig::ensure_dynamic_lds(&k, 100000) != hipSuccess || set != 1) return 1;
+    none = false;
+    if (sig::ensure_dynamic_lds(&k, 100000) != hipSuccess || set != 2) return 2;     // not remembered then, so set again
+    if (sig::ensure_dynamic_lds(&k, 100000) != hipSuccess || set != 2) return 3;
+    return 0;
+}
+"""
+
+
+def test_a_lack_of_host_memory_does_not_leave_a_launch_as_an_exception(tmp_path):
+    gxx, csrc = shutil.which("g++"), os.path.join(os.path.dirname(S.lib_path()), "csrc")
+    if gxx is None or not os.path.isdir("/opt/rocm/include"):
+        pytest.skip("no g++ or no HIP headers")
+    (tmp_path / "a.cpp").write_text(NO_MEMORY)
+    subprocess.run([gxx, "-std=c++17", "-D__HIP_PLATFORM_AMD__", "-I", csrc, "-I", "/opt/rocm/include", str(tmp_path / "a.cpp"), "-o", str(tmp_path / "a")], check=True)
+    assert subprocess.run([str(tmp_path / "a")]).returncode == 0
