@@ -10,7 +10,7 @@ import torch
 
 import paper_2602_24066_amd as S
 from tests import seq_reference as R
-from tests.test_sequence import CONV_ORDER, SCAN_ORDER, close, gpu, pack, up
+from tests.test_sequence import CONV_ORDER, SCAN_ORDER, close, gpu, pack, poison, up
 
 TOKENS = ("x", "dt", "b", "c", "gate")
 NAMES = dict(x="x", dt="dt", A="A", b="B", c="C", skip="skip", gate="gate", dt_bias="dt_bias", initial_state="initial_state")
@@ -284,3 +284,138 @@ def test_a_lack_of_host_memory_does_not_leave_a_launch_as_an_exception(tmp_path)
     (tmp_path / "a.cpp").write_text(NO_MEMORY)
     subprocess.run([gxx, "-std=c++17", "-D__HIP_PLATFORM_AMD__", "-I", csrc, "-I", "/opt/rocm/include", str(tmp_path / "a.cpp"), "-o", str(tmp_path / "a")], check=True)
     assert subprocess.run([str(tmp_path / "a")]).returncode == 0
+
+
+# ------------------------------------------------------------------------------------------------ forms that the sizes and the alignment choose
+@gpu
+@pytest.mark.parametrize("B,L,D,W,t,lengths", [
+    (3, 40, 333, 3, "f32", [40, 0, 23]),             # channels that no vector access fits, a thread each: more than a workgroup's
+    (2, 40, 1024, 4, "bf16", [40, 33]),              # as many groups of four as a workgroup has threads
+    (2, 40, 512, 4, "f32", [17, 40]),                # and of two
+    (2, 70, 258, 4, "bf16", None),
+    (2, 40, 1554, 2, "bf16", [1, 39]),
+    (1, 33, 2048, 8, "f32", None),
+])
+def test_convolutions_over_many_channels(B, L, D, W, t, lengths):
+    t = torch.float32 if t == "f32" else torch.bfloat16
+    v = R.inputs("conv", B, L, D, W=W, dtype=t, lengths=lengths, seed=D)
+    gy, gs = v.pop("grad_out"), v.pop("grad_final_state")
+    y, state, grads = R.with_gradients(R.conv, v, gy, gs)
+    d = {k: up(w) for k, w in (poison(v, ["x"]) if lengths else v).items()}
+    got_y, got_state = S.sig_conv_forward(**d, return_state=True)
+    close(got_y, y, t, "y")
+    close(got_state, state, t, "state")
+    got = S.sig_conv_backward(d["x"], d["weight"], up(gy), d["bias"], d["initial_state"], d["lengths"], True, up(gs))
+    for k, g in zip(("x", "weight", "bias", "initial_state"), got):
+        close(g, grads[k], t if k in ("x", "initial_state") else torch.float32, "grad " + k)
+
+
+@gpu
+@pytest.mark.parametrize("B,L,D,G,N,t,lengths", [
+    (2, 400, 70, 1, 40, "f32", [400, 290]),          # several time chunks, more than 32 states, more channels than a wavefront has lanes
+    (2, 330, 130, 2, 64, "bf16", [330, 17]),
+    (1, 500, 66, 1, 24, "f32", [499]),
+])
+def test_scans_of_many_states_in_time_chunks(B, L, D, G, N, t, lengths):
+    assert chunk_of("backward", B, L, D, G, N) < L
+    t = torch.float32 if t == "f32" else torch.bfloat16
+    v = R.inputs("scan", B, L, D, G=G, N=N, dtype=t, lengths=lengths, seed=N)
+    gy, gs = v.pop("grad_out"), v.pop("grad_final_state")
+    y, state, grads = R.with_gradients(R.scan, v, gy, gs)
+    hidden = poison({**v, "gy": gy}, [*TOKENS, "gy"])
+    gy = up(hidden.pop("gy"))
+    d = {k: up(w) for k, w in hidden.items()}
+    got_y, got_state, ck = S.sig_scan_forward(**d, checkpoint=True)
+    close(got_y, y, t, "y")
+    close(got_state, state, torch.float32, "state")
+    got = S.sig_scan_backward(**d, grad_out=gy, checkpoint=ck, grad_final_state=up(gs))
+    for k, name in NAMES.items():
+        close(got[name], grads[k], t if k in TOKENS else torch.float32, "grad " + name)
+
+
+@gpu
+@pytest.mark.parametrize("t", [torch.float32, torch.bfloat16])
+def test_time_strides_just_within_the_kernels_reach(t):
+    """Rows 2^24 - 8 elements apart, three tiles of them: a tile's last row lies nearly 2^30 bytes from its first."""
+    L, D, N, far = 40, 24, 16, (1 << 24) - 8
+    store = torch.empty((L - 1) * far + 4 * D, dtype=t, device="cuda")
+    v = R.inputs("scan", 1, L, D, N=N, dtype=t, lengths=[L - 3], seed=51)
+    gy, gs = up(v.pop("grad_out")), up(v.pop("grad_final_state"))
+    d = {k: up(w) for k, w in v.items()}
+    e, at = dict(d), 0
+    for k in ("x", "gate", "b", "c"):                # the rows of all lie behind one another
+        w = d[k]
+        e[k] = store.as_strided(w.shape, (1, far, *w.stride()[2:]), at)
+        e[k].copy_(w)
+        at += w[0, 0].numel()
+
+    def everything(a):
+        y, h, ck = S.sig_scan_forward(**a, checkpoint=True)
+        return [y, h, *S.sig_scan_backward(**a, grad_out=gy, checkpoint=ck, grad_final_state=gs).values()]
+
+    for p, q in zip(everything(e), everything(d)):
+        assert torch.equal(p, q)
+
+
+@gpu
+@pytest.mark.parametrize("full", [True, False])
+def test_gradients_of_the_step_sizes_at_special_values(full):
+    """States that are forgotten at once, kept and grow; step sizes that vanish."""
+    v = R.inputs("scan", 1, 40, 16, dtype=torch.float32, full=full, seed=11)
+    gy, gs = v.pop("grad_out"), v.pop("grad_final_state")
+    v["A"][:, 0], v["A"][:, 1], v["A"][:, 2] = -1e30, 0.0, 0.05
+    v["dt"][0, 5], v["dt"][0, 6] = (-200.0, -30.0) if full else (0.0, 1e-13)
+    _, _, grads = R.with_gradients(R.scan, v, gy, gs, softplus=full)
+    d = {k: up(w) for k, w in v.items()}
+    if not full:                                     # A times a state that is kept is 1e30 at token 5: the others are looked at alone
+        grads["dt"][0, 5] = 0
+    ck = S.sig_scan_forward(**d, softplus=full, checkpoint=True)[2]
+    got = S.sig_scan_backward(**d, softplus=full, grad_out=up(gy), checkpoint=ck, grad_final_state=up(gs))
+    if not full:
+        got["dt"][0, 5] = 0
+    for k in ("dt", "A", "dt_bias"):
+        if v[k] is not None:
+            close(got[k], grads[k], torch.float32, "grad " + k)
+
+
+@gpu
+@pytest.mark.parametrize("max_norm", [0.25, 1e9])
+@pytest.mark.parametrize("off", [0, 1, 3])
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+def test_clip_into_tensors_of_either_type_and_alignment(kind, off, max_norm):
+    """The products of either type into bfloat16 and float32, from and to addresses that agree or not."""
+    g = torch.Generator().manual_seed(off)
+    t = torch.float32 if kind == "f32" else torch.bfloat16
+    flat = up(torch.randn(70000, generator=g).to(t))
+    grads = [flat[1:10], flat[off + 16:off + 16 + 33 * 41].view(33, 41), flat[2001:2001 + 60000]]
+    total = math.sqrt(sum(float(w.double().square().sum()) for w in grads))
+    want = [w.double().cpu() * min(1.0, max_norm / (total + 1e-6)) for w in grads]
+    for o in (torch.float32, torch.bfloat16):
+        store = torch.full((70000,), 7.0, device="cuda", dtype=o)
+        outs = [store[off:off + 9], store[off + 30:off + 30 + 33 * 41].view(33, 41), store[5002 + off:5002 + off + 60000]]
+        norm = S.sig_grad_clip(grads, max_norm, out=outs)
+        assert abs(float(norm) - total) <= 1e-6 * total
+        for p, q in zip(outs, want):
+            close(p, q, o, "products")
+        left = torch.ones(70000, dtype=torch.bool, device="cuda")
+        for p in outs:
+            left[p.storage_offset():p.storage_offset() + p.numel()] = False
+        assert (store[left] == 7.0).all()
+
+
+@gpu
+def test_clip_of_more_than_the_cache_holds():
+    """71 million elements, 284 MB of products: they are stored past the cache, and a workgroup takes more elements than it does of fewer."""
+    n = 71_000_003
+    big = torch.randn(n, device="cuda", generator=torch.Generator(device="cuda").manual_seed(3))
+    grads = [big[1:n - 1], torch.randn(77, device="cuda").bfloat16()]
+    total = float(torch.sqrt(sum(w.double().square().sum() for w in grads)))
+    want = [w.double() * (1.0 / (total + 1e-6)) for w in grads]
+    outs = [torch.empty(n - 2, device="cuda"), torch.empty(77, device="cuda")]
+    for into in (outs, None):
+        norm = S.sig_grad_clip(grads, 1.0, out=into)
+        assert abs(float(norm) - total) <= 1e-6 * total
+        for p, q in zip(into or grads, want):
+            off = (p.double() - q).abs()
+            assert float((off - q.abs() * (2.0 ** -22 if p.dtype is torch.float32 else 2.0 ** -8)).max()) <= 0
+    assert not torch.isnan(big).any()
