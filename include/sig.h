@@ -452,7 +452,8 @@ int    sig_scan_step(const sig_scan_args* args, float* state, void* y, void* str
 /* Global 2-norm over n_tensors tensors and their products with min(1, max_norm / (norm + 1e-6)).  in, out, sizes, in_dtypes, out_dtypes:
  * host arrays of n_tensors entries (device pointers, elements, SIG_F32 / SIG_BF16), read before the call returns; tensors are
  * contiguous, out[k] may be in[k] (the same type then) and overlaps nothing else.  norm: device float32.  Squares are summed in float64.
- * A NaN among the inputs makes norm and all outputs NaN; an infinity makes the norm infinite, the infinite entries NaN and the others 0. */
+ * A NaN among the inputs makes norm and all outputs NaN; an infinity makes the norm infinite, the infinite entries NaN and the others 0 (NaN
+ * where max_norm is infinite as well); a norm of finite inputs that float32 does not hold is infinite, and the outputs are 0. */
 size_t sig_grad_clip_workspace_bytes(int64_t n_tensors, const int64_t* sizes);
 int    sig_grad_clip(int64_t n_tensors, const void* const* in, void* const* out, const int64_t* sizes, const int64_t* in_dtypes,
                      const int64_t* out_dtypes, float max_norm, float* norm, void* workspace, size_t workspace_bytes, void* stream);

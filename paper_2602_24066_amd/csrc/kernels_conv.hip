@@ -186,8 +186,8 @@ __global__ __launch_bounds__(kThreads) void conv_fwd_kernel(sig_conv_args a, T* 
 
 // The gradient walks forward as well: at token t it has s_t from the window of x, g_t from it and the upstream gradient, and with the
 // last W of them the gradient of token t - W + 1.  A chunk goes W - 1 tokens past its end for the gradients of its last tokens.
-// 8 x 2048 x 2048: 52 us in bf16, 3.9 TB/s, where s_t, the slope and three products of W taps make the vector instructions count, and 89 us in
-// float32, 4.5 TB/s.  Loads of the next group behind a condition: 60 and 101 us (waits for all that is under way, stores among it).
+// 8 x 2048 x 2048: 53 us in bf16, 3.8 TB/s, where s_t, the slope and three products of W taps make the vector instructions count, and 89 us in
+// float32, 4.5 TB/s.  Loads of the next group behind a condition: 15 % more time (waits for all that is under way, stores among it).
 template <class T, int V, int W>
 __global__ __launch_bounds__(kThreads) void conv_bwd_kernel(sig_conv_args a, ConvGrads g, float* part, Split s)
 {
@@ -287,7 +287,7 @@ __global__ __launch_bounds__(kThreads) void conv_bwd_kernel(sig_conv_args a, Con
         }
     }
     // The sums of channels that several threads of the workgroup share are added up here, in their order: otherwise the second kernel would
-    // add up a row for every 16 tokens where channels are few (gradient of 64 x 4096 x 64 in bf16: 119 us, 42 with the sums here).
+    // add up a row for every 16 tokens where channels are few (gradient of 64 x 4096 x 64 in bf16: a third of the time with the sums here, now 32 us).
     if (s.vecs >= kThreads) {
         if (!there) return;
         part += row * (W + 1) * a.D + d;

@@ -27,7 +27,7 @@ constexpr int kTile = kScanTile;
 // stores the outputs of the tokens that it prepared.  B and C of a tile lie across the 16 lanes of a row, 16 / S tokens in a
 // register, and reach the products as row broadcasts of the instruction itself: no LDS, no unpacking a token.
 // What bounds it: vector instructions, of which a state and token needs an exponential (3.5 ns on a SIMD) and four others (1.1 to 2.2 ns).
-// 8 x 4096 x 2048 bf16, 16 states: 387 us, 2.8e12 states a second; the bytes alone would take 105 us.
+// 8 x 4096 x 2048 bf16, 16 states: 380 us, 2.8e12 states a second; the bytes alone would take 105 us.
 template <int S_, int W_> struct Group { static constexpr int S = S_, W = W_; };
 
 template <int I, int N, class F> __device__ __forceinline__ void unrolled(F f)
@@ -92,7 +92,8 @@ template <class T> __device__ __forceinline__ void buffer_store(Buffer r, unsign
 template <class T> __device__ __forceinline__ void forth(T*& p, unsigned bytes) { p = (T*)((const char*)p + bytes); }
 // Keeps a row pointer in its own two scalar registers from tile to tile: the compiler otherwise makes it the sum of a start and an offset shared with
 // others, more values than there are registers, and moves them to and from vector registers.  The backward pass of 16 states takes an eighth
-// less with it; that of more than 16 spills vector registers then, and the forward pass gains nothing (large case 379 -> 403 us).
+// less with it (a hundred other scalars are still moved); that of more than 16 spills more vector registers then, and the forward pass
+// loses (large case 380 -> 403 us).
 template <class T> __device__ __forceinline__ void held(T*& p) { asm volatile("" : "+s"(p)); }
 constexpr unsigned kNowhere = 0xfffffffcu;
 // at, or kNowhere: a selection that the compiler does not turn into branches around two accesses (worth 1 % of the backward pass)
@@ -210,7 +211,7 @@ __global__ __launch_bounds__(Gr::W * 64, Gr::S == 4 ? 4 : 2) void scan_fwd_kerne
     const unsigned y_row = (unsigned)a.D * E;
     // Where the lane's state and tokens of B and C lie in a tile.  The buffers end with the row of the last token that counts (rows do not overlap, or
     // are all the same): no selection a lane, which the compiler makes branches of.  A tile is one block of instructions then, with or without
-    // states to keep (kStates): 383 us for 414 in the large case, 378 for 433 with states.
+    // states to keep (kStates): 7 % less time in the large case, 13 % less with states.
     unsigned b_at[KB], c_at[KB];
 #pragma unroll
     for (int j = 0; j < KB; j++) {
@@ -388,8 +389,10 @@ __global__ __launch_bounds__(Gr::W * 64, Gr::S == 4 ? 4 : 2) void scan_fwd_kerne
 // barriers a tile.  dB and dC are sums over channels, that is over lanes: a reduction that halves the number of values at each of its
 // six steps leaves the 64 sums of 16 tokens (2 states, dB and dC) one to a lane in 129 instructions, where a sum to all lanes would take six for
 // each; the workgroups' sums are added by a second kernel in their order, no atomics.
-// What bounds it: vector instructions, 25 a state and token (two exponentials with four states a wavefront, else one), on SIMDs that are busy
-// 70 % of the time with two wavefronts each.  8 x 2048 x 2048 bf16, 16 states: 480 us, 1.12e12 states a second; the bytes alone 105 us.
+// What bounds it: vector instructions, 24 a state and token (two exponentials with four states a wavefront, else one), on SIMDs that are busy
+// 76 % of the time with two wavefronts each.  8 x 2048 x 2048 bf16, 16 states: 492 us, 1.1e12 states a second; the bytes (seven tensors of
+// tokens, the checkpoint, the workgroups' sums, 0.67 GB) alone 131 us.  More than 32 states: 270 of the registers that a lane wants go to
+// memory, 5.6 ms where 32 states take 0.94.
 template <int K, int S> __device__ __forceinline__ void add_broadcast(float (&o)[S], float r, float v)      // o[s] += r[K + s] v
 {
     static_assert(S == 2 || S == 4, "states of a wavefront");
@@ -450,7 +453,7 @@ __global__ __launch_bounds__(Gr::W * 64, Gr::W > 8 ? 4 : 2) void scan_bwd_kernel
     extern __shared__ float lds[];
     float4(*in)[kTile / 4][64] = (float4(*)[kTile / 4][64])lds;                                          // [2][3: D log2(e), D x, dL/ds][kTile / 4][64]
     float(*sums)[3][kHalf][64] = (float(*)[3][kHalf][64])(lds + 2 * 3 * kTile * 64);                     // [2 or 1][W][3][kHalf][64]
-    // dA of the tiles before, each lane's own: registers hold a tile's sum, as thousands of tokens one by one cost half a digit (1.0e-6 off, 0.6e-6 so)
+    // dA of the tiles before, each lane's own: registers hold a tile's sum, as thousands of tokens one by one cost half a digit (1.0e-6 off, 0.57e-6 so)
     Pack<float, S>* gA_before = (Pack<float, S>*)(lds + 2 * 3 * kTile * 64 + (kTwice ? 2 : 1) * W * 3 * kHalf * 64) + threadIdx.x;
     if (kFull) *gA_before = {};
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
@@ -856,8 +859,9 @@ template <class F> auto with_shape(int64_t N, F f)
 }
 template <class F> auto with_type(int64_t dtype, F f) { return dtype == SIG_BF16 ? f(bf16()) : f(float()); }
 
-// States of a wavefront and wavefronts of a workgroup, by the number of states.  Measured at 8 x 4096 x 2048 with 16 states: 386 us with two states
-// on eight wavefronts, 504 with four on four (a wavefront alone on its SIMD), 525 with one on sixteen (their sums fill the LDS pipe).
+// States of a wavefront and wavefronts of a workgroup, by the number of states.  Measured at 8 x 4096 x 2048 with 16 states: two states on
+// eight wavefronts take 30 % less than four on four (a wavefront alone on its SIMD) and 36 % less than one on sixteen (their sums fill the
+// LDS pipe).
 template <class F> auto with_group(int64_t N, F f)
 {
     if (N <= 8) return f(Group<2, 4>());
@@ -867,11 +871,18 @@ template <class F> auto with_group(int64_t N, F f)
 }
 
 // Time chunks give a launch of few workgroups more of them, for a second pass over a part of the work (`second` of the first one's time).  The chunks are those
-// with the least time by a model: a compute unit runs `resident` workgroups at once (what LDS allows), W wavefronts each, whose SIMDs
+// with the least time by a model: a compute unit runs `resident` workgroups at once (what LDS allows; the registers allow as many), W wavefronts each, whose SIMDs
 // issue at kRate of their rate with one to four wavefronts; workgroups beyond what the chip holds wait for a round of their own.
-// Unit: a wavefront's work on a token, 104 of them a microsecond.  Measured, forward of 16 states in bf16 over 2,048 channels: 8 streams of 4,096
-// tokens 389 us with one chunk, 541 with two; 16 of 2,048 316 us; a stream of 16,384 over 1,024 channels 327 us with 8 chunks, 188 with
-// 16, 169 with 32.
+// Unit: a wavefront's work on a token, 104 of them a microsecond; with four states a wavefront it is more, which weighs a launch and the joining
+// less than it should.  Measured in bf16 with 1, 2, 4 .. 64 chunks, us: the counts taken, their neighbours behind them.
+//                                    forward                                    gradient
+//   8 x 4096 x 2048, 16 states     1: 379 (2: 503)                            1: 1003 (2: 1227)
+//   1 x 16384 x 1024, 16 states   32: 146 (16: 166, 64: 170)                 16: 336 (8: 644, 32: 335)
+//   1 x 16384 x 1024, 8 states    47: 104 (32: 108, 64: 113)                 32: 214 (16: 304, 64: 220)
+//   1 x 16384 x 1024, 32 states   32: 230 (16: 254, 64: 254)                 16: 587 (8: 1135, 32: 610)
+//   4 x 2048 x 1024, 32 states     8: 125 (4: 138, 16: 129)                   4: 302 (2: 576, 8: 314)
+//   1 x 4096 x 1024, 64 states    16: 125 (8: 220, 32: 160)                  16: 788 (8: 1262, 32: 853)
+//   2 x 2048 x 2048, 64 states     4: 222 (2: 420, 8: 240)                    4: 1535 (2: 2577, 8: 1568)
 constexpr double kRate[] = {0.45, 0.8, 0.93, 1.0};
 constexpr int kUnits = 256;
 double launch_time(int64_t workgroups, int W, int resident, double tokens)

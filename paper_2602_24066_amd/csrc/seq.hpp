@@ -42,7 +42,7 @@ hipError_t scan_step(const sig_scan_args& a, float* state, void* y, hipStream_t 
 // ---- gradient norm and clipping (kernels_clip.hip)
 constexpr int kClipTensors = 128;       // tensors that one launch takes: their table is a kernel argument (of at most 4 KB)
 constexpr int kClipBlock = 4096;        // elements of a workgroup, at least
-constexpr int kClipBlocks = 16384;      // workgroups that all tensors are spread over at most, about (166e6 elements: 341 us with 4,096, 314 with these)
+constexpr int kClipBlocks = 16384;      // workgroups that all tensors are spread over at most, about (166e6 elements: 8 % less time than with 4,096)
 struct ClipTable {
     const void* in[kClipTensors];
     void* out[kClipTensors];
@@ -78,6 +78,8 @@ template <class T, int V> struct alignas(V * sizeof(T)) Pack { T v[V]; };
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
 __device__ __forceinline__ float fast_exp(float v) { return __builtin_amdgcn_exp2f(v * kLog2e); }
+// The exponent v log2(e) is rounded, so exp is off by up to |v| 2^-24 of itself and a few units in the last place besides; so are sigmoid where v is
+// far below zero, a value of the size of exp(v), and a decay exp(D A), which that far down has little left to be off by.
 __device__ __forceinline__ float sigmoid(float v) { return __builtin_amdgcn_rcpf(1.0f + fast_exp(-v)); }
 
 // log(1 + exp(v)) = max(v, 0) + log(1 + e) with e = exp(-|v|) <= 1, and log(1 + e) = 2 artanh(s) with s = e / (2 + e) <= 1/3: the

@@ -3,7 +3,8 @@
 Tokens are CUDA tensors [batch, time, channels] in float32 or bfloat16, with contiguous channels (a slice of a wider projection is taken as
 it is; other layouts are copied once).  Parameters, recurrent states of the scan and their gradients are float32.  Every call enqueues
 on torch's current stream and returns without synchronising; results are plain tensors without autograd history, the gradients have
-functions of their own.
+functions of their own.  What a call writes in place (the states of the single-token calls, clipped gradients) does not raise the tensors'
+version counters: autograd does not notice where it kept them for a backward pass.
 """
 from __future__ import annotations
 
@@ -274,7 +275,8 @@ def sig_scan_step(x, dt, A, b, c, state, skip=None, gate=None, dt_bias=None, sof
 def sig_grad_clip(grads, max_norm, out=None):
     """Scales the tensors `grads` (float32 or bfloat16, one device) in place by min(1, max_norm / (norm + 1e-6)), norm their global 2-norm, or
     writes the products into the tensors `out` (of as many elements, either type).  Returns norm, a float32 tensor of no axes on the
-    device.  Tensors may have any order of axes as long as they fill their memory; those of `out` have that of their input."""
+    device.  Tensors may have any order of axes as long as they fill their memory; those of `out` have that of their input.  Apart from
+    that, no tensor that is written may share memory with another (as a gradient that is listed twice does): the order of accesses is not fixed."""
     torch = _t()
     grads = list(grads)
     outs = grads if out is None else list(out)
