@@ -414,7 +414,7 @@ typedef struct sig_scan_args {
     const void* gate;               /* device dtype [B, L, D] or NULL */
     const void* b;                  /* device dtype [B, L, G, N], states contiguous */
     const void* c;                  /* device dtype [B, L, G, N], states contiguous */
-    const float* A;                 /* device [D, N], finite */
+    const float* A;                 /* device [D, N], finite (beyond 2.3e38, where A log2(e) overflows, taken as that in a prompt) */
     const float* skip;              /* device [D] or NULL */
     const float* dt_bias;           /* device [D] or NULL */
     const float* initial_state;     /* device [B, D, N] or NULL (zeros) */

@@ -96,6 +96,9 @@ template <class T> __device__ __forceinline__ void forth(T*& p, unsigned bytes) 
 // loses (large case 380 -> 403 us).
 template <class T> __device__ __forceinline__ void held(T*& p) { asm volatile("" : "+s"(p)); }
 constexpr unsigned kNowhere = 0xfffffffcu;
+// v, an infinity as the largest number of its sign.  A log2(e) and a chunk's sum of step sizes are infinite where A and the steps need not be, and both
+// are multiplied with zeros: steps of tokens that do not count, rates of states that are there to fill a register.
+__device__ __forceinline__ float bounded(float v) { return fabsf(v) > 3.4028235e38f ? copysignf(3.4028235e38f, v) : v; }
 // at, or kNowhere: a selection that the compiler does not turn into branches around two accesses (worth 1 % of the backward pass)
 __device__ __forceinline__ unsigned offset_if(bool there, unsigned at)
 {
@@ -120,13 +123,13 @@ struct Blocks {
 // of its step sizes; exp(A sum D) is the chunk's decay, so the state before any chunk is a short recurrence over the chunks before it.
 struct ChunkStates {
     float* last;         // [B, chunks, N, D]
-    float* steps;        // [B, chunks, D] sums of D log2(e)
+    float* steps;        // [B, chunks, D]
 };
-// h over the chunks from `from` to `to` (without it, in either direction): h = exp2(A steps) h + last, eight chunks' loads under way at a
+// h over the chunks from `from` to `to` (without it, in either direction): h = exp2(A2 steps) h + last, eight chunks' loads under way at a
 // time.  last, steps: the lane's channel and the wavefront's first state in the stream's first chunk; n: states there are.
 // Where states grow, a chunk's factor may pass float32's range although h is zero or so small that the product does not.  What comes of it
 // is no finite number any more, so all is done again then, the factor's exponent split into one of at most 127 and a power of two.
-template <int S> __device__ __forceinline__ void join_chunks(float (&h)[S], const float (&A)[S], int from, int to, const float* last, const float* steps, int64_t N, int64_t D, int n)
+template <int S> __device__ __forceinline__ void join_chunks(float (&h)[S], const float (&A2)[S], int from, int to, const float* last, const float* steps, int64_t N, int64_t D, int n)
 {
     constexpr int U = 8;
     const int way = to >= from ? 1 : -1, count = (to - from) * way;
@@ -146,7 +149,7 @@ template <int S> __device__ __forceinline__ void join_chunks(float (&h)[S], cons
 #pragma unroll
         for (int u = 0; u < U; u++)
 #pragma unroll
-            for (int s = 0; s < S; s++) h[s] = fmaf(__builtin_amdgcn_exp2f(A[s] * sum[u]), h[s], l[u][s]);
+            for (int s = 0; s < S; s++) h[s] = fmaf(__builtin_amdgcn_exp2f(A2[s] * sum[u]), h[s], l[u][s]);
     }
     bool finite = true;
 #pragma unroll
@@ -159,7 +162,7 @@ template <int S> __device__ __forceinline__ void join_chunks(float (&h)[S], cons
         const int64_t row = from + way * j;
 #pragma unroll
         for (int s = 0; s < S; s++) {
-            const float x = A[s] * steps[row * D];
+            const float x = A2[s] * steps[row * D];
             const int k = x > 127.0f ? (int)fminf(x, 1000.0f) - 126 : 0;
             h[s] = fmaf(__builtin_amdgcn_exp2f(x > 1000.0f ? 127.0f : x - (float)k), __builtin_amdgcn_ldexpf(h[s], k), s < n ? last[(row * N + s) * D] : 0.0f);
         }
@@ -172,7 +175,7 @@ __global__ __launch_bounds__(Gr::W * 64, Gr::S == 4 ? 4 : 2) void scan_fwd_kerne
 {
     constexpr int S = Gr::S, W = Gr::W, PT = kTile / W, RT = 16 / S, KB = kTile / RT;
     extern __shared__ float lds[];
-    // D_t log2(e) and D_t x_t of two tokens for each lane, and the wavefronts' sums of four (where there are outputs), each twice
+    // D_t and D_t x_t of two tokens for each lane, and the wavefronts' sums of four (where there are outputs), each twice
     float4(*steps)[64] = (float4(*)[64])lds;                                             // [2][kTile / 2][64]
     float4(*sums)[kTile / 4][64] = (float4(*)[kTile / 4][64])(lds + 4 * kTile * 64);     // [2][W][kTile / 4][64]
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
@@ -191,7 +194,7 @@ __global__ __launch_bounds__(Gr::W * 64, Gr::S == 4 ? 4 : 2) void scan_fwd_kerne
     float A[S], h[S];
 #pragma unroll
     for (int s = 0; s < S; s++) {
-        A[s] = n0 + s < a.N ? a.A[d * a.N + n0 + s] : 0.0f;
+        A[s] = n0 + s < a.N ? bounded(a.A[d * a.N + n0 + s] * kLog2e) : 0.0f;
         h[s] = kOutputs && a.initial_state && n0 + s < a.N ? a.initial_state[(b * a.D + d) * a.N + n0 + s] : 0.0f;
     }
     if constexpr (kOutputs) {
@@ -245,15 +248,14 @@ __global__ __launch_bounds__(Gr::W * 64, Gr::S == 4 ? 4 : 2) void scan_fwd_kerne
         }
         forth(px, kTile * x_row), forth(pdt, kTile * dt_row), forth(pz, kTile * z_row), forth(pb, kTile * b_step), forth(pc, kTile * c_step);
     };
-    // D_t log2(e) and D_t x_t of the wavefront's tokens of a tile with n tokens (zero beyond: states stay, whatever finite A they are multiplied
-    // with, where A log2(e) may be infinite), and what its outputs need besides
+    // D_t and D_t x_t of the wavefront's tokens of a tile with n tokens (zero beyond: states stay), and what its outputs need besides
     auto prepare = [&](float4 (*to)[64], int n, const float (&xf)[PT], const float (&df)[PT], const float (&zf)[PT]) {
         float2 step[PT];
 #pragma unroll
         for (int i = 0; i < PT; i++) {
             float D = df[i] + bias;
             D = only_if(w * PT + i < n ? ~0u : 0u, either(soft, softplus(D), D));
-            step[i] = make_float2(D * kLog2e, D * xf[i]);
+            step[i] = make_float2(D, D * xf[i]);
             if (kOutputs) {
                 keep_next[i] = skip * xf[i];
                 f_next[i] = either(gated, zf[i] * sigmoid(zf[i]), 1.0f);
@@ -378,7 +380,7 @@ __global__ __launch_bounds__(Gr::W * 64, Gr::S == 4 ? 4 : 2) void scan_fwd_kerne
 #pragma unroll
         for (int s = 0; s < S; s++)
             if (n0 + s < a.N) (cs.last + ((b * bl.chunks + c) * a.N + n0 + s) * a.D + d0)[e] = h[s];
-        if (w == 0) cs.steps[(b * bl.chunks + c) * a.D + d] = total;
+        if (w == 0) cs.steps[(b * bl.chunks + c) * a.D + d] = bounded(total);
     }
 }
 
@@ -451,7 +453,7 @@ __global__ __launch_bounds__(Gr::W * 64, Gr::W > 8 ? 4 : 2) void scan_bwd_kernel
     constexpr bool kDecays = S == 2, kHeld = S == 2, kTwice = W <= 8;      // decays stay in registers; row pointers are held; the sums' LDS is there for either half of a tile
     constexpr unsigned E = sizeof(T);
     extern __shared__ float lds[];
-    float4(*in)[kTile / 4][64] = (float4(*)[kTile / 4][64])lds;                                          // [2][3: D log2(e), D x, dL/ds][kTile / 4][64]
+    float4(*in)[kTile / 4][64] = (float4(*)[kTile / 4][64])lds;                                          // [2][3: D, D x, dL/ds][kTile / 4][64]
     float(*sums)[3][kHalf][64] = (float(*)[3][kHalf][64])(lds + 2 * 3 * kTile * 64);                     // [2 or 1][W][3][kHalf][64]
     // dA of the tiles before, each lane's own: registers hold a tile's sum, as thousands of tokens one by one cost half a digit (1.0e-6 off, 0.57e-6 so)
     Pack<float, S>* gA_before = (Pack<float, S>*)(lds + 2 * 3 * kTile * 64 + (kTwice ? 2 : 1) * W * 3 * kHalf * 64) + threadIdx.x;
@@ -469,16 +471,17 @@ __global__ __launch_bounds__(Gr::W * 64, Gr::W > 8 ? 4 : 2) void scan_bwd_kernel
     const uint32_t soft = a.softplus ? ~0u : 0u, gated = a.gate ? ~0u : 0u;
     const int n0 = w * S;
     const int64_t tiles = (a.L + kTile - 1) / kTile;
-    float A[S], adj[S], gA[S] = {}, gskip = 0.0f, gbias = 0.0f, total = 0.0f;       // adj: a_{t+1} l_{t+1}
+    float A[S], A2[S], adj[S], gA[S] = {}, gskip = 0.0f, gbias = 0.0f, total = 0.0f;       // adj: a_{t+1} l_{t+1}
 #pragma unroll
     for (int s = 0; s < S; s++) {
         A[s] = n0 + s < a.N ? a.A[d * a.N + n0 + s] : 0.0f;
+        A2[s] = bounded(A[s] * kLog2e);
         adj[s] = kFull && g.grad_final_state && n0 + s < a.N ? g.grad_final_state[(b * a.D + d) * a.N + n0 + s] : 0.0f;
     }
     if constexpr (kFull) {
         const int after = len > 0 ? (len - 1) / bl.chunk : 0;      // the last chunk with tokens
         if (after > (int)c)
-            join_chunks(adj, A, after, (int)c, cs.last + (b * bl.chunks * a.N + n0) * a.D + d, cs.steps + b * bl.chunks * a.D + d, a.N, a.D, (int)a.N - n0);
+            join_chunks(adj, A2, after, (int)c, cs.last + (b * bl.chunks * a.N + n0) * a.D + d, cs.steps + b * bl.chunks * a.D + d, a.N, a.D, (int)a.N - n0);
     }
     // tiles with tokens that count, and the tokens of the last one: none for a chunk beyond the stream's length
     const int n_tiles = live > 0 ? (live + kTile - 1) / kTile : 0, n_last = n_tiles > 0 ? live - (n_tiles - 1) * kTile : 0;
@@ -544,7 +547,7 @@ __global__ __launch_bounds__(Gr::W * 64, Gr::W > 8 ? 4 : 2) void scan_bwd_kernel
             xs[slot][i] = v, Ds[slot][i] = D, us[slot][i] = u;
             sl[slot][i] = either(soft, sigmoid(raw), 1.0f);
             gs[slot][i] = gy * p * fmaf(zf, 1.0f - p, 1.0f);
-            ((float*)&to[0][k / 4][lane])[k % 4] = D * kLog2e;
+            ((float*)&to[0][k / 4][lane])[k % 4] = D;
             if (kFull) ((float*)&to[1][k / 4][lane])[k % 4] = on ? D * v : 0.0f;
             ((float*)&to[2][k / 4][lane])[k % 4] = !kFull || on ? u : 0.0f;
         }
@@ -604,7 +607,7 @@ __global__ __launch_bounds__(Gr::W * 64, Gr::W > 8 ? 4 : 2) void scan_bwd_kernel
         }
         prepare(slot ^ 1, in + (slot ^ 1) * 3, tile > 0 ? kTile : 0, kTile);
         fetch(tile > 1 ? kTile : 0);
-        // D[t] log2(e), D[t] x[t] and dL/ds[t] of four tokens from LDS
+        // D[t], D[t] x[t] and dL/ds[t] of four tokens from LDS
         auto four = [&](int q, int i, float (&v)[4]) {
             float4 r = now[q][i / 4][lane];
             v[0] = r.x, v[1] = r.y, v[2] = r.z, v[3] = r.w;
@@ -621,7 +624,7 @@ __global__ __launch_bounds__(Gr::W * 64, Gr::W > 8 ? 4 : 2) void scan_bwd_kernel
                     constexpr int j = decltype(it)::value;
                     unrolled<0, S>([&](auto is) {
                         constexpr int s = decltype(is)::value;
-                        float f = __builtin_amdgcn_exp2f(D[j] * A[s]);
+                        float f = __builtin_amdgcn_exp2f(D[j] * A2[s]);
                         if constexpr (kDecays) decay[i + j][s] = f;
                         h[i + j + 1][s] = fmaf(f, h[i + j][s], times_broadcast<k + j * S + s>(B[i / RT], u[j]));
                     });
@@ -643,7 +646,7 @@ __global__ __launch_bounds__(Gr::W * 64, Gr::W > 8 ? 4 : 2) void scan_bwd_kernel
                         lam[j][s] = adj[s];
                         float f;
                         if constexpr (kDecays && kFull) f = decay[i + j][s];
-                        else f = __builtin_amdgcn_exp2f(D[j] * A[s]);
+                        else f = __builtin_amdgcn_exp2f(D[j] * A2[s]);
                         adj[s] = lam[j][s] * f;
                         if constexpr (kFull) {
                             ht[j][s] = h[i + j + 1][s];
@@ -728,7 +731,7 @@ __global__ __launch_bounds__(Gr::W * 64, Gr::W > 8 ? 4 : 2) void scan_bwd_kernel
 #pragma unroll
         for (int s = 0; s < S; s++)
             if (n0 + s < a.N) {
-                parts.A[(row * a.N + n0 + s) * a.D + d] = gA_before->v[s] * kLn2;      // sums of D log2(e)
+                parts.A[(row * a.N + n0 + s) * a.D + d] = gA_before->v[s];
                 if (g.grad_initial_state && c == 0) g.grad_initial_state[(b * a.D + d) * a.N + n0 + s] = adj[s];
             }
         if (w == 0) {
@@ -744,7 +747,7 @@ __global__ __launch_bounds__(Gr::W * 64, Gr::W > 8 ? 4 : 2) void scan_bwd_kernel
 #pragma unroll
         for (int s = 0; s < S; s++)
             if (n0 + s < a.N) cs.last[(row * a.N + n0 + s) * a.D + d] = adj[s];
-        if (w == 0) cs.steps[row * a.D + d] = total;
+        if (w == 0) cs.steps[row * a.D + d] = bounded(total);
     }
 }
 

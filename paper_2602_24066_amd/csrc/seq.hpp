@@ -75,7 +75,7 @@ template <> __device__ __forceinline__ bf16 from_float<bf16>(float v)     // to 
 // V consecutive elements, one access of V * sizeof(T) bytes: the address is a multiple of that
 template <class T, int V> struct alignas(V * sizeof(T)) Pack { T v[V]; };
 
-constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+constexpr float kLog2e = 1.4426950408889634f;
 
 __device__ __forceinline__ float fast_exp(float v) { return __builtin_amdgcn_exp2f(v * kLog2e); }
 // The exponent v log2(e) is rounded, so exp is off by up to |v| 2^-24 of itself and a few units in the last place besides; so are sigmoid where v is

@@ -34,7 +34,7 @@ def chunk_of(which, B, L, D, G, N):
 
 
 # ------------------------------------------------------------------------------------------------ states that grow
-# A chunk's growth of 2^150: its exponent, 104 in natural units, is off by a rounding of A, of D log2(e) and of their product, 3 * 2^-24 each
+# A chunk's growth of 2^150: its exponent, 104 in natural units, is off by a rounding of A, of A log2(e) and of their product, 3 * 2^-24 each
 # at the most, and the factor by 104 times that, 1.9e-5; the rest as for other float32 results.
 GROWTH_TOL = 3e-5
 
@@ -123,6 +123,26 @@ def test_the_lowest_decay_rates(B, L, D, N, lengths):
     for i in range(4, 21):
         S.sig_scan_step(state=held, **{k: w[:, i] if k in TOKENS else w for k, w in first.items() if k != "initial_state"})
     close(one, held.cpu(), torch.float32, "state by steps")
+
+
+@gpu
+@pytest.mark.parametrize("B,L,D,N,lengths", [(2, 39, 20, 12, [39, 24]), (1, 700, 70, 13, None), (1, 640, 33, 40, None)])
+def test_the_largest_step_sizes(B, L, D, N, lengths):
+    """Tokens without an input whose step size is near float32's largest value forget what decays and keep what does not, several of them in a row
+    and in states that are there to fill a register only."""
+    v = R.inputs("scan", B, L, D, N=N, dtype=torch.float32, lengths=lengths, seed=34)
+    gy, gs = v.pop("grad_out"), v.pop("grad_final_state")
+    v["A"][:, 3] = 0.0
+    for t in (5, 6, 20, L // 2, L // 2 + 1):
+        v["dt"][:, t], v["x"][:, t] = 2.5e38, 0.0
+    y, state, grads = R.with_gradients(R.scan, v, gy, gs)
+    d = {k: up(w) for k, w in v.items()}
+    got_y, got_state, ck = S.sig_scan_forward(**d, checkpoint=True)
+    close(got_y, y, torch.float32, "y")
+    close(got_state, state, torch.float32, "state")
+    got = S.sig_scan_backward(**d, grad_out=up(gy), checkpoint=ck, grad_final_state=up(gs))
+    for k in ("b", "c", "gate", "skip", "initial_state"):        # those of x, dt and A are of the steps' own size
+        close(got[NAMES[k]], grads[k], torch.float32, "grad " + k)
 
 
 # ------------------------------------------------------------------------------------------------ filter weights that are not finite
