@@ -392,9 +392,9 @@ __global__ __launch_bounds__(Gr::W * 64, Gr::S == 4 ? 4 : 2) void scan_fwd_kerne
 // six steps leaves the 64 sums of 16 tokens (2 states, dB and dC) one to a lane in 129 instructions, where a sum to all lanes would take six for
 // each; the workgroups' sums are added by a second kernel in their order, no atomics.
 // What bounds it: vector instructions, 24 a state and token (two exponentials with four states a wavefront, else one), on SIMDs that are busy
-// 76 % of the time with two wavefronts each.  8 x 2048 x 2048 bf16, 16 states: 492 us, 1.1e12 states a second; the bytes (seven tensors of
-// tokens, the checkpoint, the workgroups' sums, 0.67 GB) alone 131 us.  More than 32 states: 270 of the registers that a lane wants go to
-// memory, 5.6 ms where 32 states take 0.94.
+// 76 % of the time with two wavefronts each.  8 x 2048 x 2048 bf16, 16 states: 491 us, 1.1e12 states a second; the bytes (seven tensors of
+// tokens, the checkpoint, the workgroups' sums, 0.67 GB) alone 131 us.  More than 32 states: 260 of the registers that a lane wants go to
+// memory, 5.5 ms where 32 states take 0.95.
 template <int K, int S> __device__ __forceinline__ void add_broadcast(float (&o)[S], float r, float v)      // o[s] += r[K + s] v
 {
     static_assert(S == 2 || S == 4, "states of a wavefront");
