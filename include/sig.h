@@ -458,6 +458,99 @@ size_t sig_grad_clip_workspace_bytes(int64_t n_tensors, const int64_t* sizes);
 int    sig_grad_clip(int64_t n_tensors, const void* const* in, void* const* out, const int64_t* sizes, const int64_t* in_dtypes,
                      const int64_t* out_dtypes, float max_norm, float* norm, void* workspace, size_t workspace_bytes, void* stream);
 
+/* ---- operators of a layer ---------------------------------------------------------------------------------
+ * What a layer of a model over signature tokens has besides: the norm of the stream with the residual's addition, projections (matrix products
+ * with bias, activation and residual), a gated linear recurrence as the cheaper sibling of the selective scan, their gradients and 8-bit forms.
+ *
+ * The conventions of the sequence operators hold: arithmetic, sums, states and statistics in float32, calls only enqueue kernels on `stream`, the
+ * same inputs give the same bits, no output overlaps an input unless stated, nothing has to be aligned beyond its type.  Tokens are rows here:
+ * strides count elements from one row to the next (0: a broadcast input); a row is contiguous.  SIG_E4M3 is the 8-bit float of 4 exponent and 3
+ * fraction bits without infinities (largest value 448). */
+#define SIG_E4M3 2
+
+/* Root-mean-square norm: total = x + residual, rounded to dtype (x itself without residual); y = total * rsqrt(mean(total^2) + eps) * weight. */
+typedef struct sig_norm_args {
+    int64_t dtype, rows, C;         /* SIG_F32 or SIG_BF16; C >= 1 */
+    int64_t x_stride, residual_stride;
+    double eps;                     /* >= 0 */
+    const void* x;                  /* device dtype [rows, C] */
+    const void* residual;           /* device dtype [rows, C] or NULL */
+    const float* weight;            /* device [C] */
+} sig_norm_args;
+/* total: dtype [rows, C] or NULL.  scale NULL: y is dtype [rows, C].  Else y is SIG_E4M3 [rows, C] and scale [rows]: y * scale is the norm, scale =
+ * max |row| / 448, its values taken before any rounding to dtype.  Rows of zeros have scale 0; a row with an infinity or NaN has a
+ * scale that is not finite, and its y is of no use but defined. */
+int    sig_norm_forward(const sig_norm_args* args, void* y, float* scale, void* total, void* stream);
+/* args->x: the total that the forward call gave (residual is not looked at).  grad_y and grad_total (or NULL) dtype [rows, C] with strides of their own ->
+ * grad_x dtype [rows, C], the gradient of x and of residual alike; grad_weight [C].  Both overwritten. */
+size_t sig_norm_backward_workspace_bytes(const sig_norm_args* args);
+int    sig_norm_backward(const sig_norm_args* args, const void* grad_y, int64_t gy_stride, const void* grad_total, int64_t gt_stride,
+                         void* grad_x, float* grad_weight, void* workspace, size_t workspace_bytes, void* stream);
+/* Rows to 8 bits without a norm: q SIG_E4M3 [rows, C], scale [rows], as above. */
+int    sig_quantize(int64_t dtype, int64_t rows, int64_t C, int64_t x_stride, const void* x, void* q, float* scale, void* stream);
+
+/* y = f(x weight^T + bias) + residual, f the identity, z sigmoid(z), or z Phi(z) with the normal distribution's Phi. */
+#define SIG_ACT_NONE 0
+#define SIG_ACT_SILU 1
+#define SIG_ACT_GELU 2
+typedef struct sig_linear_args {
+    int64_t dtype;                  /* of x and weight: SIG_F32, SIG_BF16 or SIG_E4M3 */
+    int64_t out_dtype;              /* of bias, residual, pre and y: SIG_F32 or SIG_BF16; dtype where that is one of them */
+    int64_t M, N, K, act;           /* rows, outputs >= 1, inputs >= 1 */
+    int64_t x_stride, residual_stride;
+    const void* x;                  /* device dtype [M, K] */
+    const void* weight;             /* device dtype [N, K] */
+    const void* bias;               /* device out_dtype [N] or NULL */
+    const void* residual;           /* device out_dtype [M, N] or NULL */
+    const float* x_scale;           /* SIG_E4M3: device [M] or NULL (ones); row m of x stands for x_scale[m] times its values */
+    const float* weight_scale;      /* SIG_E4M3: device [N] or NULL (ones) */
+} sig_linear_args;
+/* y out_dtype [M, N]; pre: NULL or out_dtype [M, N], receives what f is applied to (for the gradient). */
+size_t sig_linear_forward_workspace_bytes(const sig_linear_args* args);
+int    sig_linear_forward(const sig_linear_args* args, void* y, void* pre, void* workspace, size_t workspace_bytes, void* stream);
+/* Gradient (SIG_F32 and SIG_BF16): grad_y dtype [M, N] with a stride of its own; pre as kept (NULL where act is SIG_ACT_NONE) -> grad_x dtype [M, K],
+ * grad_weight dtype [N, K], grad_bias dtype [N]; each may be NULL, and is not computed then.  The gradient of the residual is grad_y.
+ * bias, residual and scales of args are not looked at, x only for grad_weight, weight only for grad_x. */
+size_t sig_linear_backward_workspace_bytes(const sig_linear_args* args);
+int    sig_linear_backward(const sig_linear_args* args, const void* grad_y, int64_t gy_stride, const void* pre, void* grad_x,
+                           void* grad_weight, void* grad_bias, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Gated linear recurrence, a state a channel:  u_t = exp(log_rate) sigmoid(decay_gate_t),  a_t = exp(-u_t),
+ *   h_t = a_t h_(t-1) + sqrt(1 - a_t^2) sigmoid(input_gate_t) x_t,   y_t = h_t.
+ * Tokens, strides and lengths as those of the scan; L < 2^30, time strides below 2^24, B * D < 2^31. */
+typedef struct sig_gated_args {
+    int64_t dtype, B, L, D;
+    int64_t x_stride_b, x_stride_t, decay_stride_b, decay_stride_t, input_stride_b, input_stride_t;
+    const void* x;                  /* device dtype [B, L, D] */
+    const void* decay_gate;         /* device dtype [B, L, D] */
+    const void* input_gate;         /* device dtype [B, L, D] */
+    const float* log_rate;          /* device [D]; beyond 64 taken as 64 (gates below -88 are shut: their sigmoid is zero) */
+    const float* initial_state;     /* device [B, D] or NULL (zeros) */
+    const int32_t* lengths;         /* device [B] or NULL */
+} sig_gated_args;
+/* y dtype [B, L, D]; final_state [B, D] or NULL; checkpoint: NULL, or sig_gated_scan_checkpoint_bytes bytes for the gradient (states every 16
+ * tokens), the caller's to keep until then. */
+size_t sig_gated_scan_checkpoint_bytes(const sig_gated_args* args);
+size_t sig_gated_scan_forward_workspace_bytes(const sig_gated_args* args);
+int    sig_gated_scan_forward(const sig_gated_args* args, void* y, float* final_state, void* checkpoint, size_t checkpoint_bytes,
+                              void* workspace, size_t workspace_bytes, void* stream);
+typedef struct sig_gated_grads {
+    int64_t gy_stride_b, gy_stride_t;
+    const void* grad_y;             /* device dtype [B, L, D] */
+    const float* grad_final_state;  /* device [B, D] or NULL */
+    void* grad_x;                   /* device dtype [B, L, D], like the next two */
+    void* grad_decay_gate;
+    void* grad_input_gate;
+    float* grad_log_rate;           /* device [D] */
+    float* grad_initial_state;      /* device [B, D] or NULL */
+} sig_gated_grads;
+size_t sig_gated_scan_backward_workspace_bytes(const sig_gated_args* args);
+int    sig_gated_scan_backward(const sig_gated_args* args, const sig_gated_grads* grads, const void* checkpoint, size_t checkpoint_bytes,
+                               void* workspace, size_t workspace_bytes, void* stream);
+/* One token of every stream: x and gates [B, D], y [B, D]; state float32 [B, D] is updated in place (L, time strides, initial_state and lengths are
+ * not looked at). */
+int    sig_gated_scan_step(const sig_gated_args* args, float* state, void* y, void* stream);
+
 /* ---- kernel timer ----------------------------------------------------------------------------------------
  * For benchmarks: while enabled, sig_forward / sig_backward record two HIP event pairs on the caller's stream:
  * one around their main kernel (the hot loop over segments) and one around everything the call enqueues (with

@@ -11,3 +11,5 @@ from .binding import (SigError, WindowPlan, WordSet, lib_path, load_library, sig
                       sig_wordset_build_graph, sig_wordset_build_leadlag_sparse, sig_wordset_build_truncated)
 from .sequence import (sig_conv_backward, sig_conv_forward, sig_conv_step, sig_grad_clip, sig_scan_backward, sig_scan_forward,  # noqa: F401
                        sig_scan_step)
+from .layer import (sig_gated_scan_backward, sig_gated_scan_forward, sig_gated_scan_step, sig_linear_backward, sig_linear_forward,  # noqa: F401
+                    sig_norm_backward, sig_norm_forward, sig_quantize)

@@ -124,6 +124,20 @@ def load_library():
     sig("sig_scan_step", c_int, [c_p, c_p, c_p, c_p])
     sig("sig_grad_clip_workspace_bytes", c_sz, [c_i64, c_p])
     sig("sig_grad_clip", c_int, [c_i64, c_p, c_p, c_p, c_p, c_p, ctypes.c_float, c_p, c_p, c_sz, c_p])
+    sig("sig_norm_forward", c_int, [c_p, c_p, c_p, c_p, c_p])
+    sig("sig_norm_backward_workspace_bytes", c_sz, [c_p])
+    sig("sig_norm_backward", c_int, [c_p, c_p, c_i64, c_p, c_i64, c_p, c_p, c_p, c_sz, c_p])
+    sig("sig_quantize", c_int, [c_i64, c_i64, c_i64, c_i64, c_p, c_p, c_p, c_p])
+    sig("sig_linear_forward_workspace_bytes", c_sz, [c_p])
+    sig("sig_linear_forward", c_int, [c_p, c_p, c_p, c_p, c_sz, c_p])
+    sig("sig_linear_backward_workspace_bytes", c_sz, [c_p])
+    sig("sig_linear_backward", c_int, [c_p, c_p, c_i64, c_p, c_p, c_p, c_p, c_p, c_sz, c_p])
+    sig("sig_gated_scan_checkpoint_bytes", c_sz, [c_p])
+    sig("sig_gated_scan_forward_workspace_bytes", c_sz, [c_p])
+    sig("sig_gated_scan_forward", c_int, [c_p, c_p, c_p, c_p, c_sz, c_p, c_sz, c_p])
+    sig("sig_gated_scan_backward_workspace_bytes", c_sz, [c_p])
+    sig("sig_gated_scan_backward", c_int, [c_p, c_p, c_p, c_sz, c_p, c_sz, c_p])
+    sig("sig_gated_scan_step", c_int, [c_p, c_p, c_p, c_p])
     _lib = lib
     return lib
 

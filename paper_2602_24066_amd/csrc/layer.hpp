@@ -1,0 +1,41 @@
+// Operators of a layer (norm, matrix product, gated recurrence): launch interface between the C ABI (api_layer.cpp) and the HIP kernels.
+#pragma once
+#include "seq.hpp"
+
+namespace sig {
+
+// ---- norm (kernels_norm.hip)
+struct NormGrads {
+    const void* grad_y;
+    int64_t gy_stride;
+    const void* grad_total;             // or null
+    int64_t gt_stride;
+    void* grad_x;
+    float* grad_weight;
+};
+hipError_t norm_forward(const sig_norm_args& a, void* y, float* scale, void* total, hipStream_t stream);     // weight null: rows to 8 bits as they are
+size_t norm_backward_workspace(const sig_norm_args& a);
+hipError_t norm_backward(const sig_norm_args& a, const NormGrads& g, float* workspace, hipStream_t stream);
+
+// ---- matrix product (kernels_linear.hip)
+size_t linear_forward_workspace(const sig_linear_args& a);
+hipError_t linear_forward(const sig_linear_args& a, void* y, void* pre, void* workspace, hipStream_t stream);
+size_t linear_backward_workspace(const sig_linear_args& a);
+hipError_t linear_backward(const sig_linear_args& a, const void* grad_y, int64_t gy_stride, const void* pre, void* grad_x, void* grad_weight,
+                           void* grad_bias, void* workspace, hipStream_t stream);
+
+// ---- gated recurrence (kernels_gated.hip)
+constexpr int kGatedTile = 16;          // tokens between two states of a checkpoint
+size_t gated_forward_workspace(const sig_gated_args& a);
+size_t gated_backward_workspace(const sig_gated_args& a);
+hipError_t gated_forward(const sig_gated_args& a, void* y, float* final_state, float* checkpoint, float* workspace, hipStream_t stream);
+hipError_t gated_backward(const sig_gated_args& a, const sig_gated_grads& g, const float* checkpoint, float* workspace, hipStream_t stream);
+hipError_t gated_step(const sig_gated_args& a, float* state, void* y, hipStream_t stream);
+
+#ifdef __HIPCC__
+struct e4m3 { uint8_t bits; };
+// to nearest, ties to even, values a little beyond 448 to 448, a NaN stays one (conversion of the hardware)
+template <> __device__ __forceinline__ e4m3 from_float<e4m3>(float v) { return {(uint8_t)(__builtin_amdgcn_cvt_pk_fp8_f32(v, v, 0, false) & 0xff)}; }
+#endif
+
+}  // namespace sig
