@@ -517,7 +517,7 @@ int    sig_linear_backward(const sig_linear_args* args, const void* grad_y, int6
 
 /* Gated linear recurrence, a state a channel:  u_t = exp(log_rate) sigmoid(decay_gate_t),  a_t = exp(-u_t),
  *   h_t = a_t h_(t-1) + sqrt(1 - a_t^2) sigmoid(input_gate_t) x_t,   y_t = h_t.
- * Tokens, strides and lengths as those of the scan; L < 2^30, time strides below 2^24, B * D < 2^31. */
+ * Tokens, strides and lengths as those of the scan; L < 2^30, D and time strides below 2^22, B * D < 2^31. */
 typedef struct sig_gated_args {
     int64_t dtype, B, L, D;
     int64_t x_stride_b, x_stride_t, decay_stride_b, decay_stride_t, input_stride_b, input_stride_t;

@@ -22,7 +22,7 @@ HIPCC_FLAGS = ["-O3", "-std=c++17", "-fPIC", "--offload-arch=gfx950", "-Xclang",
                "-mllvm", "-amdgpu-sched-strategy=max-ilp"]
 # kernels bound by memory, which need wavefronts more than instructions in order: the option doubles the registers of the
 # convolution (98 -> 196 at eight channels a thread)
-NO_MAX_ILP = ("kernels_conv.hip", "kernels_clip.hip")
+NO_MAX_ILP = ("kernels_conv.hip", "kernels_clip.hip", "kernels_norm.hip", "kernels_gated.hip")
 
 
 def hipcc() -> str:

@@ -58,12 +58,12 @@ int check_gated(const sig_gated_args* a, bool prompt = true)
     if (!a || bad_type(a->dtype) || a->D < 1) return SIG_EINVAL;
     int rc = check_sizes({a->B, prompt ? a->L : 1, a->D});
     if (rc != SIG_OK) return rc;
-    if (a->B > 0 && a->D > INT32_MAX / a->B) return SIG_ETOOLARGE;
+    if ((a->B > 0 && a->D > INT32_MAX / a->B) || a->D >= (1 << 22)) return SIG_ETOOLARGE;      // a round's tokens are reached by 32-bit offsets
     if (prompt && a->L >= (1 << 30)) return SIG_ETOOLARGE;        // tokens are counted in 32 bits, up to the end of a round
     rc = check_strides({a->x_stride_b, a->decay_stride_b, a->input_stride_b});
     if (rc != SIG_OK || !prompt) return rc;
     for (int64_t s : {a->x_stride_t, a->decay_stride_t, a->input_stride_t})
-        if (s < 0 || s >= (1 << 24)) return s < 0 ? SIG_EINVAL : SIG_ETOOLARGE;
+        if (s < 0 || s >= (1 << 22)) return s < 0 ? SIG_EINVAL : SIG_ETOOLARGE;
     return SIG_OK;
 }
 
@@ -159,7 +159,7 @@ int sig_gated_scan_backward(const sig_gated_args* a, const sig_gated_grads* g, c
         rc = check_strides({g->gy_stride_b});
         if (rc != SIG_OK) return rc;
         if (g->gy_stride_t < 0) return SIG_EINVAL;
-        if (g->gy_stride_t >= (1 << 24)) return SIG_ETOOLARGE;
+        if (g->gy_stride_t >= (1 << 22)) return SIG_ETOOLARGE;
         if (!checkpoint) return SIG_EWORKSPACE;
     }
     if (checkpoint_bytes < ckpt_bytes(*a)) return SIG_EWORKSPACE;

@@ -20,23 +20,86 @@ constexpr int kWaves = 8, kHalf = 8, kRound = kWaves * kGatedTile, kGroup = 64;
 
 struct Two { float v[2]; };
 
-template <class T, bool kPairs> __device__ __forceinline__ Pack<T, 2> load_two(const T* p, int c, int D)
+// Tokens first .. last - 1 of a stream's channels, as a buffer that begins with token `first` and ends with token last - 1: accesses behind it give
+// zeros and write nothing.  A lane's place in it is 32 bits, which tokens of a round do not pass (time strides below 2^22 elements).
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t tokens(const void* stream, int64_t stride_t, int64_t first, int64_t last, int64_t D, int e)
 {
-    if constexpr (kPairs) return *(const Pack<T, 2>*)(p + c);                  // D is even: c < D has c + 1 < D
-    Pack<T, 2> r;
-    r.v[0] = p[c];
-    r.v[1] = p[min(c + 1, D - 1)];
-    return r;
+    const int64_t n = min(last - first, (int64_t)kRound);
+    const uint32_t bytes = n > 0 ? (uint32_t)(((n - 1) * stride_t + D) * e) : 0;
+    return __builtin_amdgcn_make_buffer_rsrc((char*)stream + first * stride_t * e, 0, bytes, 0x27000);
 }
-template <class T, bool kPairs> __device__ __forceinline__ void store_two(T* p, int c, int D, float v0, float v1)
+// A lane's two channels of a token, in words as they lie in memory (elements of their own would take a register each)
+template <class T> struct Both { uint32_t w[sizeof(T) / 2]; };
+__device__ __forceinline__ float value(const Both<bf16>& v, int j) { return __uint_as_float(j ? v.w[0] & 0xffff0000u : v.w[0] << 16); }
+__device__ __forceinline__ float value(const Both<float>& v, int j) { return __uint_as_float(v.w[j]); }
+
+// kHalf tokens' channels, the first at `at` bytes, the others `step` bytes apart; not kPairs: `second` bytes lie between the two
+template <class T, bool kPairs> __device__ __forceinline__ void load_two(__amdgpu_buffer_rsrc_t from, int at, int second, int step, Both<T>* to)
 {
-    Pack<T, 2> r{{from_float<T>(v0), from_float<T>(v1)}};
-    if constexpr (kPairs) *(Pack<T, 2>*)(p + c) = r;
-    else {
-        p[c] = r.v[0];
-        if (c + 1 < D) p[c + 1] = r.v[1];
+#pragma unroll
+    for (int k = 0; k < kHalf; k++) {
+        if constexpr (!kPairs && sizeof(T) == 2) {
+            const uint32_t u = (uint16_t)__builtin_amdgcn_raw_buffer_load_b16(from, at, k * step, 0), v = (uint16_t)__builtin_amdgcn_raw_buffer_load_b16(from, at + second, k * step, 0);
+            to[k].w[0] = u | v << 16;
+        } else if constexpr (!kPairs) {
+            to[k].w[0] = __builtin_amdgcn_raw_buffer_load_b32(from, at, k * step, 0);
+            to[k].w[1] = __builtin_amdgcn_raw_buffer_load_b32(from, at + second, k * step, 0);
+        } else if constexpr (sizeof(T) == 2) {
+            to[k].w[0] = __builtin_amdgcn_raw_buffer_load_b32(from, at, k * step, 0);
+        } else {
+            typedef uint32_t Words __attribute__((ext_vector_type(2)));
+            const Words u = __builtin_amdgcn_raw_buffer_load_b64(from, at, k * step, 0);
+            to[k].w[0] = u[0];
+            to[k].w[1] = u[1];
+        }
     }
 }
+// All ones for a token that counts, else 0; masked() keeps v or makes it 0.  Selections by a condition the compiler turns into branches, and puts behind
+// them the work that the selected value takes, with all that this work needs held in registers; hence a mask whose origin it does not see.
+__device__ __forceinline__ uint32_t mask_of(bool counts)
+{
+    uint32_t m = counts ? ~0u : 0u;
+    asm("" : "+v"(m));
+    return m;
+}
+// v, computed here: the compiler moves what is used behind a barrier there, and holds all that it is made of instead
+__device__ __forceinline__ float here(float v)
+{
+    asm volatile("" : "+v"(v));
+    return v;
+}
+__device__ __forceinline__ float masked(float v, uint32_t mask) { return __uint_as_float(__float_as_uint(v) & mask); }
+template <class T> __device__ __forceinline__ Both<T> masked(Both<T> v, uint32_t mask)
+{
+#pragma unroll
+    for (uint32_t& word : v.w) word &= mask;
+    return v;
+}
+__device__ __forceinline__ void pack(Both<bf16>& r, float v0, float v1) { r.w[0] = from_float<bf16>(v0).bits | (uint32_t)from_float<bf16>(v1).bits << 16; }
+__device__ __forceinline__ void pack(Both<float>& r, float v0, float v1)
+{
+    r.w[0] = __float_as_uint(v0);
+    r.w[1] = __float_as_uint(v1);
+}
+template <class T, bool kPairs> __device__ __forceinline__ void store_two(__amdgpu_buffer_rsrc_t to, int at, int second, int step, uint32_t mask, float v0, float v1)
+{
+    Both<T> r;
+    pack(r, v0, v1);
+    r = masked(r, mask);
+    if constexpr (!kPairs && sizeof(T) == 2) {
+        __builtin_amdgcn_raw_buffer_store_b16((uint16_t)r.w[0], to, at, step, 0);
+        if (second) __builtin_amdgcn_raw_buffer_store_b16((uint16_t)(r.w[0] >> 16), to, at + second, step, 0);
+    } else if constexpr (!kPairs) {
+        __builtin_amdgcn_raw_buffer_store_b32(r.w[0], to, at, step, 0);
+        if (second) __builtin_amdgcn_raw_buffer_store_b32(r.w[1], to, at + second, step, 0);
+    } else if constexpr (sizeof(T) == 2) {
+        __builtin_amdgcn_raw_buffer_store_b32(r.w[0], to, at, step, 0);
+    } else {
+        typedef uint32_t Words __attribute__((ext_vector_type(2)));
+        __builtin_amdgcn_raw_buffer_store_b64(Words{r.w[0], r.w[1]}, to, at, step, 0);
+    }
+}
+constexpr int kNowhere = (int)0x80000000;      // a place behind every such buffer: its stores write nothing
 
 // sigmoid(v) and 1 - sigmoid(v) = sigmoid(-v), which keeps its relative precision where it is small
 struct Gate { float s, rest; };
@@ -89,7 +152,21 @@ __device__ __forceinline__ Where where(const sig_gated_args& a, int groups, int 
     return w;
 }
 
-template <class T> struct Raw { Pack<T, 2> x[kHalf], p[kHalf], q[kHalf]; };
+template <class T> struct Raw { Both<T> x[kHalf], p[kHalf], q[kHalf], g[kHalf]; };
+
+// Where a lane's channels are in buffers of tokens, in bytes
+struct Lane { int second, x, p, q, g, out; };
+template <class T, bool kPairs, bool kBack>
+__device__ __forceinline__ void load_round(const sig_gated_args& a, const void* gy, int64_t gy_stride, const Where& w, const Lane& l, int64_t first, int64_t end, bool inputs, Raw<T>& r)
+{
+    constexpr int e = sizeof(T);
+    load_two<T, kPairs>(tokens((const T*)a.decay_gate + w.b * a.decay_stride_b, a.decay_stride_t, first, end, a.D, e), l.p, l.second, (int)a.decay_stride_t * e, r.p);
+    if (inputs) {
+        load_two<T, kPairs>(tokens((const T*)a.x + w.b * a.x_stride_b, a.x_stride_t, first, end, a.D, e), l.x, l.second, (int)a.x_stride_t * e, r.x);
+        load_two<T, kPairs>(tokens((const T*)a.input_gate + w.b * a.input_stride_b, a.input_stride_t, first, end, a.D, e), l.q, l.second, (int)a.input_stride_t * e, r.q);
+    }
+    if constexpr (kBack) load_two<T, kPairs>(tokens(gy, gy_stride, first, end, a.D, e), l.g, l.second, (int)gy_stride * e, r.g);
+}
 
 // kSummary: only (A, H) of the chunk from a state of zero
 template <class T, bool kPairs, bool kSummary>
@@ -100,7 +177,6 @@ __global__ __launch_bounds__(kWaves * 64) void gated_forward_kernel(sig_gated_ar
     const Where w = where(a, groups, chunks, rounds);
     const int wave = threadIdx.x / 64, half = (threadIdx.x >> 5) & 1, li = threadIdx.x & 31, D = (int)a.D;
     const bool even = kPairs || w.c + 1 < D;
-    const T *x = (const T*)a.x + w.b * a.x_stride_b, *p = (const T*)a.decay_gate + w.b * a.decay_stride_b, *q = (const T*)a.input_gate + w.b * a.input_stride_b;
     const int c1 = even ? w.c + 1 : w.c;
     const float rate[2] = {rate_of(a.log_rate[w.c]), rate_of(a.log_rate[c1])};
     float state[2] = {}, decayed[2] = {1.0f, 1.0f};
@@ -117,32 +193,26 @@ __global__ __launch_bounds__(kWaves * 64) void gated_forward_kernel(sig_gated_ar
     }
     const int end = min(w.last, w.live);
     const int64_t tiles = (a.L + kGatedTile - 1) / kGatedTile;
-    auto load = [&](int t0, Raw<T>& r) {
-#pragma unroll
-        for (int k = 0; k < kHalf; k++) {
-            const int64_t t = min(t0 + k, end - 1);
-            r.x[k] = load_two<T, kPairs>(x + t * a.x_stride_t, w.c, D);
-            r.p[k] = load_two<T, kPairs>(p + t * a.decay_stride_t, w.c, D);
-            r.q[k] = load_two<T, kPairs>(q + t * a.input_stride_t, w.c, D);
-        }
-    };
-    const int mine = wave * kGatedTile + half * kHalf;
+    const int mine = wave * kGatedTile + half * kHalf, e = sizeof(T);
+    const Lane l{(c1 - w.c) * e, (int)(mine * a.x_stride_t + w.c) * e, (int)(mine * a.decay_stride_t + w.c) * e, (int)(mine * a.input_stride_t + w.c) * e, 0, w.on ? (mine * D + w.c) * e : kNowhere};
+    T* out = y + w.b * a.L * D;
     Raw<T> next;
-    if (w.first < end) load(w.first + mine, next);
+    if (w.first < end) load_round<T, kPairs, false>(a, nullptr, 0, w, l, w.first, end, true, next);
     int buf = 0;
     for (int r = w.first; r < end; r += kRound, buf ^= 1) {
         const Raw<T> now = next;
-        if (r + kRound < end) load(r + kRound + mine, next);
+        if (r + kRound < end) load_round<T, kPairs, false>(a, nullptr, 0, w, l, r + kRound, end, true, next);
         const int t0 = r + mine;
         float f[kHalf][2], d[kHalf][2], A[2] = {1.0f, 1.0f}, H[2] = {};
 #pragma unroll
         for (int k = 0; k < kHalf; k++)
 #pragma unroll
             for (int j = 0; j < 2; j++) {
-                const Decay e = decay(rate[j], sigmoid(to_float(now.p[k].v[j])));
-                const bool live = t0 + k < end;
-                d[k][j] = live ? e.a : 1.0f;
-                f[k][j] = live ? __builtin_amdgcn_sqrtf(e.w) * sigmoid(to_float(now.q[k].v[j])) * to_float(now.x[k].v[j]) : 0.0f;
+                // a token that does not count has u = 0: nothing decays, and b is 0
+                const uint32_t mask = mask_of(t0 + k < end);
+                const Decay v = decay(rate[j], masked(sigmoid(value(now.p[k], j)), mask));
+                d[k][j] = v.a;
+                f[k][j] = masked(__builtin_amdgcn_sqrtf(v.w) * sigmoid(value(now.q[k], j)) * value(now.x[k], j), mask);
                 A[j] *= d[k][j];
                 H[j] = fmaf(d[k][j], H[j], f[k][j]);
             }
@@ -179,12 +249,12 @@ __global__ __launch_bounds__(kWaves * 64) void gated_forward_kernel(sig_gated_ar
                 if (even) to[w.c + 1] = start[1];
             }
             float h[2] = {fmaf(preA[0], start[0], preH[0]), fmaf(preA[1], start[1], preH[1])};
+            const __amdgpu_buffer_rsrc_t to = tokens(out, D, r, w.last, D, e);
 #pragma unroll
             for (int k = 0; k < kHalf; k++) {
                 h[0] = fmaf(d[k][0], h[0], f[k][0]);
                 h[1] = fmaf(d[k][1], h[1], f[k][1]);
-                const bool live = t0 + k < end;
-                if (w.on && t0 + k < w.last) store_two<T, kPairs>(y + (w.b * a.L + t0 + k) * D, w.c, D, live ? h[0] : 0.0f, live ? h[1] : 0.0f);
+                store_two<T, kPairs>(to, l.out, l.second, k * D * e, mask_of(t0 + k < end), h[0], h[1]);
             }
         }
     }
@@ -201,16 +271,15 @@ __global__ __launch_bounds__(kWaves * 64) void gated_forward_kernel(sig_gated_ar
     } else {
         // what no round has reached
         const int done = w.first + (max(end - w.first, 0) + kRound - 1) / kRound * kRound;
-        for (int t = done + (threadIdx.x >> 5); t < w.last; t += kWaves * 2)
-            if (w.on) store_two<T, kPairs>(y + (w.b * a.L + t) * D, w.c, D, 0.0f, 0.0f);
+        for (int t = done; t < w.last; t += kRound)
+#pragma unroll
+            for (int k = 0; k < kHalf; k++) store_two<T, kPairs>(tokens(out, D, t, w.last, D, e), l.out, l.second, k * D * e, 0, 0.0f, 0.0f);
         if (final_state && w.chunk == chunks - 1 && threadIdx.x < 32 && w.on) {
             final_state[w.b * D + w.c] = state[0];
             if (even) final_state[w.b * D + w.c + 1] = state[1];
         }
     }
 }
-
-template <class T> struct RawBack { Pack<T, 2> x[kHalf], p[kHalf], q[kHalf], g[kHalf]; };
 
 template <class T, bool kPairs, bool kSummary>
 __global__ __launch_bounds__(kWaves * 64) void gated_backward_kernel(sig_gated_args a, sig_gated_grads g, const float* ckpt, float* sums, float* rates, int groups,
@@ -220,7 +289,6 @@ __global__ __launch_bounds__(kWaves * 64) void gated_backward_kernel(sig_gated_a
     const Where w = where(a, groups, chunks, rounds);
     const int wave = threadIdx.x / 64, half = (threadIdx.x >> 5) & 1, li = threadIdx.x & 31, D = (int)a.D;
     const bool even = kPairs || w.c + 1 < D;
-    const T *x = (const T*)a.x + w.b * a.x_stride_b, *p = (const T*)a.decay_gate + w.b * a.decay_stride_b, *q = (const T*)a.input_gate + w.b * a.input_stride_b;
     const T* gy = (const T*)g.grad_y + w.b * g.gy_stride_b;
     T *gx = (T*)g.grad_x + w.b * a.L * D, *gp = (T*)g.grad_decay_gate + w.b * a.L * D, *gq = (T*)g.grad_input_gate + w.b * a.L * D;
     const int c1 = even ? w.c + 1 : w.c;
@@ -239,34 +307,25 @@ __global__ __launch_bounds__(kWaves * 64) void gated_backward_kernel(sig_gated_a
     }
     const int end = min(w.last, w.live);
     const int64_t tiles = (a.L + kGatedTile - 1) / kGatedTile;
-    auto load = [&](int t0, RawBack<T>& r) {
-#pragma unroll
-        for (int k = 0; k < kHalf; k++) {
-            const int64_t t = min(t0 + k, end - 1);
-            r.p[k] = load_two<T, kPairs>(p + t * a.decay_stride_t, w.c, D);
-            r.g[k] = load_two<T, kPairs>(gy + t * g.gy_stride_t, w.c, D);
-            if constexpr (!kSummary) {
-                r.x[k] = load_two<T, kPairs>(x + t * a.x_stride_t, w.c, D);
-                r.q[k] = load_two<T, kPairs>(q + t * a.input_stride_t, w.c, D);
-            }
-        }
-    };
-    const int mine = wave * kGatedTile + half * kHalf;
+    const int mine = wave * kGatedTile + half * kHalf, e = sizeof(T);
+    const Lane l{(c1 - w.c) * e, (int)(mine * a.x_stride_t + w.c) * e, (int)(mine * a.decay_stride_t + w.c) * e, (int)(mine * a.input_stride_t + w.c) * e, (int)(mine * g.gy_stride_t + w.c) * e,
+                 w.on ? (mine * D + w.c) * e : kNowhere};
     const int many = (max(end - w.first, 0) + kRound - 1) / kRound;
     if constexpr (!kSummary) {
-        for (int t = w.first + many * kRound + (threadIdx.x >> 5); t < w.last; t += kWaves * 2)
-            if (w.on) {
-                store_two<T, kPairs>(gx + (int64_t)t * D, w.c, D, 0.0f, 0.0f);
-                store_two<T, kPairs>(gp + (int64_t)t * D, w.c, D, 0.0f, 0.0f);
-                store_two<T, kPairs>(gq + (int64_t)t * D, w.c, D, 0.0f, 0.0f);
+        for (int t = w.first + many * kRound; t < w.last; t += kRound)
+#pragma unroll
+            for (int k = 0; k < kHalf; k++) {
+                store_two<T, kPairs>(tokens(gx, D, t, w.last, D, e), l.out, l.second, k * D * e, 0, 0.0f, 0.0f);
+                store_two<T, kPairs>(tokens(gp, D, t, w.last, D, e), l.out, l.second, k * D * e, 0, 0.0f, 0.0f);
+                store_two<T, kPairs>(tokens(gq, D, t, w.last, D, e), l.out, l.second, k * D * e, 0, 0.0f, 0.0f);
             }
     }
-    RawBack<T> next;
-    if (many) load(w.first + (many - 1) * kRound + mine, next);
+    Raw<T> next;
+    if (many) load_round<T, kPairs, true>(a, gy, g.gy_stride_t, w, l, w.first + (many - 1) * kRound, end, !kSummary, next);
     int buf = 0;
     for (int r = w.first + (many - 1) * kRound; r >= w.first; r -= kRound, buf ^= 1) {
-        const RawBack<T> now = next;
-        if (r > w.first) load(r - kRound + mine, next);
+        Raw<T> now = next;
+        if (r > w.first) load_round<T, kPairs, true>(a, gy, g.gy_stride_t, w, l, r - kRound, end, !kSummary, next);
         const int t0 = r + mine;
         float at[2] = {};
         if constexpr (!kSummary) {
@@ -276,25 +335,38 @@ __global__ __launch_bounds__(kWaves * 64) void gated_backward_kernel(sig_gated_a
                 at[1] = from[c1];
             }
         }
-        Decay e[kHalf][2];
-        float A[2] = {1.0f, 1.0f}, H[2] = {}, C[2] = {}, fx[kHalf][2];
+        // of every token: its decay a, and what l is multiplied by in the gradients of x, q (both with b) and p; U = l (own - from h)
+        float d[kHalf][2], toward_x[kHalf][2], f[kHalf][2], toward_q[kHalf][2], shut[kHalf][2], own[kHalf][2], from[kHalf][2], A[2] = {1.0f, 1.0f}, H[2] = {}, C[2] = {};
 #pragma unroll
-        for (int k = 0; k < kHalf; k++)
+        for (int k = 0; k < kHalf; k++) {
+            __builtin_amdgcn_sched_barrier(0);      // a token's values are done before the next one's begin: all at once do not fit the registers
 #pragma unroll
             for (int j = 0; j < 2; j++) {
-                e[k][j] = decay(rate[j], sigmoid(to_float(now.p[k].v[j])));
-                const bool live = t0 + k < end;
-                if (!live) e[k][j] = {0.0f, 1.0f, 0.0f};
-                A[j] *= e[k][j].a;
+                const uint32_t mask = mask_of(t0 + k < end);
+                const Gate open = gate(value(now.p[k], j));
+                const Decay v = decay(rate[j], masked(open.s, mask));
+                d[k][j] = v.a;
+                A[j] *= d[k][j];
                 if constexpr (!kSummary) {
-                    fx[k][j] = live ? sigmoid(to_float(now.q[k].v[j])) * to_float(now.x[k].v[j]) : 0.0f;
-                    H[j] = fmaf(e[k][j].a, H[j], __builtin_amdgcn_sqrtf(e[k][j].w) * fx[k][j]);
+                    const Gate in = gate(value(now.q[k], j));
+                    const float rb = __builtin_amdgcn_rsqf(fmaxf(v.w, 1.1754944e-38f)), xi = masked(value(now.x[k], j) * in.s, mask);      // 1 / b
+                    toward_x[k][j] = here(v.w * rb * in.s);
+                    f[k][j] = here(v.w * rb * xi);
+                    toward_q[k][j] = here(in.rest);
+                    shut[k][j] = here(open.rest);
+                    own[k][j] = here(v.a * v.a * (v.u * rb) * xi);
+                    from[k][j] = here(v.a * v.u);
+                    H[j] = fmaf(d[k][j], H[j], f[k][j]);
                 }
             }
+        }
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int k = 0; k < kHalf; k++) now.g[k] = masked(now.g[k], mask_of(t0 + k < end));
 #pragma unroll
         for (int k = kHalf - 1; k >= 0; k--)
 #pragma unroll
-            for (int j = 0; j < 2; j++) C[j] = e[k][j].a * ((t0 + k < end ? to_float(now.g[k].v[j]) : 0.0f) + C[j]);
+            for (int j = 0; j < 2; j++) C[j] = d[k][j] * (value(now.g[k], j) + C[j]);
         float preA[2], preC[2], bothA[2], bothC[2], h[2];
 #pragma unroll
         for (int j = 0; j < 2; j++) {
@@ -326,37 +398,32 @@ __global__ __launch_bounds__(kWaves * 64) void gated_backward_kernel(sig_gated_a
             }
         }
         if constexpr (!kSummary) {
-            float before[kHalf][2], sum[2] = {};
+            float sum[2] = {};
 #pragma unroll
             for (int k = 0; k < kHalf; k++)
 #pragma unroll
                 for (int j = 0; j < 2; j++) {
-                    before[k][j] = h[j];
-                    h[j] = fmaf(e[k][j].a, h[j], __builtin_amdgcn_sqrtf(e[k][j].w) * fx[k][j]);
+                    own[k][j] = fmaf(-from[k][j], h[j], own[k][j]);
+                    h[j] = fmaf(d[k][j], h[j], f[k][j]);
                 }
             float c[2] = {fmaf(preA[0], start[0], preC[0]), fmaf(preA[1], start[1], preC[1])};
+            const __amdgpu_buffer_rsrc_t tx = tokens(gx, D, r, w.last, D, e), tp = tokens(gp, D, r, w.last, D, e), tq = tokens(gq, D, r, w.last, D, e);
 #pragma unroll
             for (int k = kHalf - 1; k >= 0; k--) {
                 float ox[2], op[2], oq[2];
-                const bool live = t0 + k < end;
+                const uint32_t mask = mask_of(t0 + k < end);
 #pragma unroll
                 for (int j = 0; j < 2; j++) {
-                    const Decay& v = e[k][j];
-                    const float l = to_float(now.g[k].v[j]) + c[j];
-                    const Gate i = gate(to_float(now.q[k].v[j])), s = gate(to_float(now.p[k].v[j]));
-                    const float rb = __builtin_amdgcn_rsqf(fmaxf(v.w, 1.1754944e-38f)), lb = l * (v.w * rb);      // 1 / b, and b l
-                    const float U = l * v.a * (v.u * rb * v.a * fx[k][j] - v.u * before[k][j]);
-                    ox[j] = live ? lb * i.s : 0.0f;
-                    oq[j] = live ? lb * fx[k][j] * i.rest : 0.0f;
-                    op[j] = live ? U * s.rest : 0.0f;
-                    sum[j] += live ? U : 0.0f;
-                    c[j] = live ? v.a * l : c[j];
+                    const float lam = value(now.g[k], j) + c[j], U = masked(lam * own[k][j], mask);
+                    ox[j] = lam * toward_x[k][j];
+                    oq[j] = lam * f[k][j] * toward_q[k][j];
+                    op[j] = U * shut[k][j];
+                    sum[j] += U;
+                    c[j] = d[k][j] * lam;
                 }
-                if (w.on && t0 + k < w.last) {
-                    store_two<T, kPairs>(gx + (int64_t)(t0 + k) * D, w.c, D, ox[0], ox[1]);
-                    store_two<T, kPairs>(gp + (int64_t)(t0 + k) * D, w.c, D, op[0], op[1]);
-                    store_two<T, kPairs>(gq + (int64_t)(t0 + k) * D, w.c, D, oq[0], oq[1]);
-                }
+                store_two<T, kPairs>(tx, l.out, l.second, k * D * e, mask, ox[0], ox[1]);
+                store_two<T, kPairs>(tp, l.out, l.second, k * D * e, mask, op[0], op[1]);
+                store_two<T, kPairs>(tq, l.out, l.second, k * D * e, mask, oq[0], oq[1]);
             }
             total[0] += sum[0];
             total[1] += sum[1];

@@ -22,13 +22,15 @@ typedef int Int8 __attribute__((ext_vector_type(8)));
 
 constexpr int kSlab = 128, kChunk = 16, kChunks = kSlab / kChunk;      // bytes; bytes; chunks of a slab
 
+struct Tiles { int64_t M, N, K; int m, n, splits; int64_t slabs; int tile; };            // tiles along m and n; slabs of a split; edge of a tile
+
 struct Out {                            // what becomes of a sum
     const void *bias, *residual;
     int64_t residual_stride;
     const float *x_scale, *weight_scale;
     void *y, *pre;
     int act;
-    bool vec;                           // four neighbouring outputs are one access everywhere
+    bool vec;                           // 16 bytes of neighbouring outputs are one access everywhere
 };
 
 // f and f': the normal distribution's Phi by the error function
@@ -47,60 +49,95 @@ __device__ __forceinline__ float slope_of(float z, int act)
     return 0.5f * (1.0f + erff(z * 0.70710678f)) + z * fast_exp(-0.5f * z * z) * 0.39894228f;
 }
 
-template <class O> __device__ __forceinline__ void finish(const Out& o, int64_t m, int64_t n, int64_t N, Acc v)
+// What becomes of V neighbouring sums of row m from output n on
+template <class O, int V> __device__ __forceinline__ void finish(const Out& o, int64_t m, int64_t n, int64_t N, float* z)
 {
-    const bool all = n + 4 <= N;
+    const bool wide = o.vec && n + V <= N;
     const int64_t at = m * N + n;
-    float z[4] = {v[0], v[1], v[2], v[3]}, b[4], r[4];
     auto take = [&](const O* p, float* to) {
-        if (o.vec && all) {
-            const Pack<O, 4> q = *(const Pack<O, 4>*)p;
+        if (wide) {
+            const Pack<O, V> q = *(const Pack<O, V>*)p;
 #pragma unroll
-            for (int j = 0; j < 4; j++) to[j] = to_float(q.v[j]);
+            for (int j = 0; j < V; j++) to[j] = to_float(q.v[j]);
         } else
 #pragma unroll
-            for (int j = 0; j < 4; j++) to[j] = n + j < N ? to_float(p[j]) : 0.0f;
+            for (int j = 0; j < V; j++) to[j] = n + j < N ? to_float(p[j]) : 0.0f;
     };
     auto give = [&](O* p, const float* from) {
-        if (o.vec && all) {
-            Pack<O, 4> q;
+        if (wide) {
+            Pack<O, V> q;
 #pragma unroll
-            for (int j = 0; j < 4; j++) q.v[j] = from_float<O>(from[j]);
-            *(Pack<O, 4>*)p = q;
+            for (int j = 0; j < V; j++) q.v[j] = from_float<O>(from[j]);
+            *(Pack<O, V>*)p = q;
         } else
 #pragma unroll
-            for (int j = 0; j < 4; j++)
+            for (int j = 0; j < V; j++)
                 if (n + j < N) p[j] = from_float<O>(from[j]);
     };
-    const float xs = o.x_scale ? o.x_scale[m] : 1.0f;
-    if (o.x_scale || o.weight_scale)
+    float b[V], r[V];
+    if (o.x_scale || o.weight_scale) {
+        const float xs = o.x_scale ? o.x_scale[m] : 1.0f;
 #pragma unroll
-        for (int j = 0; j < 4; j++) z[j] = z[j] * xs * (o.weight_scale ? o.weight_scale[min(n + j, N - 1)] : 1.0f);
+        for (int j = 0; j < V; j++) z[j] = z[j] * xs * (o.weight_scale ? o.weight_scale[min(n + j, N - 1)] : 1.0f);
+    }
     if (o.bias) {
         take((const O*)o.bias + n, b);
 #pragma unroll
-        for (int j = 0; j < 4; j++) z[j] += b[j];
+        for (int j = 0; j < V; j++) z[j] += b[j];
     }
     if (o.pre) give((O*)o.pre + at, z);
+    if (o.act == SIG_ACT_SILU) {
 #pragma unroll
-    for (int j = 0; j < 4; j++) z[j] = act_of(z[j], o.act);
+        for (int j = 0; j < V; j++) z[j] = act_of(z[j], SIG_ACT_SILU);
+    } else if (o.act == SIG_ACT_GELU)
+#pragma unroll
+        for (int j = 0; j < V; j++) z[j] = act_of(z[j], SIG_ACT_GELU);
     if (o.residual) {
         take((const O*)o.residual + m * o.residual_stride + n, r);
 #pragma unroll
-        for (int j = 0; j < 4; j++) z[j] += r[j];
+        for (int j = 0; j < V; j++) z[j] += r[j];
     }
     give((O*)o.y + at, z);
 }
 
-template <class T> struct alignas(sizeof(T)) Loose { T v[kChunk / sizeof(T)]; } __attribute__((packed));
+// The sums of a wavefront's tile, 16 FM tokens by 16 FN outputs, to where they belong.  A lane holds four outputs of sixteen tokens' rows; 16 rows at a
+// time go through LDS (4 KB and a little a wavefront, its own), after which neighbouring lanes hold neighbouring outputs and a row is whole lines.
+template <class O, int FM, int FN> __device__ __forceinline__ void put(const Tiles& t, const Out& o, float* parts, int split, int64_t m0, int64_t n0, Acc (&acc)[FN][FM], float* lds)
+{
+    constexpr int V = 16 / sizeof(O), kWide = FN * 16, kPitch = kWide + 4, kLanes = kWide / V, kRows = 64 / kLanes;
+    const int lane = threadIdx.x & 63, c = lane % kLanes * V;
+    const int64_t N4 = (t.N + 3) / 4 * 4, n = n0 + c;
+#pragma unroll
+    for (int j = 0; j < FM; j++) {
+#pragma unroll
+        for (int i = 0; i < FN; i++) *(Acc*)(lds + (lane & 15) * kPitch + i * 16 + lane / 16 * 4) = acc[i][j];
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll
+        for (int r = 0; r < 16; r += kRows) {
+            const int row = r + lane / kLanes;
+            const int64_t m = m0 + j * 16 + row;
+            float z[V];
+#pragma unroll
+            for (int k = 0; k < V; k += 4) *(Acc*)(z + k) = *(const Acc*)(lds + row * kPitch + c + k);
+            if (m < t.M && n < t.N) {
+                if (t.splits > 1) {
+                    float* to = parts + ((int64_t)split * t.M + m) * N4 + n;
+#pragma unroll
+                    for (int k = 0; k < V; k += 4)
+                        if (n + k < N4) *(Acc*)(to + k) = *(const Acc*)(z + k);
+                } else finish<O, V>(o, m, n, t.N, z);
+            }
+        }
+        __builtin_amdgcn_wave_barrier();
+    }
+}
 
 // 16 bytes of a row from element k on, zeros from element K on
-template <class T> __device__ __forceinline__ Chunk take_chunk(const T* row, int64_t k, int64_t K, bool aligned)
+template <class T> __device__ __forceinline__ Chunk take_chunk(const T* row, int64_t k, int64_t K)
 {
     constexpr int E = kChunk / sizeof(T);
     Chunk c;
     if (k + E <= K) {
-        if (aligned) return *(const Chunk*)(row + k);
         __builtin_memcpy(&c, row + k, kChunk);
         return c;
     }
@@ -114,28 +151,33 @@ template <class T> __device__ __forceinline__ Chunk take_chunk(const T* row, int
     return c;
 }
 
-// Sum over the contraction of 16 x 16 products: one chunk a lane of each operand (e4m3: two)
-template <class T> __device__ __forceinline__ Acc products(const Chunk* w, const Chunk* x, Acc acc)
+// Sums over the contraction of 16 x 16 products, one chunk a lane of each operand (e4m3: two).  float32 takes four instructions a pair of chunks: all
+// pairs' first ones come first, so that none waits for the one before.
+template <class T, int FN, int FM, int F> __device__ __forceinline__ void products(const Chunk (&w)[FN][F], const Chunk (&x)[FM][F], Acc (&acc)[FN][FM])
 {
-    if constexpr (std::is_same_v<T, bf16>) {
-        Bf8 a, b;
-        __builtin_memcpy(&a, w, 16);
-        __builtin_memcpy(&b, x, 16);
-        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, acc, 0, 0, 0);
-    } else if constexpr (std::is_same_v<T, float>) {
 #pragma unroll
-        for (int j = 0; j < 4; j++) acc = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float((*w)[j]), __uint_as_float((*x)[j]), acc, 0, 0, 0);
-        return acc;
-    } else {
-        Int8 a, b;
-        __builtin_memcpy(&a, w, 32);
-        __builtin_memcpy(&b, x, 32);
-        return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, acc, 0, 0, 0, 0x7f7f7f7f, 0, 0x7f7f7f7f);     // block scales of one
-    }
+    for (int q = 0; q < (std::is_same_v<T, float> ? 4 : 1); q++)
+#pragma unroll
+        for (int j = 0; j < FM; j++)
+#pragma unroll
+            for (int i = 0; i < FN; i++) {
+                if constexpr (std::is_same_v<T, float>) {
+                    acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(w[i][0][q]), __uint_as_float(x[j][0][q]), acc[i][j], 0, 0, 0);
+                } else if constexpr (std::is_same_v<T, bf16>) {
+                    Bf8 a, b;
+                    __builtin_memcpy(&a, w[i], 16);
+                    __builtin_memcpy(&b, x[j], 16);
+                    acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, acc[i][j], 0, 0, 0);
+                } else {
+                    Int8 a, b;
+                    __builtin_memcpy(&a, w[i], 32);
+                    __builtin_memcpy(&b, x[j], 32);
+                    acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, acc[i][j], 0, 0, 0, 0x7f7f7f7f, 0, 0x7f7f7f7f);     // block scales of one
+                }
+            }
 }
 template <class T> constexpr int kFeed = std::is_same_v<T, e4m3> ? 2 : 1;       // chunks of a row that a step takes
 
-struct Tiles { int64_t M, N, K; int m, n, splits; int64_t slabs; };            // tiles along m and n; slabs of a split
 
 // Workgroups are dealt out to the eight dies in turn: each die gets a run of neighbouring tiles, walked in bands of eight along m
 struct Place { int m, n, split; };
@@ -152,7 +194,7 @@ __device__ __forceinline__ Place place_of(const Tiles& t)
 constexpr int kTile = 128;
 
 // A workgroup's tile is 128 tokens by 128 outputs, 64 by 64 a wavefront.
-template <class T, class O> __global__ __launch_bounds__(256) void product_kernel(Tiles t, const T* x, int64_t ldx, const T* w, int64_t ldw, bool aligned, Out o, float* parts)
+template <class T, class O> __global__ __launch_bounds__(256) void product_kernel(Tiles t, const T* x, int64_t ldx, const T* w, int64_t ldw, Out o, float* parts)
 {
     constexpr int E = kChunk / sizeof(T), kLoads = kTile * kChunks / 256;
     __shared__ Chunk lds[2][2][kTile * kChunks];
@@ -166,8 +208,8 @@ template <class T, class O> __global__ __launch_bounds__(256) void product_kerne
         for (int i = 0; i < kLoads; i++) {
             const int id = threadIdx.x + i * 256, row = id / kChunks;
             const int64_t e = k + (id % kChunks) * E;
-            rx[i] = take_chunk(x + min(m0 + row, t.M - 1) * ldx, e, last, aligned);
-            rw[i] = take_chunk(w + min(n0 + row, t.N - 1) * ldw, e, last, aligned);
+            rx[i] = take_chunk(x + min(m0 + row, t.M - 1) * ldx, e, last);
+            rw[i] = take_chunk(w + min(n0 + row, t.N - 1) * ldw, e, last);
         }
     };
     auto keep = [&](int buf) {
@@ -198,26 +240,86 @@ template <class T, class O> __global__ __launch_bounds__(256) void product_kerne
                     fx[i][f] = lds[buf][0][(wm * 64 + row) * kChunks + (c ^ (row & 7))];
                     fw[i][f] = lds[buf][1][(wn * 64 + row) * kChunks + (c ^ (row & 7))];
                 }
-#pragma unroll
-            for (int i = 0; i < 4; i++)
-#pragma unroll
-                for (int j = 0; j < 4; j++) acc[i][j] = products<T>(fw[i], fx[j], acc[i][j]);
+            products<T>(fw, fx, acc);
         }
         if (more) keep(buf ^ 1);
         __syncthreads();
     }
+    put<O, 4, 4>(t, o, parts, p.split, m0 + wm * 64, n0 + wn * 64, acc, (float*)lds + wave * 16 * 68);
+}
+
+// One slab of N rows a thread, 16 bytes of each, into LDS; `step` threads lie between a thread's rows
+template <int N> __device__ __forceinline__ void fetch(__amdgpu_buffer_rsrc_t from, __attribute__((address_space(3))) Chunk* to, int step, const int* rows, int at, int k)
+{
 #pragma unroll
-    for (int j = 0; j < 4; j++) {
-        const int64_t m = m0 + wm * 64 + j * 16 + (lane & 15);
-        if (m >= t.M) continue;
+    for (int i = 0; i < N; i++) __builtin_amdgcn_raw_ptr_buffer_load_lds(from, to + i * step, 16, rows[i] + at, k, 0, 0);
+}
+
+// ---- the same for operands whose rows are multiples of 16 bytes, 16-byte aligned: chunks go from memory to LDS without passing registers.
+// A wavefront's load fills 1,024 bytes of LDS in lane order, so lane l of row r fetches chunk (l ^ r) & 7.
+template <class T, class O, int BM, int BN, int WM, int WN, int kStages>
+__global__ __launch_bounds__(WM * WN * 64) void aligned_kernel(Tiles t, const T* x, int64_t ldx, const T* w, int64_t ldw, Out o, float* parts)
+{
+    constexpr int kThreads = WM * WN * 64, FM = BM / WM / 16, FN = BN / WN / 16, E = kChunk / sizeof(T), kStep = kSlab / sizeof(T);
+    constexpr int kStage = (BM + BN) * kChunks, LX = BM * kChunks / kThreads, LW = BN * kChunks / kThreads;
+    extern __shared__ Chunk lds[];                                             // [kStages][BM rows of x, BN rows of weight][kChunks]
+    const Place p = place_of(t);
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), wm = wave % WM, wn = wave / WM;
+    const int64_t m0 = (int64_t)p.m * BM, n0 = (int64_t)p.n * BN;
+    const int first = (int)(p.split * t.slabs), last = (int)min((int64_t)((t.K + kStep - 1) / kStep), first + t.slabs);
+    const __amdgpu_buffer_rsrc_t bx = __builtin_amdgcn_make_buffer_rsrc((void*)(x + m0 * ldx), 0, 0x7fffffff, 0x27000);
+    const __amdgpu_buffer_rsrc_t bw = __builtin_amdgcn_make_buffer_rsrc((void*)(w + n0 * ldw), 0, 0x7fffffff, 0x27000);
+    // rows beyond the last are the last one again, chunks beyond the end of a row its slab's first (they become zeros in LDS)
+    const int place = threadIdx.x / kChunks, chunk = (threadIdx.x ^ place) & 7;
+    int ox[LX], ow[LW];
 #pragma unroll
-        for (int i = 0; i < 4; i++) {
-            const int64_t n = n0 + wn * 64 + i * 16 + (lane / 16) * 4;
-            if (n >= t.N) continue;
-            if (t.splits > 1) *(Acc*)(parts + ((int64_t)p.split * t.M + m) * ((t.N + 3) / 4 * 4) + n) = acc[i][j];
-            else finish<O>(o, m, n, t.N, acc[i][j]);
+    for (int i = 0; i < LX; i++) ox[i] = (int)(min((int64_t)(place + i * (kThreads / kChunks)), t.M - 1 - m0) * ldx * (int)sizeof(T));
+#pragma unroll
+    for (int i = 0; i < LW; i++) ow[i] = (int)(min((int64_t)(place + i * (kThreads / kChunks)), t.N - 1 - n0) * ldw * (int)sizeof(T));
+    auto* base = (__attribute__((address_space(3))) Chunk*)lds + wave * 64;
+    auto inside = [&](int slab) { return (int64_t)slab * kStep + chunk * E < t.K ? chunk * kChunk : 0; };
+    Acc acc[FN][FM] = {};
+#pragma unroll
+    for (int s = 0; s < kStages - 1; s++)
+        if (first + s < last) {
+            fetch<LX>(bx, base + s * kStage, kThreads, ox, inside(first + s), (first + s) * kSlab);
+            fetch<LW>(bw, base + s * kStage + BM * kChunks, kThreads, ow, inside(first + s), (first + s) * kSlab);
         }
+    int stage = 0;
+    for (int s = first; s < last; s++) {
+        // this slab has landed, and nobody reads the stage that is loaded next any more
+        if (kStages > 2 && s + kStages - 2 < last) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((kStages - 2) * (LX + LW)) : "memory");
+        else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        if (const int next = s + kStages - 1; next < last) {
+            auto* to = base + (stage == 0 ? kStages - 1 : stage - 1) * kStage;
+            fetch<LX>(bx, to, kThreads, ox, inside(next), next * kSlab);
+            fetch<LW>(bw, to + BM * kChunks, kThreads, ow, inside(next), next * kSlab);
+        }
+        Chunk* in = lds + stage * kStage;
+        if ((int64_t)(s + 1) * kStep > t.K) {                                  // zeros behind the end of the rows
+            const int there = (int)((t.K - (int64_t)s * kStep) / E);
+            for (int id = threadIdx.x; id < kStage; id += kThreads)
+                if (((id ^ (id / kChunks)) & 7) >= there) in[id] = Chunk{};
+            asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        }
+        constexpr int F = kFeed<T>;
+#pragma unroll
+        for (int c = 0; c < kChunks / 4; c += F) {
+            Chunk fx[FM][F], fw[FN][F];
+#pragma unroll
+            for (int f = 0; f < F; f++) {
+                const int at = ((c + f) * 4 + lane / 16) ^ (lane & 7);
+#pragma unroll
+                for (int i = 0; i < FN; i++) fw[i][f] = in[(BM + wn * (BN / WN) + i * 16 + (lane & 15)) * kChunks + at];
+#pragma unroll
+                for (int j = 0; j < FM; j++) fx[j][f] = in[(wm * (BM / WM) + j * 16 + (lane & 15)) * kChunks + at];
+            }
+            products<T>(fw, fx, acc);
+        }
+        stage = stage == kStages - 1 ? 0 : stage + 1;
     }
+    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    put<O, FM, FN>(t, o, parts, p.split, m0 + wm * (BM / WM), n0 + wn * (BN / WN), acc, (float*)lds + wave * 16 * (FN * 16 + 4));
 }
 
 // The splits' sums, added up in order, and what becomes of them
@@ -227,7 +329,8 @@ template <class O> __global__ __launch_bounds__(256) void join_kernel(Tiles t, O
     if (id >= t.M * quads) return;
     Acc v = *(const Acc*)(parts + id * 4);
     for (int s = 1; s < t.splits; s++) v += *(const Acc*)(parts + (s * t.M * quads + id) * 4);
-    finish<O>(o, id / quads, id % quads * 4, t.N, v);
+    float z[4] = {v[0], v[1], v[2], v[3]};
+    finish<O, 4>(o, id / quads, id % quads * 4, t.N, z);
 }
 
 // [R, C] to [C, padded R], zeros behind R.  pre: the gradient that comes in is multiplied by the activation's slope first, rounded to T, and kept
@@ -269,30 +372,76 @@ template <class T> __global__ __launch_bounds__(1024) void bias_kernel(const flo
     if (threadIdx.x < 64 && c < N) grad_bias[c] = from_float<T>(s);
 }
 
-Tiles tiles_of(int64_t M, int64_t N, int64_t K, int e)
+// ---- which tile, and how many splits.  A model of the launch, in us: `slab` is what a tile's slab costs a compute unit that is busy with as many
+// as it holds, `alone` what it costs at least, `over` what a tile costs besides (first loads, outputs).  Measured on large squares (us a slab):
+//   bfloat16 256: 8192^3 in 871 us, 128: 1,033 us     float32 256: 4096^3 in 981, 128: 998, 64: 1,040     e4m3 256: 8192^3 in 478, 128: 556
+// and 16384 x 4096 x 1024 (16 slabs): 159 us with tiles of 256, 167 of 128.
+struct Cost { int tile; double slab, alone, over; };
+constexpr Cost kCosts[3][3] = {
+    {{64, 0.51, 0.70, 1.0}, {128, 1.95, 1.95, 3.0}, {256, 7.66, 7.66, 14.0}},          // float32
+    {{64, 0.17, 0.50, 0.8}, {128, 0.50, 0.80, 2.4}, {256, 1.70, 1.70, 12.0}},          // bfloat16
+    {{64, 0.18, 0.50, 0.8}, {128, 0.54, 0.80, 1.2}, {256, 1.87, 1.87, 9.7}},           // e4m3
+};
+constexpr int kUnits = 256;                                                            // compute units
+
+Tiles tiles_of(int64_t M, int64_t N, int64_t K, int e, bool aligned)
 {
-    Tiles t{M, N, K, (int)((M + kTile - 1) / kTile), (int)((N + kTile - 1) / kTile), 1, 0};
-    const int64_t slabs = std::max<int64_t>(1, (K * e + kSlab - 1) / kSlab), tiles = (int64_t)t.m * t.n;
-    int64_t splits = 1;
-    if (tiles && tiles < 256) splits = std::max<int64_t>(1, std::min<int64_t>({512 / tiles, slabs / 8, 32}));
-    t.slabs = (slabs + splits - 1) / splits;
-    t.splits = (int)((slabs + t.slabs - 1) / t.slabs);
-    return t;
+    const int64_t slabs = std::max<int64_t>(1, (K * e + kSlab - 1) / kSlab);
+    Tiles best{};
+    double least = 0.0;
+    for (const Cost& c : kCosts[e == 4 ? 0 : e == 2 ? 1 : 2]) {
+        if (!aligned && c.tile != kTile) continue;
+        const int64_t m = (M + c.tile - 1) / c.tile, n = (N + c.tile - 1) / c.tile;
+        for (int64_t want : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32}) {
+            if (want > 1 && slabs / want < 4) break;
+            const int64_t each = (slabs + want - 1) / want, splits = (slabs + each - 1) / each, rows = (m * n * splits + kUnits - 1) / kUnits;
+            double us = (double)each * std::max(rows * c.slab, c.alone) + rows * c.over;
+            if (splits > 1) us += 4.0 + (double)M * N * 4.0 * (splits + 1) / 3e6;     // the sums, written and read again
+            if (best.tile == 0 || us < least) {
+                least = us;
+                best = Tiles{M, N, K, (int)m, (int)n, (int)splits, each, c.tile};
+            }
+        }
+    }
+    return best;
 }
 size_t parts_bytes(const Tiles& t) { return t.splits > 1 ? (size_t)t.splits * t.M * ((t.N + 3) / 4 * 4) * 4 : 0; }
+// for either alignment: it may not be known yet
+size_t parts_bytes(int64_t M, int64_t N, int64_t K, int e) { return std::max(parts_bytes(tiles_of(M, N, K, e, false)), parts_bytes(tiles_of(M, N, K, e, true))); }
 
-template <class T, class O> hipError_t product(const Tiles& t, const T* x, int64_t ldx, const T* w, int64_t ldw, Out o, float* parts, hipStream_t stream)
+template <class T, class O, int kSize, int WM, int WN> hipError_t launch(const Tiles& t, const T* x, int64_t ldx, const T* w, int64_t ldw, const Out& o, float* parts, uint32_t blocks, hipStream_t stream)
 {
-    const int64_t blocks = (int64_t)t.m * t.n * t.splits, e = sizeof(T);
-    if (!launchable(blocks, 256)) return kTooManyThreads;
-    const bool aligned = (uintptr_t)x % 16 == 0 && (uintptr_t)w % 16 == 0 && ldx * e % 16 == 0 && ldw * e % 16 == 0;
-    const int q = 4 * sizeof(O);
-    auto fits = [&](const void* p) { return (uintptr_t)p % q == 0; };
-    o.vec = t.N % 4 == 0 && o.residual_stride % 4 == 0 && fits(o.bias) && fits(o.residual) && fits(o.y) && fits(o.pre);
-    product_kernel<T, O><<<(uint32_t)blocks, 256, 0, stream>>>(t, x, ldx, w, ldw, aligned, o, parts);
-    hipError_t err = hipGetLastError();
+    constexpr int kStages = 2, kLds = kStages * 2 * kSize * kSlab;
+    auto kernel = aligned_kernel<T, O, kSize, kSize, WM, WN, kStages>;
+    if (kLds > 64 * 1024) {
+        hipError_t err = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, kLds);
+        if (err != hipSuccess) return err;
+    }
+    kernel<<<blocks, WM * WN * 64, kLds, stream>>>(t, x, ldx, w, ldw, o, parts);
+    return hipGetLastError();
+}
+
+template <class T, class O> hipError_t product(int64_t M, int64_t N, int64_t K, const T* x, int64_t ldx, const T* w, int64_t ldw, Out o, float* parts, hipStream_t stream)
+{
+    constexpr int V = 16 / sizeof(O);
+    const int64_t e = sizeof(T);
+    // whole chunks only; a tile's rows and the contraction are reached by 32-bit offsets
+    const bool aligned = (uintptr_t)x % 16 == 0 && (uintptr_t)w % 16 == 0 && ldx * e % 16 == 0 && ldw * e % 16 == 0 && K * e % 16 == 0 && K > 0 &&
+                         256 * std::max(ldx, ldw) * e + K * e < (1ll << 31);
+    const Tiles t = tiles_of(M, N, K, (int)e, aligned);
+    const int64_t blocks = (int64_t)t.m * t.n * t.splits;
+    if (!launchable(blocks, 512)) return kTooManyThreads;
+    auto fits = [&](const void* p) { return (uintptr_t)p % 16 == 0; };
+    o.vec = N % V == 0 && o.residual_stride % V == 0 && fits(o.bias) && fits(o.residual) && fits(o.y) && fits(o.pre);
+    hipError_t err;
+    if (!aligned) {
+        product_kernel<T, O><<<(uint32_t)blocks, 256, 0, stream>>>(t, x, ldx, w, ldw, o, parts);
+        err = hipGetLastError();
+    } else if (t.tile == 256) err = launch<T, O, 256, 4, 2>(t, x, ldx, w, ldw, o, parts, (uint32_t)blocks, stream);
+    else if (t.tile == 128) err = launch<T, O, 128, 2, 2>(t, x, ldx, w, ldw, o, parts, (uint32_t)blocks, stream);
+    else err = launch<T, O, 64, 2, 2>(t, x, ldx, w, ldw, o, parts, (uint32_t)blocks, stream);
     if (err != hipSuccess || t.splits == 1) return err;
-    const int64_t joins = (t.M * ((t.N + 3) / 4) + 255) / 256;
+    const int64_t joins = (M * ((N + 3) / 4) + 255) / 256;
     if (!launchable(joins, 256)) return kTooManyThreads;
     join_kernel<O><<<(uint32_t)joins, 256, 0, stream>>>(t, o, parts);
     return hipGetLastError();
@@ -303,7 +452,7 @@ int64_t round_up(int64_t v, int64_t to) { return (v + to - 1) / to * to; }
 
 // What the gradient keeps in its workspace, in bytes from its start
 struct Keep {
-    Tiles gx, gw;                       // grad_x = g weight, contraction N; grad_weight = g^T x, contraction M
+    // grad_x = g weight, contraction N; grad_weight = g^T x, contraction M
     int64_t padN, padM;
     size_t flat, turned_g, turned_w, turned_x, sums, parts, all;
 };
@@ -313,8 +462,6 @@ Keep keep_of(const sig_linear_args& a)
     const int e = bytes_of(a.dtype);
     k.padN = round_up(a.N, 64);
     k.padM = round_up(a.M, 64);
-    k.gx = tiles_of(a.M, a.K, a.N, e);
-    k.gw = tiles_of(a.N, a.K, a.M, e);
     size_t at = 0;
     auto take = [&](int64_t n) {
         size_t was = at;
@@ -326,7 +473,7 @@ Keep keep_of(const sig_linear_args& a)
     k.turned_w = take(a.K * k.padN * e);
     k.turned_x = take(a.K * k.padM * e);
     k.sums = take((a.M + 63) / 64 * a.N * 4);
-    k.parts = take((int64_t)std::max(parts_bytes(k.gx), parts_bytes(k.gw)));
+    k.parts = take((int64_t)std::max(parts_bytes(a.M, a.K, a.N, e), parts_bytes(a.N, a.K, a.M, e)));
     k.all = at;
     return k;
 }
@@ -355,13 +502,13 @@ template <class T> hipError_t backward_of(const sig_linear_args& a, const T* gy,
         err = turn<T>((const T*)a.weight, a.K, a.N, a.K, nullptr, 0, nullptr, turned_w, k.padN, nullptr, stream);
         Out o{};
         o.y = gx;
-        if (err == hipSuccess) err = product<T, T>(k.gx, pre ? flat : gy, pre ? a.N : ld, turned_w, k.padN, o, parts, stream);
+        if (err == hipSuccess) err = product<T, T>(a.M, a.K, a.N, pre ? flat : gy, pre ? a.N : ld, turned_w, k.padN, o, parts, stream);
     }
     if (err == hipSuccess && gw) {
         err = turn<T>((const T*)a.x, a.x_stride, a.M, a.K, nullptr, 0, nullptr, turned_x, k.padM, nullptr, stream);
         Out o{};
         o.y = gw;
-        if (err == hipSuccess) err = product<T, T>(k.gw, turned_g, k.padM, turned_x, k.padM, o, parts, stream);
+        if (err == hipSuccess) err = product<T, T>(a.N, a.K, a.M, turned_g, k.padM, turned_x, k.padM, o, parts, stream);
     }
     return err;
 }
@@ -369,12 +516,12 @@ template <class T> hipError_t backward_of(const sig_linear_args& a, const T* gy,
 template <class T, class O> hipError_t forward_of(const sig_linear_args& a, void* y, void* pre, float* parts, hipStream_t stream)
 {
     const Out o{a.bias, a.residual, a.residual_stride, a.x_scale, a.weight_scale, y, pre, (int)a.act, false};
-    return product<T, O>(tiles_of(a.M, a.N, a.K, sizeof(T)), (const T*)a.x, a.x_stride, (const T*)a.weight, a.K, o, parts, stream);
+    return product<T, O>(a.M, a.N, a.K, (const T*)a.x, a.x_stride, (const T*)a.weight, a.K, o, parts, stream);
 }
 
 }  // namespace
 
-size_t linear_forward_workspace(const sig_linear_args& a) { return parts_bytes(tiles_of(a.M, a.N, a.K, bytes_of(a.dtype))); }
+size_t linear_forward_workspace(const sig_linear_args& a) { return parts_bytes(a.M, a.N, a.K, bytes_of(a.dtype)); }
 hipError_t linear_forward(const sig_linear_args& a, void* y, void* pre, void* workspace, hipStream_t stream)
 {
     float* parts = (float*)workspace;

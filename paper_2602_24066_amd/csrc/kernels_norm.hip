@@ -47,12 +47,23 @@ template <class T, int V> __device__ __forceinline__ void store(T* p, const floa
     *(Pack<T, V>*)p = r;
 }
 
-struct Scaled { float scale, times; };
+// A row's scale, and its values over it: v 448 / top.  The quotient is corrected once, so that one that float32 holds is met: quotients of bfloat16 values
+// lie on the borders between two values of e4m3 now and then, and ties go to even.
+struct Scaled {
+    float scale, up, times, top;
+    __device__ __forceinline__ float of(float v) const
+    {
+        const float t = v * times;
+        return fmaf(fmaf(-t, top, v * up), times * (1.0f / 448.0f), t);
+    }
+};
 __device__ __forceinline__ Scaled scale_of(float top)
 {
-    // 448 / top would overflow where top is tiny; 2^126 takes such values to at most 128
-    if (top > 0.0f && top < 0x1p-119f) return {0x1p-126f, 0x1p126f};
-    return {top / 448.0f, top == 0.0f ? 1.0f : 448.0f / top};
+    // 448 / top would overflow where top is tiny; 2^126 takes such values to at most 128.  Products with 448 stay finite below 2^100.
+    if (top == 0.0f) return {0.0f, 1.0f, 1.0f, 1.0f};
+    if (top < 0x1p-100f) return top < 0x1p-119f ? Scaled{0x1p-126f, 0.0f, 0x1p126f, 0.0f} : Scaled{top / 448.0f, 0.0f, 448.0f / top, 0.0f};
+    if (!(top < 0x1p100f)) return {top / 448.0f, 0.0f, 448.0f / top, 0.0f};
+    return {top / 448.0f, 448.0f, 448.0f / top, top};
 }
 
 // T: type of x, residual and total; O: of y.  V elements an access, N accesses of a thread, kThreads threads a row (64: four rows a workgroup).
@@ -90,13 +101,13 @@ __global__ __launch_bounds__(kThreads == 64 ? 256 : kThreads) void norm_kernel(s
             }
         }
     }
-    float top = 0.0f;
+    float top = 0.0f, s = 1.0f;
     if constexpr (kNorm) {
 #pragma unroll
         for (int i = 0; i < N; i++)
 #pragma unroll
             for (int j = 0; j < V; j++) sum = fmaf(v[i][j], v[i][j], sum);
-        const float s = rsqrtf(over_row<kThreads, false>(sum) / (float)C + (float)a.eps);
+        s = rsqrtf(over_row<kThreads, false>(sum) / (float)C + (float)a.eps);
 #pragma unroll
         for (int i = 0; i < N; i++) {
             const int c = (i * kThreads + lane) * V;
@@ -104,7 +115,7 @@ __global__ __launch_bounds__(kThreads == 64 ? 256 : kThreads) void norm_kernel(s
             float w[V];
             load<float, V>(a.weight + c, w);
 #pragma unroll
-            for (int j = 0; j < V; j++) v[i][j] = v[i][j] * s * w[j];
+            for (int j = 0; j < V; j++) v[i][j] = kEight ? v[i][j] * w[j] : v[i][j] * s * w[j];     // in 8 bits the row's factor goes into its scale
         }
     }
     if constexpr (kEight) {
@@ -113,11 +124,11 @@ __global__ __launch_bounds__(kThreads == 64 ? 256 : kThreads) void norm_kernel(s
 #pragma unroll
             for (int j = 0; j < V; j++) top = top > fabsf(v[i][j]) || top != top ? top : fabsf(v[i][j]);
         const Scaled q = scale_of(over_row<kThreads, true>(top));
-        if (lane == 0) scale[row] = q.scale;
+        if (lane == 0) scale[row] = q.scale * s;
 #pragma unroll
         for (int i = 0; i < N; i++)
 #pragma unroll
-            for (int j = 0; j < V; j++) v[i][j] *= q.times;
+            for (int j = 0; j < V; j++) v[i][j] = q.of(v[i][j]);
     }
 #pragma unroll
     for (int i = 0; i < N; i++) {
@@ -146,8 +157,8 @@ template <class T, class O, bool kNorm> __global__ __launch_bounds__(1024) void 
         }
         s = rsqrtf(over_row<1024, false>(sum) / (float)C + (float)a.eps);
     }
-    auto out = [&](int64_t c) { return kNorm ? at(c) * s * a.weight[c] : at(c); };
-    Scaled q{1.0f, 1.0f};
+    auto out = [&](int64_t c) { return !kNorm ? at(c) : kEight ? at(c) * a.weight[c] : at(c) * s * a.weight[c]; };
+    Scaled q{};
     if constexpr (kEight) {
         float top = 0.0f;
         for (int64_t c = threadIdx.x; c < C; c += 1024) {
@@ -155,9 +166,9 @@ template <class T, class O, bool kNorm> __global__ __launch_bounds__(1024) void 
             top = top > v || top != top ? top : v;
         }
         q = scale_of(over_row<1024, true>(top));
-        if (threadIdx.x == 0) scale[row] = q.scale;
+        if (threadIdx.x == 0) scale[row] = q.scale * s;
     }
-    for (int64_t c = threadIdx.x; c < C; c += 1024) y[row * C + c] = from_float<O>(kEight ? out(c) * q.times : out(c));
+    for (int64_t c = threadIdx.x; c < C; c += 1024) y[row * C + c] = from_float<O>(kEight ? q.of(out(c)) : out(c));
 }
 
 template <class T, int V, int N, int kThreads>

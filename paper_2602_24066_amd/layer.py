@@ -20,6 +20,7 @@ _GATED = struct.Struct("16q")
 _GATED_GRADS = struct.Struct("9q")
 _ACTS = {None: 0, "silu": 1, "gelu": 2}
 _MOST_STRIDE = 1 << 38
+_REACH = 1 << 22                                             # time strides from there on are copied away: the recurrence's kernels do not reach them
 
 
 def _start(x, name="x"):
@@ -207,9 +208,9 @@ def _gated_args(x, decay_gate, input_gate, log_rate, initial_state, lengths, dim
     if len(shape) != dims:
         raise ValueError("x must be [B, L, D]" if dims == 3 else "x must be [B, D]")
     D = shape[-1]
-    x, xs = _tokens("x", x, shape, t, index)
-    decay_gate, ps = _tokens("decay_gate", decay_gate, shape, t, index)
-    input_gate, qs = _tokens("input_gate", input_gate, shape, t, index)
+    x, xs = _tokens("x", x, shape, t, index, _REACH)
+    decay_gate, ps = _tokens("decay_gate", decay_gate, shape, t, index, _REACH)
+    input_gate, qs = _tokens("input_gate", input_gate, shape, t, index, _REACH)
     log_rate = _whole("log_rate", log_rate, (D,), _s._f32, index)
     pi = pl = 0
     B, L = shape[0], 1
@@ -250,7 +251,7 @@ def sig_gated_scan_backward(x, decay_gate, input_gate, log_rate, grad_out, check
     make, args, kept = _gated_args(x, decay_gate, input_gate, log_rate, initial_state, lengths, 3)
     B, L, D = x.shape
     index = x.get_device()
-    grad_out, (sb, st, _) = _tokens("grad_out", grad_out, x.shape, x.dtype, index)
+    grad_out, (sb, st, _) = _tokens("grad_out", grad_out, x.shape, x.dtype, index, _REACH)
     pf = 0
     if grad_final_state is not None:
         grad_final_state = _whole("grad_final_state", grad_final_state, (B, D), _s._f32, index)

@@ -510,7 +510,7 @@ def test_more_refusals_of_the_linear():
 
 
 @pytest.mark.parametrize("change,code", [({"dtype": 2}, -1), ({"B": -1}, -1), ({"L": -1}, -1), ({"D": 0}, -1), ({"x": 0}, -1), ({"decay": 0}, -1), ({"input": 0}, -1), ({"rate": 0}, -1),
-                                         ({"xb": -1}, -1), ({"dt": -1}, -1), ({"it": 1 << 24}, -7), ({"L": 1 << 30}, -7), ({"B": 1 << 30}, -7), ({"B": 0}, 0)])
+                                         ({"xb": -1}, -1), ({"dt": -1}, -1), ({"it": 1 << 22}, -7), ({"D": 1 << 22}, -7), ({"L": 1 << 30}, -7), ({"B": 1 << 30}, -7), ({"B": 0}, 0)])
 def test_gated_scan_refuses_through_the_c_abi(change, code):
     lib = S.load_library()
     a = pack({**GATED_OK, **change}, GATED_ORDER)
@@ -534,7 +534,7 @@ def test_more_refusals_of_the_gated_scan():
     assert need > 0 and call(cb=ck - 1) == -5 and call(c=0) == -5 and call(w=0) == -5 and call(n=need - 1) == -5 and call(g=None) == -1
     for k in ("gy", "gx", "gd", "gi", "grate"):
         assert call({**every, k: 0}) == -1, k
-    assert call({**every, "gt": -1}) == -1 and call({**every, "gt": 1 << 24}) == -7 and call({**every, "gb": -1}) == -1
+    assert call({**every, "gt": -1}) == -1 and call({**every, "gt": 1 << 22}) == -7 and call({**every, "gb": -1}) == -1
     assert lib.sig_gated_scan_step(a, 0, 4096, 0) == -1 and lib.sig_gated_scan_step(a, 4096, 0, 0) == -1
     assert lib.sig_gated_scan_checkpoint_bytes(None) == 0 and lib.sig_gated_scan_backward_workspace_bytes(None) == 0
     long = pack({**GATED_OK, "B": 1, "L": 1 << 16}, GATED_ORDER)
