@@ -505,7 +505,8 @@ typedef struct sig_linear_args {
     const float* x_scale;           /* SIG_E4M3: device [M] or NULL (ones); row m of x stands for x_scale[m] times its values */
     const float* weight_scale;      /* SIG_E4M3: device [N] or NULL (ones) */
 } sig_linear_args;
-/* y out_dtype [M, N]; pre: NULL or out_dtype [M, N], receives what f is applied to (for the gradient). */
+/* y out_dtype [M, N]; pre: NULL or out_dtype [M, N], receives what f is applied to (for the gradient).  The workspace is that of a call with the
+ * same args, pointers among them. */
 size_t sig_linear_forward_workspace_bytes(const sig_linear_args* args);
 int    sig_linear_forward(const sig_linear_args* args, void* y, void* pre, void* workspace, size_t workspace_bytes, void* stream);
 /* Gradient (SIG_F32 and SIG_BF16): grad_y dtype [M, N] with a stride of its own; pre as kept (NULL where act is SIG_ACT_NONE) -> grad_x dtype [M, K],

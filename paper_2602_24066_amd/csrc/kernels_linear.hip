@@ -22,7 +22,7 @@ typedef int Int8 __attribute__((ext_vector_type(8)));
 
 constexpr int kSlab = 128, kChunk = 16, kChunks = kSlab / kChunk;      // bytes; bytes; chunks of a slab
 
-struct Tiles { int64_t M, N, K; int m, n, splits; int64_t slabs; int tile; };            // tiles along m and n; slabs of a split; edge of a tile
+struct Tiles { int64_t M, N, K; int m, n, splits; int64_t slabs; int tile; bool few; };            // tiles along m and n; slabs of a split; edge of a tile (few: in 16 tokens)
 
 struct Out {                            // what becomes of a sum
     const void *bias, *residual;
@@ -33,11 +33,27 @@ struct Out {                            // what becomes of a sum
     bool vec;                           // 16 bytes of neighbouring outputs are one access everywhere
 };
 
-// f and f': the normal distribution's Phi by the error function
+// The normal distribution's Phi and its density.  exp(x^2) erfc(x) = t P(t) with t = 1 / (1 + 0.3 x), P of degree 8 fitted to the smallest relative
+// error over x in [0, 14] (4e-8; with float32's roundings 5e-7), so both tails keep their relative precision, and the exponential is the density's.
+struct Normal { float below, density; };
+__device__ __forceinline__ Normal normal_of(float z)
+{
+    const float t = __builtin_amdgcn_rcpf(fmaf(fabsf(z), 0.3f * 0.70710678f, 1.0f)), g = fast_exp(-0.5f * z * z);
+    float p = fmaf(t, -0.12661661f, 0.47182638f);
+    p = fmaf(p, t, -0.48469207f);
+    p = fmaf(p, t, 0.51704908f);
+    p = fmaf(p, t, -0.074049273f);
+    p = fmaf(p, t, 0.2063852f);
+    p = fmaf(p, t, 0.15046886f);
+    p = fmaf(p, t, 0.17042372f);
+    p = fmaf(p, t, 0.16920475f);
+    const float tail = 0.5f * (p * t) * g;
+    return {z > 0.0f ? 1.0f - tail : tail, 0.39894228f * g};
+}
 __device__ __forceinline__ float act_of(float z, int act)
 {
     if (act == SIG_ACT_SILU) return z * sigmoid(z);
-    if (act == SIG_ACT_GELU) return 0.5f * z * (1.0f + erff(z * 0.70710678f));
+    if (act == SIG_ACT_GELU) return z * normal_of(z).below;
     return z;
 }
 __device__ __forceinline__ float slope_of(float z, int act)
@@ -46,58 +62,74 @@ __device__ __forceinline__ float slope_of(float z, int act)
         const float s = sigmoid(z);
         return s * fmaf(z, 1.0f - s, 1.0f);
     }
-    return 0.5f * (1.0f + erff(z * 0.70710678f)) + z * fast_exp(-0.5f * z * z) * 0.39894228f;
+    const Normal v = normal_of(z);
+    return fmaf(z, v.density, v.below);
 }
 
-// What becomes of V neighbouring sums of row m from output n on
-template <class O, int V> __device__ __forceinline__ void finish(const Out& o, int64_t m, int64_t n, int64_t N, float* z)
+template <class O, int V> __device__ __forceinline__ void take(const O* p, bool wide, int64_t n, int64_t N, float* to)
 {
-    const bool wide = o.vec && n + V <= N;
-    const int64_t at = m * N + n;
-    auto take = [&](const O* p, float* to) {
-        if (wide) {
-            const Pack<O, V> q = *(const Pack<O, V>*)p;
+    if (wide) {
+        const Pack<O, V> q = *(const Pack<O, V>*)p;
 #pragma unroll
-            for (int j = 0; j < V; j++) to[j] = to_float(q.v[j]);
-        } else
+        for (int j = 0; j < V; j++) to[j] = to_float(q.v[j]);
+    } else
 #pragma unroll
-            for (int j = 0; j < V; j++) to[j] = n + j < N ? to_float(p[j]) : 0.0f;
-    };
-    auto give = [&](O* p, const float* from) {
-        if (wide) {
-            Pack<O, V> q;
+        for (int j = 0; j < V; j++) to[j] = n + j < N ? to_float(p[j]) : 0.0f;
+}
+template <class O, int V> __device__ __forceinline__ void give(O* p, bool wide, int64_t n, int64_t N, const float* from)
+{
+    if (wide) {
+        Pack<O, V> q;
 #pragma unroll
-            for (int j = 0; j < V; j++) q.v[j] = from_float<O>(from[j]);
-            *(Pack<O, V>*)p = q;
-        } else
+        for (int j = 0; j < V; j++) q.v[j] = from_float<O>(from[j]);
+        *(Pack<O, V>*)p = q;
+    } else
 #pragma unroll
-            for (int j = 0; j < V; j++)
-                if (n + j < N) p[j] = from_float<O>(from[j]);
-    };
-    float b[V], r[V];
+        for (int j = 0; j < V; j++)
+            if (n + j < N) p[j] = from_float<O>(from[j]);
+}
+
+// What V neighbouring outputs from n < N on have in common over the tokens
+template <class O, int V> struct Columns {
+    float bias[V], scale[V];
+    int64_t n;
+    bool wide;
+    __device__ __forceinline__ Columns(const Out& o, int64_t n, int64_t N) : n(n), wide(o.vec && n + V <= N)
+    {
+#pragma unroll
+        for (int j = 0; j < V; j++) {
+            bias[j] = 0.0f;
+            scale[j] = o.weight_scale ? o.weight_scale[min(n + j, N - 1)] : 1.0f;
+        }
+        if (o.bias && n < N) take<O, V>((const O*)o.bias + n, wide, n, N, bias);
+    }
+};
+
+// What becomes of their sums of token m
+template <class O, int V> __device__ __forceinline__ void finish(const Out& o, const Columns<O, V>& c, int64_t m, int64_t N, float* z)
+{
+    const int64_t at = m * N + c.n;
+    float r[V];
+    if (o.residual) take<O, V>((const O*)o.residual + m * o.residual_stride + c.n, c.wide, c.n, N, r);
     if (o.x_scale || o.weight_scale) {
         const float xs = o.x_scale ? o.x_scale[m] : 1.0f;
 #pragma unroll
-        for (int j = 0; j < V; j++) z[j] = z[j] * xs * (o.weight_scale ? o.weight_scale[min(n + j, N - 1)] : 1.0f);
+        for (int j = 0; j < V; j++) z[j] = z[j] * xs * c.scale[j];
     }
-    if (o.bias) {
-        take((const O*)o.bias + n, b);
+    if (o.bias)
 #pragma unroll
-        for (int j = 0; j < V; j++) z[j] += b[j];
-    }
-    if (o.pre) give((O*)o.pre + at, z);
+        for (int j = 0; j < V; j++) z[j] += c.bias[j];
+    if (o.pre) give<O, V>((O*)o.pre + at, c.wide, c.n, N, z);
     if (o.act == SIG_ACT_SILU) {
 #pragma unroll
         for (int j = 0; j < V; j++) z[j] = act_of(z[j], SIG_ACT_SILU);
     } else if (o.act == SIG_ACT_GELU)
 #pragma unroll
         for (int j = 0; j < V; j++) z[j] = act_of(z[j], SIG_ACT_GELU);
-    if (o.residual) {
-        take((const O*)o.residual + m * o.residual_stride + n, r);
+    if (o.residual)
 #pragma unroll
         for (int j = 0; j < V; j++) z[j] += r[j];
-    }
-    give((O*)o.y + at, z);
+    give<O, V>((O*)o.y + at, c.wide, c.n, N, z);
 }
 
 // The sums of a wavefront's tile, 16 FM tokens by 16 FN outputs, to where they belong.  A lane holds four outputs of sixteen tokens' rows; 16 rows at a
@@ -107,6 +139,7 @@ template <class O, int FM, int FN> __device__ __forceinline__ void put(const Til
     constexpr int V = 16 / sizeof(O), kWide = FN * 16, kPitch = kWide + 4, kLanes = kWide / V, kRows = 64 / kLanes;
     const int lane = threadIdx.x & 63, c = lane % kLanes * V;
     const int64_t N4 = (t.N + 3) / 4 * 4, n = n0 + c;
+    const Columns<O, V> columns(o, n, t.N);
 #pragma unroll
     for (int j = 0; j < FM; j++) {
 #pragma unroll
@@ -125,7 +158,7 @@ template <class O, int FM, int FN> __device__ __forceinline__ void put(const Til
 #pragma unroll
                     for (int k = 0; k < V; k += 4)
                         if (n + k < N4) *(Acc*)(to + k) = *(const Acc*)(z + k);
-                } else finish<O, V>(o, m, n, t.N, z);
+                } else finish<O, V>(o, columns, m, t.N, z);
             }
         }
         __builtin_amdgcn_wave_barrier();
@@ -322,6 +355,59 @@ __global__ __launch_bounds__(WM * WN * 64) void aligned_kernel(Tiles t, const T*
     put<O, FM, FN>(t, o, parts, p.split, m0 + wm * (BM / WM), n0 + wn * (BN / WN), acc, (float*)lds + wave * 16 * (FN * 16 + 4));
 }
 
+// ---- few tokens (single tokens of up to 64 streams): 16 FN outputs a workgroup, the contraction over its wavefronts.  Bound by the weights' way from
+// memory: operands go to registers as the matrix instructions take them, several steps' loads at once, and the wavefronts' sums meet in LDS once.
+template <class T, class O, int FM, int FN, int kW> __global__ __launch_bounds__(kW * 64) void few_kernel(Tiles t, const T* x, int64_t ldx, const T* w, int64_t ldw, Out o)
+{
+    constexpr int F = kFeed<T>, kStep = 64 * F, U = (FM + FN) * F > 4 ? 2 : 4, kPitch = FN * 16;      // bytes of a row a step
+    __shared__ float sums[kW][FM * 16][kPitch];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x / 64;
+    const Place p = place_of(t);
+    const int64_t m0 = (int64_t)p.m * FM * 16, n0 = (int64_t)p.n * FN * 16, bytes = t.K * (int)sizeof(T);
+    const char *px[FM], *pw[FN];
+#pragma unroll
+    for (int j = 0; j < FM; j++) px[j] = (const char*)(x + min(m0 + j * 16 + (lane & 15), t.M - 1) * ldx) + lane / 16 * 16;
+#pragma unroll
+    for (int i = 0; i < FN; i++) pw[i] = (const char*)(w + min(n0 + i * 16 + (lane & 15), t.N - 1) * ldw) + lane / 16 * 16;
+    Acc acc[FN][FM] = {};
+    struct { Chunk x[U][FM][F], w[U][FN][F]; } now, next;
+    auto load = [&](int64_t k, auto& to) {
+#pragma unroll
+        for (int u = 0; u < U; u++)
+#pragma unroll
+            for (int f = 0; f < F; f++) {
+                const int64_t at = k + (int64_t)u * kW * kStep + f * 64;
+                const bool there = at + lane / 16 * 16 < bytes;                // rows are whole chunks
+#pragma unroll
+                for (int i = 0; i < FN; i++) to.w[u][i][f] = there ? *(const Chunk*)(pw[i] + at) : Chunk{};
+#pragma unroll
+                for (int j = 0; j < FM; j++) to.x[u][j][f] = there ? *(const Chunk*)(px[j] + at) : Chunk{};
+            }
+    };
+    int64_t k = (int64_t)wave * kStep;
+    if (k < bytes) load(k, now);
+    for (; k < bytes; k += (int64_t)kW * kStep * U) {
+        if (k + (int64_t)kW * kStep * U < bytes) load(k + (int64_t)kW * kStep * U, next);
+#pragma unroll
+        for (int u = 0; u < U; u++) products<T>(now.w[u], now.x[u], acc);
+        now = next;
+    }
+#pragma unroll
+    for (int j = 0; j < FM; j++)
+#pragma unroll
+        for (int i = 0; i < FN; i++) *(Acc*)&sums[wave][j * 16 + (lane & 15)][i * 16 + lane / 16 * 4] = acc[i][j];
+    __syncthreads();
+    for (int id = threadIdx.x; id < FM * 16 * FN * 4; id += kW * 64) {
+        const int m = id / (FN * 4), n = id % (FN * 4) * 4;
+        if (m0 + m >= t.M || n0 + n >= t.N) continue;
+        Acc v = *(const Acc*)&sums[0][m][n];
+#pragma unroll
+        for (int i = 1; i < kW; i++) v += *(const Acc*)&sums[i][m][n];
+        float z[4] = {v[0], v[1], v[2], v[3]};
+        finish<O, 4>(o, Columns<O, 4>(o, n0 + n, t.N), m0 + m, t.N, z);
+    }
+}
+
 // The splits' sums, added up in order, and what becomes of them
 template <class O> __global__ __launch_bounds__(256) void join_kernel(Tiles t, Out o, const float* parts)
 {
@@ -330,39 +416,82 @@ template <class O> __global__ __launch_bounds__(256) void join_kernel(Tiles t, O
     Acc v = *(const Acc*)(parts + id * 4);
     for (int s = 1; s < t.splits; s++) v += *(const Acc*)(parts + (s * t.M * quads + id) * 4);
     float z[4] = {v[0], v[1], v[2], v[3]};
-    finish<O, 4>(o, id / quads, id % quads * 4, t.N, z);
+    finish<O, 4>(o, Columns<O, 4>(o, id % quads * 4, t.N), id / quads, t.N, z);
 }
 
-// [R, C] to [C, padded R], zeros behind R.  pre: the gradient that comes in is multiplied by the activation's slope first, rounded to T, and kept
-// in its own order too (flat); sums: its sums over the rows of a tile, before rounding, for the bias's gradient.
+// [R, C] to [C, padded R], zeros behind R: tiles of 64 x 64 through LDS, 16 bytes an access on both sides (vec).  pre: the gradient that comes in is
+// multiplied by the activation's slope first, rounded to T, and kept in its own order too (flat); sums: its sums over the rows of a tile, for
+// the bias's gradient.
 template <class T> __global__ __launch_bounds__(256) void turn_kernel(const T* in, int64_t ld, int64_t R, int64_t C, const T* pre, int act, T* flat, T* turned, int64_t padded,
-                                                                       float* sums, int64_t tiles_c)
+                                                                       float* sums, int64_t tiles_c, bool vec)
 {
+    constexpr int V = 16 / sizeof(T), kAcross = 64 / V;                        // elements of an access, accesses of a tile's row
     __shared__ T tile[64][64 + 4 / sizeof(T)];
-    __shared__ float part[4][64];
     const int64_t r0 = (int64_t)(blockIdx.x / tiles_c) * 64, c0 = (int64_t)(blockIdx.x % tiles_c) * 64;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x / 64;
-    const int64_t c = c0 + lane;
-    float sum = 0.0f;
-    for (int i = wave; i < 64; i += 4) {
-        const int64_t r = r0 + i;
-        float v = 0.0f;
+    auto take = [&](const T* p, int64_t c, float* v) {
+        if (vec) {
+            const Pack<T, V> q = *(const Pack<T, V>*)(p + c);
+#pragma unroll
+            for (int k = 0; k < V; k++) v[k] = to_float(q.v[k]);
+        } else
+#pragma unroll
+            for (int k = 0; k < V; k++) v[k] = c + k < C ? to_float(p[c + k]) : 0.0f;
+    };
+    float v[kAcross / 4][V], z[kAcross / 4][V];
+#pragma unroll
+    for (int i = 0; i < kAcross / 4; i++) {
+        const int id = threadIdx.x + i * 256;
+        const int64_t r = r0 + id / kAcross, c = c0 + id % kAcross * V;
+#pragma unroll
+        for (int k = 0; k < V; k++) v[i][k] = z[i][k] = 0.0f;
         if (r < R && c < C) {
-            v = to_float(in[r * ld + c]);
-            if (pre) {
-                v *= slope_of(to_float(pre[r * C + c]), act);
-                if (flat) flat[r * C + c] = from_float<T>(v);
-            }
-            sum += v;
+            take(in + r * ld, c, v[i]);
+            if (pre) take(pre + r * C, c, z[i]);
         }
-        tile[i][lane] = from_float<T>(v);
     }
-    part[wave][lane] = sum;
+#pragma unroll
+    for (int i = 0; i < kAcross / 4; i++) {
+        const int id = threadIdx.x + i * 256, row = id / kAcross, at = id % kAcross * V;
+        const int64_t r = r0 + row, c = c0 + at;
+        Pack<T, V> q;
+        if (pre && act == SIG_ACT_SILU) {
+#pragma unroll
+            for (int k = 0; k < V; k++) v[i][k] *= slope_of(z[i][k], SIG_ACT_SILU);
+        } else if (pre)
+#pragma unroll
+            for (int k = 0; k < V; k++) v[i][k] *= slope_of(z[i][k], SIG_ACT_GELU);
+#pragma unroll
+        for (int k = 0; k < V; k++) q.v[k] = from_float<T>(v[i][k]);
+        if (flat && r < R && c < C) {
+            if (vec) *(Pack<T, V>*)(flat + r * C + c) = q;
+            else
+#pragma unroll
+                for (int k = 0; k < V; k++)
+                    if (c + k < C) flat[r * C + c + k] = q.v[k];
+        }
+#pragma unroll
+        for (int k = 0; k < V; k++) tile[row][at + k] = q.v[k];
+    }
+    if (!turned && !sums) return;
     __syncthreads();
-    if (sums && wave == 0 && c < C) sums[blockIdx.x / tiles_c * C + c] = (part[0][lane] + part[1][lane]) + (part[2][lane] + part[3][lane]);
-    if (turned)
-        for (int i = wave; i < 64; i += 4)
-            if (c0 + i < C && r0 + lane < padded) turned[(c0 + i) * padded + r0 + lane] = tile[lane][i];
+    // V rows of a column a thread: neighbouring lanes have neighbouring rows
+#pragma unroll
+    for (int i = 0; i < kAcross / 4; i++) {
+        const int id = threadIdx.x + i * 256, col = id / kAcross, at = id % kAcross * V;
+        Pack<T, V> q;
+        float sum = 0.0f;
+#pragma unroll
+        for (int k = 0; k < V; k++) {
+            q.v[k] = tile[at + k][col];
+            sum += to_float(q.v[k]);
+        }
+        if (turned && c0 + col < C) *(Pack<T, V>*)(turned + (c0 + col) * padded + r0 + at) = q;
+        if (sums) {
+#pragma unroll
+            for (int m = 1; m < kAcross; m *= 2) sum += __shfl_xor(sum, m);
+            if (at == 0 && c0 + col < C) sums[blockIdx.x / tiles_c * C + c0 + col] = sum;
+        }
+    }
 }
 
 template <class T> __global__ __launch_bounds__(1024) void bias_kernel(const float* sums, int64_t rows, int64_t N, T* grad_bias)
@@ -374,15 +503,30 @@ template <class T> __global__ __launch_bounds__(1024) void bias_kernel(const flo
 
 // ---- which tile, and how many splits.  A model of the launch, in us: `slab` is what a tile's slab costs a compute unit that is busy with as many
 // as it holds, `alone` what it costs at least, `over` what a tile costs besides (first loads, outputs).  Measured on large squares (us a slab):
-//   bfloat16 256: 8192^3 in 871 us, 128: 1,033 us     float32 256: 4096^3 in 981, 128: 998, 64: 1,040     e4m3 256: 8192^3 in 478, 128: 556
-// and 16384 x 4096 x 1024 (16 slabs): 159 us with tiles of 256, 167 of 128.
+//   bfloat16 256: 8192^3 in 856 us, 128: 1,022 us     float32 256: 4096^3 in 981, 128: 998, 64: 1,040     e4m3 256: 8192^3 in 476, 128: 550
+// and 16384 x 4096 x 1024 (16 slabs): 148 us with tiles of 256, 172 of 128; e4m3 16384 x 2048 x 2048: 72 and 79.
 struct Cost { int tile; double slab, alone, over; };
 constexpr Cost kCosts[3][3] = {
     {{64, 0.51, 0.70, 1.0}, {128, 1.95, 1.95, 3.0}, {256, 7.66, 7.66, 14.0}},          // float32
-    {{64, 0.17, 0.50, 0.8}, {128, 0.50, 0.80, 2.4}, {256, 1.70, 1.70, 12.0}},          // bfloat16
-    {{64, 0.18, 0.50, 0.8}, {128, 0.54, 0.80, 1.2}, {256, 1.87, 1.87, 9.7}},           // e4m3
+    {{64, 0.17, 0.50, 0.8}, {128, 0.50, 0.80, 2.4}, {256, 1.68, 1.68, 10.5}},          // bfloat16
+    {{64, 0.18, 0.50, 0.8}, {128, 0.54, 0.80, 1.2}, {256, 1.86, 1.86, 6.3}},           // e4m3
 };
 constexpr int kUnits = 256;                                                            // compute units
+
+// Up to 64 tokens: what few_kernel takes, in us, by the rate at which a compute unit's wavefronts get its operands (measured 40 GB/s, 64 tokens bfloat16:
+// 2048 to 1024 5.9 us with tiles of 16 x 16, 1024 to 4096 6.4 with 32 x 32, 8192 to 8192 45 with 64 x 32).
+constexpr int kFew = 64;
+struct FewPlan { int fm, fn; double us; };
+FewPlan few_plan(int64_t M, int64_t N, int64_t bytes)
+{
+    FewPlan best{0, 0, 0.0};
+    for (FewPlan p : {FewPlan{1, 1, 0.0}, FewPlan{2, 2, 0.0}, FewPlan{4, 2, 0.0}}) {
+        const int64_t blocks = (M + p.fm * 16 - 1) / (p.fm * 16) * ((N + p.fn * 16 - 1) / (p.fn * 16));
+        p.us = 3.0 + (double)((blocks + kUnits - 1) / kUnits) * (p.fm + p.fn) * 16 * bytes / 40e3;
+        if (best.fm == 0 || p.us < best.us) best = p;
+    }
+    return best;
+}
 
 Tiles tiles_of(int64_t M, int64_t N, int64_t K, int e, bool aligned)
 {
@@ -399,10 +543,13 @@ Tiles tiles_of(int64_t M, int64_t N, int64_t K, int e, bool aligned)
             if (splits > 1) us += 4.0 + (double)M * N * 4.0 * (splits + 1) / 3e6;     // the sums, written and read again
             if (best.tile == 0 || us < least) {
                 least = us;
-                best = Tiles{M, N, K, (int)m, (int)n, (int)splits, each, c.tile};
+                best = Tiles{M, N, K, (int)m, (int)n, (int)splits, each, c.tile, false};
             }
         }
     }
+    if (aligned && M <= kFew)
+        if (const FewPlan p = few_plan(M, N, K * e); p.us < 3.0 + least)
+            return Tiles{M, N, K, (int)((M + p.fm * 16 - 1) / (p.fm * 16)), (int)((N + p.fn * 16 - 1) / (p.fn * 16)), 1, 0, p.fm, true};
     return best;
 }
 size_t parts_bytes(const Tiles& t) { return t.splits > 1 ? (size_t)t.splits * t.M * ((t.N + 3) / 4 * 4) * 4 : 0; }
@@ -421,18 +568,30 @@ template <class T, class O, int kSize, int WM, int WN> hipError_t launch(const T
     return hipGetLastError();
 }
 
+// whole chunks only; a tile's rows and the contraction are reached by 32-bit offsets
+bool aligned_rows(const void* x, int64_t ldx, const void* w, int64_t ldw, int64_t K, int64_t e)
+{
+    return (uintptr_t)x % 16 == 0 && (uintptr_t)w % 16 == 0 && ldx * e % 16 == 0 && ldw * e % 16 == 0 && K * e % 16 == 0 && K > 0 &&
+           256 * std::max(ldx, ldw) * e + K * e < (1ll << 31);
+}
+
 template <class T, class O> hipError_t product(int64_t M, int64_t N, int64_t K, const T* x, int64_t ldx, const T* w, int64_t ldw, Out o, float* parts, hipStream_t stream)
 {
     constexpr int V = 16 / sizeof(O);
     const int64_t e = sizeof(T);
-    // whole chunks only; a tile's rows and the contraction are reached by 32-bit offsets
-    const bool aligned = (uintptr_t)x % 16 == 0 && (uintptr_t)w % 16 == 0 && ldx * e % 16 == 0 && ldw * e % 16 == 0 && K * e % 16 == 0 && K > 0 &&
-                         256 * std::max(ldx, ldw) * e + K * e < (1ll << 31);
-    const Tiles t = tiles_of(M, N, K, (int)e, aligned);
-    const int64_t blocks = (int64_t)t.m * t.n * t.splits;
-    if (!launchable(blocks, 512)) return kTooManyThreads;
+    const bool aligned = aligned_rows(x, ldx, w, ldw, K, e);
     auto fits = [&](const void* p) { return (uintptr_t)p % 16 == 0; };
     o.vec = N % V == 0 && o.residual_stride % V == 0 && fits(o.bias) && fits(o.residual) && fits(o.y) && fits(o.pre);
+    const Tiles t = tiles_of(M, N, K, (int)e, aligned);
+    if (t.few) {
+        const int64_t blocks = (int64_t)t.m * t.n;
+        if (!launchable(blocks, 512)) return kTooManyThreads;
+        auto go = [&](auto kernel) { kernel<<<(uint32_t)blocks, 512, 0, stream>>>(t, x, ldx, w, ldw, o); };
+        t.tile == 1 ? go(few_kernel<T, O, 1, 1, 8>) : t.tile == 2 ? go(few_kernel<T, O, 2, 2, 8>) : go(few_kernel<T, O, 4, 2, 8>);
+        return hipGetLastError();
+    }
+    const int64_t blocks = (int64_t)t.m * t.n * t.splits;
+    if (!launchable(blocks, 512)) return kTooManyThreads;
     hipError_t err;
     if (!aligned) {
         product_kernel<T, O><<<(uint32_t)blocks, 256, 0, stream>>>(t, x, ldx, w, ldw, o, parts);
@@ -480,9 +639,10 @@ Keep keep_of(const sig_linear_args& a)
 
 template <class T> hipError_t turn(const T* in, int64_t ld, int64_t R, int64_t C, const T* pre, int act, T* flat, T* turned, int64_t padded, float* sums, hipStream_t stream)
 {
-    const int64_t tiles_c = (C + 63) / 64, blocks = (R + 63) / 64 * tiles_c;
+    const int64_t tiles_c = (C + 63) / 64, blocks = (R + 63) / 64 * tiles_c, V = 16 / sizeof(T);
     if (!launchable(blocks, 256)) return kTooManyThreads;
-    if (blocks) turn_kernel<T><<<(uint32_t)blocks, 256, 0, stream>>>(in, ld, R, C, pre, act, flat, turned, padded, sums, tiles_c);
+    const bool vec = C % V == 0 && ld % V == 0 && (uintptr_t)in % 16 == 0 && (uintptr_t)pre % 16 == 0;
+    if (blocks) turn_kernel<T><<<(uint32_t)blocks, 256, 0, stream>>>(in, ld, R, C, pre, act, flat, turned, padded, sums, tiles_c, vec);
     return hipGetLastError();
 }
 
@@ -493,7 +653,7 @@ template <class T> hipError_t backward_of(const sig_linear_args& a, const T* gy,
     T *flat = (T*)(ws + k.flat), *turned_g = (T*)(ws + k.turned_g), *turned_w = (T*)(ws + k.turned_w), *turned_x = (T*)(ws + k.turned_x);
     float *sums = (float*)(ws + k.sums), *parts = (float*)(ws + k.parts);
     hipError_t err = hipSuccess;
-    if (pre || gw || gb) err = turn<T>(gy, ld, a.M, a.N, pre, (int)a.act, gx ? flat : nullptr, gw ? turned_g : nullptr, k.padM, gb ? sums : nullptr, stream);
+    if (pre || gw || gb) err = turn<T>(gy, ld, a.M, a.N, pre, (int)a.act, pre && gx ? flat : nullptr, gw ? turned_g : nullptr, k.padM, gb ? sums : nullptr, stream);
     if (err == hipSuccess && gb) {
         bias_kernel<T><<<(uint32_t)((a.N + 63) / 64), 1024, 0, stream>>>(sums, (a.M + 63) / 64, a.N, gb);
         err = hipGetLastError();
@@ -521,7 +681,12 @@ template <class T, class O> hipError_t forward_of(const sig_linear_args& a, void
 
 }  // namespace
 
-size_t linear_forward_workspace(const sig_linear_args& a) { return parts_bytes(a.M, a.N, a.K, bytes_of(a.dtype)); }
+size_t linear_forward_workspace(const sig_linear_args& a)
+{
+    const int e = bytes_of(a.dtype);
+    const bool aligned = aligned_rows(a.x, a.x_stride, a.weight, a.K, a.K, e);
+    return parts_bytes(tiles_of(a.M, a.N, a.K, e, aligned));
+}
 hipError_t linear_forward(const sig_linear_args& a, void* y, void* pre, void* workspace, hipStream_t stream)
 {
     float* parts = (float*)workspace;

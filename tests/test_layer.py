@@ -119,7 +119,7 @@ def test_special_rows_in_8_bits():
 LINEAR = [
     # rows, inputs, outputs
     (1, 1, 1), (1, 30, 64), (3, 64, 5), (1, 2048, 1024), (17, 33, 18), (64, 2048, 100), (5, 5460, 333), (130, 258, 130), (128, 64, 128), (129, 129, 257),
-    (300, 1554, 340), (512, 512, 512), (1025, 96, 700), (2, 64, 4099), (4099, 7, 3), (33, 8200, 48),
+    (16, 96, 8200), (20, 80, 8208), (64, 160, 8224), (40, 304, 33), (31, 16, 64), (65, 208, 130), (300, 1554, 340), (512, 512, 512), (1025, 96, 700), (2, 64, 4099), (4099, 7, 3), (33, 8200, 48),
 ]
 
 
@@ -497,7 +497,7 @@ def test_more_refusals_of_the_linear():
     lib = S.load_library()
     a = pack(LINEAR_OK, LINEAR_ORDER)
     assert lib.sig_linear_forward(None, 4096, 0, 4096, BIG, 0) == -1 and lib.sig_linear_forward(a, 0, 0, 4096, BIG, 0) == -1
-    long = pack({**LINEAR_OK, "K": 1 << 16, "xs": 1 << 16}, LINEAR_ORDER)
+    long = pack({**LINEAR_OK, "M": 100, "K": 1 << 16, "xs": 1 << 16}, LINEAR_ORDER)
     need = lib.sig_linear_forward_workspace_bytes(long)
     assert need > 0 and lib.sig_linear_forward(long, 4096, 0, 4096, need - 1, 0) == -5 and lib.sig_linear_forward(long, 4096, 0, 0, need, 0) == -5
     need = lib.sig_linear_backward_workspace_bytes(a)
