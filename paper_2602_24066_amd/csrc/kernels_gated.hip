@@ -168,29 +168,134 @@ __device__ __forceinline__ void load_round(const sig_gated_args& a, const void* 
     if constexpr (kBack) load_two<T, kPairs>(tokens(gy, gy_stride, first, end, a.D, e), l.g, l.second, (int)gy_stride * e, r.g);
 }
 
-// kSummary: only (A, H) of the chunk from a state of zero
-template <class T, bool kPairs, bool kSummary>
+// The maps (A, H) of sixteen half wavefronts' stretches, in the order of time or (kBack) against it: `state`, the value before all of them, becomes the one
+// behind them; `wave` is the value before this wavefront's stretch, `half` the one before this half's.  One barrier.
+template <bool kBack> __device__ __forceinline__ void cross(float4 (*joined)[32], const float* A, const float* H, float* state, float* wave_start, float* start)
+{
+    const int w = threadIdx.x / 64, li = threadIdx.x & 31;
+    const bool upper = threadIdx.x & 32, first = upper == kBack;
+    float preA[2], preH[2], bothA[2], bothH[2];
+#pragma unroll
+    for (int j = 0; j < 2; j++) {
+        const float oA = __shfl_xor(A[j], 32), oH = __shfl_xor(H[j], 32);
+        preA[j] = first ? 1.0f : oA;
+        preH[j] = first ? 0.0f : oH;
+        bothA[j] = oA * A[j];
+        bothH[j] = first ? fmaf(oA, H[j], oH) : fmaf(A[j], oH, H[j]);
+    }
+    if (!upper) joined[w][li] = float4{bothA[0], bothA[1], bothH[0], bothH[1]};
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < kWaves; k++) {
+        const int j = kBack ? kWaves - 1 - k : k;
+        const float4 v = joined[j][li];
+        if (j == w) {
+            wave_start[0] = state[0];
+            wave_start[1] = state[1];
+        }
+        state[0] = fmaf(v.x, state[0], v.z);
+        state[1] = fmaf(v.y, state[1], v.w);
+    }
+#pragma unroll
+    for (int j = 0; j < 2; j++) start[j] = fmaf(preA[j], wave_start[j], preH[j]);
+}
+
+// `state`, given for the stream's beginning (kBack: end), becomes the value before this workgroup's chunk: the maps of the chunks on the way, a sixteenth of
+// them each half wavefront
+template <bool kBack> __device__ __forceinline__ void enter(float4 (*joined)[32], const float* sums, int64_t D, int c, int c1, int chunk, int chunks, float* state)
+{
+    const int n = kBack ? chunks - 1 - chunk : chunk, base = kBack ? chunk + 1 : 0, part = threadIdx.x >> 5;
+    const int from = part * n / (2 * kWaves), to = (part + 1) * n / (2 * kWaves);
+    float A[2] = {1.0f, 1.0f}, H[2] = {}, wave_start[2], start[2];
+#pragma unroll 4
+    for (int k = from; k < to; k++) {
+        const float* s = sums + (int64_t)(base + (kBack ? to - 1 - (k - from) : k)) * 2 * D;
+        H[0] = fmaf(s[c], H[0], s[D + c]);
+        H[1] = fmaf(s[c1], H[1], s[D + c1]);
+        A[0] *= s[c];
+        A[1] *= s[c1];
+    }
+    cross<kBack>(joined, A, H, state, wave_start, start);
+}
+
+// A chunk's map (A, H): a wavefront has a sixteenth of its tokens, in a row
+template <class T, bool kPairs, bool kBack>
+__global__ __launch_bounds__(kWaves * 64) void gated_sums_kernel(sig_gated_args a, sig_gated_grads g, float* sums, int groups, int chunks, int rounds)
+{
+    __shared__ float4 joined[kWaves][32];
+    const Where w = where(a, groups, chunks, rounds);
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), half = (threadIdx.x >> 5) & 1, D = (int)a.D, e = sizeof(T);
+    const bool even = kPairs || w.c + 1 < D;
+    const int c1 = even ? w.c + 1 : w.c, mine = half * kHalf;
+    const float rate[2] = {rate_of(a.log_rate[w.c]), rate_of(a.log_rate[c1])};
+    const T* gy = kBack ? (const T*)g.grad_y + w.b * g.gy_stride_b : nullptr;
+    const Lane l{(c1 - w.c) * e, (int)(mine * a.x_stride_t + w.c) * e, (int)(mine * a.decay_stride_t + w.c) * e, (int)(mine * a.input_stride_t + w.c) * e, (int)(mine * g.gy_stride_t + w.c) * e, 0};
+    const int end = min(w.last, w.live), from = w.first + wave * rounds * kGatedTile, to = min(end, from + rounds * kGatedTile);
+    const int many = (max(to - from, 0) + kGatedTile - 1) / kGatedTile;
+    auto at = [&](int k) { return from + (kBack ? many - 1 - k : k) * kGatedTile; };
+    float A[2] = {1.0f, 1.0f}, H[2] = {};                                      // of the tokens so far
+    Raw<T> next;
+    if (many) load_round<T, kPairs, kBack>(a, gy, g.gy_stride_t, w, l, at(0), to, !kBack, next);
+    for (int n = 0; n < many; n++) {
+        const Raw<T> now = next;
+        if (n + 1 < many) load_round<T, kPairs, kBack>(a, gy, g.gy_stride_t, w, l, at(n + 1), to, !kBack, next);
+        const int t0 = at(n) + mine;
+        float B[2] = {1.0f, 1.0f}, G[2] = {};
+#pragma unroll
+        for (int q = 0; q < kHalf; q++) {
+            const int k = kBack ? kHalf - 1 - q : q;
+            const uint32_t mask = mask_of(t0 + k < to);
+#pragma unroll
+            for (int j = 0; j < 2; j++) {
+                const Decay v = decay(rate[j], masked(sigmoid(value(now.p[k], j)), mask));
+                if constexpr (kBack) G[j] = v.a * (masked(value(now.g[k], j), mask) + G[j]);
+                else G[j] = fmaf(v.a, G[j], masked(__builtin_amdgcn_sqrtf(v.w) * sigmoid(value(now.q[k], j)) * value(now.x[k], j), mask));
+                B[j] *= v.a;
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < 2; j++) {
+            const float oB = __shfl_xor(B[j], 32), oG = __shfl_xor(G[j], 32);
+            const float bothG = (half == 1) == kBack ? fmaf(oB, G[j], oG) : fmaf(B[j], oG, G[j]), bothB = oB * B[j];
+            H[j] = fmaf(bothB, H[j], bothG);
+            A[j] *= bothB;
+        }
+    }
+    if (!half) joined[wave][threadIdx.x & 31] = float4{A[0], A[1], H[0], H[1]};
+    __syncthreads();
+    if (threadIdx.x < 32 && w.on) {
+        float4 all = joined[kBack ? kWaves - 1 : 0][threadIdx.x];
+#pragma unroll
+        for (int k = 1; k < kWaves; k++) {
+            const float4 v = joined[kBack ? kWaves - 1 - k : k][threadIdx.x];
+            all = float4{all.x * v.x, all.y * v.y, fmaf(v.x, all.z, v.z), fmaf(v.y, all.w, v.w)};
+        }
+        float* s = sums + ((w.b * chunks + w.chunk) * 2) * D;
+        s[w.c] = all.x;
+        s[D + w.c] = all.z;
+        if (even) {
+            s[w.c + 1] = all.y;
+            s[D + w.c + 1] = all.w;
+        }
+    }
+}
+
+template <class T, bool kPairs>
 __global__ __launch_bounds__(kWaves * 64) void gated_forward_kernel(sig_gated_args a, T* y, float* final_state, float* ckpt, float* sums, int groups, int chunks,
                                                                      int rounds)
 {
     __shared__ float4 joined[2][kWaves][32];
     const Where w = where(a, groups, chunks, rounds);
-    const int wave = threadIdx.x / 64, half = (threadIdx.x >> 5) & 1, li = threadIdx.x & 31, D = (int)a.D;
+    const int wave = threadIdx.x / 64, half = (threadIdx.x >> 5) & 1, D = (int)a.D;
     const bool even = kPairs || w.c + 1 < D;
     const int c1 = even ? w.c + 1 : w.c;
     const float rate[2] = {rate_of(a.log_rate[w.c]), rate_of(a.log_rate[c1])};
-    float state[2] = {}, decayed[2] = {1.0f, 1.0f};
-    if constexpr (!kSummary) {
-        if (a.initial_state) {
-            state[0] = a.initial_state[w.b * D + w.c];
-            state[1] = a.initial_state[w.b * D + c1];
-        }
-        for (int j = 0; j < w.chunk; j++) {                                    // the chunks before this one
-            const float* s = sums + ((w.b * chunks + j) * 2) * D;
-            state[0] = fmaf(s[w.c], state[0], s[D + w.c]);
-            state[1] = fmaf(s[c1], state[1], s[D + c1]);
-        }
+    float state[2] = {};
+    if (a.initial_state) {
+        state[0] = a.initial_state[w.b * D + w.c];
+        state[1] = a.initial_state[w.b * D + c1];
     }
+    if (chunks > 1) enter<false>(joined[1], sums + w.b * chunks * 2 * D, D, w.c, c1, w.chunk, chunks, state);
     const int end = min(w.last, w.live);
     const int64_t tiles = (a.L + kGatedTile - 1) / kGatedTile;
     const int mine = wave * kGatedTile + half * kHalf, e = sizeof(T);
@@ -216,72 +321,33 @@ __global__ __launch_bounds__(kWaves * 64) void gated_forward_kernel(sig_gated_ar
                 A[j] *= d[k][j];
                 H[j] = fmaf(d[k][j], H[j], f[k][j]);
             }
-        float preA[2], preH[2], bothA[2], bothH[2];
-#pragma unroll
-        for (int j = 0; j < 2; j++) {
-            const float oA = __shfl_xor(A[j], 32), oH = __shfl_xor(H[j], 32);
-            preA[j] = half ? oA : 1.0f;
-            preH[j] = half ? oH : 0.0f;
-            bothA[j] = oA * A[j];
-            bothH[j] = half ? fmaf(A[j], oH, H[j]) : fmaf(oA, H[j], oH);
+        float wave_start[2], h[2];
+        cross<false>(joined[buf], A, H, state, wave_start, h);
+        if (ckpt && !half && w.on && t0 < end) {
+            float* to = ckpt + (w.b * tiles + t0 / kGatedTile) * D;
+            to[w.c] = wave_start[0];
+            if (even) to[w.c + 1] = wave_start[1];
         }
-        if (!half) joined[buf][wave][li] = float4{bothA[0], bothA[1], bothH[0], bothH[1]};
-        __syncthreads();
-        float start[2];
+        const __amdgpu_buffer_rsrc_t to = tokens(out, D, r, w.last, D, e);
 #pragma unroll
-        for (int j = 0; j < kWaves; j++) {
-            const float4 v = joined[buf][j][li];
-            if (j == wave) {
-                start[0] = state[0];
-                start[1] = state[1];
-            }
-            state[0] = fmaf(v.x, state[0], v.z);
-            state[1] = fmaf(v.y, state[1], v.w);
-            if constexpr (kSummary) {
-                decayed[0] *= v.x;
-                decayed[1] *= v.y;
-            }
-        }
-        if constexpr (!kSummary) {
-            if (ckpt && !half && w.on && t0 < end) {
-                float* to = ckpt + (w.b * tiles + t0 / kGatedTile) * D;
-                to[w.c] = start[0];
-                if (even) to[w.c + 1] = start[1];
-            }
-            float h[2] = {fmaf(preA[0], start[0], preH[0]), fmaf(preA[1], start[1], preH[1])};
-            const __amdgpu_buffer_rsrc_t to = tokens(out, D, r, w.last, D, e);
-#pragma unroll
-            for (int k = 0; k < kHalf; k++) {
-                h[0] = fmaf(d[k][0], h[0], f[k][0]);
-                h[1] = fmaf(d[k][1], h[1], f[k][1]);
-                store_two<T, kPairs>(to, l.out, l.second, k * D * e, mask_of(t0 + k < end), h[0], h[1]);
-            }
+        for (int k = 0; k < kHalf; k++) {
+            h[0] = fmaf(d[k][0], h[0], f[k][0]);
+            h[1] = fmaf(d[k][1], h[1], f[k][1]);
+            store_two<T, kPairs>(to, l.out, l.second, k * D * e, mask_of(t0 + k < end), h[0], h[1]);
         }
     }
-    if constexpr (kSummary) {
-        if (threadIdx.x < 32 && w.on) {
-            float* s = sums + ((w.b * chunks + w.chunk) * 2) * D;
-            s[w.c] = decayed[0];
-            s[D + w.c] = state[0];
-            if (even) {
-                s[w.c + 1] = decayed[1];
-                s[D + w.c + 1] = state[1];
-            }
-        }
-    } else {
-        // what no round has reached
-        const int done = w.first + (max(end - w.first, 0) + kRound - 1) / kRound * kRound;
-        for (int t = done; t < w.last; t += kRound)
+    // what no round has reached
+    const int done = w.first + (max(end - w.first, 0) + kRound - 1) / kRound * kRound;
+    for (int t = done; t < w.last; t += kRound)
 #pragma unroll
-            for (int k = 0; k < kHalf; k++) store_two<T, kPairs>(tokens(out, D, t, w.last, D, e), l.out, l.second, k * D * e, 0, 0.0f, 0.0f);
-        if (final_state && w.chunk == chunks - 1 && threadIdx.x < 32 && w.on) {
-            final_state[w.b * D + w.c] = state[0];
-            if (even) final_state[w.b * D + w.c + 1] = state[1];
-        }
+        for (int k = 0; k < kHalf; k++) store_two<T, kPairs>(tokens(out, D, t, w.last, D, e), l.out, l.second, k * D * e, 0, 0.0f, 0.0f);
+    if (final_state && w.chunk == chunks - 1 && threadIdx.x < 32 && w.on) {
+        final_state[w.b * D + w.c] = state[0];
+        if (even) final_state[w.b * D + w.c + 1] = state[1];
     }
 }
 
-template <class T, bool kPairs, bool kSummary>
+template <class T, bool kPairs>
 __global__ __launch_bounds__(kWaves * 64) void gated_backward_kernel(sig_gated_args a, sig_gated_grads g, const float* ckpt, float* sums, float* rates, int groups,
                                                                       int chunks, int rounds)
 {
@@ -293,47 +359,37 @@ __global__ __launch_bounds__(kWaves * 64) void gated_backward_kernel(sig_gated_a
     T *gx = (T*)g.grad_x + w.b * a.L * D, *gp = (T*)g.grad_decay_gate + w.b * a.L * D, *gq = (T*)g.grad_input_gate + w.b * a.L * D;
     const int c1 = even ? w.c + 1 : w.c;
     const float rate[2] = {rate_of(a.log_rate[w.c]), rate_of(a.log_rate[c1])};
-    float back[2] = {}, decayed[2] = {1.0f, 1.0f}, total[2] = {};
-    if constexpr (!kSummary) {
-        if (g.grad_final_state) {
-            back[0] = g.grad_final_state[w.b * D + w.c];
-            back[1] = g.grad_final_state[w.b * D + c1];
-        }
-        for (int j = chunks - 1; j > w.chunk; j--) {
-            const float* s = sums + ((w.b * chunks + j) * 2) * D;
-            back[0] = fmaf(s[w.c], back[0], s[D + w.c]);
-            back[1] = fmaf(s[c1], back[1], s[D + c1]);
-        }
+    float back[2] = {}, total[2] = {};
+    if (g.grad_final_state) {
+        back[0] = g.grad_final_state[w.b * D + w.c];
+        back[1] = g.grad_final_state[w.b * D + c1];
     }
+    if (chunks > 1) enter<true>(joined[1], sums + w.b * chunks * 2 * D, D, w.c, c1, w.chunk, chunks, back);
     const int end = min(w.last, w.live);
     const int64_t tiles = (a.L + kGatedTile - 1) / kGatedTile;
     const int mine = wave * kGatedTile + half * kHalf, e = sizeof(T);
     const Lane l{(c1 - w.c) * e, (int)(mine * a.x_stride_t + w.c) * e, (int)(mine * a.decay_stride_t + w.c) * e, (int)(mine * a.input_stride_t + w.c) * e, (int)(mine * g.gy_stride_t + w.c) * e,
                  w.on ? (mine * D + w.c) * e : kNowhere};
     const int many = (max(end - w.first, 0) + kRound - 1) / kRound;
-    if constexpr (!kSummary) {
-        for (int t = w.first + many * kRound; t < w.last; t += kRound)
+    for (int t = w.first + many * kRound; t < w.last; t += kRound)
 #pragma unroll
-            for (int k = 0; k < kHalf; k++) {
-                store_two<T, kPairs>(tokens(gx, D, t, w.last, D, e), l.out, l.second, k * D * e, 0, 0.0f, 0.0f);
-                store_two<T, kPairs>(tokens(gp, D, t, w.last, D, e), l.out, l.second, k * D * e, 0, 0.0f, 0.0f);
-                store_two<T, kPairs>(tokens(gq, D, t, w.last, D, e), l.out, l.second, k * D * e, 0, 0.0f, 0.0f);
-            }
-    }
+        for (int k = 0; k < kHalf; k++) {
+            store_two<T, kPairs>(tokens(gx, D, t, w.last, D, e), l.out, l.second, k * D * e, 0, 0.0f, 0.0f);
+            store_two<T, kPairs>(tokens(gp, D, t, w.last, D, e), l.out, l.second, k * D * e, 0, 0.0f, 0.0f);
+            store_two<T, kPairs>(tokens(gq, D, t, w.last, D, e), l.out, l.second, k * D * e, 0, 0.0f, 0.0f);
+        }
     Raw<T> next;
-    if (many) load_round<T, kPairs, true>(a, gy, g.gy_stride_t, w, l, w.first + (many - 1) * kRound, end, !kSummary, next);
+    if (many) load_round<T, kPairs, true>(a, gy, g.gy_stride_t, w, l, w.first + (many - 1) * kRound, end, true, next);
     int buf = 0;
     for (int r = w.first + (many - 1) * kRound; r >= w.first; r -= kRound, buf ^= 1) {
         Raw<T> now = next;
-        if (r > w.first) load_round<T, kPairs, true>(a, gy, g.gy_stride_t, w, l, r - kRound, end, !kSummary, next);
+        if (r > w.first) load_round<T, kPairs, true>(a, gy, g.gy_stride_t, w, l, r - kRound, end, true, next);
         const int t0 = r + mine;
         float at[2] = {};
-        if constexpr (!kSummary) {
-            if (t0 - half * kHalf < end) {
-                const float* from = ckpt + (w.b * tiles + t0 / kGatedTile) * D;
-                at[0] = from[w.c];
-                at[1] = from[c1];
-            }
+        if (t0 - half * kHalf < end) {
+            const float* from = ckpt + (w.b * tiles + t0 / kGatedTile) * D;
+            at[0] = from[w.c];
+            at[1] = from[c1];
         }
         // of every token: its decay a, and what l is multiplied by in the gradients of x, q (both with b) and p; U = l (own - from h)
         float d[kHalf][2], toward_x[kHalf][2], f[kHalf][2], toward_q[kHalf][2], shut[kHalf][2], own[kHalf][2], from[kHalf][2], A[2] = {1.0f, 1.0f}, H[2] = {}, C[2] = {};
@@ -347,17 +403,15 @@ __global__ __launch_bounds__(kWaves * 64) void gated_backward_kernel(sig_gated_a
                 const Decay v = decay(rate[j], masked(open.s, mask));
                 d[k][j] = v.a;
                 A[j] *= d[k][j];
-                if constexpr (!kSummary) {
-                    const Gate in = gate(value(now.q[k], j));
-                    const float rb = __builtin_amdgcn_rsqf(fmaxf(v.w, 1.1754944e-38f)), xi = masked(value(now.x[k], j) * in.s, mask);      // 1 / b
-                    toward_x[k][j] = here(v.w * rb * in.s);
-                    f[k][j] = here(v.w * rb * xi);
-                    toward_q[k][j] = here(in.rest);
-                    shut[k][j] = here(open.rest);
-                    own[k][j] = here(v.a * v.a * (v.u * rb) * xi);
-                    from[k][j] = here(v.a * v.u);
-                    H[j] = fmaf(d[k][j], H[j], f[k][j]);
-                }
+                const Gate in = gate(value(now.q[k], j));
+                const float rb = __builtin_amdgcn_rsqf(fmaxf(v.w, 1.1754944e-38f)), xi = masked(value(now.x[k], j) * in.s, mask);      // 1 / b
+                toward_x[k][j] = here(v.w * rb * in.s);
+                f[k][j] = here(v.w * rb * xi);
+                toward_q[k][j] = here(in.rest);
+                shut[k][j] = here(open.rest);
+                own[k][j] = here(v.a * v.a * (v.u * rb) * xi);
+                from[k][j] = here(v.a * v.u);
+                H[j] = fmaf(d[k][j], H[j], f[k][j]);
             }
         }
         __builtin_amdgcn_sched_barrier(0);
@@ -367,99 +421,61 @@ __global__ __launch_bounds__(kWaves * 64) void gated_backward_kernel(sig_gated_a
         for (int k = kHalf - 1; k >= 0; k--)
 #pragma unroll
             for (int j = 0; j < 2; j++) C[j] = d[k][j] * (value(now.g[k], j) + C[j]);
-        float preA[2], preC[2], bothA[2], bothC[2], h[2];
+        float wave_start[2], c[2], h[2];
 #pragma unroll
         for (int j = 0; j < 2; j++) {
-            const float oA = __shfl_xor(A[j], 32), oC = __shfl_xor(C[j], 32);
-            preA[j] = half ? 1.0f : oA;
-            preC[j] = half ? 0.0f : oC;
-            bothA[j] = oA * A[j];
-            bothC[j] = half ? fmaf(oA, C[j], oC) : fmaf(A[j], oC, C[j]);
-            if constexpr (!kSummary) {
-                const float oH = __shfl_xor(H[j], 32);
-                h[j] = half ? fmaf(oA, at[j], oH) : at[j];
-            }
+            const float oA = __shfl_xor(A[j], 32), oH = __shfl_xor(H[j], 32);
+            h[j] = half ? fmaf(oA, at[j], oH) : at[j];
         }
-        if (!half) joined[buf][wave][li] = float4{bothA[0], bothA[1], bothC[0], bothC[1]};
-        __syncthreads();
-        float start[2];
+        cross<true>(joined[buf], A, C, back, wave_start, c);
+        float sum[2] = {};
 #pragma unroll
-        for (int j = kWaves - 1; j >= 0; j--) {
-            const float4 v = joined[buf][j][li];
-            if (j == wave) {
-                start[0] = back[0];
-                start[1] = back[1];
+        for (int k = 0; k < kHalf; k++)
+#pragma unroll
+            for (int j = 0; j < 2; j++) {
+                own[k][j] = fmaf(-from[k][j], h[j], own[k][j]);
+                h[j] = fmaf(d[k][j], h[j], f[k][j]);
             }
-            back[0] = fmaf(v.x, back[0], v.z);
-            back[1] = fmaf(v.y, back[1], v.w);
-            if constexpr (kSummary) {
-                decayed[0] *= v.x;
-                decayed[1] *= v.y;
+        const __amdgpu_buffer_rsrc_t tx = tokens(gx, D, r, w.last, D, e), tp = tokens(gp, D, r, w.last, D, e), tq = tokens(gq, D, r, w.last, D, e);
+#pragma unroll
+        for (int k = kHalf - 1; k >= 0; k--) {
+            float ox[2], op[2], oq[2];
+            const uint32_t mask = mask_of(t0 + k < end);
+#pragma unroll
+            for (int j = 0; j < 2; j++) {
+                const float lam = value(now.g[k], j) + c[j], U = masked(lam * own[k][j], mask);
+                ox[j] = lam * toward_x[k][j];
+                oq[j] = lam * f[k][j] * toward_q[k][j];
+                op[j] = U * shut[k][j];
+                sum[j] += U;
+                c[j] = d[k][j] * lam;
             }
+            store_two<T, kPairs>(tx, l.out, l.second, k * D * e, mask, ox[0], ox[1]);
+            store_two<T, kPairs>(tp, l.out, l.second, k * D * e, mask, op[0], op[1]);
+            store_two<T, kPairs>(tq, l.out, l.second, k * D * e, mask, oq[0], oq[1]);
         }
-        if constexpr (!kSummary) {
-            float sum[2] = {};
-#pragma unroll
-            for (int k = 0; k < kHalf; k++)
-#pragma unroll
-                for (int j = 0; j < 2; j++) {
-                    own[k][j] = fmaf(-from[k][j], h[j], own[k][j]);
-                    h[j] = fmaf(d[k][j], h[j], f[k][j]);
-                }
-            float c[2] = {fmaf(preA[0], start[0], preC[0]), fmaf(preA[1], start[1], preC[1])};
-            const __amdgpu_buffer_rsrc_t tx = tokens(gx, D, r, w.last, D, e), tp = tokens(gp, D, r, w.last, D, e), tq = tokens(gq, D, r, w.last, D, e);
-#pragma unroll
-            for (int k = kHalf - 1; k >= 0; k--) {
-                float ox[2], op[2], oq[2];
-                const uint32_t mask = mask_of(t0 + k < end);
-#pragma unroll
-                for (int j = 0; j < 2; j++) {
-                    const float lam = value(now.g[k], j) + c[j], U = masked(lam * own[k][j], mask);
-                    ox[j] = lam * toward_x[k][j];
-                    oq[j] = lam * f[k][j] * toward_q[k][j];
-                    op[j] = U * shut[k][j];
-                    sum[j] += U;
-                    c[j] = d[k][j] * lam;
-                }
-                store_two<T, kPairs>(tx, l.out, l.second, k * D * e, mask, ox[0], ox[1]);
-                store_two<T, kPairs>(tp, l.out, l.second, k * D * e, mask, op[0], op[1]);
-                store_two<T, kPairs>(tq, l.out, l.second, k * D * e, mask, oq[0], oq[1]);
-            }
-            total[0] += sum[0];
-            total[1] += sum[1];
-        }
+        total[0] += sum[0];
+        total[1] += sum[1];
     }
-    if constexpr (kSummary) {
-        if (threadIdx.x < 32 && w.on) {
-            float* s = sums + ((w.b * chunks + w.chunk) * 2) * D;
-            s[w.c] = decayed[0];
-            s[D + w.c] = back[0];
-            if (even) {
-                s[w.c + 1] = decayed[1];
-                s[D + w.c + 1] = back[1];
-            }
-        }
-    } else {
-        if (g.grad_initial_state && w.chunk == 0 && threadIdx.x < 32 && w.on) {
-            g.grad_initial_state[w.b * D + w.c] = back[0];
-            if (even) g.grad_initial_state[w.b * D + w.c + 1] = back[1];
-        }
-        __syncthreads();
-        float* parts = (float*)joined;                                         // [16 halves][64 channels]
-        parts[(threadIdx.x >> 5) * 64 + li * 2] = total[0];
-        parts[(threadIdx.x >> 5) * 64 + li * 2 + 1] = total[1];
-        __syncthreads();
-        if (threadIdx.x < 32 && w.on) {
-            float s0 = 0.0f, s1 = 0.0f;
+    if (g.grad_initial_state && w.chunk == 0 && threadIdx.x < 32 && w.on) {
+        g.grad_initial_state[w.b * D + w.c] = back[0];
+        if (even) g.grad_initial_state[w.b * D + w.c + 1] = back[1];
+    }
+    __syncthreads();
+    float* parts = (float*)joined;                                             // [16 halves][64 channels]
+    parts[(threadIdx.x >> 5) * 64 + li * 2] = total[0];
+    parts[(threadIdx.x >> 5) * 64 + li * 2 + 1] = total[1];
+    __syncthreads();
+    if (threadIdx.x < 32 && w.on) {
+        float s0 = 0.0f, s1 = 0.0f;
 #pragma unroll
-            for (int k = 0; k < kWaves * 2; k++) {
-                s0 += parts[k * 64 + li * 2];
-                s1 += parts[k * 64 + li * 2 + 1];
-            }
-            float* to = rates + (w.b * chunks + w.chunk) * D;
-            to[w.c] = s0;
-            if (even) to[w.c + 1] = s1;
+        for (int k = 0; k < kWaves * 2; k++) {
+            s0 += parts[k * 64 + li * 2];
+            s1 += parts[k * 64 + li * 2 + 1];
         }
+        float* to = rates + (w.b * chunks + w.chunk) * D;
+        to[w.c] = s0;
+        if (even) to[w.c + 1] = s1;
     }
 }
 
@@ -509,11 +525,13 @@ template <class T> hipError_t forward_of(const sig_gated_args& a, T* y, float* f
                        pairs_fit(a.input_gate, a.input_stride_b, a.input_stride_t, e);
     auto go = [&](auto k) { k<<<(uint32_t)blocks, kWaves * 64, 0, stream>>>(a, y, final_state, ckpt, sums, p.groups, p.chunks, p.rounds); };
     if (p.chunks > 1) {
-        pairs ? go(gated_forward_kernel<T, true, true>) : go(gated_forward_kernel<T, false, true>);
+        const sig_gated_grads none{};
+        auto first = [&](auto k) { k<<<(uint32_t)blocks, kWaves * 64, 0, stream>>>(a, none, sums, p.groups, p.chunks, p.rounds); };
+        pairs ? first(gated_sums_kernel<T, true, false>) : first(gated_sums_kernel<T, false, false>);
         hipError_t err = hipGetLastError();
         if (err != hipSuccess) return err;
     }
-    pairs ? go(gated_forward_kernel<T, true, false>) : go(gated_forward_kernel<T, false, false>);
+    pairs ? go(gated_forward_kernel<T, true>) : go(gated_forward_kernel<T, false>);
     return hipGetLastError();
 }
 
@@ -530,11 +548,12 @@ template <class T> hipError_t backward_of(const sig_gated_args& a, const sig_gat
                            pairs_fit(a.decay_gate, a.decay_stride_b, a.decay_stride_t, e) && pairs_fit(a.input_gate, a.input_stride_b, a.input_stride_t, e);
         auto go = [&](auto k) { k<<<(uint32_t)blocks, kWaves * 64, 0, stream>>>(a, g, ckpt, sums, rates, p.groups, p.chunks, p.rounds); };
         if (p.chunks > 1) {
-            pairs ? go(gated_backward_kernel<T, true, true>) : go(gated_backward_kernel<T, false, true>);
+            auto first = [&](auto k) { k<<<(uint32_t)blocks, kWaves * 64, 0, stream>>>(a, g, sums, p.groups, p.chunks, p.rounds); };
+            pairs ? first(gated_sums_kernel<T, true, true>) : first(gated_sums_kernel<T, false, true>);
             hipError_t err = hipGetLastError();
             if (err != hipSuccess) return err;
         }
-        pairs ? go(gated_backward_kernel<T, true, false>) : go(gated_backward_kernel<T, false, false>);
+        pairs ? go(gated_backward_kernel<T, true>) : go(gated_backward_kernel<T, false>);
         hipError_t err = hipGetLastError();
         if (err != hipSuccess) return err;
     }

@@ -220,12 +220,24 @@ __global__ __launch_bounds__(kThreads == 64 ? 256 : kThreads) void norm_grad_ker
             store<T, V>((T*)g.grad_x + row * C + c, o);
         }
     }
-    float* to = parts + ((int64_t)blockIdx.x * kRows + (kThreads == 64 ? threadIdx.x / 64 : 0)) * C;
+    float* to = parts + (int64_t)blockIdx.x * C;
+    if constexpr (kThreads == 64) {                                            // the four rows' sums
+        __shared__ float join[4][64 * V];
 #pragma unroll
-    for (int i = 0; i < N; i++) {
-        const int c = (i * kThreads + lane) * V;
-        if (c < C) store<float, V>(to + c, sums[i]);
-    }
+        for (int i = 0; i < N; i++) {
+            __syncthreads();
+#pragma unroll
+            for (int j = 0; j < V; j++) join[threadIdx.x / 64][lane * V + j] = sums[i][j];
+            __syncthreads();
+            for (int k = threadIdx.x; k < 64 * V; k += 256)
+                if (i * 64 * V + k < C) to[i * 64 * V + k] = (join[0][k] + join[1][k]) + (join[2][k] + join[3][k]);
+        }
+    } else
+#pragma unroll
+        for (int i = 0; i < N; i++) {
+            const int c = (i * kThreads + lane) * V;
+            if (c < C) store<float, V>(to + c, sums[i]);
+        }
 }
 
 // Long rows: the tokens' gradient and the row's factor s, then the weight's sums by columns
@@ -264,17 +276,20 @@ __global__ __launch_bounds__(1024) void norm_weight_kernel(const float* parts, i
 
 constexpr int64_t kLongParts = 64;
 
-// Threads of a row, and accesses of a thread, for rows of `vecs` accesses: the first that holds them
-template <class F> bool held(int64_t vecs, F&& f)
+// Threads of a row, and accesses of a thread, for rows of `vecs` accesses of V elements: the first that holds them (a wavefront for as long as it can: it
+// needs no barrier)
+template <int V, class F> bool held(int64_t vecs, F&& f)
 {
     auto pick = [&](auto n, auto t) { f(n, t); return true; };
     using std::integral_constant;
     if (vecs <= 64) return pick(integral_constant<int, 1>(), integral_constant<int, 64>());
     if (vecs <= 128) return pick(integral_constant<int, 2>(), integral_constant<int, 64>());
     if (vecs <= 256) return pick(integral_constant<int, 4>(), integral_constant<int, 64>());
-    if (vecs <= 512) return pick(integral_constant<int, 2>(), integral_constant<int, 256>());
+    if constexpr (V < 8)
+        if (vecs <= 512) return pick(integral_constant<int, 8>(), integral_constant<int, 64>());
     if (vecs <= 1024) return pick(integral_constant<int, 4>(), integral_constant<int, 256>());
-    if (vecs <= 2048) return pick(integral_constant<int, 2>(), integral_constant<int, 1024>());
+    if constexpr (V < 8)
+        if (vecs <= 2048) return pick(integral_constant<int, 8>(), integral_constant<int, 256>());
     if (vecs <= 4096) return pick(integral_constant<int, 4>(), integral_constant<int, 1024>());
     return false;
 }
@@ -284,19 +299,21 @@ bool wide(const void* p, int64_t stride, int bytes, int e) { return !p || ((uint
 template <class T, class O, bool kNorm> hipError_t forward_of(const sig_norm_args& a, O* y, float* scale, T* total, hipStream_t stream)
 {
     constexpr int V = 16 / sizeof(T), e = sizeof(T);
-    const bool vec = a.C % V == 0 && wide(a.x, a.x_stride, 16, e) && wide(a.residual, a.residual_stride, 16, e) && wide(total, 0, 16, e) && wide(a.weight, 0, V * 4, 4) &&
-                     wide(y, 0, V * (int)sizeof(O), 1);
+    auto fits = [&](int v) {
+        return a.C % v == 0 && wide(a.x, a.x_stride, v * e, e) && wide(a.residual, a.residual_stride, v * e, e) && wide(total, 0, v * e, e) && wide(a.weight, 0, v * 4, 4) &&
+               wide(y, 0, v * (int)sizeof(O), 1);
+    };
     hipError_t err = hipSuccess;
     auto run = [&](auto v) {
         constexpr int kV = decltype(v)::value;
-        return held((a.C + kV - 1) / kV, [&](auto n, auto t) {
+        return held<kV>((a.C + kV - 1) / kV, [&](auto n, auto t) {
             constexpr int kN = decltype(n)::value, kThreads = decltype(t)::value;
             const int64_t blocks = kThreads == 64 ? (a.rows + 3) / 4 : a.rows, threads = kThreads == 64 ? 256 : kThreads;
             if (!launchable(blocks, threads)) err = kTooManyThreads;
             else norm_kernel<T, O, kNorm, kV, kN, kThreads><<<(uint32_t)blocks, threads, 0, stream>>>(a, y, scale, total);
         });
     };
-    const bool done = vec ? run(std::integral_constant<int, V>()) : run(std::integral_constant<int, 1>());
+    const bool done = fits(V) ? run(std::integral_constant<int, V>()) : V > 4 && fits(2) ? run(std::integral_constant<int, V / 4 < 1 ? 1 : V / 4>()) : run(std::integral_constant<int, 1>());
     if (!done) {
         if (!launchable(a.rows, 1024)) return kTooManyThreads;
         norm_long_kernel<T, O, kNorm><<<(uint32_t)a.rows, 1024, 0, stream>>>(a, y, scale, total);
@@ -304,37 +321,28 @@ template <class T, class O, bool kNorm> hipError_t forward_of(const sig_norm_arg
     return err == hipSuccess ? hipGetLastError() : err;
 }
 
-struct GradPlan { bool vec, registers; int64_t blocks, parts; };       // parts: rows of partial sums of the weight's gradient
-GradPlan grad_plan(const sig_norm_args& a, bool vec)
+struct GradPlan { bool registers; int64_t blocks, parts; };            // parts: rows of partial sums of the weight's gradient, one a workgroup
+template <int V> GradPlan grad_plan(const sig_norm_args& a)
 {
-    const int V = vec ? (a.dtype == SIG_BF16 ? 8 : 4) : 1;
-    GradPlan p{vec, false, 0, 0};
-    p.registers = held((a.C + V - 1) / V, [&](auto, auto t) {
+    GradPlan p{false, 0, 0};
+    p.registers = held<V>((a.C + V - 1) / V, [&](auto, auto t) {
         constexpr int kThreads = decltype(t)::value, kRows = kThreads == 64 ? 4 : 1;
-        p.blocks = std::min<int64_t>((a.rows + kRows - 1) / kRows, kThreads == 1024 ? 512 : 1024);
-        p.parts = p.blocks * kRows;
+        p.blocks = p.parts = std::min<int64_t>((a.rows + kRows - 1) / kRows, kThreads == 1024 ? 512 : 1024);
     });
     if (!p.registers) p.parts = std::min<int64_t>(kLongParts, a.rows);
     return p;
 }
 
-template <class T> hipError_t backward_of(const sig_norm_args& a, const NormGrads& g, float* ws, hipStream_t stream)
+template <class T, int V> hipError_t backward_by(const sig_norm_args& a, const NormGrads& g, float* ws, hipStream_t stream)
 {
-    constexpr int V = 16 / sizeof(T), e = sizeof(T);
-    const bool vec = a.C % V == 0 && wide(a.x, a.x_stride, 16, e) && wide(g.grad_y, g.gy_stride, 16, e) && wide(g.grad_total, g.gt_stride, 16, e) &&
-                     wide(g.grad_x, 0, 16, e) && wide(a.weight, 0, 16, 4) && wide(ws, 0, 16, 4);
-    const GradPlan p = grad_plan(a, vec);
+    const GradPlan p = grad_plan<V>(a);
     const int64_t groups = (a.C + 63) / 64;
     if (!launchable(groups, 1024)) return kTooManyThreads;
     if (a.rows && p.registers) {
-        auto run = [&](auto v) {
-            constexpr int kV = decltype(v)::value;
-            held((a.C + kV - 1) / kV, [&](auto n, auto t) {
-                constexpr int kN = decltype(n)::value, kThreads = decltype(t)::value;
-                norm_grad_kernel<T, kV, kN, kThreads><<<(uint32_t)p.blocks, kThreads == 64 ? 256 : kThreads, 0, stream>>>(a, g, ws);
-            });
-        };
-        vec ? run(std::integral_constant<int, V>()) : run(std::integral_constant<int, 1>());
+        held<V>((a.C + V - 1) / V, [&](auto n, auto t) {
+            constexpr int kN = decltype(n)::value, kThreads = decltype(t)::value;
+            norm_grad_kernel<T, V, kN, kThreads><<<(uint32_t)p.blocks, kThreads == 64 ? 256 : kThreads, 0, stream>>>(a, g, ws);
+        });
     } else if (a.rows) {
         const int64_t wide_groups = (a.C + 255) / 256, span = (a.rows + p.parts - 1) / p.parts;
         if (!launchable(a.rows, 1024) || !launchable(wide_groups * p.parts, 256)) return kTooManyThreads;
@@ -350,6 +358,20 @@ template <class T> hipError_t backward_of(const sig_norm_args& a, const NormGrad
     return hipGetLastError();
 }
 
+// 16 bytes an access where everything allows it, else pairs of bfloat16 values, else single values
+template <class T> hipError_t backward_of(const sig_norm_args& a, const NormGrads& g, float* ws, hipStream_t stream)
+{
+    constexpr int V = 16 / sizeof(T), e = sizeof(T);
+    auto fits = [&](int v) {
+        return a.C % v == 0 && wide(a.x, a.x_stride, v * e, e) && wide(g.grad_y, g.gy_stride, v * e, e) && wide(g.grad_total, g.gt_stride, v * e, e) && wide(g.grad_x, 0, v * e, e) &&
+               wide(a.weight, 0, v * 4, 4) && wide(ws, 0, 16, 4);
+    };
+    if (fits(V)) return backward_by<T, V>(a, g, ws, stream);
+    if constexpr (V > 4)
+        if (fits(2)) return backward_by<T, 2>(a, g, ws, stream);
+    return backward_by<T, 1>(a, g, ws, stream);
+}
+
 }  // namespace
 
 hipError_t norm_forward(const sig_norm_args& a, void* y, float* scale, void* total, hipStream_t stream)
@@ -363,10 +385,8 @@ hipError_t norm_forward(const sig_norm_args& a, void* y, float* scale, void* tot
 size_t norm_backward_workspace(const sig_norm_args& a)
 {
     size_t most = 0;
-    for (bool vec : {false, true}) {
-        const GradPlan p = grad_plan(a, vec);
+    for (const GradPlan& p : {grad_plan<1>(a), grad_plan<2>(a), a.dtype == SIG_BF16 ? grad_plan<8>(a) : grad_plan<4>(a)})
         most = std::max(most, (size_t)(p.parts * a.C + (p.registers ? 0 : a.rows)) * 4);
-    }
     return most;
 }
 hipError_t norm_backward(const sig_norm_args& a, const NormGrads& g, float* workspace, hipStream_t stream)
