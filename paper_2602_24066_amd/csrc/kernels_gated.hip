@@ -11,6 +11,8 @@
 // Gradient: with c_t what comes back from the tokens after t, l_t = grad_y_t + c_t and c_(t-1) = a_t l_t, the same structure from the end.  With U_t = u_t dL/du_t
 //   grad x = l b i,  grad q = l b x i (1 - i),  U = l (u a^2 / b i x - u a h_(t-1)),  grad p = U (1 - sigmoid(p)),  grad log_rate = sum U:
 // u / b goes to zero like sqrt(u / 2), so nothing here is infinite at u = 0.
+#include <type_traits>
+
 #include "layer.hpp"
 
 namespace sig {
@@ -56,8 +58,10 @@ template <class T, bool kPairs> __device__ __forceinline__ void load_two(__amdgp
 }
 // All ones for a token that counts, else 0; masked() keeps v or makes it 0.  Selections by a condition the compiler turns into branches, and puts behind
 // them the work that the selected value takes, with all that this work needs held in registers; hence a mask whose origin it does not see.
-__device__ __forceinline__ uint32_t mask_of(bool counts)
+// kAll: every token of the round counts, and nothing is masked.
+template <bool kAll> __device__ __forceinline__ uint32_t mask_of(bool counts)
 {
+    if constexpr (kAll) return ~0u;
     uint32_t m = counts ? ~0u : 0u;
     asm("" : "+v"(m));
     return m;
@@ -109,26 +113,25 @@ __device__ __forceinline__ Gate gate(float v)
     return {s, v > 0.0f ? e * s : 1.0f - s};
 }
 
-// exp(-u) and 1 - exp(-2 u) for u >= 0.  Small u: -expm1(-v) = v (1 - v/2 (1 - v/3 (1 - ...))) with v = 2u < 1/2, whose first omitted term is
-// v^7 / 8! < 2e-7 of the value; from there on 1 - a^2 >= 0.39 loses a bit and a half at most.  u is bounded, as 0 times infinity would follow.
-struct Decay { float u, a, w; };
-__device__ __forceinline__ Decay decay(float rate, float open)
+// u log2(e) = x, a = 2^-x and w = 1 - a^2 for x >= 0.  Small x: the power series of 1 - exp(-v), v = 2 u < 1/2, up to v^7, whose first omitted term is
+// v^7 / 8! < 2e-7 of the value; from there on 1 - a^2 >= 0.39 loses a bit and a half at most.
+struct Decay { float x, a, w; };
+__device__ __forceinline__ Decay decay(float rate, float open)                 // rate: exp(log_rate) log2(e)
 {
-    float u = rate * open;
-    u = u > 128.0f ? 128.0f : u;                                               // exp(-128) is 0 in float32's normal range; a NaN stays one
-    float a = fast_exp(-u), v = 2.0f * u;
-    float p = fmaf(v, -1.0f / 8.0f, 1.0f);
-    p = fmaf(p * v, -1.0f / 7.0f, 1.0f);
-    p = fmaf(p * v, -1.0f / 6.0f, 1.0f);
-    p = fmaf(p * v, -1.0f / 5.0f, 1.0f);
-    p = fmaf(p * v, -1.0f / 4.0f, 1.0f);
-    p = fmaf(p * v, -1.0f / 3.0f, 1.0f);
-    p = fmaf(p * v, -1.0f / 2.0f, 1.0f);
-    return {u, a, v < 0.5f ? p * v : fmaf(-a, a, 1.0f)};
+    constexpr float v = 1.3862943611f;                                         // of an x of one
+    constexpr float k1 = v, k2 = -k1 * v / 2, k3 = -k2 * v / 3, k4 = -k3 * v / 4, k5 = -k4 * v / 5, k6 = -k5 * v / 6, k7 = -k6 * v / 7;
+    const float x = rate * open, a = __builtin_amdgcn_exp2f(-x);
+    float p = fmaf(x, k7, k6);
+    p = fmaf(p, x, k5);
+    p = fmaf(p, x, k4);
+    p = fmaf(p, x, k3);
+    p = fmaf(p, x, k2);
+    p = fmaf(p, x, k1);
+    return {x, a, x < 0.5f / v ? p * x : fmaf(-a, a, 1.0f)};
 }
 
-// exp(log_rate), log_rate taken as 64 beyond that: a product with a shut gate's zero stays one.  A NaN stays one.
-__device__ __forceinline__ float rate_of(float log_rate) { return fast_exp(log_rate > 64.0f ? 64.0f : log_rate); }
+// exp(log_rate) log2(e), log_rate taken as 64 beyond that: u is finite, and a product with a shut gate's zero stays one.  A NaN stays one.
+__device__ __forceinline__ float rate_of(float log_rate) { return fast_exp(log_rate > 64.0f ? 64.0f : log_rate) * kLog2e; }
 
 struct Where {                       // of a workgroup: stream, channels, tokens of its chunk, and how many of them count
     int64_t b;
@@ -241,18 +244,22 @@ __global__ __launch_bounds__(kWaves * 64) void gated_sums_kernel(sig_gated_args 
         if (n + 1 < many) load_round<T, kPairs, kBack>(a, gy, g.gy_stride_t, w, l, at(n + 1), to, !kBack, next);
         const int t0 = at(n) + mine;
         float B[2] = {1.0f, 1.0f}, G[2] = {};
+        auto tile = [&](auto all) {
 #pragma unroll
-        for (int q = 0; q < kHalf; q++) {
-            const int k = kBack ? kHalf - 1 - q : q;
-            const uint32_t mask = mask_of(t0 + k < to);
+            for (int q = 0; q < kHalf; q++) {
+                const int k = kBack ? kHalf - 1 - q : q;
+                const uint32_t mask = mask_of<decltype(all)::value>(t0 + k < to);
 #pragma unroll
-            for (int j = 0; j < 2; j++) {
-                const Decay v = decay(rate[j], masked(sigmoid(value(now.p[k], j)), mask));
-                if constexpr (kBack) G[j] = v.a * (masked(value(now.g[k], j), mask) + G[j]);
-                else G[j] = fmaf(v.a, G[j], masked(__builtin_amdgcn_sqrtf(v.w) * sigmoid(value(now.q[k], j)) * value(now.x[k], j), mask));
-                B[j] *= v.a;
+                for (int j = 0; j < 2; j++) {
+                    const Decay v = decay(rate[j], masked(sigmoid(value(now.p[k], j)), mask));
+                    if constexpr (kBack) G[j] = v.a * (masked(value(now.g[k], j), mask) + G[j]);
+                    else G[j] = fmaf(v.a, G[j], masked(__builtin_amdgcn_sqrtf(v.w) * sigmoid(value(now.q[k], j)) * value(now.x[k], j), mask));
+                    B[j] *= v.a;
+                }
             }
-        }
+        };
+        if (at(n) + kGatedTile <= to) tile(std::true_type());
+        else tile(std::false_type());
 #pragma unroll
         for (int j = 0; j < 2; j++) {
             const float oB = __shfl_xor(B[j], 32), oG = __shfl_xor(G[j], 32);
@@ -307,34 +314,38 @@ __global__ __launch_bounds__(kWaves * 64) void gated_forward_kernel(sig_gated_ar
     for (int r = w.first; r < end; r += kRound, buf ^= 1) {
         const Raw<T> now = next;
         if (r + kRound < end) load_round<T, kPairs, false>(a, nullptr, 0, w, l, r + kRound, end, true, next);
-        const int t0 = r + mine;
-        float f[kHalf][2], d[kHalf][2], A[2] = {1.0f, 1.0f}, H[2] = {};
+        auto round = [&](auto all) {
+            const int t0 = r + mine;
+            float f[kHalf][2], d[kHalf][2], A[2] = {1.0f, 1.0f}, H[2] = {};
 #pragma unroll
-        for (int k = 0; k < kHalf; k++)
+            for (int k = 0; k < kHalf; k++)
 #pragma unroll
-            for (int j = 0; j < 2; j++) {
-                // a token that does not count has u = 0: nothing decays, and b is 0
-                const uint32_t mask = mask_of(t0 + k < end);
-                const Decay v = decay(rate[j], masked(sigmoid(value(now.p[k], j)), mask));
-                d[k][j] = v.a;
-                f[k][j] = masked(__builtin_amdgcn_sqrtf(v.w) * sigmoid(value(now.q[k], j)) * value(now.x[k], j), mask);
-                A[j] *= d[k][j];
-                H[j] = fmaf(d[k][j], H[j], f[k][j]);
+                for (int j = 0; j < 2; j++) {
+                    // a token that does not count has u = 0: nothing decays, and b is 0
+                    const uint32_t mask = mask_of<decltype(all)::value>(t0 + k < end);
+                    const Decay v = decay(rate[j], masked(sigmoid(value(now.p[k], j)), mask));
+                    d[k][j] = v.a;
+                    f[k][j] = masked(__builtin_amdgcn_sqrtf(v.w) * sigmoid(value(now.q[k], j)) * value(now.x[k], j), mask);
+                    A[j] *= d[k][j];
+                    H[j] = fmaf(d[k][j], H[j], f[k][j]);
+                }
+            float wave_start[2], h[2];
+            cross<false>(joined[buf], A, H, state, wave_start, h);
+            if (ckpt && !half && w.on && t0 < end) {
+                float* to = ckpt + (w.b * tiles + t0 / kGatedTile) * D;
+                to[w.c] = wave_start[0];
+                if (even) to[w.c + 1] = wave_start[1];
             }
-        float wave_start[2], h[2];
-        cross<false>(joined[buf], A, H, state, wave_start, h);
-        if (ckpt && !half && w.on && t0 < end) {
-            float* to = ckpt + (w.b * tiles + t0 / kGatedTile) * D;
-            to[w.c] = wave_start[0];
-            if (even) to[w.c + 1] = wave_start[1];
-        }
-        const __amdgpu_buffer_rsrc_t to = tokens(out, D, r, w.last, D, e);
+            const __amdgpu_buffer_rsrc_t to = tokens(out, D, r, w.last, D, e);
 #pragma unroll
-        for (int k = 0; k < kHalf; k++) {
-            h[0] = fmaf(d[k][0], h[0], f[k][0]);
-            h[1] = fmaf(d[k][1], h[1], f[k][1]);
-            store_two<T, kPairs>(to, l.out, l.second, k * D * e, mask_of(t0 + k < end), h[0], h[1]);
-        }
+            for (int k = 0; k < kHalf; k++) {
+                h[0] = fmaf(d[k][0], h[0], f[k][0]);
+                h[1] = fmaf(d[k][1], h[1], f[k][1]);
+                store_two<T, kPairs>(to, l.out, l.second, k * D * e, mask_of<decltype(all)::value>(t0 + k < end), h[0], h[1]);
+            }
+        };
+        if (r + kRound <= end) round(std::true_type());
+        else round(std::false_type());
     }
     // what no round has reached
     const int done = w.first + (max(end - w.first, 0) + kRound - 1) / kRound * kRound;
@@ -398,7 +409,7 @@ __global__ __launch_bounds__(kWaves * 64) void gated_backward_kernel(sig_gated_a
             __builtin_amdgcn_sched_barrier(0);      // a token's values are done before the next one's begin: all at once do not fit the registers
 #pragma unroll
             for (int j = 0; j < 2; j++) {
-                const uint32_t mask = mask_of(t0 + k < end);
+                const uint32_t mask = mask_of<false>(t0 + k < end);
                 const Gate open = gate(value(now.p[k], j));
                 const Decay v = decay(rate[j], masked(open.s, mask));
                 d[k][j] = v.a;
@@ -409,14 +420,14 @@ __global__ __launch_bounds__(kWaves * 64) void gated_backward_kernel(sig_gated_a
                 f[k][j] = here(v.w * rb * xi);
                 toward_q[k][j] = here(in.rest);
                 shut[k][j] = here(open.rest);
-                own[k][j] = here(v.a * v.a * (v.u * rb) * xi);
-                from[k][j] = here(v.a * v.u);
+                own[k][j] = here(v.a * v.a * (v.x * 0.69314718f * rb) * xi);
+                from[k][j] = here(v.a * (v.x * 0.69314718f));
                 H[j] = fmaf(d[k][j], H[j], f[k][j]);
             }
         }
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int k = 0; k < kHalf; k++) now.g[k] = masked(now.g[k], mask_of(t0 + k < end));
+        for (int k = 0; k < kHalf; k++) now.g[k] = masked(now.g[k], mask_of<false>(t0 + k < end));
 #pragma unroll
         for (int k = kHalf - 1; k >= 0; k--)
 #pragma unroll
@@ -440,7 +451,7 @@ __global__ __launch_bounds__(kWaves * 64) void gated_backward_kernel(sig_gated_a
 #pragma unroll
         for (int k = kHalf - 1; k >= 0; k--) {
             float ox[2], op[2], oq[2];
-            const uint32_t mask = mask_of(t0 + k < end);
+            const uint32_t mask = mask_of<false>(t0 + k < end);
 #pragma unroll
             for (int j = 0; j < 2; j++) {
                 const float lam = value(now.g[k], j) + c[j], U = masked(lam * own[k][j], mask);
@@ -504,7 +515,7 @@ Plan plan(const sig_gated_args& a)
     Plan p;
     p.groups = (int)((a.D + kGroup - 1) / kGroup);
     const int64_t all = (a.L + kRound - 1) / kRound, rows = a.B * p.groups;
-    int64_t chunks = rows >= 256 ? 1 : (512 + rows - 1) / (rows > 0 ? rows : 1);
+    int64_t chunks = rows >= 256 ? 1 : (256 + rows - 1) / (rows > 0 ? rows : 1);
     chunks = chunks > all ? (all ? all : 1) : chunks;
     p.rounds = (int)((all + chunks - 1) / chunks);
     if (p.rounds < 1) p.rounds = 1;
