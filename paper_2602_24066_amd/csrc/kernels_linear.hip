@@ -105,12 +105,32 @@ template <class O, int V> struct Columns {
     }
 };
 
+// V values in words, as they lie in memory (elements of their own would take a register each)
+template <class O, int V> struct Words {
+    typedef uint32_t Vector __attribute__((ext_vector_type(V * sizeof(O) / 4)));
+    Vector w;
+    __device__ __forceinline__ float value(int j) const { return sizeof(O) == 4 ? __uint_as_float(w[j]) : __uint_as_float(j % 2 ? w[j / 2] & 0xffff0000u : w[j / 2] << 16); }
+};
+
+// The residual of V outputs of token m, fetched ahead of the sums
+template <class O, int V> __device__ __forceinline__ Words<O, V> residual_of(const Out& o, const Columns<O, V>& c, int64_t m, int64_t N)
+{
+    const O* p = (const O*)o.residual + m * o.residual_stride + c.n;
+    Words<O, V> r;
+    if (c.wide) r.w = *(const typename Words<O, V>::Vector*)p;
+    else {
+        O v[V];
+#pragma unroll
+        for (int j = 0; j < V; j++) v[j] = p[c.n + j < N ? j : 0];
+        __builtin_memcpy(&r.w, v, sizeof(v));
+    }
+    return r;
+}
+
 // What becomes of their sums of token m
-template <class O, int V> __device__ __forceinline__ void finish(const Out& o, const Columns<O, V>& c, int64_t m, int64_t N, float* z)
+template <class O, int V> __device__ __forceinline__ void finish(const Out& o, const Columns<O, V>& c, int64_t m, int64_t N, float* z, const Words<O, V>& r)
 {
     const int64_t at = m * N + c.n;
-    float r[V];
-    if (o.residual) take<O, V>((const O*)o.residual + m * o.residual_stride + c.n, c.wide, c.n, N, r);
     if (o.x_scale || o.weight_scale) {
         const float xs = o.x_scale ? o.x_scale[m] : 1.0f;
 #pragma unroll
@@ -128,7 +148,7 @@ template <class O, int V> __device__ __forceinline__ void finish(const Out& o, c
         for (int j = 0; j < V; j++) z[j] = act_of(z[j], SIG_ACT_GELU);
     if (o.residual)
 #pragma unroll
-        for (int j = 0; j < V; j++) z[j] += r[j];
+        for (int j = 0; j < V; j++) z[j] += r.value(j);
     give<O, V>((O*)o.y + at, c.wide, c.n, N, z);
 }
 
@@ -140,8 +160,19 @@ template <class O, int FM, int FN> __device__ __forceinline__ void put(const Til
     const int lane = threadIdx.x & 63, c = lane % kLanes * V;
     const int64_t N4 = (t.N + 3) / 4 * 4, n = n0 + c;
     const Columns<O, V> columns(o, n, t.N);
+    const bool residual = o.residual && t.splits == 1 && n < t.N;
+    Words<O, V> next[16 / kRows];                                              // the residual of the next sixteen rows
+    auto fetch = [&](int j) {
+#pragma unroll
+        for (int r = 0; r < 16; r += kRows) next[r / kRows] = residual_of<O, V>(o, columns, min(m0 + j * 16 + r + lane / kLanes, t.M - 1), t.N);
+    };
+    if (residual) fetch(0);
 #pragma unroll
     for (int j = 0; j < FM; j++) {
+        Words<O, V> now[16 / kRows];
+#pragma unroll
+        for (int r = 0; r < 16 / kRows; r++) now[r] = next[r];
+        if (residual && j + 1 < FM) fetch(j + 1);
 #pragma unroll
         for (int i = 0; i < FN; i++) *(Acc*)(lds + (lane & 15) * kPitch + i * 16 + lane / 16 * 4) = acc[i][j];
         __builtin_amdgcn_wave_barrier();
@@ -158,7 +189,7 @@ template <class O, int FM, int FN> __device__ __forceinline__ void put(const Til
 #pragma unroll
                     for (int k = 0; k < V; k += 4)
                         if (n + k < N4) *(Acc*)(to + k) = *(const Acc*)(z + k);
-                } else finish<O, V>(o, columns, m, t.N, z);
+                } else finish<O, V>(o, columns, m, t.N, z, now[r / kRows]);
             }
         }
         __builtin_amdgcn_wave_barrier();
@@ -404,7 +435,10 @@ template <class T, class O, int FM, int FN, int kW> __global__ __launch_bounds__
 #pragma unroll
         for (int i = 1; i < kW; i++) v += *(const Acc*)&sums[i][m][n];
         float z[4] = {v[0], v[1], v[2], v[3]};
-        finish<O, 4>(o, Columns<O, 4>(o, n0 + n, t.N), m0 + m, t.N, z);
+        const Columns<O, 4> columns(o, n0 + n, t.N);
+        Words<O, 4> r{};
+        if (o.residual) r = residual_of<O, 4>(o, columns, m0 + m, t.N);
+        finish<O, 4>(o, columns, m0 + m, t.N, z, r);
     }
 }
 
@@ -416,7 +450,10 @@ template <class O> __global__ __launch_bounds__(256) void join_kernel(Tiles t, O
     Acc v = *(const Acc*)(parts + id * 4);
     for (int s = 1; s < t.splits; s++) v += *(const Acc*)(parts + (s * t.M * quads + id) * 4);
     float z[4] = {v[0], v[1], v[2], v[3]};
-    finish<O, 4>(o, Columns<O, 4>(o, id % quads * 4, t.N), id / quads, t.N, z);
+    const Columns<O, 4> columns(o, id % quads * 4, t.N);
+    Words<O, 4> r{};
+    if (o.residual) r = residual_of<O, 4>(o, columns, id / quads, t.N);
+    finish<O, 4>(o, columns, id / quads, t.N, z, r);
 }
 
 // [R, C] to [C, padded R], zeros behind R: tiles of 64 x 64 through LDS, 16 bytes an access on both sides (vec).  pre: the gradient that comes in is
