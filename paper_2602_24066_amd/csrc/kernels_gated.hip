@@ -79,7 +79,11 @@ template <class T> __device__ __forceinline__ Both<T> masked(Both<T> v, uint32_t
     for (uint32_t& word : v.w) word &= mask;
     return v;
 }
-__device__ __forceinline__ void pack(Both<bf16>& r, float v0, float v1) { r.w[0] = from_float<bf16>(v0).bits | (uint32_t)from_float<bf16>(v1).bits << 16; }
+__device__ __forceinline__ void pack(Both<bf16>& r, float v0, float v1)
+{
+    const float v[2] = {v0, v1};
+    r.w[0] = word_of(v, (bf16*)nullptr);
+}
 __device__ __forceinline__ void pack(Both<float>& r, float v0, float v1)
 {
     r.w[0] = __float_as_uint(v0);

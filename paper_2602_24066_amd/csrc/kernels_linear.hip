@@ -79,10 +79,7 @@ template <class O, int V> __device__ __forceinline__ void take(const O* p, bool 
 template <class O, int V> __device__ __forceinline__ void give(O* p, bool wide, int64_t n, int64_t N, const float* from)
 {
     if (wide) {
-        Pack<O, V> q;
-#pragma unroll
-        for (int j = 0; j < V; j++) q.v[j] = from_float<O>(from[j]);
-        *(Pack<O, V>*)p = q;
+        store_words<O, V>(p, from);
     } else
 #pragma unroll
         for (int j = 0; j < V; j++)

@@ -41,10 +41,10 @@ template <class T, int V> __device__ __forceinline__ void load(const T* p, float
 }
 template <class T, int V> __device__ __forceinline__ void store(T* p, const float* v)
 {
-    Pack<T, V> r;
+    if constexpr (V * sizeof(T) >= 4) store_words<T, V>(p, v);
+    else
 #pragma unroll
-    for (int j = 0; j < V; j++) r.v[j] = from_float<T>(v[j]);
-    *(Pack<T, V>*)p = r;
+        for (int j = 0; j < V; j++) p[j] = from_float<T>(v[j]);
 }
 
 // A row's scale, and its values over it: v 448 / top.  The quotient is corrected once, so that one that float32 holds is met: quotients of bfloat16 values

@@ -36,6 +36,31 @@ hipError_t gated_step(const sig_gated_args& a, float* state, void* y, hipStream_
 struct e4m3 { uint8_t bits; };
 // to nearest, ties to even, values a little beyond 448 to 448, a NaN stays one (conversion of the hardware)
 template <> __device__ __forceinline__ e4m3 from_float<e4m3>(float v) { return {(uint8_t)(__builtin_amdgcn_cvt_pk_fp8_f32(v, v, 0, false) & 0xff)}; }
+
+// Neighbouring values as they lie in memory, converted two (bfloat16, e4m3) an instruction; V a multiple of the values of a word
+__device__ __forceinline__ uint32_t word_of(const float* v, bf16*)
+{
+    typedef float F2 __attribute__((ext_vector_type(2)));
+    typedef __bf16 B2 __attribute__((ext_vector_type(2)));
+    const B2 h = __builtin_convertvector(F2{v[0], v[1]}, B2);
+    uint32_t w;
+    __builtin_memcpy(&w, &h, 4);
+    return w;
+}
+__device__ __forceinline__ uint32_t word_of(const float* v, float*) { return __float_as_uint(v[0]); }
+__device__ __forceinline__ uint32_t word_of(const float* v, e4m3*)
+{
+    return __builtin_amdgcn_cvt_pk_fp8_f32(v[2], v[3], __builtin_amdgcn_cvt_pk_fp8_f32(v[0], v[1], 0, false), true);
+}
+template <class T, int V> __device__ __forceinline__ void store_words(T* p, const float* v)
+{
+    constexpr int kEach = 4 / sizeof(T), kWords = V / kEach;
+    typedef uint32_t Vector __attribute__((ext_vector_type(kWords)));
+    Vector w;
+#pragma unroll
+    for (int i = 0; i < kWords; i++) w[i] = word_of(v + i * kEach, (T*)nullptr);
+    *(Vector*)p = w;
+}
 #endif
 
 }  // namespace sig
