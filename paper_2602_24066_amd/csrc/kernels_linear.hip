@@ -102,13 +102,6 @@ template <class O, int V> struct Columns {
     }
 };
 
-// V values in words, as they lie in memory (elements of their own would take a register each)
-template <class O, int V> struct Words {
-    typedef uint32_t Vector __attribute__((ext_vector_type(V * sizeof(O) / 4)));
-    Vector w;
-    __device__ __forceinline__ float value(int j) const { return sizeof(O) == 4 ? __uint_as_float(w[j]) : __uint_as_float(j % 2 ? w[j / 2] & 0xffff0000u : w[j / 2] << 16); }
-};
-
 // The residual of V outputs of token m, fetched ahead of the sums
 template <class O, int V> __device__ __forceinline__ Words<O, V> residual_of(const Out& o, const Columns<O, V>& c, int64_t m, int64_t N)
 {

@@ -177,20 +177,29 @@ __global__ __launch_bounds__(kThreads == 64 ? 256 : kThreads) void norm_grad_ker
     constexpr int kRows = kThreads == 64 ? 4 : 1;
     const int lane = kThreads == 64 ? threadIdx.x & 63 : threadIdx.x, C = (int)a.C;
     float sums[N][V] = {};
-    // every wavefront (or workgroup) takes as many rows as the others: barriers inside over_row need that only where the workgroup is the row
-    for (int64_t row = (int64_t)blockIdx.x * kRows + (kThreads == 64 ? threadIdx.x / 64 : 0); row < a.rows; row += (int64_t)gridDim.x * kRows) {
+    // a row's values are under way while the row before is worked on, where the registers hold both.  Every wavefront (or workgroup) walks its own rows: barriers inside over_row only
+    // where the workgroup is the row.
+    struct { Words<T, V> r[N], gy[N], gt[N]; } now, next;
+    auto load_row = [&](int64_t row, auto& to) {
         const T *r = (const T*)a.x + row * a.x_stride, *gy = (const T*)g.grad_y + row * g.gy_stride, *gt = (const T*)g.grad_total + row * g.gt_stride;
-        float v[N][V], h[N][V], square = 0.0f, dot = 0.0f;
 #pragma unroll
         for (int i = 0; i < N; i++) {
             const int c = (i * kThreads + lane) * V;
-            if (c < C) {
-                load<T, V>(r + c, v[i]);
-                load<T, V>(gy + c, h[i]);
-            } else
-#pragma unroll
-                for (int j = 0; j < V; j++) v[i][j] = h[i][j] = 0.0f;
+            if (c >= C) continue;
+            to.r[i].load(r + c);
+            to.gy[i].load(gy + c);
+            if (g.grad_total) to.gt[i].load(gt + c);
         }
+    };
+    int64_t row = (int64_t)blockIdx.x * kRows + (kThreads == 64 ? threadIdx.x / 64 : 0);
+    constexpr bool kAhead = kThreads < 1024 && N * V * (6 * (int)sizeof(T) / 4 + 1) <= 160;
+    if (kAhead && row < a.rows) load_row(row, next);
+    for (; row < a.rows; row += (int64_t)gridDim.x * kRows) {
+        if constexpr (kAhead) {
+            now = next;
+            if (row + (int64_t)gridDim.x * kRows < a.rows) load_row(row + (int64_t)gridDim.x * kRows, next);
+        } else load_row(row, now);
+        float square = 0.0f, dot = 0.0f;
 #pragma unroll
         for (int i = 0; i < N; i++) {
             const int c = (i * kThreads + lane) * V;
@@ -199,8 +208,9 @@ __global__ __launch_bounds__(kThreads == 64 ? 256 : kThreads) void norm_grad_ker
             load<float, V>(a.weight + c, w);
 #pragma unroll
             for (int j = 0; j < V; j++) {
-                square = fmaf(v[i][j], v[i][j], square);
-                dot = fmaf(v[i][j] * w[j], h[i][j], dot);
+                const float v = now.r[i].value(j);
+                square = fmaf(v, v, square);
+                dot = fmaf(v * w[j], now.gy[i].value(j), dot);
             }
         }
         const float s = rsqrtf(over_row<kThreads, false>(square) / (float)C + (float)a.eps);
@@ -209,13 +219,14 @@ __global__ __launch_bounds__(kThreads == 64 ? 256 : kThreads) void norm_grad_ker
         for (int i = 0; i < N; i++) {
             const int c = (i * kThreads + lane) * V;
             if (c >= C) continue;
-            float w[V], t[V], o[V];
+            float w[V], o[V];
             load<float, V>(a.weight + c, w);
-            if (g.grad_total) load<T, V>(gt + c, t);
 #pragma unroll
             for (int j = 0; j < V; j++) {
-                o[j] = s * (h[i][j] * w[j] - v[i][j] * m) + (g.grad_total ? t[j] : 0.0f);
-                sums[i][j] = fmaf(h[i][j], v[i][j] * s, sums[i][j]);
+                const float v = now.r[i].value(j), h = now.gy[i].value(j);
+                o[j] = s * (h * w[j] - v * m);
+                if (g.grad_total) o[j] += now.gt[i].value(j);
+                sums[i][j] = fmaf(h, v * s, sums[i][j]);
             }
             store<T, V>((T*)g.grad_x + row * C + c, o);
         }
@@ -267,11 +278,30 @@ template <class T> __global__ __launch_bounds__(256) void norm_grad_columns_kern
     parts[part * a.C + c] = v;
 }
 
+// The partial sums' rows added up: sixteen columns a workgroup, a sixty-fourth of the rows each thread, then in order.  (Sixty-four columns leave a few
+// workgroups: 1,024 rows of 333 columns took 5.2 us.)
 __global__ __launch_bounds__(1024) void norm_weight_kernel(const float* parts, int64_t rows, int64_t C, float* grad_weight)
 {
-    const int64_t c = (int64_t)blockIdx.x * 64 + (threadIdx.x & 63);
-    const float s = sum_rows(parts + min(c, C - 1), rows, C);
-    if (threadIdx.x < 64 && c < C) grad_weight[c] = s;
+    __shared__ float part[64][16];
+    const int col = threadIdx.x & 15, r0 = threadIdx.x >> 4;
+    const int64_t c = (int64_t)blockIdx.x * 16 + col;
+    const float* p = parts + min(c, C - 1);
+    float v[8] = {};
+    int64_t r = r0;
+    for (; r + 7 * 64 < rows; r += 8 * 64)
+#pragma unroll
+        for (int i = 0; i < 8; i++) v[i] += p[(r + i * 64) * C];
+    for (; r < rows; r += 64) v[0] += p[r * C];
+    part[r0][col] = ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7]));
+    __syncthreads();
+    if (threadIdx.x < 16 && c < C) {
+        float s[4] = {};
+#pragma unroll
+        for (int i = 0; i < 64; i += 4)
+#pragma unroll
+            for (int k = 0; k < 4; k++) s[k] += part[i + k][col];
+        grad_weight[c] = (s[0] + s[1]) + (s[2] + s[3]);
+    }
 }
 
 constexpr int64_t kLongParts = 64;
@@ -336,7 +366,7 @@ template <int V> GradPlan grad_plan(const sig_norm_args& a)
 template <class T, int V> hipError_t backward_by(const sig_norm_args& a, const NormGrads& g, float* ws, hipStream_t stream)
 {
     const GradPlan p = grad_plan<V>(a);
-    const int64_t groups = (a.C + 63) / 64;
+    const int64_t groups = (a.C + 15) / 16;
     if (!launchable(groups, 1024)) return kTooManyThreads;
     if (a.rows && p.registers) {
         held<V>((a.C + V - 1) / V, [&](auto n, auto t) {

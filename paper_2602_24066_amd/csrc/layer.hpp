@@ -37,6 +37,19 @@ struct e4m3 { uint8_t bits; };
 // to nearest, ties to even, values a little beyond 448 to 448, a NaN stays one (conversion of the hardware)
 template <> __device__ __forceinline__ e4m3 from_float<e4m3>(float v) { return {(uint8_t)(__builtin_amdgcn_cvt_pk_fp8_f32(v, v, 0, false) & 0xff)}; }
 
+// V values of float32 or bfloat16 in words, as they lie in memory (elements of their own would take a register each)
+template <class T, int V, bool kWhole = V * sizeof(T) % 4 == 0> struct Words {
+    typedef uint32_t Vector __attribute__((ext_vector_type(V * sizeof(T) / 4)));
+    Vector w;
+    __device__ __forceinline__ void load(const T* p) { w = *(const Vector*)p; }
+    __device__ __forceinline__ float value(int j) const { return sizeof(T) == 4 ? __uint_as_float(w[j]) : __uint_as_float(j % 2 ? w[j / 2] & 0xffff0000u : w[j / 2] << 16); }
+};
+template <> struct Words<bf16, 1, false> {
+    uint16_t w;
+    __device__ __forceinline__ void load(const bf16* p) { w = p->bits; }
+    __device__ __forceinline__ float value(int) const { return __uint_as_float((uint32_t)w << 16); }
+};
+
 // Neighbouring values as they lie in memory, converted two (bfloat16, e4m3) an instruction; V a multiple of the values of a word
 __device__ __forceinline__ uint32_t word_of(const float* v, bf16*)
 {
