@@ -530,11 +530,11 @@ template <class T> __global__ __launch_bounds__(1024) void bias_kernel(const flo
 
 // ---- which tile, and how many splits.  A model of the launch, in us: `slab` is what a tile's slab costs a compute unit that is busy with as many
 // as it holds, `alone` what it costs at least, `over` what a tile costs besides (first loads, outputs).  Measured on large squares (us a slab):
-//   bfloat16 256: 8192^3 in 856 us, 128: 1,022 us     float32 256: 4096^3 in 981, 128: 998, 64: 1,040     e4m3 256: 8192^3 in 476, 128: 550
+//   bfloat16 256: 8192^3 in 856 us, 128: 1,022 us     float32 128: 4096^3 in 998, 64: 1,040     e4m3 256: 8192^3 in 476, 128: 550
 // and 16384 x 4096 x 1024 (16 slabs): 148 us with tiles of 256, 172 of 128; e4m3 16384 x 2048 x 2048: 72 and 79.
 struct Cost { int tile; double slab, alone, over; };
 constexpr Cost kCosts[3][3] = {
-    {{64, 0.51, 0.70, 1.0}, {128, 1.95, 1.95, 3.0}, {256, 7.66, 7.66, 14.0}},          // float32
+    {{64, 0.51, 0.70, 1.0}, {128, 1.95, 1.95, 3.0}, {}},                               // float32: tiles of 256 gain 2 % at most
     {{64, 0.17, 0.50, 0.8}, {128, 0.50, 0.80, 2.4}, {256, 1.68, 1.68, 10.5}},          // bfloat16
     {{64, 0.18, 0.50, 0.8}, {128, 0.54, 0.80, 1.2}, {256, 1.86, 1.86, 6.3}},           // e4m3
 };
@@ -561,7 +561,7 @@ Tiles tiles_of(int64_t M, int64_t N, int64_t K, int e, bool aligned)
     Tiles best{};
     double least = 0.0;
     for (const Cost& c : kCosts[e == 4 ? 0 : e == 2 ? 1 : 2]) {
-        if (!aligned && c.tile != kTile) continue;
+        if (c.tile == 0 || (!aligned && c.tile != kTile)) continue;
         const int64_t m = (M + c.tile - 1) / c.tile, n = (N + c.tile - 1) / c.tile;
         for (int64_t want : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32}) {
             if (want > 1 && slabs / want < 4) break;
@@ -619,12 +619,13 @@ template <class T, class O> hipError_t product(int64_t M, int64_t N, int64_t K, 
     }
     const int64_t blocks = (int64_t)t.m * t.n * t.splits;
     if (!launchable(blocks, 512)) return kTooManyThreads;
-    hipError_t err;
+    hipError_t err = hipSuccess;
     if (!aligned) {
         product_kernel<T, O><<<(uint32_t)blocks, 256, 0, stream>>>(t, x, ldx, w, ldw, o, parts);
         err = hipGetLastError();
-    } else if (t.tile == 256) err = launch<T, O, 256, 4, 2>(t, x, ldx, w, ldw, o, parts, (uint32_t)blocks, stream);
-    else if (t.tile == 128) err = launch<T, O, 128, 2, 2>(t, x, ldx, w, ldw, o, parts, (uint32_t)blocks, stream);
+    } else if (t.tile == 256) {
+        if constexpr (sizeof(T) < 4) err = launch<T, O, 256, 4, 2>(t, x, ldx, w, ldw, o, parts, (uint32_t)blocks, stream);
+    } else if (t.tile == 128) err = launch<T, O, 128, 2, 2>(t, x, ldx, w, ldw, o, parts, (uint32_t)blocks, stream);
     else err = launch<T, O, 64, 2, 2>(t, x, ldx, w, ldw, o, parts, (uint32_t)blocks, stream);
     if (err != hipSuccess || t.splits == 1) return err;
     const int64_t joins = (M * ((N + 3) / 4) + 255) / 256;

@@ -1,0 +1,316 @@
+"""Operators of a layer where they can go wrong: large tiles and every path of the matrix product, values next to what counts, far offsets, gradients by
+differences, special values that stay in their rows.  Whole numbers are exact in float32, so products of them are compared for equality; other tolerances are
+stated where they are used."""
+import math
+
+import pytest
+import torch
+
+import paper_2602_24066_amd as S
+from tests import layer_reference as R
+from tests.test_layer import B16, E8, F32, H, normal, whole, within
+from tests.test_sequence import close, up
+
+gpu = pytest.mark.gpu
+
+
+def product(x, w, *more):
+    """x w^T in float64 on the GPU by slices of the contraction, of whole numbers, exact; more: added."""
+    out = torch.zeros(x.shape[0], w.shape[0], dtype=torch.float64, device="cuda")
+    for k in range(0, x.shape[1], 256):
+        out += x[:, k:k + 256].float().double() @ w[:, k:k + 256].float().double().t()
+    for m in more:
+        out += m.double()
+    return out
+
+
+@gpu
+@pytest.mark.parametrize("t", [F32, B16, E8])
+@pytest.mark.parametrize("M,K,N", [(4099, 1040, 4096), (4096, 1040, 4100), (2500, 4112, 2050), (300, 16400, 70), (65, 16384, 64), (700, 40, 9000), (4100, 523, 2100), (130, 2056, 515)])
+def test_tiles_and_splits(M, K, N, t):
+    """Tiles of every size, their edges along all three sides, splits of the contraction, rows that are no multiples of 16 bytes; epilogues with everything."""
+    n = whole(M + N, 2)
+    out = B16 if t is E8 else t
+    x, w, b, r = up(n(M, K).to(t)), up(n(N, K).to(t)), up(n(N).to(out)), up(n(M, N).to(out))
+    want = product(x, w, b, r)
+    assert torch.equal(S.sig_linear_forward(x, w, b, r), want.to(out))
+    if t is not E8:
+        g = up(whole(K, 2)(M, N).to(t))
+        gx, gw, gb = S.sig_linear_backward(x, w, g, bias=True)
+        assert torch.equal(gx, product(g, w.t().contiguous()).to(t))
+        assert torch.equal(gw, product(g.t().contiguous(), x.t().contiguous()).to(t))
+        assert torch.equal(gb, g.double().sum(0).to(t))
+
+
+@gpu
+@pytest.mark.parametrize("t", [F32, B16, E8])
+@pytest.mark.parametrize("M", [3, 40, 64, 70, 300])
+@pytest.mark.parametrize("K,pad", [(64, 16), (80, 16), (208, 48), (33, 3), (100, 1)])
+def test_what_lies_beside_the_rows_is_not_used(M, K, pad, t):
+    """NaN behind the end of every row, behind the last row and before the first: a sum that takes one of them is NaN."""
+    n, N = whole(M + K, 3), 90
+    nan = lambda v: v.to(t) if t is not E8 else v.to(t)                                      # noqa: E731
+    big = torch.full((M + 2, K + pad), math.nan)
+    big[1:M + 1, :K] = n(M, K)
+    weights = torch.full((N + 2, K), math.nan)
+    weights[1:N + 1] = n(N, K)
+    x, w = up(nan(big))[1:M + 1, :K], up(nan(weights))[1:N + 1]
+    out = B16 if t is E8 else t
+    want = product(x, w)
+    assert torch.equal(S.sig_linear_forward(x, w), want.to(out))
+    edge = torch.full((M, N + 3), math.nan)
+    edge[:, :N] = n(M, N)
+    r = up(edge.to(out))[:, :N]
+    assert torch.equal(S.sig_linear_forward(x, w, residual=r), (want + r.double()).to(out))
+    if t is not E8:
+        g = r
+        gx, gw, gb = S.sig_linear_backward(x, w, g, bias=True)
+        assert torch.equal(gx, product(g, w.t().contiguous()).to(t)) and torch.equal(gw, product(g.t().contiguous(), x.t().contiguous()).to(t))
+        assert torch.equal(gb, g.double().sum(0).to(t))
+    if t is not E8:
+        y, _ = S.sig_norm_forward(x, torch.ones(K, device="cuda"), x)
+        assert torch.isfinite(y).all() and torch.equal(y, S.sig_norm_forward(x.contiguous(), torch.ones(K, device="cuda"), x.contiguous())[0])
+
+
+@gpu
+@pytest.mark.parametrize("t", [F32, B16])
+def test_outputs_end_where_they_end(t):
+    """Rows behind the outputs stay as they were (through the C ABI, into one larger buffer)."""
+    from tests.test_layer import GATED_ORDER, LINEAR_ORDER, norm_args, pack
+    lib, kind = S.load_library(), 0 if t is F32 else 1
+    stream = torch.cuda.current_stream().cuda_stream
+    for M, K, N in ((5, 48, 33), (70, 64, 40), (300, 128, 130)):
+        x, w = torch.ones(M, K, dtype=t, device="cuda"), torch.ones(N, K, dtype=t, device="cuda")
+        y = torch.full((M * N + 64,), 7.0, dtype=t, device="cuda")
+        a = pack(dict.fromkeys(LINEAR_ORDER, 0) | dict(dtype=kind, out=kind, M=M, N=N, K=K, xs=K, x=x.data_ptr(), weight=w.data_ptr()), LINEAR_ORDER)
+        ws = torch.empty(lib.sig_linear_forward_workspace_bytes(a) + 1, dtype=torch.uint8, device="cuda")
+        assert lib.sig_linear_forward(a, y.data_ptr(), 0, ws.data_ptr(), ws.numel(), stream) == 0
+        assert (y[:M * N] == K).all() and (y[M * N:] == 7).all()
+        z = torch.full((M * K + 64,), 7.0, dtype=t, device="cuda")
+        ones = torch.ones(K, device="cuda")
+        assert lib.sig_norm_forward(norm_args(dtype=kind, rows=M, C=K, xs=K, rs=0, x=x.data_ptr(), residual=0, weight=ones.data_ptr()), z.data_ptr(), 0, 0, stream) == 0
+        assert ((z[:M * K] - 1).abs() < 1e-2).all() and (z[M * K:] == 7).all()
+    for B, L, D in ((1, 130, 6), (2, 17, 33)):
+        x, rate = torch.ones(B, L, D, dtype=t, device="cuda"), torch.zeros(D, device="cuda")
+        y = torch.full((B * L * D + 256,), 7.0, dtype=t, device="cuda")
+        lens = torch.tensor([L] + [3] * (B - 1), dtype=torch.int32, device="cuda")
+        p = x.data_ptr()
+        a = pack(dict(dtype=kind, B=B, L=L, D=D, xb=L * D, xt=D, db=L * D, dt=D, ib=L * D, it=D, x=p, decay=p, input=p, rate=rate.data_ptr(), initial=0, lengths=lens.data_ptr()), GATED_ORDER)
+        ws = torch.empty(lib.sig_gated_scan_forward_workspace_bytes(a) + 1, dtype=torch.uint8, device="cuda")
+        assert lib.sig_gated_scan_forward(a, y.data_ptr(), 0, 0, 0, ws.data_ptr(), ws.numel(), stream) == 0
+        got = y[:B * L * D].reshape(B, L, D)
+        assert (got[0] > 0).all() and (got[1:, :3] > 0).all() and not got[1:, 3:].any() and (y[B * L * D:] == 7).all()
+
+
+@gpu
+def test_offsets_beyond_32_bits():
+    """Rows and streams that lie gigabytes apart."""
+    far = 1 << 30
+    held = torch.zeros(3 * far + 64, dtype=B16, device="cuda")
+    x = held.as_strided((3, 48), (far, 1))
+    x.copy_(whole(5, 3)(3, 48))
+    near, w, ones = x.clone(), up(whole(6, 3)(40, 48).to(B16)), torch.ones(48, device="cuda")
+    assert torch.equal(S.sig_linear_forward(x, w), S.sig_linear_forward(near, w))
+    assert torch.equal(S.sig_norm_forward(x, ones, x)[0], S.sig_norm_forward(near, ones, near)[0])
+    assert torch.equal(S.sig_quantize(x)[1], S.sig_quantize(near)[1])
+    g = up(whole(7, 3)(3, 40).to(B16))
+    assert torch.equal(S.sig_linear_backward(x, w, g)[1], S.sig_linear_backward(near, w, g)[1])
+    s = held.as_strided((3, 8, 6), (far, 6, 1))
+    s.copy_(normal(8)(3, 8, 6))
+    c, rate = s.clone(), torch.zeros(6, device="cuda")
+    one, two = S.sig_gated_scan_forward(s, s, s, rate, checkpoint=True), S.sig_gated_scan_forward(c, c, c, rate, checkpoint=True)
+    assert torch.equal(one[0], two[0]) and torch.equal(one[1], two[1])
+    assert torch.equal(S.sig_gated_scan_backward(s, s, s, rate, s, one[2])["x"], S.sig_gated_scan_backward(c, c, c, rate, c, two[2])["x"])
+    time = held.as_strided((1, 5, 6), (0, 1 << 22, 1))                                       # beyond the kernels' reach: copied
+    time.copy_(normal(9)(1, 5, 6))
+    c = time.clone()
+    assert torch.equal(S.sig_gated_scan_forward(time, time, time, rate)[0], S.sig_gated_scan_forward(c, c, c, rate)[0])
+    time = held.as_strided((1, 300, 6), (0, (1 << 22) - 2, 1))                               # just within it
+    time.copy_(normal(10)(1, 300, 6))
+    c = time.clone()
+    one, two = S.sig_gated_scan_forward(time, time, time, rate, checkpoint=True), S.sig_gated_scan_forward(c, c, c, rate, checkpoint=True)
+    assert torch.equal(one[0], two[0])
+    g1, g2 = S.sig_gated_scan_backward(time, time, time, rate, time, one[2]), S.sig_gated_scan_backward(c, c, c, rate, c, two[2])
+    assert all(torch.equal(g1[k], g2[k]) for k in ("x", "decay_gate", "input_gate", "log_rate"))
+
+
+@gpu
+def test_more_than_32_bits_of_outputs():
+    M, N, K = (1 << 16) + 3, (1 << 15) + 8, 16
+    x, w = up(whole(1, 3)(M, K).to(B16)), up(whole(2, 3)(N, K).to(B16))
+    y = S.sig_linear_forward(x, w)
+    for rows in (slice(0, 300), slice(M - 300, M), slice(40000, 40100)):
+        assert torch.equal(y[rows], product(x[rows], w).to(B16))
+    del y
+    rows, C = (1 << 20) + 1, 2056
+    v = torch.ones(rows, C, dtype=B16, device="cuda")
+    v[-1] = 2.0
+    y, _ = S.sig_norm_forward(v, torch.ones(C, device="cuda"))
+    assert ((y[-5:] - 1).abs() < 1e-2).all() and ((y[:5] - 1).abs() < 1e-2).all() and float(y.float().min()) > 0.99
+
+
+@gpu
+@pytest.mark.parametrize("bad", [math.nan, math.inf])
+@pytest.mark.parametrize("t", [F32, B16])
+def test_values_that_are_not_finite_stay_in_their_rows(t, bad):
+    n = normal(3)
+    for M, K, N in ((9, 64, 40), (130, 96, 70), (130, 97, 70), (600, 520, 600)):
+        x, w = up(n(M, K).to(t)), up(n(N, K).to(t))
+        clean = S.sig_linear_forward(x, w)
+        y0, _ = S.sig_norm_forward(x, torch.ones(K, device="cuda"))
+        x[4, 5] = bad
+        got = S.sig_linear_forward(x, w)
+        keep = [i for i in range(M) if i != 4]
+        assert torch.equal(got[keep], clean[keep]) and not torch.isfinite(got[4]).all()
+        y, _ = S.sig_norm_forward(x, torch.ones(K, device="cuda"))
+        assert torch.equal(y[keep], y0[keep])
+    x = up(n(3, 200, 10).to(t))
+    rate = torch.zeros(10, device="cuda")
+    clean = S.sig_gated_scan_forward(x, x, x, rate)[0]
+    x[1, 50, 4] = bad
+    got, _, ck = S.sig_gated_scan_forward(x, x, x, rate, checkpoint=True)
+    same = torch.ones_like(got, dtype=torch.bool)
+    same[1, 50:, 4] = False
+    assert torch.equal(got[same], clean[same]) and not torch.isfinite(got[1, 50, 4])
+    g = S.sig_gated_scan_backward(x, x, x, rate, clean, ck)
+    for k in ("x", "decay_gate", "input_gate"):
+        assert torch.isfinite(g[k][[0, 2]]).all() and torch.isfinite(g[k][1][:, [0, 1, 2, 3, 5, 6, 7, 8, 9]]).all(), k
+
+
+@gpu
+def test_gradients_that_are_not_finite_leave_hidden_tokens_zero():
+    B, L, D = 2, 150, 6
+    x, rate = torch.randn(B, L, D, device="cuda"), torch.zeros(D, device="cuda")
+    lens = torch.tensor([3, 140], dtype=torch.int32, device="cuda")
+    _, _, ck = S.sig_gated_scan_forward(x, x, x, rate, lengths=lens, checkpoint=True, initial_state=torch.zeros(B, D, device="cuda"))
+    for bad in (math.nan, math.inf):
+        last = torch.full((B, D), bad, device="cuda")
+        last[1] = 0.0
+        g = S.sig_gated_scan_backward(x, x, x, rate, x, ck, torch.zeros(B, D, device="cuda"), lens, last)
+        for k in ("x", "decay_gate", "input_gate"):
+            assert not g[k][0, 3:].any() and not g[k][1, 140:].any() and torch.isfinite(g[k][1]).all() and not torch.isfinite(g[k][0, :3]).all(), k
+
+
+def differences(f, leaves, grads, what):
+    """The slope of f along a random direction of every leaf by central differences of the kernels' own float32 outputs, against the gradient.  f is summed in
+    float64; steps of 2^-7 leave errors of the third order below 1e-3 of values around one and of rounding below 1e-4."""
+    for k, v in leaves.items():
+        d = up(normal(len(k))(*v.shape)) if v.dim() else None
+        h = 2.0 ** -7
+        a, b = (f({**leaves, k: v + s * h * d}) for s in (1, -1))
+        want, got = float(a - b) / (2 * h), float((grads[k].double() * d.double()).sum())
+        size = float((grads[k].double().square().sum() * d.double().square().mean()).sqrt())
+        assert abs(got - want) <= 5e-3 * max(abs(want), size), f"{what}: {k}: {got} for {want}"
+
+
+@gpu
+def test_gradients_are_slopes():
+    n = normal(12)
+    x, w, m, b, gy, gt = up(n(7, 40)), up(1 + 0.2 * n(40)), up(n(24, 40) / 6), up(0.3 * n(24)), up(n(7, 24)), up(n(7, 40))
+    f = lambda v: (S.sig_norm_forward(v["x"], v["w"])[0].double() * gt.double()).sum()      # noqa: E731
+    gx, gw = S.sig_norm_backward(x, w, gt)
+    differences(f, {"x": x, "w": w}, {"x": gx, "w": gw}, "norm")
+    for act in ("silu", "gelu"):
+        f = lambda v: (S.sig_linear_forward(v["x"], v["m"], v["b"], activation=act).double() * gy.double()).sum()   # noqa: E731
+        _, pre = S.sig_linear_forward(x, m, b, activation=act, keep=True)
+        gx, gm, gb = S.sig_linear_backward(x, m, gy, act, pre, bias=True)
+        differences(f, {"x": x, "m": m, "b": b}, {"x": gx, "m": gm, "b": gb}, act)
+    v = {k: up(t) for k, t in R.gated_inputs(2, 40, 9, seed=4).items() if t is not None}
+    go, gs = up(n(2, 40, 9)), up(n(2, 9))
+
+    def g(v):
+        y, s = S.sig_gated_scan_forward(**v)
+        return (y.double() * go.double()).sum() + (s.double() * gs.double()).sum()
+
+    _, _, ck = S.sig_gated_scan_forward(**v, checkpoint=True)
+    grads = S.sig_gated_scan_backward(v["x"], v["decay_gate"], v["input_gate"], v["log_rate"], go, ck, v["initial_state"], grad_final_state=gs)
+    differences(g, v, grads, "gated scan")
+
+
+@gpu
+@pytest.mark.parametrize("L", [127, 128, 129, 1000, 4097])
+@pytest.mark.parametrize("t", [F32, B16])
+def test_chunks_of_long_streams(L, t):
+    """Few streams of any length: time chunks, against the same recurrence token by token (the single-token calls)."""
+    B, D = 2, 70
+    v = {k: up(w) for k, w in R.gated_inputs(B, L, D, t, seed=L, rate=0.02).items() if w is not None}
+    lens = torch.tensor([L, L - 100], dtype=torch.int32, device="cuda")
+    y, last, ck = S.sig_gated_scan_forward(**v, lengths=lens, checkpoint=True)
+    held = v["initial_state"].clone()
+    rows, end = [], None
+    for i in range(L):
+        if i == L - 100:
+            end = held[1].clone()
+        rows.append(S.sig_gated_scan_step(v["x"][:, i], v["decay_gate"][:, i], v["input_gate"][:, i], v["log_rate"], held))
+    want = torch.stack(rows, 1)
+    want[1, L - 100:] = 0
+    close(y, want.cpu(), t, "y")
+    close(last, torch.stack([held[0], end]).cpu(), F32, "state")
+    g = up(normal(L)(B, L, D).to(t))
+    whole_pass = S.sig_gated_scan_backward(v["x"], v["decay_gate"], v["input_gate"], v["log_rate"], g, ck, v["initial_state"], lens, last)
+    # the same from the definition, reversed in time, in 64 bits on the GPU
+    s = {k: w.double() for k, w in v.items()}
+    open_, i = torch.sigmoid(s["decay_gate"]), torch.sigmoid(s["input_gate"])
+    u = torch.exp(s["log_rate"]) * open_
+    a, size = torch.exp(-u), torch.sqrt(-torch.expm1(-2 * u))
+    h = [s["initial_state"]]
+    for k in range(L):
+        on = (k < lens)[:, None]
+        h.append(torch.where(on, a[:, k] * h[-1] + size[:, k] * i[:, k] * s["x"][:, k], h[-1]))
+    back, gx, gp = last.double(), torch.zeros_like(s["x"]), torch.zeros_like(s["x"])
+    for k in reversed(range(L)):
+        on = (k < lens)[:, None]
+        lam = torch.where(on, back + g[:, k].double(), 0)
+        gx[:, k] = lam * size[:, k] * i[:, k]
+        gp[:, k] = lam * u[:, k] * (1 - open_[:, k]) * (a[:, k] ** 2 / size[:, k] * i[:, k] * s["x"][:, k] - a[:, k] * h[k])
+        back = torch.where(on, lam * a[:, k], back)
+    close(whole_pass["x"], gx.cpu(), t, "grad x")
+    close(whole_pass["decay_gate"], gp.cpu(), t, "grad decay gate")
+    close(whole_pass["initial_state"], back.cpu(), F32, "grad initial state")
+
+
+@gpu
+def test_rates_next_to_nothing_keep_their_precision():
+    """1 - a^2 of decays next to one: relative precision of the states that a first token gives, over the border between the two ways it is computed."""
+    u = torch.logspace(-12, 1, 400).double()
+    u = torch.cat([u, torch.linspace(0.24, 0.26, 101).double()])
+    D = u.numel()
+    rate = torch.log(2 * u).float()                                                          # gates of zero: half of it
+    x = torch.ones(1, 1, D, device="cuda")
+    z = torch.zeros_like(x)
+    y, _ = S.sig_gated_scan_forward(x, z, z, up(rate))
+    want = 0.5 * torch.sqrt(-torch.expm1(-torch.exp(rate.double())))
+    # exp(log_rate) carries |log_rate| 2^-24 of rounding, half of it after the root; the series' end and the difference 2e-7 and 4e-7, likewise
+    within(y[0, 0], want, want * (8 + rate.double().abs()) * 2.0 ** -24 + want * 5e-7, "y")
+
+
+@gpu
+def test_two_graphs_and_eager_work_side_by_side():
+    """Two captured calls of the same operators on other inputs, replayed in turn with eager work between: workspaces are not shared."""
+    n = normal(30)
+    def make(seed):
+        m = normal(seed)
+        x, w, g = up(m(2, 300, 72).to(B16)), up((m(40, 72) / 8).to(B16)), up(m(2, 300, 40).to(B16))
+        rate, norm = up(m(72) - 2), up(1 + 0.1 * m(72))
+
+        def run():
+            y, s, ck = S.sig_gated_scan_forward(x, x, x, rate, checkpoint=True)
+            b = S.sig_gated_scan_backward(x, x, x, rate, x, ck)
+            q, total = S.sig_norm_forward(y, norm, x)
+            z, pre = S.sig_linear_forward(q, w, activation="gelu", keep=True)
+            return [y, s, b["x"], b["log_rate"], q, z, *S.sig_linear_backward(q, w, g, "gelu", pre, bias=True), *S.sig_norm_backward(total, norm, y)]
+        return run
+    runs = [make(1), make(2)]
+    want = [[v.clone() for v in r()] for r in runs]
+    graphs, held = [], []
+    for r in runs:
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1]):
+            held.append(r())
+    for k in range(4):
+        graphs[k % 2].replay()
+        eager = runs[1 - k % 2]()
+        graphs[1 - k % 2].replay()
+        torch.cuda.synchronize()
+        for got, ok in ((held[0], want[0]), (held[1], want[1]), (eager, want[1 - k % 2])):
+            assert all(torch.equal(a, b) for a, b in zip(got, ok)), k
