@@ -302,58 +302,132 @@ template <class T, class O> __global__ __launch_bounds__(256) void product_kerne
     put<O, 4, 4>(t, o, parts, p.split, m0 + wm * 64, n0 + wn * 64, acc, (float*)lds + wave * 16 * 68);
 }
 
-// One slab of N rows a thread, 16 bytes of each, into LDS; `step` threads lie between a thread's rows
-template <int N> __device__ __forceinline__ void fetch(__amdgpu_buffer_rsrc_t from, __attribute__((address_space(3))) Chunk* to, int step, const int* rows, int at, int k)
-{
-#pragma unroll
-    for (int i = 0; i < N; i++) __builtin_amdgcn_raw_ptr_buffer_load_lds(from, to + i * step, 16, rows[i] + at, k, 0, 0);
-}
+// ---- the same for operands whose rows are multiples of 16 bytes, 16-byte aligned: chunks go from memory to LDS without passing registers, a wavefront's
+// load filling 1,024 bytes in lane order; what a lane fetches decides where it lies.
+//
+// An operand of B rows along the contraction is as above.  One that lies the other way (kAcross, bfloat16: rows of outputs, one for every place of the
+// contraction, as the gradients' operands do) comes as 64 such rows of B outputs a slab, and the LDS reads turn it: a transposing read gives each of sixteen
+// lanes four rows of its own column.  Row r keeps chunk c at place c ^ turn(r): the rows that one read touches (four, and the four that lie eight further on)
+// are whole multiples of the banks apart otherwise.
+template <class T, bool kAcross, int B, int kThreads> struct Side {
+    static constexpr int E = kChunk / sizeof(T), kStep = kSlab / sizeof(T), kLoads = B * kChunks / kThreads, kRow = kAcross ? B / E : kChunks;     // chunks of a row
+    typedef __attribute__((address_space(3))) Chunk Lds;
+    const T* base;
+    int64_t ld;
+    int offset[kLoads], row, chunk;
 
-// ---- the same for operands whose rows are multiples of 16 bytes, 16-byte aligned: chunks go from memory to LDS without passing registers.
-// A wavefront's load fills 1,024 bytes of LDS in lane order, so lane l of row r fetches chunk (l ^ r) & 7.
-template <class T, class O, int BM, int BN, int WM, int WN, int kStages>
+    static __device__ __forceinline__ int turn(int r) { return (((r & 3) | (r >> 1 & 4)) << 1) & (kRow - 1); }
+
+    // outputs first .. of `outs`; rows and chunks behind the last are others that are there
+    __device__ __forceinline__ Side(const T* p, int64_t ld, int64_t first, int64_t outs) : base(p + (kAcross ? first : first * ld)), ld(ld)
+    {
+        row = threadIdx.x / kRow;
+        chunk = (threadIdx.x ^ (kAcross ? turn(row) : row)) & (kRow - 1);
+        if (kAcross && first + chunk * E >= outs) chunk = 0;
+#pragma unroll
+        for (int i = 0; i < kLoads; i++) {
+            const int r = row + i * (kThreads / kRow);
+            offset[i] = kAcross ? (int)((r * ld + chunk * E) * (int)sizeof(T)) : (int)(min((int64_t)r, outs - 1 - first) * ld * (int)sizeof(T));
+        }
+    }
+    __device__ __forceinline__ void fetch(Lds* to, int slab, int64_t K) const
+    {
+        if constexpr (kAcross) {
+            const __amdgpu_buffer_rsrc_t from = __builtin_amdgcn_make_buffer_rsrc((void*)(base + (int64_t)slab * kStep * ld), 0, 0x7fffffff, 0x27000);
+            const int left = (int)min(K - (int64_t)slab * kStep, (int64_t)kStep);
+            if (left == kStep)
+#pragma unroll
+                for (int i = 0; i < kLoads; i++) __builtin_amdgcn_raw_ptr_buffer_load_lds(from, to + i * kThreads, 16, offset[i], 0, 0, 0);
+            else
+#pragma unroll
+                for (int i = 0; i < kLoads; i++)
+                    __builtin_amdgcn_raw_ptr_buffer_load_lds(from, to + i * kThreads, 16, (int)((min(row + i * (kThreads / kRow), left - 1) * ld + chunk * E) * (int)sizeof(T)), 0, 0, 0);
+        } else {
+            const __amdgpu_buffer_rsrc_t from = __builtin_amdgcn_make_buffer_rsrc((void*)base, 0, 0x7fffffff, 0x27000);
+            const int at = (int64_t)slab * kStep + chunk * E < K ? chunk * kChunk : 0;       // beyond the row's end its slab's first chunk
+#pragma unroll
+            for (int i = 0; i < kLoads; i++) __builtin_amdgcn_raw_ptr_buffer_load_lds(from, to + i * kThreads, 16, offset[i] + at, slab * kSlab, 0, 0);
+        }
+    }
+    // zeros behind the end of the contraction, `left` places of the slab being before it
+    static __device__ __forceinline__ void clear(Chunk* in, int left)
+    {
+        for (int id = threadIdx.x; id < B * kChunks; id += kThreads)
+            if (kAcross ? id / kRow >= left : ((id ^ (id / kRow)) & 7) >= left / E) in[id] = Chunk{};
+    }
+    // What a lane feeds for outputs o .. o + 16 N - 1 of the tile at step c of the slab (f: of a feed of kF chunks)
+    template <int N, int kF> static __device__ __forceinline__ void read(const Chunk* in, int o, int c, int f, Chunk (&to)[N][kF])
+    {
+        const int lane = threadIdx.x & 63;
+        if constexpr (!kAcross) {
+#pragma unroll
+            for (int i = 0; i < N; i++) to[i][f] = in[(o + i * 16 + (lane & 15)) * kChunks + ((c * 4 + lane / 16) ^ (lane & 7))];
+        } else {
+            // The compiler would wait for the next slab's loads before a transposing read, which it does not tell from what they write.  So the reads are written
+            // out, two or four outputs' at a time with their own wait, while the products of those before are under way.
+            static_assert(N % 2 == 0);
+            const int r = lane / 16 * 8 + (lane & 15) / 4;                                   // and the row four further on, whose turn is the same
+            const uint32_t start = (uint32_t)(uintptr_t)(const Lds*)in + r * kRow * kChunk + (lane & 1) * 8;
+            constexpr int kHigh = 4 * kRow * kChunk;
+            auto place = [&](int i) { return start + c * (32 * kRow * kChunk) + (((o / E + i * 2 + (lane & 3) / 2) ^ turn(r)) * kChunk); };
+            typedef uint64_t Halves __attribute__((ext_vector_type(2)));
+#pragma unroll
+            for (int i = 0; i < N; i += N % 4 ? 2 : 4) {
+                uint64_t l0, h0, l1, h1;
+                if constexpr (N % 4 == 0) {
+                    uint64_t l2, h2, l3, h3;
+                    asm volatile("ds_read_b64_tr_b16 %0, %8\n\tds_read_b64_tr_b16 %1, %8 offset:%12\n\tds_read_b64_tr_b16 %2, %9\n\tds_read_b64_tr_b16 %3, %9 offset:%12\n\t"
+                                 "ds_read_b64_tr_b16 %4, %10\n\tds_read_b64_tr_b16 %5, %10 offset:%12\n\tds_read_b64_tr_b16 %6, %11\n\tds_read_b64_tr_b16 %7, %11 offset:%12\n\t"
+                                 "s_waitcnt lgkmcnt(0)"
+                                 : "=&v"(l0), "=&v"(h0), "=&v"(l1), "=&v"(h1), "=&v"(l2), "=&v"(h2), "=&v"(l3), "=&v"(h3)
+                                 : "v"(place(i)), "v"(place(i + 1)), "v"(place(i + 2)), "v"(place(i + 3)), "n"(kHigh));
+                    to[i + 2][f] = __builtin_bit_cast(Chunk, Halves{l2, h2});
+                    to[i + 3][f] = __builtin_bit_cast(Chunk, Halves{l3, h3});
+                } else
+                    asm volatile("ds_read_b64_tr_b16 %0, %4\n\tds_read_b64_tr_b16 %1, %4 offset:%6\n\tds_read_b64_tr_b16 %2, %5\n\tds_read_b64_tr_b16 %3, %5 offset:%6\n\t"
+                                 "s_waitcnt lgkmcnt(0)"
+                                 : "=&v"(l0), "=&v"(h0), "=&v"(l1), "=&v"(h1)
+                                 : "v"(place(i)), "v"(place(i + 1)), "n"(kHigh));
+                to[i][f] = __builtin_bit_cast(Chunk, Halves{l0, h0});
+                to[i + 1][f] = __builtin_bit_cast(Chunk, Halves{l1, h1});
+            }
+        }
+    }
+};
+
+template <class T, class O, int B, int WM, int WN, bool kAcrossX, bool kAcrossW>
 __global__ __launch_bounds__(WM * WN * 64) void aligned_kernel(Tiles t, const T* x, int64_t ldx, const T* w, int64_t ldw, Out o, float* parts)
 {
-    constexpr int kThreads = WM * WN * 64, FM = BM / WM / 16, FN = BN / WN / 16, E = kChunk / sizeof(T), kStep = kSlab / sizeof(T);
-    constexpr int kStage = (BM + BN) * kChunks, LX = BM * kChunks / kThreads, LW = BN * kChunks / kThreads;
-    extern __shared__ Chunk lds[];                                             // [kStages][BM rows of x, BN rows of weight][kChunks]
+#ifdef __HIP_DEVICE_COMPILE__                                                  // the host's pass, which makes the launch, drops kernels with buffers and transposing reads
+    constexpr int kThreads = WM * WN * 64, FM = B / WM / 16, FN = B / WN / 16, kStep = kSlab / sizeof(T), kStage = 2 * B * kChunks;
+    typedef Side<T, kAcrossX, B, kThreads> X;
+    typedef Side<T, kAcrossW, B, kThreads> W;
+    extern __shared__ Chunk lds[];                                             // two stages of x and weight
     const Place p = place_of(t);
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), wm = wave % WM, wn = wave / WM;
-    const int64_t m0 = (int64_t)p.m * BM, n0 = (int64_t)p.n * BN;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), wm = wave % WM, wn = wave / WM;
+    const int64_t m0 = (int64_t)p.m * B, n0 = (int64_t)p.n * B;
     const int first = (int)(p.split * t.slabs), last = (int)min((int64_t)((t.K + kStep - 1) / kStep), first + t.slabs);
-    const __amdgpu_buffer_rsrc_t bx = __builtin_amdgcn_make_buffer_rsrc((void*)(x + m0 * ldx), 0, 0x7fffffff, 0x27000);
-    const __amdgpu_buffer_rsrc_t bw = __builtin_amdgcn_make_buffer_rsrc((void*)(w + n0 * ldw), 0, 0x7fffffff, 0x27000);
-    // rows beyond the last are the last one again, chunks beyond the end of a row its slab's first (they become zeros in LDS)
-    const int place = threadIdx.x / kChunks, chunk = (threadIdx.x ^ place) & 7;
-    int ox[LX], ow[LW];
-#pragma unroll
-    for (int i = 0; i < LX; i++) ox[i] = (int)(min((int64_t)(place + i * (kThreads / kChunks)), t.M - 1 - m0) * ldx * (int)sizeof(T));
-#pragma unroll
-    for (int i = 0; i < LW; i++) ow[i] = (int)(min((int64_t)(place + i * (kThreads / kChunks)), t.N - 1 - n0) * ldw * (int)sizeof(T));
+    const X sx(x, ldx, m0, t.M);
+    const W sw(w, ldw, n0, t.N);
     auto* base = (__attribute__((address_space(3))) Chunk*)lds + wave * 64;
-    auto inside = [&](int slab) { return (int64_t)slab * kStep + chunk * E < t.K ? chunk * kChunk : 0; };
     Acc acc[FN][FM] = {};
-#pragma unroll
-    for (int s = 0; s < kStages - 1; s++)
-        if (first + s < last) {
-            fetch<LX>(bx, base + s * kStage, kThreads, ox, inside(first + s), (first + s) * kSlab);
-            fetch<LW>(bw, base + s * kStage + BM * kChunks, kThreads, ow, inside(first + s), (first + s) * kSlab);
-        }
-    int stage = 0;
+    if (first < last) {
+        sx.fetch(base, first, t.K);
+        sw.fetch(base + B * kChunks, first, t.K);
+    }
     for (int s = first; s < last; s++) {
+        const int stage = (s - first) & 1;
         // this slab has landed, and nobody reads the stage that is loaded next any more
-        if (kStages > 2 && s + kStages - 2 < last) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((kStages - 2) * (LX + LW)) : "memory");
-        else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-        if (const int next = s + kStages - 1; next < last) {
-            auto* to = base + (stage == 0 ? kStages - 1 : stage - 1) * kStage;
-            fetch<LX>(bx, to, kThreads, ox, inside(next), next * kSlab);
-            fetch<LW>(bw, to + BM * kChunks, kThreads, ow, inside(next), next * kSlab);
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        if (s + 1 < last) {
+            auto* to = base + (stage ^ 1) * kStage;
+            sx.fetch(to, s + 1, t.K);
+            sw.fetch(to + B * kChunks, s + 1, t.K);
         }
         Chunk* in = lds + stage * kStage;
-        if ((int64_t)(s + 1) * kStep > t.K) {                                  // zeros behind the end of the rows
-            const int there = (int)((t.K - (int64_t)s * kStep) / E);
-            for (int id = threadIdx.x; id < kStage; id += kThreads)
-                if (((id ^ (id / kChunks)) & 7) >= there) in[id] = Chunk{};
+        if (const int64_t left = t.K - (int64_t)s * kStep; left < kStep) {
+            X::clear(in, (int)left);
+            W::clear(in + B * kChunks, (int)left);
             asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
         }
         constexpr int F = kFeed<T>;
@@ -362,18 +436,15 @@ __global__ __launch_bounds__(WM * WN * 64) void aligned_kernel(Tiles t, const T*
             Chunk fx[FM][F], fw[FN][F];
 #pragma unroll
             for (int f = 0; f < F; f++) {
-                const int at = ((c + f) * 4 + lane / 16) ^ (lane & 7);
-#pragma unroll
-                for (int i = 0; i < FN; i++) fw[i][f] = in[(BM + wn * (BN / WN) + i * 16 + (lane & 15)) * kChunks + at];
-#pragma unroll
-                for (int j = 0; j < FM; j++) fx[j][f] = in[(wm * (BM / WM) + j * 16 + (lane & 15)) * kChunks + at];
+                X::template read<FM, F>(in, wm * (B / WM), c + f, f, fx);
+                W::template read<FN, F>(in + B * kChunks, wn * (B / WN), c + f, f, fw);
             }
             products<T>(fw, fx, acc);
         }
-        stage = stage == kStages - 1 ? 0 : stage + 1;
     }
     asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
-    put<O, FM, FN>(t, o, parts, p.split, m0 + wm * (BM / WM), n0 + wn * (BN / WN), acc, (float*)lds + wave * 16 * (FN * 16 + 4));
+    put<O, FM, FN>(t, o, parts, p.split, m0 + wm * (B / WM), n0 + wn * (B / WN), acc, (float*)lds + wave * 16 * (FN * 16 + 4));
+#endif
 }
 
 // ---- few tokens (single tokens of up to 64 streams): 16 FN outputs a workgroup, the contraction over its wavefronts.  Bound by the weights' way from
@@ -555,7 +626,7 @@ FewPlan few_plan(int64_t M, int64_t N, int64_t bytes)
     return best;
 }
 
-Tiles tiles_of(int64_t M, int64_t N, int64_t K, int e, bool aligned)
+Tiles tiles_of(int64_t M, int64_t N, int64_t K, int e, bool aligned, bool few = true)
 {
     const int64_t slabs = std::max<int64_t>(1, (K * e + kSlab - 1) / kSlab);
     Tiles best{};
@@ -574,19 +645,22 @@ Tiles tiles_of(int64_t M, int64_t N, int64_t K, int e, bool aligned)
             }
         }
     }
-    if (aligned && M <= kFew)
+    if (aligned && few && M <= kFew)
         if (const FewPlan p = few_plan(M, N, K * e); p.us < 3.0 + least)
             return Tiles{M, N, K, (int)((M + p.fm * 16 - 1) / (p.fm * 16)), (int)((N + p.fn * 16 - 1) / (p.fn * 16)), 1, 0, p.fm, true};
     return best;
 }
 size_t parts_bytes(const Tiles& t) { return t.splits > 1 ? (size_t)t.splits * t.M * ((t.N + 3) / 4 * 4) * 4 : 0; }
-// for either alignment: it may not be known yet
-size_t parts_bytes(int64_t M, int64_t N, int64_t K, int e) { return std::max(parts_bytes(tiles_of(M, N, K, e, false)), parts_bytes(tiles_of(M, N, K, e, true))); }
-
-template <class T, class O, int kSize, int WM, int WN> hipError_t launch(const Tiles& t, const T* x, int64_t ldx, const T* w, int64_t ldw, const Out& o, float* parts, uint32_t blocks, hipStream_t stream)
+// for every way that the product may take: the alignment may not be known yet
+size_t parts_bytes(int64_t M, int64_t N, int64_t K, int e)
 {
-    constexpr int kStages = 2, kLds = kStages * 2 * kSize * kSlab;
-    auto kernel = aligned_kernel<T, O, kSize, kSize, WM, WN, kStages>;
+    return std::max({parts_bytes(tiles_of(M, N, K, e, false)), parts_bytes(tiles_of(M, N, K, e, true)), parts_bytes(tiles_of(M, N, K, e, true, false))});
+}
+
+template <class T, class O, int kSize, int WM, int WN, bool kAcrossX, bool kAcrossW> hipError_t launch(const Tiles& t, const T* x, int64_t ldx, const T* w, int64_t ldw, const Out& o, float* parts, uint32_t blocks, hipStream_t stream)
+{
+    constexpr int kLds = 2 * 2 * kSize * kSlab;                                // two stages of both operands
+    auto kernel = aligned_kernel<T, O, kSize, WM, WN, kAcrossX, kAcrossW>;
     if (kLds > 64 * 1024) {
         hipError_t err = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, kLds);
         if (err != hipSuccess) return err;
@@ -602,31 +676,31 @@ bool aligned_rows(const void* x, int64_t ldx, const void* w, int64_t ldw, int64_
            256 * std::max(ldx, ldw) * e + K * e < (1ll << 31);
 }
 
-template <class T, class O> hipError_t product(int64_t M, int64_t N, int64_t K, const T* x, int64_t ldx, const T* w, int64_t ldw, Out o, float* parts, hipStream_t stream)
+template <class T, class O, bool kAcrossX = false, bool kAcrossW = false>
+hipError_t product(int64_t M, int64_t N, int64_t K, const T* x, int64_t ldx, const T* w, int64_t ldw, Out o, float* parts, hipStream_t stream)
 {
     constexpr int V = 16 / sizeof(O);
     const int64_t e = sizeof(T);
-    const bool aligned = aligned_rows(x, ldx, w, ldw, K, e);
+    const bool aligned = kAcrossX || kAcrossW || aligned_rows(x, ldx, w, ldw, K, e);         // operands across: the caller has looked at them
     auto fits = [&](const void* p) { return (uintptr_t)p % 16 == 0; };
     o.vec = N % V == 0 && o.residual_stride % V == 0 && fits(o.bias) && fits(o.residual) && fits(o.y) && fits(o.pre);
-    const Tiles t = tiles_of(M, N, K, (int)e, aligned);
-    if (t.few) {
-        const int64_t blocks = (int64_t)t.m * t.n;
-        if (!launchable(blocks, 512)) return kTooManyThreads;
-        auto go = [&](auto kernel) { kernel<<<(uint32_t)blocks, 512, 0, stream>>>(t, x, ldx, w, ldw, o); };
-        t.tile == 1 ? go(few_kernel<T, O, 1, 1, 8>) : t.tile == 2 ? go(few_kernel<T, O, 2, 2, 8>) : go(few_kernel<T, O, 4, 2, 8>);
-        return hipGetLastError();
-    }
+    const Tiles t = tiles_of(M, N, K, (int)e, aligned, !kAcrossX && !kAcrossW);
     const int64_t blocks = (int64_t)t.m * t.n * t.splits;
     if (!launchable(blocks, 512)) return kTooManyThreads;
     hipError_t err = hipSuccess;
-    if (!aligned) {
+    if (t.few) {
+        if constexpr (!kAcrossX && !kAcrossW) {
+            auto go = [&](auto kernel) { kernel<<<(uint32_t)blocks, 512, 0, stream>>>(t, x, ldx, w, ldw, o); };
+            t.tile == 1 ? go(few_kernel<T, O, 1, 1, 8>) : t.tile == 2 ? go(few_kernel<T, O, 2, 2, 8>) : go(few_kernel<T, O, 4, 2, 8>);
+            err = hipGetLastError();
+        }
+    } else if (!aligned) {
         product_kernel<T, O><<<(uint32_t)blocks, 256, 0, stream>>>(t, x, ldx, w, ldw, o, parts);
         err = hipGetLastError();
     } else if (t.tile == 256) {
-        if constexpr (sizeof(T) < 4) err = launch<T, O, 256, 4, 2>(t, x, ldx, w, ldw, o, parts, (uint32_t)blocks, stream);
-    } else if (t.tile == 128) err = launch<T, O, 128, 2, 2>(t, x, ldx, w, ldw, o, parts, (uint32_t)blocks, stream);
-    else err = launch<T, O, 64, 2, 2>(t, x, ldx, w, ldw, o, parts, (uint32_t)blocks, stream);
+        if constexpr (sizeof(T) < 4) err = launch<T, O, 256, 4, 2, kAcrossX, kAcrossW>(t, x, ldx, w, ldw, o, parts, (uint32_t)blocks, stream);
+    } else if (t.tile == 128) err = launch<T, O, 128, 2, 2, kAcrossX, kAcrossW>(t, x, ldx, w, ldw, o, parts, (uint32_t)blocks, stream);
+    else err = launch<T, O, 64, 2, 2, kAcrossX, kAcrossW>(t, x, ldx, w, ldw, o, parts, (uint32_t)blocks, stream);
     if (err != hipSuccess || t.splits == 1) return err;
     const int64_t joins = (M * ((N + 3) / 4) + 255) / 256;
     if (!launchable(joins, 256)) return kTooManyThreads;
@@ -637,9 +711,10 @@ template <class T, class O> hipError_t product(int64_t M, int64_t N, int64_t K, 
 int bytes_of(int64_t dtype) { return dtype == SIG_F32 ? 4 : dtype == SIG_BF16 ? 2 : 1; }
 int64_t round_up(int64_t v, int64_t to) { return (v + to - 1) / to * to; }
 
-// What the gradient keeps in its workspace, in bytes from its start
+// What the gradient keeps in its workspace, in bytes from its start.  direct: the products read their operands as they lie (bfloat16, whole chunks in the rows
+// of the gradient, the weight and x); else what lies across the contraction is transposed first.
 struct Keep {
-    // grad_x = g weight, contraction N; grad_weight = g^T x, contraction M
+    bool direct;
     int64_t padN, padM;
     size_t flat, turned_g, turned_w, turned_x, sums, parts, all;
 };
@@ -647,6 +722,8 @@ Keep keep_of(const sig_linear_args& a)
 {
     Keep k;
     const int e = bytes_of(a.dtype);
+    k.direct = e == 2 && a.M > 0 && a.N % 8 == 0 && a.K % 8 == 0 && a.x_stride % 8 == 0 && (uintptr_t)a.x % 16 == 0 && (uintptr_t)a.weight % 16 == 0 &&
+               256 * std::max({a.x_stride, a.N, a.K}) * e + std::max(a.N, a.K) * e < (1ll << 31);
     k.padN = round_up(a.N, 64);
     k.padM = round_up(a.M, 64);
     size_t at = 0;
@@ -655,13 +732,13 @@ Keep keep_of(const sig_linear_args& a)
         at += (size_t)round_up(n, 256);
         return was;
     };
-    k.flat = take(a.act ? a.M * a.N * e : 0);
-    k.turned_g = take(a.N * k.padM * e);
-    k.turned_w = take(a.K * k.padN * e);
-    k.turned_x = take(a.K * k.padM * e);
+    k.flat = take(a.act || k.direct ? a.M * a.N * e : 0);                      // direct: a gradient whose rows are not aligned is copied there as well
+    k.turned_g = take(k.direct ? 0 : a.N * k.padM * e);
+    k.turned_w = take(k.direct ? 0 : a.K * k.padN * e);
+    k.turned_x = take(k.direct ? 0 : a.K * k.padM * e);
     k.sums = take((a.M + 63) / 64 * a.N * 4);
     k.parts = take((int64_t)std::max(parts_bytes(a.M, a.K, a.N, e), parts_bytes(a.N, a.K, a.M, e)));
-    k.all = at;
+    k.all = at + 16;                                                           // for a workspace whose start is not aligned
     return k;
 }
 
@@ -678,25 +755,38 @@ template <class T> hipError_t backward_of(const sig_linear_args& a, const T* gy,
 {
     const Keep k = keep_of(a);
     if (a.act == SIG_ACT_NONE) pre = nullptr;
+    ws += -(uintptr_t)ws & 15;
     T *flat = (T*)(ws + k.flat), *turned_g = (T*)(ws + k.turned_g), *turned_w = (T*)(ws + k.turned_w), *turned_x = (T*)(ws + k.turned_x);
     float *sums = (float*)(ws + k.sums), *parts = (float*)(ws + k.parts);
+    const bool copy = pre || (k.direct && (ld % 8 != 0 || (uintptr_t)gy % 16 != 0 || 256 * ld * (int64_t)sizeof(T) >= (1ll << 30)));
+    const T* g = copy ? flat : gy;
+    const int64_t ldg = copy ? a.N : ld;
+    const bool across = k.direct || !gw;                                       // no transposed gradient is needed
     hipError_t err = hipSuccess;
-    if (pre || gw || gb) err = turn<T>(gy, ld, a.M, a.N, pre, (int)a.act, pre && gx ? flat : nullptr, gw ? turned_g : nullptr, k.padM, gb ? sums : nullptr, stream);
+    if ((copy && (gx || gw)) || gb || !across)
+        err = turn<T>(gy, ld, a.M, a.N, pre, (int)a.act, copy && (gx || (gw && k.direct)) ? flat : nullptr, across ? nullptr : turned_g, k.padM, gb ? sums : nullptr, stream);
     if (err == hipSuccess && gb) {
         bias_kernel<T><<<(uint32_t)((a.N + 63) / 64), 1024, 0, stream>>>(sums, (a.M + 63) / 64, a.N, gb);
         err = hipGetLastError();
     }
+    Out o{};
     if (err == hipSuccess && gx && a.M) {
-        err = turn<T>((const T*)a.weight, a.K, a.N, a.K, nullptr, 0, nullptr, turned_w, k.padN, nullptr, stream);
-        Out o{};
         o.y = gx;
-        if (err == hipSuccess) err = product<T, T>(a.M, a.K, a.N, pre ? flat : gy, pre ? a.N : ld, turned_w, k.padN, o, parts, stream);
+        if constexpr (sizeof(T) == 2)
+            if (k.direct) err = product<T, T, false, true>(a.M, a.K, a.N, g, ldg, (const T*)a.weight, a.K, o, parts, stream);
+        if (!k.direct) {
+            err = turn<T>((const T*)a.weight, a.K, a.N, a.K, nullptr, 0, nullptr, turned_w, k.padN, nullptr, stream);
+            if (err == hipSuccess) err = product<T, T>(a.M, a.K, a.N, g, ldg, turned_w, k.padN, o, parts, stream);
+        }
     }
     if (err == hipSuccess && gw) {
-        err = turn<T>((const T*)a.x, a.x_stride, a.M, a.K, nullptr, 0, nullptr, turned_x, k.padM, nullptr, stream);
-        Out o{};
         o.y = gw;
-        if (err == hipSuccess) err = product<T, T>(a.N, a.K, a.M, turned_g, k.padM, turned_x, k.padM, o, parts, stream);
+        if constexpr (sizeof(T) == 2)
+            if (k.direct) err = product<T, T, true, true>(a.N, a.K, a.M, g, ldg, (const T*)a.x, a.x_stride, o, parts, stream);
+        if (!k.direct) {
+            err = turn<T>((const T*)a.x, a.x_stride, a.M, a.K, nullptr, 0, nullptr, turned_x, k.padM, nullptr, stream);
+            if (err == hipSuccess) err = product<T, T>(a.N, a.K, a.M, turned_g, k.padM, turned_x, k.padM, o, parts, stream);
+        }
     }
     return err;
 }
@@ -712,12 +802,12 @@ template <class T, class O> hipError_t forward_of(const sig_linear_args& a, void
 size_t linear_forward_workspace(const sig_linear_args& a)
 {
     const int e = bytes_of(a.dtype);
-    const bool aligned = aligned_rows(a.x, a.x_stride, a.weight, a.K, a.K, e);
-    return parts_bytes(tiles_of(a.M, a.N, a.K, e, aligned));
+    const size_t n = parts_bytes(tiles_of(a.M, a.N, a.K, e, aligned_rows(a.x, a.x_stride, a.weight, a.K, a.K, e)));
+    return n ? n + 16 : 0;                                                     // for a workspace whose start is not aligned
 }
 hipError_t linear_forward(const sig_linear_args& a, void* y, void* pre, void* workspace, hipStream_t stream)
 {
-    float* parts = (float*)workspace;
+    float* parts = (float*)((char*)workspace + (-(uintptr_t)workspace & 15));
     if (a.dtype == SIG_BF16) return forward_of<bf16, bf16>(a, y, pre, parts, stream);
     if (a.dtype == SIG_F32) return forward_of<float, float>(a, y, pre, parts, stream);
     return a.out_dtype == SIG_BF16 ? forward_of<e4m3, bf16>(a, y, pre, parts, stream) : forward_of<e4m3, float>(a, y, pre, parts, stream);
