@@ -33,36 +33,47 @@ struct Out {                            // what becomes of a sum
     bool vec;                           // 16 bytes of neighbouring outputs are one access everywhere
 };
 
-// The normal distribution's Phi and its density.  exp(x^2) erfc(x) = t P(t) with t = 1 / (1 + 0.3 x), P of degree 8 fitted to the smallest relative
-// error over x in [0, 14] (4e-8; with float32's roundings 5e-7), so both tails keep their relative precision, and the exponential is the density's.
+// The normal distribution's Phi and its density.  exp(x^2) erfc(x) = t P(t) with t = 1 / (1 + c x), P fitted to the smallest relative error over x in
+// [0, 14], so both tails keep their relative precision, and the exponential is the density's.  For float32 of degree 8, c = 0.3 (4e-8; with float32's
+// roundings 5e-7); for values rounded to bfloat16, whose half step is 4e-3, of degree 5, c = 0.45 (1e-5): the epilogue of a product is bound by this.
 struct Normal { float below, density; };
-__device__ __forceinline__ Normal normal_of(float z)
+template <class O> __device__ __forceinline__ Normal normal_of(float z)
 {
-    const float t = __builtin_amdgcn_rcpf(fmaf(fabsf(z), 0.3f * 0.70710678f, 1.0f)), g = fast_exp(-0.5f * z * z);
-    float p = fmaf(t, -0.12661661f, 0.47182638f);
-    p = fmaf(p, t, -0.48469207f);
-    p = fmaf(p, t, 0.51704908f);
-    p = fmaf(p, t, -0.074049273f);
-    p = fmaf(p, t, 0.2063852f);
-    p = fmaf(p, t, 0.15046886f);
-    p = fmaf(p, t, 0.17042372f);
-    p = fmaf(p, t, 0.16920475f);
+    constexpr bool kShort = sizeof(O) == 2;
+    const float t = __builtin_amdgcn_rcpf(fmaf(fabsf(z), (kShort ? 0.45f : 0.3f) * 0.70710678f, 1.0f)), g = fast_exp(-0.5f * z * z);
+    float p;
+    if constexpr (kShort) {
+        p = fmaf(t, -0.13586082f, 0.29224834f);
+        p = fmaf(p, t, 0.089452292f);
+        p = fmaf(p, t, 0.24848109f);
+        p = fmaf(p, t, 0.25170138f);
+        p = fmaf(p, t, 0.25396823f);
+    } else {
+        p = fmaf(t, -0.12661661f, 0.47182638f);
+        p = fmaf(p, t, -0.48469207f);
+        p = fmaf(p, t, 0.51704908f);
+        p = fmaf(p, t, -0.074049273f);
+        p = fmaf(p, t, 0.2063852f);
+        p = fmaf(p, t, 0.15046886f);
+        p = fmaf(p, t, 0.17042372f);
+        p = fmaf(p, t, 0.16920475f);
+    }
     const float tail = 0.5f * (p * t) * g;
     return {z > 0.0f ? 1.0f - tail : tail, 0.39894228f * g};
 }
-__device__ __forceinline__ float act_of(float z, int act)
+template <class O> __device__ __forceinline__ float act_of(float z, int act)
 {
     if (act == SIG_ACT_SILU) return z * sigmoid(z);
-    if (act == SIG_ACT_GELU) return z * normal_of(z).below;
+    if (act == SIG_ACT_GELU) return z * normal_of<O>(z).below;
     return z;
 }
-__device__ __forceinline__ float slope_of(float z, int act)
+template <class O> __device__ __forceinline__ float slope_of(float z, int act)
 {
     if (act == SIG_ACT_SILU) {
         const float s = sigmoid(z);
         return s * fmaf(z, 1.0f - s, 1.0f);
     }
-    const Normal v = normal_of(z);
+    const Normal v = normal_of<O>(z);
     return fmaf(z, v.density, v.below);
 }
 
@@ -132,10 +143,10 @@ template <class O, int V> __device__ __forceinline__ void finish(const Out& o, c
     if (o.pre) give<O, V>((O*)o.pre + at, c.wide, c.n, N, z);
     if (o.act == SIG_ACT_SILU) {
 #pragma unroll
-        for (int j = 0; j < V; j++) z[j] = act_of(z[j], SIG_ACT_SILU);
+        for (int j = 0; j < V; j++) z[j] = act_of<O>(z[j], SIG_ACT_SILU);
     } else if (o.act == SIG_ACT_GELU)
 #pragma unroll
-        for (int j = 0; j < V; j++) z[j] = act_of(z[j], SIG_ACT_GELU);
+        for (int j = 0; j < V; j++) z[j] = act_of<O>(z[j], SIG_ACT_GELU);
     if (o.residual)
 #pragma unroll
         for (int j = 0; j < V; j++) z[j] += r.value(j);
@@ -207,7 +218,7 @@ template <class T> __device__ __forceinline__ Chunk take_chunk(const T* row, int
 
 // Sums over the contraction of 16 x 16 products, one chunk a lane of each operand (e4m3: two).  float32 takes four instructions a pair of chunks: all
 // pairs' first ones come first, so that none waits for the one before.
-template <class T, int FN, int FM, int F> __device__ __forceinline__ void products(const Chunk (&w)[FN][F], const Chunk (&x)[FM][F], Acc (&acc)[FN][FM])
+template <class T, int FN, int FM, int F> __device__ __forceinline__ void products(const Chunk (&w)[FN][F], const Chunk (&x)[FM][F], Acc (*acc)[FM])
 {
 #pragma unroll
     for (int q = 0; q < (std::is_same_v<T, float> ? 4 : 1); q++)
@@ -433,13 +444,19 @@ __global__ __launch_bounds__(WM * WN * 64) void aligned_kernel(Tiles t, const T*
         constexpr int F = kFeed<T>;
 #pragma unroll
         for (int c = 0; c < kChunks / 4; c += F) {
-            Chunk fx[FM][F], fw[FN][F];
+            // reads that wait for themselves come four outputs at a time, those of the next four while the products of these are under way
+            constexpr int G = kAcrossW && FN > 4 ? 4 : FN;
+            Chunk fx[FM][F];
 #pragma unroll
-            for (int f = 0; f < F; f++) {
-                X::template read<FM, F>(in, wm * (B / WM), c + f, f, fx);
-                W::template read<FN, F>(in + B * kChunks, wn * (B / WN), c + f, f, fw);
+            for (int f = 0; f < F; f++) X::template read<FM, F>(in, wm * (B / WM), c + f, f, fx);
+#pragma unroll
+            for (int i = 0; i < FN; i += G) {
+                Chunk fw[G][F];
+#pragma unroll
+                for (int f = 0; f < F; f++) W::template read<G, F>(in + B * kChunks, wn * (B / WN) + i * 16, c + f, f, fw);
+                products<T>(fw, fx, acc + i);
+                if (G < FN) __builtin_amdgcn_sched_barrier(0);
             }
-            products<T>(fw, fx, acc);
         }
     }
     asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
@@ -554,10 +571,10 @@ template <class T> __global__ __launch_bounds__(256) void turn_kernel(const T* i
         Pack<T, V> q;
         if (pre && act == SIG_ACT_SILU) {
 #pragma unroll
-            for (int k = 0; k < V; k++) v[i][k] *= slope_of(z[i][k], SIG_ACT_SILU);
+            for (int k = 0; k < V; k++) v[i][k] *= slope_of<T>(z[i][k], SIG_ACT_SILU);
         } else if (pre)
 #pragma unroll
-            for (int k = 0; k < V; k++) v[i][k] *= slope_of(z[i][k], SIG_ACT_GELU);
+            for (int k = 0; k < V; k++) v[i][k] *= slope_of<T>(z[i][k], SIG_ACT_GELU);
 #pragma unroll
         for (int k = 0; k < V; k++) q.v[k] = from_float<T>(v[i][k]);
         if (flat && r < R && c < C) {
