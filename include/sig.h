@@ -478,7 +478,7 @@ typedef struct sig_norm_args {
     const float* weight;            /* device [C] */
 } sig_norm_args;
 /* total: dtype [rows, C] or NULL.  scale NULL: y is dtype [rows, C].  Else y is SIG_E4M3 [rows, C] and scale [rows]: y * scale is the norm, scale =
- * max |row| / 448, its values taken before any rounding to dtype.  Rows of zeros have scale 0; a row with an infinity or NaN has a
+ * max |row| / 448, its values taken before any rounding to dtype.  Squares are summed in float32: rows with values beyond 1e19 give zeros.  Rows of zeros have scale 0; a row with an infinity or NaN has a
  * scale that is not finite, and its y is of no use but defined. */
 int    sig_norm_forward(const sig_norm_args* args, void* y, float* scale, void* total, void* stream);
 /* args->x: the total that the forward call gave (residual is not looked at).  grad_y and grad_total (or NULL) dtype [rows, C] with strides of their own ->
@@ -505,8 +505,8 @@ typedef struct sig_linear_args {
     const float* x_scale;           /* SIG_E4M3: device [M] or NULL (ones); row m of x stands for x_scale[m] times its values */
     const float* weight_scale;      /* SIG_E4M3: device [N] or NULL (ones) */
 } sig_linear_args;
-/* y out_dtype [M, N]; pre: NULL or out_dtype [M, N], receives what f is applied to (for the gradient).  The workspace is that of a call with the
- * same args, pointers among them. */
+/* y out_dtype [M, N]; pre: NULL or out_dtype [M, N], receives what f is applied to (for the gradient).  The workspaces of this call and of
+ * its gradient are those for the same args, pointers among them. */
 size_t sig_linear_forward_workspace_bytes(const sig_linear_args* args);
 int    sig_linear_forward(const sig_linear_args* args, void* y, void* pre, void* workspace, size_t workspace_bytes, void* stream);
 /* Gradient (SIG_F32 and SIG_BF16): grad_y dtype [M, N] with a stride of its own; pre as kept (NULL where act is SIG_ACT_NONE) -> grad_x dtype [M, K],

