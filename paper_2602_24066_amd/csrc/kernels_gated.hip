@@ -8,9 +8,14 @@
 // states follow from what is in registers.  So everything is read once, and the next round's loads are under way meanwhile.  Few streams get
 // time chunks: a first pass over the inputs leaves every chunk's (A, H).
 //
+// Bound by memory where there are many streams: 8 x 2048 x 2048 in bfloat16 takes 68 us forward (277 MB with the states that are kept, 4.1 TB/s) and 106
+// backward (478 MB, 4.5 TB/s); the vector units have about 40 and 72 instructions a token and channel.  One stream reads its inputs twice: 1 x 16384 x 1024
+// takes 23 us for the chunks' maps and 30 for the outputs.
+//
 // Gradient: with c_t what comes back from the tokens after t, l_t = grad_y_t + c_t and c_(t-1) = a_t l_t, the same structure from the end.  With U_t = u_t dL/du_t
 //   grad x = l b i,  grad q = l b x i (1 - i),  U = l (u a^2 / b i x - u a h_(t-1)),  grad p = U (1 - sigmoid(p)),  grad log_rate = sum U:
 // u / b goes to zero like sqrt(u / 2), so nothing here is infinite at u = 0.
+#include <algorithm>
 #include <type_traits>
 
 #include "layer.hpp"
@@ -501,6 +506,7 @@ __global__ __launch_bounds__(1024) void gated_rates_kernel(const float* rates, i
     if (threadIdx.x < 64 && c < D) grad_log_rate[c] = s;
 }
 
+// One token: bound by latency and the call (64 x 2048 in bfloat16: 3.0 us)
 template <class T> __global__ __launch_bounds__(256) void gated_step_kernel(sig_gated_args a, float* state, T* y)
 {
     const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x;
@@ -513,13 +519,17 @@ template <class T> __global__ __launch_bounds__(256) void gated_step_kernel(sig_
     y[id] = from_float<T>(h);
 }
 
+// Time chunks: as many as the compute units have room for with one workgroup each (1 x 16384 x 1024 in bfloat16, forward and backward: 256 workgroups 51 and
+// 63 us, 128 83 and 102, 512 56 and 70; 1 x 8192 x 1536: 240 workgroups 43 and 54 us, 264 62 and 74).  None forward where the streams give half of that
+// already: a first pass costs more than the idle half (4 x 8192 x 2048: 185 us without, 208 with one; backward 346 without, 269 with one).  Four rounds in a
+// row are already worse than two passes over chunks of them (7 x 301 x 277 float32 training step: 53.6 us for 43).
 struct Plan { int groups, chunks, rounds; };
-Plan plan(const sig_gated_args& a)
+Plan plan(const sig_gated_args& a, bool back)
 {
     Plan p;
     p.groups = (int)((a.D + kGroup - 1) / kGroup);
     const int64_t all = (a.L + kRound - 1) / kRound, rows = a.B * p.groups;
-    int64_t chunks = rows >= 256 ? 1 : (256 + rows - 1) / (rows > 0 ? rows : 1);
+    int64_t chunks = rows >= (back ? 256 : 128) ? 1 : 256 / std::max<int64_t>(rows, 1);
     chunks = chunks > all ? (all ? all : 1) : chunks;
     p.rounds = (int)((all + chunks - 1) / chunks);
     if (p.rounds < 1) p.rounds = 1;
@@ -532,7 +542,7 @@ bool pairs_fit(const void* p, int64_t sb, int64_t st, int e) { return (uintptr_t
 
 template <class T> hipError_t forward_of(const sig_gated_args& a, T* y, float* final_state, float* ckpt, float* sums, hipStream_t stream)
 {
-    const Plan p = plan(a);
+    const Plan p = plan(a, false);
     const int64_t blocks = a.B * p.groups * p.chunks;
     if (!launchable(blocks, kWaves * 64)) return kTooManyThreads;
     const int e = sizeof(T);
@@ -552,7 +562,7 @@ template <class T> hipError_t forward_of(const sig_gated_args& a, T* y, float* f
 
 template <class T> hipError_t backward_of(const sig_gated_args& a, const sig_gated_grads& g, const float* ckpt, float* ws, hipStream_t stream)
 {
-    const Plan p = plan(a);
+    const Plan p = plan(a, true);
     const int64_t blocks = a.B * p.groups * p.chunks, parts = a.B * p.chunks;
     if (!launchable(blocks, kWaves * 64) || !launchable(p.groups, 1024)) return kTooManyThreads;
     float *sums = ws, *rates = ws + (p.chunks > 1 ? parts * 2 * a.D : 0);
@@ -580,12 +590,12 @@ template <class T> hipError_t backward_of(const sig_gated_args& a, const sig_gat
 
 size_t gated_forward_workspace(const sig_gated_args& a)
 {
-    const Plan p = plan(a);
+    const Plan p = plan(a, false);
     return p.chunks > 1 ? (size_t)(a.B * p.chunks * 2 * a.D * 4) : 0;
 }
 size_t gated_backward_workspace(const sig_gated_args& a)
 {
-    const Plan p = plan(a);
+    const Plan p = plan(a, true);
     return (size_t)(a.B * p.chunks * (p.chunks > 1 ? 3 : 1) * a.D * 4);
 }
 hipError_t gated_forward(const sig_gated_args& a, void* y, float* final_state, float* checkpoint, float* workspace, hipStream_t stream)
