@@ -6,7 +6,7 @@
 // the instruction's first operand: a lane then holds four neighbouring outputs of one token.
 // LDS: row r keeps chunk c at place c ^ (r & 7), so that eight rows' chunks lie in different banks.
 // Few tiles and a long contraction: the contraction is split over workgroups, whose float32 sums a second kernel adds up in order.
-// The gradient's operands lie the other way, a row for every place of the contraction: bfloat16 ones of whole chunks are turned by the LDS reads
+// The gradient's operands lie the other way, a row for every place of the contraction: rows of whole chunks are turned by the LDS reads
 // (see Side), others are transposed in memory first, and the product is the same as forward.
 //
 // Bound by the matrix units where the contraction is long: bfloat16 8192^3 in 840 us (1,308 TFLOP/s), e4m3 in 476 (2,310), float32 4096^3 in 1,000 (137).
@@ -323,29 +323,33 @@ template <class T, class O> __global__ __launch_bounds__(256) void product_kerne
 // ---- the same for operands whose rows are multiples of 16 bytes, 16-byte aligned: chunks go from memory to LDS without passing registers, a wavefront's
 // load filling 1,024 bytes in lane order; what a lane fetches decides where it lies.
 //
-// An operand of B rows along the contraction is as above.  One that lies the other way (kAcross, bfloat16: rows of outputs, one for every place of the
-// contraction, as the gradients' operands do) comes as 64 such rows of B outputs a slab, and the LDS reads turn it: a transposing read gives each of sixteen
-// lanes four rows of its own column.  Row r keeps chunk c at place c ^ turn(r): the rows that one read touches (four, and the four that lie eight further on)
-// are whole multiples of the banks apart otherwise.
+// An operand of B rows along the contraction is as above.  One that lies the other way (kAcross: rows of outputs, one for every place of the contraction, as
+// the gradients' operands do) comes as 64 (float32: 32) such rows of B outputs a slab, and the LDS reads turn it: a transposing read gives each of sixteen
+// lanes four bfloat16 values of its own column; float32 values are read one by one, for which the matrix instructions leave time.  Row r keeps chunk c at place
+// c ^ turn(r): the rows that one read touches (four, and the four that lie eight further on; float32: every fourth) are whole multiples of the banks
+// apart otherwise.
 template <class T, bool kAcross, int B, int kThreads> struct Side {
     static constexpr int E = kChunk / sizeof(T), kStep = kSlab / sizeof(T), kLoads = B * kChunks / kThreads, kRow = kAcross ? B / E : kChunks;     // chunks of a row
     typedef __attribute__((address_space(3))) Chunk Lds;
     const T* base;
     int64_t ld;
-    int offset[kLoads], row, chunk;
+    int offset[kLoads], row, width;                                            // width (kAcross): outputs that are there
 
-    static __device__ __forceinline__ int turn(int r) { return (((r & 3) | (r >> 1 & 4)) << 1) & (kRow - 1); }
+    static __device__ __forceinline__ int turn(int r) { return (sizeof(T) == 4 ? (r >> 2 & 3) << 2 : ((r & 3) | (r >> 1 & 4)) << 1) & (kRow - 1); }
+    // the chunk of row r that this thread fetches
+    __device__ __forceinline__ int chunk_of(int r) const
+    {
+        const int c = (threadIdx.x ^ (kAcross ? turn(r) : r)) & (kRow - 1);
+        return kAcross && c * E >= width ? 0 : c;
+    }
 
     // outputs first .. of `outs`; rows and chunks behind the last are others that are there
-    __device__ __forceinline__ Side(const T* p, int64_t ld, int64_t first, int64_t outs) : base(p + (kAcross ? first : first * ld)), ld(ld)
+    __device__ __forceinline__ Side(const T* p, int64_t ld, int64_t first, int64_t outs) : base(p + (kAcross ? first : first * ld)), ld(ld), row(threadIdx.x / kRow), width((int)min(outs - first, (int64_t)B))
     {
-        row = threadIdx.x / kRow;
-        chunk = (threadIdx.x ^ (kAcross ? turn(row) : row)) & (kRow - 1);
-        if (kAcross && first + chunk * E >= outs) chunk = 0;
 #pragma unroll
         for (int i = 0; i < kLoads; i++) {
             const int r = row + i * (kThreads / kRow);
-            offset[i] = kAcross ? (int)((r * ld + chunk * E) * (int)sizeof(T)) : (int)(min((int64_t)r, outs - 1 - first) * ld * (int)sizeof(T));
+            offset[i] = kAcross ? (int)((r * ld + chunk_of(r) * E) * (int)sizeof(T)) : (int)(min((int64_t)r, outs - 1 - first) * ld * (int)sizeof(T));
         }
     }
     __device__ __forceinline__ void fetch(Lds* to, int slab, int64_t K) const
@@ -358,11 +362,13 @@ template <class T, bool kAcross, int B, int kThreads> struct Side {
                 for (int i = 0; i < kLoads; i++) __builtin_amdgcn_raw_ptr_buffer_load_lds(from, to + i * kThreads, 16, offset[i], 0, 0, 0);
             else
 #pragma unroll
-                for (int i = 0; i < kLoads; i++)
-                    __builtin_amdgcn_raw_ptr_buffer_load_lds(from, to + i * kThreads, 16, (int)((min(row + i * (kThreads / kRow), left - 1) * ld + chunk * E) * (int)sizeof(T)), 0, 0, 0);
+                for (int i = 0; i < kLoads; i++) {
+                    const int r = row + i * (kThreads / kRow);
+                    __builtin_amdgcn_raw_ptr_buffer_load_lds(from, to + i * kThreads, 16, (int)((min(r, left - 1) * ld + chunk_of(r) * E) * (int)sizeof(T)), 0, 0, 0);
+                }
         } else {
             const __amdgpu_buffer_rsrc_t from = __builtin_amdgcn_make_buffer_rsrc((void*)base, 0, 0x7fffffff, 0x27000);
-            const int at = (int64_t)slab * kStep + chunk * E < K ? chunk * kChunk : 0;       // beyond the row's end its slab's first chunk
+            const int chunk = chunk_of(row), at = (int64_t)slab * kStep + chunk * E < K ? chunk * kChunk : 0;       // beyond the row's end its slab's first chunk
 #pragma unroll
             for (int i = 0; i < kLoads; i++) __builtin_amdgcn_raw_ptr_buffer_load_lds(from, to + i * kThreads, 16, offset[i] + at, slab * kSlab, 0, 0);
         }
@@ -380,6 +386,13 @@ template <class T, bool kAcross, int B, int kThreads> struct Side {
         if constexpr (!kAcross) {
 #pragma unroll
             for (int i = 0; i < N; i++) to[i][f] = in[(o + i * 16 + (lane & 15)) * kChunks + ((c * 4 + lane / 16) ^ (lane & 7))];
+        } else if constexpr (sizeof(T) == 4) {
+            const uint32_t* words = (const uint32_t*)in;
+            const int r = c * 16 + lane / 16 * 4;                                            // and the three rows behind it, whose turn is the same
+#pragma unroll
+            for (int i = 0; i < N; i++)
+#pragma unroll
+                for (int q = 0; q < 4; q++) to[i][f][q] = words[((r + q) * kRow + ((o / E + i * 4 + (lane & 15) / 4) ^ turn(r))) * 4 + (lane & 3)];
         } else {
             // The compiler would wait for the next slab's loads before a transposing read, which it does not tell from what they write.  So the reads are written
             // out, two or four outputs' at a time with their own wait, while the products of those before are under way.
@@ -616,18 +629,18 @@ template <class T> __global__ __launch_bounds__(256) void turn_kernel(const T* i
     }
 }
 
-// The same where nothing is to be transposed (bfloat16, rows of whole chunks): 64 rows by 128 values a workgroup, the bias's sums in registers, of
-// unrounded values; what the products read is rounded, as their other operands are bfloat16 too.  Bound by memory: 16384 x 4096 with GELU's slope 85 us, 4.75
+// The same where nothing is to be transposed (rows of whole chunks): 64 rows by 128 bfloat16 or 64 float32 values a workgroup, the bias's sums in registers, of
+// unrounded values; what the products read is rounded to T, as their other operands are of that type.  Bound by memory: 16384 x 4096 with GELU's slope 85 us, 4.75
 // TB/s (by tiles through LDS as above 109).
-__global__ __launch_bounds__(256) void slope_kernel(const bf16* in, int64_t ld, int64_t R, int64_t C, const bf16* pre, int act, bf16* flat, float* sums, int64_t groups, bool vec)
+template <class T> __global__ __launch_bounds__(256) void slope_kernel(const T* in, int64_t ld, int64_t R, int64_t C, const T* pre, int act, T* flat, float* sums, int64_t groups, bool vec)
 {
-    constexpr int V = 8, kRows = 4, kWide = 16 * V;
+    constexpr int V = 16 / sizeof(T), kRows = 4, kWide = 16 * V;
     __shared__ alignas(32) float part[4][kWide];
     const int64_t r0 = (int64_t)(blockIdx.x / groups) * 64 + threadIdx.x / 16, c = (int64_t)(blockIdx.x % groups) * kWide + (threadIdx.x & 15) * V;
     float sum[V] = {};
     if (c < C) {
-        Words<bf16, V> g[kRows], z[kRows];
-        auto fetch = [&](const bf16* p, Words<bf16, V>& to) {
+        Words<T, V> g[kRows], z[kRows];
+        auto fetch = [&](const T* p, Words<T, V>& to) {
             if (vec) to.load(p);
             else __builtin_memcpy(&to.w, p, sizeof(to.w));
         };
@@ -645,13 +658,13 @@ __global__ __launch_bounds__(256) void slope_kernel(const bf16* in, int64_t ld, 
             for (int k = 0; k < V; k++) v[k] = g[i].value(k);
             if (pre && act == SIG_ACT_SILU) {
 #pragma unroll
-                for (int k = 0; k < V; k++) v[k] *= slope_of<bf16>(z[i].value(k), SIG_ACT_SILU);
+                for (int k = 0; k < V; k++) v[k] *= slope_of<T>(z[i].value(k), SIG_ACT_SILU);
             } else if (pre)
 #pragma unroll
-                for (int k = 0; k < V; k++) v[k] *= slope_of<bf16>(z[i].value(k), SIG_ACT_GELU);
+                for (int k = 0; k < V; k++) v[k] *= slope_of<T>(z[i].value(k), SIG_ACT_GELU);
 #pragma unroll
             for (int k = 0; k < V; k++) sum[k] += v[k];
-            if (flat) store_words<bf16, V>(flat + (r0 + i * 16) * C + c, v);
+            if (flat) store_words<T, V>(flat + (r0 + i * 16) * C + c, v);
         }
     }
     if (!sums) return;
@@ -785,7 +798,7 @@ hipError_t product(int64_t M, int64_t N, int64_t K, const T* x, int64_t ldx, con
 int bytes_of(int64_t dtype) { return dtype == SIG_F32 ? 4 : dtype == SIG_BF16 ? 2 : 1; }
 int64_t round_up(int64_t v, int64_t to) { return (v + to - 1) / to * to; }
 
-// What the gradient keeps in its workspace, in bytes from its start.  direct: the products read their operands as they lie (bfloat16, whole chunks in the rows
+// What the gradient keeps in its workspace, in bytes from its start.  direct: the products read their operands as they lie (whole chunks in the rows
 // of the gradient, the weight and x); else what lies across the contraction is transposed first.
 struct Keep {
     bool direct;
@@ -796,7 +809,7 @@ Keep keep_of(const sig_linear_args& a)
 {
     Keep k;
     const int e = bytes_of(a.dtype);
-    k.direct = e == 2 && a.M > 0 && a.N % 8 == 0 && a.K % 8 == 0 && a.x_stride % 8 == 0 && (uintptr_t)a.x % 16 == 0 && (uintptr_t)a.weight % 16 == 0 &&
+    k.direct = a.M > 0 && a.N * e % 16 == 0 && a.K * e % 16 == 0 && a.x_stride * e % 16 == 0 && (uintptr_t)a.x % 16 == 0 && (uintptr_t)a.weight % 16 == 0 &&
                256 * std::max({a.x_stride, a.N, a.K}) * e + std::max(a.N, a.K) * e < (1ll << 31);
     k.padN = round_up(a.N, 64);
     k.padM = round_up(a.M, 64);
@@ -825,12 +838,12 @@ template <class T> hipError_t turn(const T* in, int64_t ld, int64_t R, int64_t C
     return hipGetLastError();
 }
 
-hipError_t slopes(const bf16* in, int64_t ld, int64_t R, int64_t C, const bf16* pre, int act, bf16* flat, float* sums, hipStream_t stream)
+template <class T> hipError_t slopes(const T* in, int64_t ld, int64_t R, int64_t C, const T* pre, int act, T* flat, float* sums, hipStream_t stream)
 {
-    const int64_t groups = (C + 127) / 128, blocks = (R + 63) / 64 * groups;
+    const int64_t wide = 256 / sizeof(T), groups = (C + wide - 1) / wide, blocks = (R + 63) / 64 * groups;
     if (!launchable(blocks, 256)) return kTooManyThreads;
-    const bool vec = ld % 8 == 0 && (uintptr_t)in % 16 == 0 && (uintptr_t)pre % 16 == 0;
-    slope_kernel<<<(uint32_t)blocks, 256, 0, stream>>>(in, ld, R, C, pre, act, flat, sums, groups, vec);
+    const bool vec = ld * sizeof(T) % 16 == 0 && (uintptr_t)in % 16 == 0 && (uintptr_t)pre % 16 == 0;
+    slope_kernel<T><<<(uint32_t)blocks, 256, 0, stream>>>(in, ld, R, C, pre, act, flat, sums, groups, vec);
     return hipGetLastError();
 }
 
@@ -843,14 +856,14 @@ template <class T> hipError_t backward_of(const sig_linear_args& a, const T* gy,
     ws += -(uintptr_t)ws & 15;
     T *flat = (T*)(ws + k.flat), *turned_g = (T*)(ws + k.turned_g), *turned_w = (T*)(ws + k.turned_w), *turned_x = (T*)(ws + k.turned_x);
     float *sums = (float*)(ws + k.sums), *parts = (float*)(ws + k.parts);
-    const bool copy = pre || (k.direct && (ld % 8 != 0 || (uintptr_t)gy % 16 != 0 || 256 * ld * (int64_t)sizeof(T) >= (1ll << 30)));
+    const bool copy = pre || (k.direct && (ld * sizeof(T) % 16 != 0 || (uintptr_t)gy % 16 != 0 || 256 * ld * (int64_t)sizeof(T) >= (1ll << 30)));
     const T* g = copy ? flat : gy;
     const int64_t ldg = copy ? a.N : ld;
     const bool across = k.direct || !gw;                                       // no transposed gradient is needed
     hipError_t err = hipSuccess;
     const bool pass = (copy && (gx || gw)) || gb || !across;
     if (pass && k.direct) {
-        if constexpr (sizeof(T) == 2) err = slopes(gy, ld, a.M, a.N, pre, (int)a.act, copy && (gx || gw) ? flat : nullptr, gb ? sums : nullptr, stream);
+        err = slopes<T>(gy, ld, a.M, a.N, pre, (int)a.act, copy && (gx || gw) ? flat : nullptr, gb ? sums : nullptr, stream);
     } else if (pass)
         err = turn<T>(gy, ld, a.M, a.N, pre, (int)a.act, copy && gx ? flat : nullptr, across ? nullptr : turned_g, k.padM, gb ? sums : nullptr, stream);
     if (err == hipSuccess && gb) {
@@ -860,8 +873,7 @@ template <class T> hipError_t backward_of(const sig_linear_args& a, const T* gy,
     Out o{};
     if (err == hipSuccess && gx && a.M) {
         o.y = gx;
-        if constexpr (sizeof(T) == 2)
-            if (k.direct) err = product<T, T, false, true>(a.M, a.K, a.N, g, ldg, (const T*)a.weight, a.K, o, parts, stream);
+        if (k.direct) err = product<T, T, false, true>(a.M, a.K, a.N, g, ldg, (const T*)a.weight, a.K, o, parts, stream);
         if (!k.direct) {
             err = turn<T>((const T*)a.weight, a.K, a.N, a.K, nullptr, 0, nullptr, turned_w, k.padN, nullptr, stream);
             if (err == hipSuccess) err = product<T, T>(a.M, a.K, a.N, g, ldg, turned_w, k.padN, o, parts, stream);
@@ -869,8 +881,7 @@ template <class T> hipError_t backward_of(const sig_linear_args& a, const T* gy,
     }
     if (err == hipSuccess && gw) {
         o.y = gw;
-        if constexpr (sizeof(T) == 2)
-            if (k.direct) err = product<T, T, true, true>(a.N, a.K, a.M, g, ldg, (const T*)a.x, a.x_stride, o, parts, stream);
+        if (k.direct) err = product<T, T, true, true>(a.N, a.K, a.M, g, ldg, (const T*)a.x, a.x_stride, o, parts, stream);
         if (!k.direct) {
             err = turn<T>((const T*)a.x, a.x_stride, a.M, a.K, nullptr, 0, nullptr, turned_x, k.padM, nullptr, stream);
             if (err == hipSuccess) err = product<T, T>(a.N, a.K, a.M, turned_g, k.padM, turned_x, k.padM, o, parts, stream);
