@@ -511,7 +511,7 @@ size_t sig_linear_forward_workspace_bytes(const sig_linear_args* args);
 int    sig_linear_forward(const sig_linear_args* args, void* y, void* pre, void* workspace, size_t workspace_bytes, void* stream);
 /* Gradient (SIG_F32 and SIG_BF16): grad_y dtype [M, N] with a stride of its own; pre as kept (NULL where act is SIG_ACT_NONE) -> grad_x dtype [M, K],
  * grad_weight dtype [N, K], grad_bias dtype [N]; each may be NULL, and is not computed then.  The gradient of the residual is grad_y.
- * bias, residual and scales of args are not looked at, x only for grad_weight, weight only for grad_x. */
+ * bias, residual and scales of args are not looked at, x only for grad_weight, weight only for grad_x.  Rows of N or K elements are shorter than 4 MB. */
 size_t sig_linear_backward_workspace_bytes(const sig_linear_args* args);
 int    sig_linear_backward(const sig_linear_args* args, const void* grad_y, int64_t gy_stride, const void* pre, void* grad_x,
                            void* grad_weight, void* grad_bias, void* workspace, size_t workspace_bytes, void* stream);

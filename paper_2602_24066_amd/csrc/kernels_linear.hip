@@ -7,7 +7,7 @@
 // LDS: row r keeps chunk c at place c ^ (r & 7), so that eight rows' chunks lie in different banks.
 // Few tiles and a long contraction: the contraction is split over workgroups, whose float32 sums a second kernel adds up in order.
 // The gradient's operands lie the other way, a row for every place of the contraction: rows of whole chunks are turned by the LDS reads
-// (see Side), others are transposed in memory first, and the product is the same as forward.
+// (see Side).  Operands whose rows are not whole chunks are copied first where that pays, for the gradient always.
 //
 // Bound by the matrix units where the contraction is long: bfloat16 8192^3 in 840 us (1,308 TFLOP/s), e4m3 in 476 (2,310), float32 4096^3 in 1,000 (137).
 // Where it is short, by the outputs: 16384 x 1024 to 4096 in bfloat16 with SiLU 158 us, of which the product alone takes 127 at the rate above's; a
@@ -28,7 +28,7 @@ typedef int Int8 __attribute__((ext_vector_type(8)));
 
 constexpr int kSlab = 128, kChunk = 16, kChunks = kSlab / kChunk;      // bytes; bytes; chunks of a slab
 
-struct Tiles { int64_t M, N, K; int m, n, splits; int64_t slabs; int tile; bool few; };            // tiles along m and n; slabs of a split; edge of a tile (few: in 16 tokens)
+struct Tiles { int64_t M, N, K; int m, n, splits; int64_t slabs; int tile; bool few; double us; };            // tiles along m and n; slabs of a split; edge of a tile (few: in 16 tokens); what the launch's model says
 
 struct Out {                            // what becomes of a sum
     const void *bias, *residual;
@@ -373,11 +373,11 @@ template <class T, bool kAcross, int B, int kThreads> struct Side {
             for (int i = 0; i < kLoads; i++) __builtin_amdgcn_raw_ptr_buffer_load_lds(from, to + i * kThreads, 16, offset[i] + at, slab * kSlab, 0, 0);
         }
     }
-    // zeros behind the end of the contraction, `left` places of the slab being before it
+    // zeros behind the end of the contraction, `left` places of the slab being before it (the last one's chunk of a row along the contraction ends in zeros)
     static __device__ __forceinline__ void clear(Chunk* in, int left)
     {
         for (int id = threadIdx.x; id < B * kChunks; id += kThreads)
-            if (kAcross ? id / kRow >= left : ((id ^ (id / kRow)) & 7) >= left / E) in[id] = Chunk{};
+            if (kAcross ? id / kRow >= left : ((id ^ (id / kRow)) & 7) >= (left + E - 1) / E) in[id] = Chunk{};
     }
     // What a lane feeds for outputs o .. o + 16 N - 1 of the tile at step c of the slab (f: of a feed of kF chunks)
     template <int N, int kF> static __device__ __forceinline__ void read(const Chunk* in, int o, int c, int f, Chunk (&to)[N][kF])
@@ -554,85 +554,17 @@ template <class O> __global__ __launch_bounds__(256) void join_kernel(Tiles t, O
     finish<O, 4>(o, columns, id / quads, t.N, z, r);
 }
 
-// The gradient's pass over what comes in.  [R, C] to [C, padded R], zeros behind R: tiles of 64 x 64 through LDS, 16 bytes an access on both sides (vec).  pre: the gradient that comes in is
-// multiplied by the activation's slope first, rounded to T, and kept in its own order too (flat); sums: its sums over the rows of a tile, for
-// the bias's gradient.
-template <class T> __global__ __launch_bounds__(256) void turn_kernel(const T* in, int64_t ld, int64_t R, int64_t C, const T* pre, int act, T* flat, T* turned, int64_t padded,
-                                                                       float* sums, int64_t tiles_c, bool vec)
+// Rows [R, C] of any alignment to rows of whole chunks, zeros behind the C: 16 bytes a thread.  Bound by memory.
+template <class T> __global__ __launch_bounds__(256) void pad_kernel(const T* in, int64_t ld, int64_t R, int64_t C, Chunk* out, uint32_t chunks)
 {
-    constexpr int V = 16 / sizeof(T), kAcross = 64 / V;                        // elements of an access, accesses of a tile's row
-    __shared__ T tile[64][64 + 4 / sizeof(T)];
-    const int64_t r0 = (int64_t)(blockIdx.x / tiles_c) * 64, c0 = (int64_t)(blockIdx.x % tiles_c) * 64;
-    auto take = [&](const T* p, int64_t c, float* v) {
-        if (vec) {
-            const Pack<T, V> q = *(const Pack<T, V>*)(p + c);
-#pragma unroll
-            for (int k = 0; k < V; k++) v[k] = to_float(q.v[k]);
-        } else
-#pragma unroll
-            for (int k = 0; k < V; k++) v[k] = c + k < C ? to_float(p[c + k]) : 0.0f;
-    };
-    float v[kAcross / 4][V], z[kAcross / 4][V];
-#pragma unroll
-    for (int i = 0; i < kAcross / 4; i++) {
-        const int id = threadIdx.x + i * 256;
-        const int64_t r = r0 + id / kAcross, c = c0 + id % kAcross * V;
-#pragma unroll
-        for (int k = 0; k < V; k++) v[i][k] = z[i][k] = 0.0f;
-        if (r < R && c < C) {
-            take(in + r * ld, c, v[i]);
-            if (pre) take(pre + r * C, c, z[i]);
-        }
-    }
-#pragma unroll
-    for (int i = 0; i < kAcross / 4; i++) {
-        const int id = threadIdx.x + i * 256, row = id / kAcross, at = id % kAcross * V;
-        const int64_t r = r0 + row, c = c0 + at;
-        Pack<T, V> q;
-        if (pre && act == SIG_ACT_SILU) {
-#pragma unroll
-            for (int k = 0; k < V; k++) v[i][k] *= slope_of<T>(z[i][k], SIG_ACT_SILU);
-        } else if (pre)
-#pragma unroll
-            for (int k = 0; k < V; k++) v[i][k] *= slope_of<T>(z[i][k], SIG_ACT_GELU);
-#pragma unroll
-        for (int k = 0; k < V; k++) q.v[k] = from_float<T>(v[i][k]);
-        if (flat && r < R && c < C) {
-            if (vec) *(Pack<T, V>*)(flat + r * C + c) = q;
-            else
-#pragma unroll
-                for (int k = 0; k < V; k++)
-                    if (c + k < C) flat[r * C + c + k] = q.v[k];
-        }
-#pragma unroll
-        for (int k = 0; k < V; k++) tile[row][at + k] = q.v[k];
-    }
-    if (!turned && !sums) return;
-    __syncthreads();
-    // V rows of a column a thread: neighbouring lanes have neighbouring rows
-#pragma unroll
-    for (int i = 0; i < kAcross / 4; i++) {
-        const int id = threadIdx.x + i * 256, col = id / kAcross, at = id % kAcross * V;
-        Pack<T, V> q;
-        float sum = 0.0f;
-#pragma unroll
-        for (int k = 0; k < V; k++) {
-            q.v[k] = tile[at + k][col];
-            sum += to_float(q.v[k]);
-        }
-        if (turned && c0 + col < C) *(Pack<T, V>*)(turned + (c0 + col) * padded + r0 + at) = q;
-        if (sums) {
-#pragma unroll
-            for (int m = 1; m < kAcross; m *= 2) sum += __shfl_xor(sum, m);
-            if (at == 0 && c0 + col < C) sums[blockIdx.x / tiles_c * C + c0 + col] = sum;
-        }
-    }
+    const uint32_t id = blockIdx.x * 256 + threadIdx.x, row = id / chunks, c = id % chunks;
+    if (row < R) out[id] = take_chunk(in + row * ld, c * (kChunk / (int)sizeof(T)), C);
 }
 
-// The same where nothing is to be transposed (rows of whole chunks): 64 rows by 128 bfloat16 or 64 float32 values a workgroup, the bias's sums in registers, of
-// unrounded values; what the products read is rounded to T, as their other operands are of that type.  Bound by memory: 16384 x 4096 with GELU's slope 85 us, 4.75
-// TB/s (by tiles through LDS as above 109).
-template <class T> __global__ __launch_bounds__(256) void slope_kernel(const T* in, int64_t ld, int64_t R, int64_t C, const T* pre, int act, T* flat, float* sums, int64_t groups, bool vec)
+// The gradient's pass over what comes in: times the activation's slope (pre), rounded to T as the products' other operands are of that type, into rows
+// of whole chunks (flat, `padded` elements apart), and its sums over 64 rows, unrounded, for the bias's gradient.  64 rows by 128 bfloat16 or 64 float32 values
+// a workgroup.  Bound by memory: 16384 x 4096 in bfloat16 with GELU's slope 85 us, 4.75 TB/s (by tiles through LDS 109).
+template <class T> __global__ __launch_bounds__(256) void slope_kernel(const T* in, int64_t ld, int64_t R, int64_t C, const T* pre, int act, T* flat, int64_t padded, float* sums, int64_t groups, bool vec)
 {
     constexpr int V = 16 / sizeof(T), kRows = 4, kWide = 16 * V;
     __shared__ alignas(32) float part[4][kWide];
@@ -641,14 +573,17 @@ template <class T> __global__ __launch_bounds__(256) void slope_kernel(const T* 
     if (c < C) {
         Words<T, V> g[kRows], z[kRows];
         auto fetch = [&](const T* p, Words<T, V>& to) {
-            if (vec) to.load(p);
-            else __builtin_memcpy(&to.w, p, sizeof(to.w));
+            if (vec) to.load(p + c);
+            else {
+                const Chunk q = take_chunk(p, c, C);
+                __builtin_memcpy(&to.w, &q, sizeof(q));
+            }
         };
 #pragma unroll
         for (int i = 0; i < kRows; i++) {
             const int64_t r = min(r0 + i * 16, R - 1);
-            fetch(in + r * ld + c, g[i]);
-            if (pre) fetch(pre + r * C + c, z[i]);
+            fetch(in + r * ld, g[i]);
+            if (pre) fetch(pre + r * C, z[i]);
         }
 #pragma unroll
         for (int i = 0; i < kRows; i++) {
@@ -664,7 +599,7 @@ template <class T> __global__ __launch_bounds__(256) void slope_kernel(const T* 
                 for (int k = 0; k < V; k++) v[k] *= slope_of<T>(z[i].value(k), SIG_ACT_GELU);
 #pragma unroll
             for (int k = 0; k < V; k++) sum[k] += v[k];
-            if (flat) store_words<T, V>(flat + (r0 + i * 16) * C + c, v);
+            if (flat) store_words<T, V>(flat + (r0 + i * 16) * padded + c, v);
         }
     }
     if (!sums) return;
@@ -690,7 +625,9 @@ template <class T> __global__ __launch_bounds__(1024) void bias_kernel(const flo
 // as it holds, `alone` what it costs at least, `over` what a tile costs besides (first loads, outputs).  Measured on large squares (us a slab):
 //   bfloat16 256: 8192^3 in 856 us, 128: 1,022 us     float32 128: 4096^3 in 998, 64: 1,040     e4m3 256: 8192^3 in 476, 128: 550
 // and 16384 x 4096 x 1024 (16 slabs): 148 us with tiles of 256, 172 of 128; e4m3 16384 x 2048 x 2048: 72 and 79.
+// Rows that are not whole chunks (product_kernel) take `rough` times the slab: bfloat16 16384 x 5460 to 1024 272 us, of 5456 189; float32 5000 x 1001 to 1001 139.
 struct Cost { int tile; double slab, alone, over; };
+constexpr double kRough[3] = {1.07, 1.5, 1.5};                                         // float32, bfloat16, e4m3
 constexpr Cost kCosts[3][3] = {
     {{64, 0.51, 0.70, 1.0}, {128, 1.95, 1.95, 3.0}, {}},                               // float32: tiles of 256 gain 2 % at most
     {{64, 0.17, 0.50, 0.8}, {128, 0.50, 0.80, 2.4}, {256, 1.68, 1.68, 10.5}},          // bfloat16
@@ -724,26 +661,20 @@ Tiles tiles_of(int64_t M, int64_t N, int64_t K, int e, bool aligned, bool few = 
         for (int64_t want : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32}) {
             if (want > 1 && slabs / want < 4) break;
             const int64_t each = (slabs + want - 1) / want, splits = (slabs + each - 1) / each, rows = (m * n * splits + kUnits - 1) / kUnits;
-            double us = (double)each * std::max(rows * c.slab, c.alone) + rows * c.over;
+            double us = (double)each * std::max(rows * c.slab, c.alone) * (aligned ? 1.0 : kRough[e == 4 ? 0 : e == 2 ? 1 : 2]) + rows * c.over;
             if (splits > 1) us += 4.0 + (double)M * N * 4.0 * (splits + 1) / 3e6;     // the sums, written and read again
             if (best.tile == 0 || us < least) {
                 least = us;
-                best = Tiles{M, N, K, (int)m, (int)n, (int)splits, each, c.tile, false};
+                best = Tiles{M, N, K, (int)m, (int)n, (int)splits, each, c.tile, false, us};
             }
         }
     }
     if (aligned && few && M <= kFew)
         if (const FewPlan p = few_plan(M, N, K * e); p.us < 3.0 + least)
-            return Tiles{M, N, K, (int)((M + p.fm * 16 - 1) / (p.fm * 16)), (int)((N + p.fn * 16 - 1) / (p.fn * 16)), 1, 0, p.fm, true};
+            return Tiles{M, N, K, (int)((M + p.fm * 16 - 1) / (p.fm * 16)), (int)((N + p.fn * 16 - 1) / (p.fn * 16)), 1, 0, p.fm, true, p.us};
     return best;
 }
 size_t parts_bytes(const Tiles& t) { return t.splits > 1 ? (size_t)t.splits * t.M * ((t.N + 3) / 4 * 4) * 4 : 0; }
-// for every way that the product may take: the alignment may not be known yet
-size_t parts_bytes(int64_t M, int64_t N, int64_t K, int e)
-{
-    return std::max({parts_bytes(tiles_of(M, N, K, e, false)), parts_bytes(tiles_of(M, N, K, e, true)), parts_bytes(tiles_of(M, N, K, e, true, false))});
-}
-
 template <class T, class O, int kSize, int WM, int WN, bool kAcrossX, bool kAcrossW> hipError_t launch(const Tiles& t, const T* x, int64_t ldx, const T* w, int64_t ldw, const Out& o, float* parts, uint32_t blocks, hipStream_t stream)
 {
     constexpr int kLds = 2 * 2 * kSize * kSlab;                                // two stages of both operands
@@ -798,118 +729,142 @@ hipError_t product(int64_t M, int64_t N, int64_t K, const T* x, int64_t ldx, con
 int bytes_of(int64_t dtype) { return dtype == SIG_F32 ? 4 : dtype == SIG_BF16 ? 2 : 1; }
 int64_t round_up(int64_t v, int64_t to) { return (v + to - 1) / to * to; }
 
-// What the gradient keeps in its workspace, in bytes from its start.  direct: the products read their operands as they lie (whole chunks in the rows
-// of the gradient, the weight and x); else what lies across the contraction is transposed first.
+// Rows that the aligned kernels read as they lie
+bool whole(const void* p, int64_t ld, int64_t cols, int64_t e) { return (uintptr_t)p % 16 == 0 && ld * e % 16 == 0 && cols * e % 16 == 0 && 256 * ld * e < (1ll << 30); }
+
+template <class T> hipError_t pad(const T* in, int64_t ld, int64_t R, int64_t C, T* out, hipStream_t stream)
+{
+    const int64_t chunks = (C * (int)sizeof(T) + kChunk - 1) / kChunk, blocks = (R * chunks + 255) / 256;
+    if (!launchable(blocks, 256)) return kTooManyThreads;
+    if (blocks) pad_kernel<T><<<(uint32_t)blocks, 256, 0, stream>>>(in, ld, R, C, (Chunk*)out, (uint32_t)chunks);
+    return hipGetLastError();
+}
+
+// What a forward call keeps in its workspace, in bytes from its start: x and the weight in rows of whole chunks where they are not and the launch's model says
+// that the copies (a launch each, read and written at 3 TB/s) cost less than they gain, and the sums of splits.  float32 5000 x 1001 to 1001: 112 us with
+// copies, 139 without; 600 x 1554 to 640 24 either way.
+struct Ahead {
+    bool pad_x, pad_w;
+    int64_t padK;
+    size_t x, w, parts, all;
+};
+Ahead ahead_of(const sig_linear_args& a)
+{
+    const int e = bytes_of(a.dtype);
+    Ahead k{};
+    k.padK = a.K;
+    Tiles t = tiles_of(a.M, a.N, a.K, e, aligned_rows(a.x, a.x_stride, a.weight, a.K, a.K, e));
+    size_t at = 0;
+    if (const int64_t padK = round_up(a.K, kChunk / e); !aligned_rows(a.x, a.x_stride, a.weight, a.K, a.K, e) && 256 * padK * e < (1ll << 30)) {
+        const bool x = !whole(a.x, a.x_stride, a.K, e), w = !whole(a.weight, a.K, a.K, e);
+        const Tiles u = tiles_of(a.M, a.N, padK, e, true);
+        if (u.us + (x ? 4.0 + 2.0 * a.M * padK * e / 3e6 : 0.0) + (w ? 4.0 + 2.0 * a.N * padK * e / 3e6 : 0.0) < t.us) {
+            k = Ahead{x, w, padK};
+            t = u;
+            k.w = x ? (size_t)round_up(a.M * padK * e, 256) : 0;
+            at = k.w + (w ? (size_t)round_up(a.N * padK * e, 256) : 0);
+        }
+    }
+    k.parts = at;
+    k.all = at + parts_bytes(t);
+    if (k.all) k.all += 16;                                                    // for a workspace whose start is not aligned
+    return k;
+}
+
+// What the gradient keeps in its workspace: the gradient that comes in where it is multiplied by a slope or not whole chunks, and copies of the weight and
+// of x in rows of whole chunks where theirs are not
 struct Keep {
-    bool direct;
-    int64_t padN, padM;
-    size_t flat, turned_g, turned_w, turned_x, sums, parts, all;
+    bool pad_x, pad_w;
+    int64_t padN, padK;
+    size_t flat, x, w, sums, parts, all;
 };
 Keep keep_of(const sig_linear_args& a)
 {
     Keep k;
     const int e = bytes_of(a.dtype);
-    k.direct = a.M > 0 && a.N * e % 16 == 0 && a.K * e % 16 == 0 && a.x_stride * e % 16 == 0 && (uintptr_t)a.x % 16 == 0 && (uintptr_t)a.weight % 16 == 0 &&
-               256 * std::max({a.x_stride, a.N, a.K}) * e + std::max(a.N, a.K) * e < (1ll << 31);
-    k.padN = round_up(a.N, 64);
-    k.padM = round_up(a.M, 64);
+    k.pad_x = !whole(a.x, a.x_stride, a.K, e);
+    k.pad_w = !whole(a.weight, a.K, a.K, e);
+    k.padN = round_up(a.N, kChunk / e);
+    k.padK = round_up(a.K, kChunk / e);
     size_t at = 0;
     auto take = [&](int64_t n) {
         size_t was = at;
         at += (size_t)round_up(n, 256);
         return was;
     };
-    k.flat = take(a.act || k.direct ? a.M * a.N * e : 0);                      // direct: a gradient whose rows are not aligned is copied there as well
-    k.turned_g = take(k.direct ? 0 : a.N * k.padM * e);
-    k.turned_w = take(k.direct ? 0 : a.K * k.padN * e);
-    k.turned_x = take(k.direct ? 0 : a.K * k.padM * e);
+    k.flat = take(a.M * k.padN * e);
+    k.x = take(k.pad_x ? a.M * k.padK * e : 0);
+    k.w = take(k.pad_w ? a.N * k.padK * e : 0);
     k.sums = take((a.M + 63) / 64 * a.N * 4);
-    k.parts = take((int64_t)std::max(parts_bytes(a.M, a.K, a.N, e), parts_bytes(a.N, a.K, a.M, e)));
+    k.parts = take((int64_t)std::max(parts_bytes(tiles_of(a.M, a.K, a.N, e, true, false)), parts_bytes(tiles_of(a.N, a.K, a.M, e, true, false))));
     k.all = at + 16;                                                           // for a workspace whose start is not aligned
     return k;
 }
 
-template <class T> hipError_t turn(const T* in, int64_t ld, int64_t R, int64_t C, const T* pre, int act, T* flat, T* turned, int64_t padded, float* sums, hipStream_t stream)
-{
-    const int64_t tiles_c = (C + 63) / 64, blocks = (R + 63) / 64 * tiles_c, V = 16 / sizeof(T);
-    if (!launchable(blocks, 256)) return kTooManyThreads;
-    const bool vec = C % V == 0 && ld % V == 0 && (uintptr_t)in % 16 == 0 && (uintptr_t)pre % 16 == 0;
-    if (blocks) turn_kernel<T><<<(uint32_t)blocks, 256, 0, stream>>>(in, ld, R, C, pre, act, flat, turned, padded, sums, tiles_c, vec);
-    return hipGetLastError();
-}
-
-template <class T> hipError_t slopes(const T* in, int64_t ld, int64_t R, int64_t C, const T* pre, int act, T* flat, float* sums, hipStream_t stream)
+template <class T> hipError_t slopes(const T* in, int64_t ld, int64_t R, int64_t C, const T* pre, int act, T* flat, int64_t padded, float* sums, hipStream_t stream)
 {
     const int64_t wide = 256 / sizeof(T), groups = (C + wide - 1) / wide, blocks = (R + 63) / 64 * groups;
     if (!launchable(blocks, 256)) return kTooManyThreads;
-    const bool vec = ld * sizeof(T) % 16 == 0 && (uintptr_t)in % 16 == 0 && (uintptr_t)pre % 16 == 0;
-    slope_kernel<T><<<(uint32_t)blocks, 256, 0, stream>>>(in, ld, R, C, pre, act, flat, sums, groups, vec);
+    const bool vec = C * sizeof(T) % 16 == 0 && ld * sizeof(T) % 16 == 0 && (uintptr_t)in % 16 == 0 && (uintptr_t)pre % 16 == 0;
+    if (blocks) slope_kernel<T><<<(uint32_t)blocks, 256, 0, stream>>>(in, ld, R, C, pre, act, flat, padded, sums, groups, vec);
     return hipGetLastError();
 }
 
 template <class T> hipError_t backward_of(const sig_linear_args& a, const T* gy, int64_t ld, const T* pre, T* gx, T* gw, T* gb, char* ws, hipStream_t stream)
 {
     const Keep k = keep_of(a);
-    const int64_t bias_blocks = (a.N + 63) / 64;
-    if (gb && !launchable(bias_blocks, 1024)) return kTooManyThreads;
+    const int64_t e = sizeof(T);
+    if (256 * std::max(k.padN, k.padK) * e >= (1ll << 30)) return kTooManyThreads;        // rows of a tile are reached by 32-bit offsets
     if (a.act == SIG_ACT_NONE) pre = nullptr;
     ws += -(uintptr_t)ws & 15;
-    T *flat = (T*)(ws + k.flat), *turned_g = (T*)(ws + k.turned_g), *turned_w = (T*)(ws + k.turned_w), *turned_x = (T*)(ws + k.turned_x);
+    T *flat = (T*)(ws + k.flat), *x = (T*)(ws + k.x), *w = (T*)(ws + k.w);
     float *sums = (float*)(ws + k.sums), *parts = (float*)(ws + k.parts);
-    const bool copy = pre || (k.direct && (ld * sizeof(T) % 16 != 0 || (uintptr_t)gy % 16 != 0 || 256 * ld * (int64_t)sizeof(T) >= (1ll << 30)));
-    const T* g = copy ? flat : gy;
-    const int64_t ldg = copy ? a.N : ld;
-    const bool across = k.direct || !gw;                                       // no transposed gradient is needed
+    gx = a.M ? gx : nullptr;
+    const bool copy = (gx || gw) && (pre || !whole(gy, ld, a.N, e));
+    const T *g = copy ? flat : gy, *px = k.pad_x ? x : (const T*)a.x, *pw = k.pad_w ? w : (const T*)a.weight;
+    const int64_t ldg = copy ? k.padN : ld;
     hipError_t err = hipSuccess;
-    const bool pass = (copy && (gx || gw)) || gb || !across;
-    if (pass && k.direct) {
-        err = slopes<T>(gy, ld, a.M, a.N, pre, (int)a.act, copy && (gx || gw) ? flat : nullptr, gb ? sums : nullptr, stream);
-    } else if (pass)
-        err = turn<T>(gy, ld, a.M, a.N, pre, (int)a.act, copy && gx ? flat : nullptr, across ? nullptr : turned_g, k.padM, gb ? sums : nullptr, stream);
+    if (copy || gb) err = slopes<T>(gy, ld, a.M, a.N, pre, (int)a.act, copy ? flat : nullptr, k.padN, gb ? sums : nullptr, stream);
     if (err == hipSuccess && gb) {
-        bias_kernel<T><<<(uint32_t)bias_blocks, 1024, 0, stream>>>(sums, (a.M + 63) / 64, a.N, gb);
+        bias_kernel<T><<<(uint32_t)((a.N + 63) / 64), 1024, 0, stream>>>(sums, (a.M + 63) / 64, a.N, gb);
         err = hipGetLastError();
     }
     Out o{};
-    if (err == hipSuccess && gx && a.M) {
+    if (err == hipSuccess && gx) {
+        if (k.pad_w) err = pad((const T*)a.weight, a.K, a.N, a.K, w, stream);
         o.y = gx;
-        if (k.direct) err = product<T, T, false, true>(a.M, a.K, a.N, g, ldg, (const T*)a.weight, a.K, o, parts, stream);
-        if (!k.direct) {
-            err = turn<T>((const T*)a.weight, a.K, a.N, a.K, nullptr, 0, nullptr, turned_w, k.padN, nullptr, stream);
-            if (err == hipSuccess) err = product<T, T>(a.M, a.K, a.N, g, ldg, turned_w, k.padN, o, parts, stream);
-        }
+        if (err == hipSuccess) err = product<T, T, false, true>(a.M, a.K, a.N, g, ldg, pw, k.pad_w ? k.padK : a.K, o, parts, stream);
     }
     if (err == hipSuccess && gw) {
+        if (k.pad_x) err = pad((const T*)a.x, a.x_stride, a.M, a.K, x, stream);
         o.y = gw;
-        if (k.direct) err = product<T, T, true, true>(a.N, a.K, a.M, g, ldg, (const T*)a.x, a.x_stride, o, parts, stream);
-        if (!k.direct) {
-            err = turn<T>((const T*)a.x, a.x_stride, a.M, a.K, nullptr, 0, nullptr, turned_x, k.padM, nullptr, stream);
-            if (err == hipSuccess) err = product<T, T>(a.N, a.K, a.M, turned_g, k.padM, turned_x, k.padM, o, parts, stream);
-        }
+        if (err == hipSuccess) err = product<T, T, true, true>(a.N, a.K, a.M, g, ldg, px, k.pad_x ? k.padK : a.x_stride, o, parts, stream);
     }
     return err;
 }
 
-template <class T, class O> hipError_t forward_of(const sig_linear_args& a, void* y, void* pre, float* parts, hipStream_t stream)
+template <class T, class O> hipError_t forward_of(const sig_linear_args& a, void* y, void* pre, char* ws, hipStream_t stream)
 {
     const Out o{a.bias, a.residual, a.residual_stride, a.x_scale, a.weight_scale, y, pre, (int)a.act, false};
-    return product<T, O>(a.M, a.N, a.K, (const T*)a.x, a.x_stride, (const T*)a.weight, a.K, o, parts, stream);
+    const Ahead k = ahead_of(a);
+    ws += -(uintptr_t)ws & 15;
+    T *x = (T*)(ws + k.x), *w = (T*)(ws + k.w);
+    hipError_t err = hipSuccess;
+    if (k.pad_x) err = pad((const T*)a.x, a.x_stride, a.M, a.K, x, stream);
+    if (err == hipSuccess && k.pad_w) err = pad((const T*)a.weight, a.K, a.N, a.K, w, stream);
+    if (err != hipSuccess) return err;
+    return product<T, O>(a.M, a.N, k.padK, k.pad_x ? x : (const T*)a.x, k.pad_x ? k.padK : a.x_stride, k.pad_w ? w : (const T*)a.weight, k.pad_w ? k.padK : a.K, o, (float*)(ws + k.parts), stream);
 }
 
 }  // namespace
 
-size_t linear_forward_workspace(const sig_linear_args& a)
-{
-    const int e = bytes_of(a.dtype);
-    const size_t n = parts_bytes(tiles_of(a.M, a.N, a.K, e, aligned_rows(a.x, a.x_stride, a.weight, a.K, a.K, e)));
-    return n ? n + 16 : 0;                                                     // for a workspace whose start is not aligned
-}
+size_t linear_forward_workspace(const sig_linear_args& a) { return ahead_of(a).all; }
 hipError_t linear_forward(const sig_linear_args& a, void* y, void* pre, void* workspace, hipStream_t stream)
 {
-    float* parts = (float*)((char*)workspace + (-(uintptr_t)workspace & 15));
-    if (a.dtype == SIG_BF16) return forward_of<bf16, bf16>(a, y, pre, parts, stream);
-    if (a.dtype == SIG_F32) return forward_of<float, float>(a, y, pre, parts, stream);
-    return a.out_dtype == SIG_BF16 ? forward_of<e4m3, bf16>(a, y, pre, parts, stream) : forward_of<e4m3, float>(a, y, pre, parts, stream);
+    char* ws = (char*)workspace;
+    if (a.dtype == SIG_BF16) return forward_of<bf16, bf16>(a, y, pre, ws, stream);
+    if (a.dtype == SIG_F32) return forward_of<float, float>(a, y, pre, ws, stream);
+    return a.out_dtype == SIG_BF16 ? forward_of<e4m3, bf16>(a, y, pre, ws, stream) : forward_of<e4m3, float>(a, y, pre, ws, stream);
 }
 size_t linear_backward_workspace(const sig_linear_args& a) { return keep_of(a).all; }
 hipError_t linear_backward(const sig_linear_args& a, const void* grad_y, int64_t gy_stride, const void* pre, void* grad_x, void* grad_weight, void* grad_bias,

@@ -398,3 +398,33 @@ def test_more_outputs_than_a_launch_numbers():
     from tests.test_layer import BIG, LINEAR_OK, LINEAR_ORDER, pack
     a = pack({**LINEAR_OK, "M": 0, "N": 1 << 28}, LINEAR_ORDER)
     assert S.load_library().sig_linear_backward(a, 4096, 8, 0, 0, 0, 4096, 4096, BIG, 0) == -7
+
+
+@gpu
+@pytest.mark.parametrize("t", [F32, B16, E8])
+def test_long_products_of_rows_that_are_no_whole_chunks(t):
+    """Large enough that the operands are copied into aligned rows first: both, x alone (rows aligned, their start not), or the weight alone; NaN between the rows."""
+    M, K, N = 4000, 3999, 2050
+    n, out = whole(1, 2), B16 if t is E8 else t
+    wide = torch.full((M, K + 18), math.nan)
+    wide[:, 1:K + 2] = n(M, K + 1)
+    wide, w0, b, r = up(wide.to(t)), up(n(N, K + 1).to(t)), up(n(N).to(out)), up(n(M, N).to(out))
+    flat = torch.empty(N * 4000 + 16, dtype=t, device="cuda")
+    moved = flat[1:1 + N * 4000].view(N, 4000)                       # whole rows that begin beside a 16-byte address
+    moved.copy_(w0)
+    aligned = wide[:, 1:].contiguous()[:, :4000].contiguous()
+    for x, w in ((wide[:, 1:K + 1], w0[:, :K].contiguous()), (wide[:, 1:K + 2], w0), (aligned, moved)):
+        g = up(whole(2, 2)(M, N).to(out))
+        assert torch.equal(S.sig_linear_forward(x, w, b, r), product(x, w, b, r).to(out))
+        if t is not E8:
+            gx, gw, gb = S.sig_linear_backward(x, w, g, bias=True)
+            assert torch.equal(gx, product(g, w.t().contiguous()).to(t)) and torch.equal(gw, product(g.t().contiguous(), x.t().contiguous()).to(t))
+            assert torch.equal(gb, g.double().sum(0).to(t))
+
+
+def test_gradient_of_rows_beyond_32_bit_offsets():
+    """Rows of a tile are reached by 32-bit offsets: refused before anything is enqueued (the pointers here lead nowhere)."""
+    from tests.test_layer import BIG, LINEAR_OK, LINEAR_ORDER, pack
+    for change in ({"N": 1 << 22}, {"K": 1 << 22, "xs": 1 << 22}):
+        a = pack({**LINEAR_OK, **change}, LINEAR_ORDER)
+        assert S.load_library().sig_linear_backward(a, 4096, 1 << 22, 0, 4096, 4096, 4096, 4096, BIG, 0) == -7
