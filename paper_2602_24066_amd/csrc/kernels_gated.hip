@@ -18,12 +18,13 @@
 #include <algorithm>
 #include <type_traits>
 
+#include "gated_lane.hpp"
 #include "layer.hpp"
 
 namespace sig {
 namespace {
 
-constexpr int kWaves = 8, kHalf = 8, kRound = kWaves * kGatedTile, kGroup = 64;
+constexpr int kWaves = 8, kHalf = 8, kRound = kWaves * kGatedTile, kGroup = kGatedGroup;
 
 struct Two { float v[2]; };
 
@@ -144,19 +145,21 @@ __device__ __forceinline__ float rate_of(float log_rate) { return fast_exp(log_r
 
 struct Where {                       // of a workgroup: stream, channels, tokens of its chunk, and how many of them count
     int64_t b;
-    int chunk, c, first, last, live;
-    bool on;
+    int chunk, c, c1, first, last, live;
+    bool on, even;                   // see GatedLane
 };
-__device__ __forceinline__ Where where(const sig_gated_args& a, int groups, int chunks, int rounds)
+template <bool kPairs> __device__ __forceinline__ Where where(const sig_gated_args& a, int groups, int chunks, int rounds)
 {
     Where w;
     const uint32_t id = blockIdx.x;
     w.chunk = id % chunks;
     const uint32_t row = id / chunks;
     w.b = row / groups;
-    w.c = (row % groups) * kGroup + (threadIdx.x & 31) * 2;
-    w.on = w.c < a.D;
-    w.c = min(w.c, (int)a.D - 1);
+    const GatedLane lane = gated_lane(row % groups, threadIdx.x & 31, (int)a.D, kPairs);
+    w.c = lane.c;
+    w.c1 = lane.c1;
+    w.on = lane.on;
+    w.even = lane.even;
     const int64_t span = (int64_t)rounds * kRound;
     w.first = (int)min((int64_t)w.chunk * span, a.L);
     w.last = (int)min((w.chunk + 1) * span, a.L);
@@ -235,10 +238,10 @@ template <class T, bool kPairs, bool kBack>
 __global__ __launch_bounds__(kWaves * 64) void gated_sums_kernel(sig_gated_args a, sig_gated_grads g, float* sums, int groups, int chunks, int rounds)
 {
     __shared__ float4 joined[kWaves][32];
-    const Where w = where(a, groups, chunks, rounds);
+    const Where w = where<kPairs>(a, groups, chunks, rounds);
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), half = (threadIdx.x >> 5) & 1, D = (int)a.D, e = sizeof(T);
-    const bool even = kPairs || w.c + 1 < D;
-    const int c1 = even ? w.c + 1 : w.c, mine = half * kHalf;
+    const bool even = w.even;
+    const int c1 = w.c1, mine = half * kHalf;
     const float rate[2] = {rate_of(a.log_rate[w.c]), rate_of(a.log_rate[c1])};
     const T* gy = kBack ? (const T*)g.grad_y + w.b * g.gy_stride_b : nullptr;
     const Lane l{(c1 - w.c) * e, (int)(mine * a.x_stride_t + w.c) * e, (int)(mine * a.decay_stride_t + w.c) * e, (int)(mine * a.input_stride_t + w.c) * e, (int)(mine * g.gy_stride_t + w.c) * e, 0};
@@ -301,10 +304,10 @@ __global__ __launch_bounds__(kWaves * 64) void gated_forward_kernel(sig_gated_ar
                                                                      int rounds)
 {
     __shared__ float4 joined[2][kWaves][32];
-    const Where w = where(a, groups, chunks, rounds);
+    const Where w = where<kPairs>(a, groups, chunks, rounds);
     const int wave = threadIdx.x / 64, half = (threadIdx.x >> 5) & 1, D = (int)a.D;
-    const bool even = kPairs || w.c + 1 < D;
-    const int c1 = even ? w.c + 1 : w.c;
+    const bool even = w.even;
+    const int c1 = w.c1;
     const float rate[2] = {rate_of(a.log_rate[w.c]), rate_of(a.log_rate[c1])};
     float state[2] = {};
     if (a.initial_state) {
@@ -372,12 +375,12 @@ __global__ __launch_bounds__(kWaves * 64) void gated_backward_kernel(sig_gated_a
                                                                       int chunks, int rounds)
 {
     __shared__ float4 joined[2][kWaves][32];
-    const Where w = where(a, groups, chunks, rounds);
+    const Where w = where<kPairs>(a, groups, chunks, rounds);
     const int wave = threadIdx.x / 64, half = (threadIdx.x >> 5) & 1, li = threadIdx.x & 31, D = (int)a.D;
-    const bool even = kPairs || w.c + 1 < D;
+    const bool even = w.even;
     const T* gy = (const T*)g.grad_y + w.b * g.gy_stride_b;
     T *gx = (T*)g.grad_x + w.b * a.L * D, *gp = (T*)g.grad_decay_gate + w.b * a.L * D, *gq = (T*)g.grad_input_gate + w.b * a.L * D;
-    const int c1 = even ? w.c + 1 : w.c;
+    const int c1 = w.c1;
     const float rate[2] = {rate_of(a.log_rate[w.c]), rate_of(a.log_rate[c1])};
     float back[2] = {}, total[2] = {};
     if (g.grad_final_state) {
