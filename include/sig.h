@@ -465,7 +465,11 @@ int    sig_grad_clip(int64_t n_tensors, const void* const* in, void* const* out,
  * The conventions of the sequence operators hold: arithmetic, sums, states and statistics in float32, calls only enqueue kernels on `stream`, the
  * same inputs give the same bits, no output overlaps an input unless stated, nothing has to be aligned beyond its type.  Tokens are rows here:
  * strides count elements from one row to the next (0: a broadcast input); a row is contiguous.  SIG_E4M3 is the 8-bit float of 4 exponent and 3
- * fraction bits without infinities (largest value 448). */
+ * fraction bits without infinities (largest value 448).  SIG_ETOOLARGE: sizes whose product passes 2^38, strides beyond it,
+ * what is stated below, and a launch of 2^32 threads or more, before anything is enqueued: the norm takes 64, 256 or 1,024 threads a row, the longer
+ * the more; the product 256 for every 128 x 128 float32 outputs (other types always fit), its gradient the same for both of its products, 256 for
+ * every 64 rows of 256 bytes of grad_y, and one for every 16 bytes of rows that it copies; the recurrence 512 for 64 channels of a stream, its step
+ * one a channel. */
 #define SIG_E4M3 2
 
 /* Root-mean-square norm: total = x + residual, rounded to dtype (x itself without residual); y = total * rsqrt(mean(total^2) + eps) * weight. */

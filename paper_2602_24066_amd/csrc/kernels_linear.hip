@@ -17,6 +17,7 @@
 #include <type_traits>
 
 #include "layer.hpp"
+#include "linear_tiles.hpp"
 
 namespace sig {
 namespace {
@@ -25,10 +26,6 @@ typedef float Acc __attribute__((ext_vector_type(4)));
 typedef uint32_t Chunk __attribute__((ext_vector_type(4)));
 typedef __bf16 Bf8 __attribute__((ext_vector_type(8)));
 typedef int Int8 __attribute__((ext_vector_type(8)));
-
-constexpr int kSlab = 128, kChunk = 16, kChunks = kSlab / kChunk;      // bytes; bytes; chunks of a slab
-
-struct Tiles { int64_t M, N, K; int m, n, splits; int64_t slabs; int tile; bool few; double us; };            // tiles along m and n; slabs of a split; edge of a tile (few: in 16 tokens); what the launch's model says
 
 struct Out {                            // what becomes of a sum
     const void *bias, *residual;
@@ -261,8 +258,6 @@ __device__ __forceinline__ Place place_of(const Tiles& t)
     const uint32_t band = id / (8 * t.n), in = id % (8 * t.n), high = min(8u, (uint32_t)t.m - band * 8);
     return {(int)(band * 8 + in % high), (int)(in / high), (int)split};
 }
-
-constexpr int kTile = 128;
 
 // Rows of any alignment: a workgroup's tile is 128 tokens by 128 outputs, 64 by 64 a wavefront; chunks pass through registers, where the ends of rows are
 // put in order.  16384 x 5460 to 1024 in bfloat16: 272 us (673 TFLOP/s), where rows of 5456 take 189 by aligned_kernel.
@@ -621,59 +616,6 @@ template <class T> __global__ __launch_bounds__(1024) void bias_kernel(const flo
     if (threadIdx.x < 64 && c < N) grad_bias[c] = from_float<T>(s);
 }
 
-// ---- which tile, and how many splits.  A model of the launch, in us: `slab` is what a tile's slab costs a compute unit that is busy with as many
-// as it holds, `alone` what it costs at least, `over` what a tile costs besides (first loads, outputs).  Measured on large squares (us a slab):
-//   bfloat16 256: 8192^3 in 856 us, 128: 1,022 us     float32 128: 4096^3 in 998, 64: 1,040     e4m3 256: 8192^3 in 476, 128: 550
-// and 16384 x 4096 x 1024 (16 slabs): 148 us with tiles of 256, 172 of 128; e4m3 16384 x 2048 x 2048: 72 and 79.
-// Rows that are not whole chunks (product_kernel) take `rough` times the slab: bfloat16 16384 x 5460 to 1024 272 us, of 5456 189; float32 5000 x 1001 to 1001 139.
-struct Cost { int tile; double slab, alone, over; };
-constexpr double kRough[3] = {1.07, 1.5, 1.5};                                         // float32, bfloat16, e4m3
-constexpr Cost kCosts[3][3] = {
-    {{64, 0.51, 0.70, 1.0}, {128, 1.95, 1.95, 3.0}, {}},                               // float32: tiles of 256 gain 2 % at most
-    {{64, 0.17, 0.50, 0.8}, {128, 0.50, 0.80, 2.4}, {256, 1.68, 1.68, 10.5}},          // bfloat16
-    {{64, 0.18, 0.50, 0.8}, {128, 0.54, 0.80, 1.2}, {256, 1.86, 1.86, 6.3}},           // e4m3
-};
-constexpr int kUnits = 256;                                                            // compute units
-
-// Up to 64 tokens: what few_kernel takes, in us, by the rate at which a compute unit's wavefronts get its operands (measured 40 GB/s, 64 tokens bfloat16:
-// 2048 to 1024 5.9 us with tiles of 16 x 16, 1024 to 4096 6.4 with 32 x 32, 8192 to 8192 45 with 64 x 32).
-constexpr int kFew = 64;
-struct FewPlan { int fm, fn; double us; };
-FewPlan few_plan(int64_t M, int64_t N, int64_t bytes)
-{
-    FewPlan best{0, 0, 0.0};
-    for (FewPlan p : {FewPlan{1, 1, 0.0}, FewPlan{2, 2, 0.0}, FewPlan{4, 2, 0.0}}) {
-        const int64_t blocks = (M + p.fm * 16 - 1) / (p.fm * 16) * ((N + p.fn * 16 - 1) / (p.fn * 16));
-        p.us = 3.0 + (double)((blocks + kUnits - 1) / kUnits) * (p.fm + p.fn) * 16 * bytes / 40e3;
-        if (best.fm == 0 || p.us < best.us) best = p;
-    }
-    return best;
-}
-
-Tiles tiles_of(int64_t M, int64_t N, int64_t K, int e, bool aligned, bool few = true)
-{
-    const int64_t slabs = std::max<int64_t>(1, (K * e + kSlab - 1) / kSlab);
-    Tiles best{};
-    double least = 0.0;
-    for (const Cost& c : kCosts[e == 4 ? 0 : e == 2 ? 1 : 2]) {
-        if (c.tile == 0 || (!aligned && c.tile != kTile)) continue;
-        const int64_t m = (M + c.tile - 1) / c.tile, n = (N + c.tile - 1) / c.tile;
-        for (int64_t want : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32}) {
-            if (want > 1 && slabs / want < 4) break;
-            const int64_t each = (slabs + want - 1) / want, splits = (slabs + each - 1) / each, rows = (m * n * splits + kUnits - 1) / kUnits;
-            double us = (double)each * std::max(rows * c.slab, c.alone) * (aligned ? 1.0 : kRough[e == 4 ? 0 : e == 2 ? 1 : 2]) + rows * c.over;
-            if (splits > 1) us += 4.0 + (double)M * N * 4.0 * (splits + 1) / 3e6;     // the sums, written and read again
-            if (best.tile == 0 || us < least) {
-                least = us;
-                best = Tiles{M, N, K, (int)m, (int)n, (int)splits, each, c.tile, false, us};
-            }
-        }
-    }
-    if (aligned && few && M <= kFew)
-        if (const FewPlan p = few_plan(M, N, K * e); p.us < 3.0 + least)
-            return Tiles{M, N, K, (int)((M + p.fm * 16 - 1) / (p.fm * 16)), (int)((N + p.fn * 16 - 1) / (p.fn * 16)), 1, 0, p.fm, true, p.us};
-    return best;
-}
 size_t parts_bytes(const Tiles& t) { return t.splits > 1 ? (size_t)t.splits * t.M * ((t.N + 3) / 4 * 4) * 4 : 0; }
 template <class T, class O, int kSize, int WM, int WN, bool kAcrossX, bool kAcrossW> hipError_t launch(const Tiles& t, const T* x, int64_t ldx, const T* w, int64_t ldw, const Out& o, float* parts, uint32_t blocks, hipStream_t stream)
 {
@@ -694,35 +636,30 @@ bool aligned_rows(const void* x, int64_t ldx, const void* w, int64_t ldw, int64_
            256 * std::max(ldx, ldw) * e + K * e < (1ll << 31);
 }
 
+// The launches of a product, whose tiles the caller has found launchable.  aligned: whether aligned_rows holds (operands across: the caller has looked at them).
 template <class T, class O, bool kAcrossX = false, bool kAcrossW = false>
-hipError_t product(int64_t M, int64_t N, int64_t K, const T* x, int64_t ldx, const T* w, int64_t ldw, Out o, float* parts, hipStream_t stream)
+hipError_t product(const Tiles& t, bool aligned, const T* x, int64_t ldx, const T* w, int64_t ldw, Out o, float* parts, hipStream_t stream)
 {
     constexpr int V = 16 / sizeof(O);
-    const int64_t e = sizeof(T);
-    const bool aligned = kAcrossX || kAcrossW || aligned_rows(x, ldx, w, ldw, K, e);         // operands across: the caller has looked at them
     auto fits = [&](const void* p) { return (uintptr_t)p % 16 == 0; };
-    o.vec = N % V == 0 && o.residual_stride % V == 0 && fits(o.bias) && fits(o.residual) && fits(o.y) && fits(o.pre);
-    const Tiles t = tiles_of(M, N, K, (int)e, aligned, !kAcrossX && !kAcrossW);
-    const int64_t blocks = (int64_t)t.m * t.n * t.splits;
-    if (!launchable(blocks, 512)) return kTooManyThreads;
+    o.vec = t.N % V == 0 && o.residual_stride % V == 0 && fits(o.bias) && fits(o.residual) && fits(o.y) && fits(o.pre);
+    const uint32_t blocks = (uint32_t)t.blocks();
     hipError_t err = hipSuccess;
     if (t.few) {
         if constexpr (!kAcrossX && !kAcrossW) {
-            auto go = [&](auto kernel) { kernel<<<(uint32_t)blocks, 512, 0, stream>>>(t, x, ldx, w, ldw, o); };
-            t.tile == 1 ? go(few_kernel<T, O, 1, 1, 8>) : t.tile == 2 ? go(few_kernel<T, O, 2, 2, 8>) : go(few_kernel<T, O, 4, 2, 8>);
+            auto go = [&](auto kernel) { kernel<<<blocks, kFewThreads, 0, stream>>>(t, x, ldx, w, ldw, o); };
+            t.tile == 1 ? go(few_kernel<T, O, 1, 1, kFewThreads / 64>) : t.tile == 2 ? go(few_kernel<T, O, 2, 2, kFewThreads / 64>) : go(few_kernel<T, O, 4, 2, kFewThreads / 64>);
             err = hipGetLastError();
         }
     } else if (!aligned) {
-        product_kernel<T, O><<<(uint32_t)blocks, 256, 0, stream>>>(t, x, ldx, w, ldw, o, parts);
+        product_kernel<T, O><<<blocks, 256, 0, stream>>>(t, x, ldx, w, ldw, o, parts);
         err = hipGetLastError();
     } else if (t.tile == 256) {
-        if constexpr (sizeof(T) < 4) err = launch<T, O, 256, 4, 2, kAcrossX, kAcrossW>(t, x, ldx, w, ldw, o, parts, (uint32_t)blocks, stream);
-    } else if (t.tile == 128) err = launch<T, O, 128, 2, 2, kAcrossX, kAcrossW>(t, x, ldx, w, ldw, o, parts, (uint32_t)blocks, stream);
-    else err = launch<T, O, 64, 2, 2, kAcrossX, kAcrossW>(t, x, ldx, w, ldw, o, parts, (uint32_t)blocks, stream);
+        if constexpr (sizeof(T) < 4) err = launch<T, O, 256, 4, 2, kAcrossX, kAcrossW>(t, x, ldx, w, ldw, o, parts, blocks, stream);
+    } else if (t.tile == 128) err = launch<T, O, 128, 2, 2, kAcrossX, kAcrossW>(t, x, ldx, w, ldw, o, parts, blocks, stream);
+    else err = launch<T, O, 64, 2, 2, kAcrossX, kAcrossW>(t, x, ldx, w, ldw, o, parts, blocks, stream);
     if (err != hipSuccess || t.splits == 1) return err;
-    const int64_t joins = (M * ((N + 3) / 4) + 255) / 256;
-    if (!launchable(joins, 256)) return kTooManyThreads;
-    join_kernel<O><<<(uint32_t)joins, 256, 0, stream>>>(t, o, parts);
+    join_kernel<O><<<(uint32_t)t.joins(), 256, 0, stream>>>(t, o, parts);
     return hipGetLastError();
 }
 
@@ -732,11 +669,12 @@ int64_t round_up(int64_t v, int64_t to) { return (v + to - 1) / to * to; }
 // Rows that the aligned kernels read as they lie
 bool whole(const void* p, int64_t ld, int64_t cols, int64_t e) { return (uintptr_t)p % 16 == 0 && ld * e % 16 == 0 && cols * e % 16 == 0 && 256 * ld * e < (1ll << 30); }
 
+// Workgroups of the copy of R rows of C values of e bytes into whole chunks
+int64_t pad_blocks(int64_t R, int64_t C, int64_t e) { return (R * ((C * e + kChunk - 1) / kChunk) + 255) / 256; }
 template <class T> hipError_t pad(const T* in, int64_t ld, int64_t R, int64_t C, T* out, hipStream_t stream)
 {
-    const int64_t chunks = (C * (int)sizeof(T) + kChunk - 1) / kChunk, blocks = (R * chunks + 255) / 256;
-    if (!launchable(blocks, 256)) return kTooManyThreads;
-    if (blocks) pad_kernel<T><<<(uint32_t)blocks, 256, 0, stream>>>(in, ld, R, C, (Chunk*)out, (uint32_t)chunks);
+    const int64_t blocks = pad_blocks(R, C, sizeof(T));
+    if (blocks) pad_kernel<T><<<(uint32_t)blocks, 256, 0, stream>>>(in, ld, R, C, (Chunk*)out, (uint32_t)((C * (int)sizeof(T) + kChunk - 1) / kChunk));
     return hipGetLastError();
 }
 
@@ -744,8 +682,9 @@ template <class T> hipError_t pad(const T* in, int64_t ld, int64_t R, int64_t C,
 // that the copies (a launch each, read and written at 3 TB/s) cost less than they gain, and the sums of splits.  float32 5000 x 1001 to 1001: 112 us with
 // copies, 139 without; 600 x 1554 to 640 stays without (24 us; the model puts its copies at 13).
 struct Ahead {
-    bool pad_x, pad_w;
+    bool pad_x, pad_w, aligned;
     int64_t padK;
+    Tiles tiles;
     size_t x, w, parts, all;
 };
 Ahead ahead_of(const sig_linear_args& a)
@@ -753,20 +692,25 @@ Ahead ahead_of(const sig_linear_args& a)
     const int e = bytes_of(a.dtype);
     Ahead k{};
     k.padK = a.K;
-    Tiles t = tiles_of(a.M, a.N, a.K, e, aligned_rows(a.x, a.x_stride, a.weight, a.K, a.K, e));
+    k.aligned = aligned_rows(a.x, a.x_stride, a.weight, a.K, a.K, e);
+    k.tiles = tiles_of(a.M, a.N, a.K, e, k.aligned);
     size_t at = 0;
-    if (const int64_t padK = round_up(a.K, kChunk / e); !aligned_rows(a.x, a.x_stride, a.weight, a.K, a.K, e) && 256 * padK * e < (1ll << 30)) {
+    if (const int64_t padK = round_up(a.K, kChunk / e); !k.aligned && 256 * padK * e < (1ll << 30)) {
         const bool x = !whole(a.x, a.x_stride, a.K, e), w = !whole(a.weight, a.K, a.K, e);
         const Tiles u = tiles_of(a.M, a.N, padK, e, true);
-        if (u.us + (x ? 4.0 + 2.0 * a.M * padK * e / 3e6 : 0.0) + (w ? 4.0 + 2.0 * a.N * padK * e / 3e6 : 0.0) < t.us) {
-            k = Ahead{x, w, padK};
-            t = u;
+        if (u.us + (x ? 4.0 + 2.0 * a.M * padK * e / 3e6 : 0.0) + (w ? 4.0 + 2.0 * a.N * padK * e / 3e6 : 0.0) < k.tiles.us &&
+            (!x || launchable(pad_blocks(a.M, a.K, e), 256)) && (!w || launchable(pad_blocks(a.N, a.K, e), 256))) {
+            k.pad_x = x;
+            k.pad_w = w;
+            k.aligned = true;
+            k.padK = padK;
+            k.tiles = u;
             k.w = x ? (size_t)round_up(a.M * padK * e, 256) : 0;
             at = k.w + (w ? (size_t)round_up(a.N * padK * e, 256) : 0);
         }
     }
     k.parts = at;
-    k.all = at + parts_bytes(t);
+    k.all = at + parts_bytes(k.tiles);
     if (k.all) k.all += 16;                                                    // for a workspace whose start is not aligned
     return k;
 }
@@ -776,6 +720,7 @@ Ahead ahead_of(const sig_linear_args& a)
 struct Keep {
     bool pad_x, pad_w;
     int64_t padN, padK;
+    Tiles to_x, to_w;                   // of the products that give the gradients of x and of the weight
     size_t flat, x, w, sums, parts, all;
 };
 Keep keep_of(const sig_linear_args& a)
@@ -796,17 +741,21 @@ Keep keep_of(const sig_linear_args& a)
     k.x = take(k.pad_x ? a.M * k.padK * e : 0);
     k.w = take(k.pad_w ? a.N * k.padK * e : 0);
     k.sums = take((a.M + 63) / 64 * a.N * 4);
-    k.parts = take((int64_t)std::max(parts_bytes(tiles_of(a.M, a.K, a.N, e, true, false)), parts_bytes(tiles_of(a.N, a.K, a.M, e, true, false))));
+    k.to_x = tiles_of(a.M, a.K, a.N, e, true, false);
+    k.to_w = tiles_of(a.N, a.K, a.M, e, true, false);
+    k.parts = take((int64_t)std::max(parts_bytes(k.to_x), parts_bytes(k.to_w)));
     k.all = at + 16;                                                           // for a workspace whose start is not aligned
     return k;
 }
 
+// Workgroups of the pass over the incoming gradient: 64 rows of 256 bytes each
+int64_t slope_groups(int64_t C, int64_t e) { return (C * e + 255) / 256; }
+int64_t slope_blocks(int64_t R, int64_t C, int64_t e) { return (R + 63) / 64 * slope_groups(C, e); }
 template <class T> hipError_t slopes(const T* in, int64_t ld, int64_t R, int64_t C, const T* pre, int act, T* flat, int64_t padded, float* sums, hipStream_t stream)
 {
-    const int64_t wide = 256 / sizeof(T), groups = (C + wide - 1) / wide, blocks = (R + 63) / 64 * groups;
-    if (!launchable(blocks, 256)) return kTooManyThreads;
+    const int64_t blocks = slope_blocks(R, C, sizeof(T));
     const bool vec = C * sizeof(T) % 16 == 0 && ld * sizeof(T) % 16 == 0 && (uintptr_t)in % 16 == 0 && (uintptr_t)pre % 16 == 0;
-    if (blocks) slope_kernel<T><<<(uint32_t)blocks, 256, 0, stream>>>(in, ld, R, C, pre, act, flat, padded, sums, groups, vec);
+    if (blocks) slope_kernel<T><<<(uint32_t)blocks, 256, 0, stream>>>(in, ld, R, C, pre, act, flat, padded, sums, slope_groups(C, sizeof(T)), vec);
     return hipGetLastError();
 }
 
@@ -823,6 +772,9 @@ template <class T> hipError_t backward_of(const sig_linear_args& a, const T* gy,
     const bool copy = (gx || gw) && (pre || !whole(gy, ld, a.N, e));
     const T *g = copy ? flat : gy, *px = k.pad_x ? x : (const T*)a.x, *pw = k.pad_w ? w : (const T*)a.weight;
     const int64_t ldg = copy ? k.padN : ld;
+    if (((copy || gb) && !launchable(slope_blocks(a.M, a.N, e), 256)) || (gx && !(k.to_x.launchable() && (!k.pad_w || launchable(pad_blocks(a.N, a.K, e), 256)))) ||
+        (gw && !(k.to_w.launchable() && (!k.pad_x || launchable(pad_blocks(a.M, a.K, e), 256)))))
+        return kTooManyThreads;
     hipError_t err = hipSuccess;
     if (copy || gb) err = slopes<T>(gy, ld, a.M, a.N, pre, (int)a.act, copy ? flat : nullptr, k.padN, gb ? sums : nullptr, stream);
     if (err == hipSuccess && gb) {
@@ -833,12 +785,12 @@ template <class T> hipError_t backward_of(const sig_linear_args& a, const T* gy,
     if (err == hipSuccess && gx) {
         if (k.pad_w) err = pad((const T*)a.weight, a.K, a.N, a.K, w, stream);
         o.y = gx;
-        if (err == hipSuccess) err = product<T, T, false, true>(a.M, a.K, a.N, g, ldg, pw, k.pad_w ? k.padK : a.K, o, parts, stream);
+        if (err == hipSuccess) err = product<T, T, false, true>(k.to_x, true, g, ldg, pw, k.pad_w ? k.padK : a.K, o, parts, stream);
     }
     if (err == hipSuccess && gw) {
         if (k.pad_x) err = pad((const T*)a.x, a.x_stride, a.M, a.K, x, stream);
         o.y = gw;
-        if (err == hipSuccess) err = product<T, T, true, true>(a.N, a.K, a.M, g, ldg, px, k.pad_x ? k.padK : a.x_stride, o, parts, stream);
+        if (err == hipSuccess) err = product<T, T, true, true>(k.to_w, true, g, ldg, px, k.pad_x ? k.padK : a.x_stride, o, parts, stream);
     }
     return err;
 }
@@ -847,13 +799,14 @@ template <class T, class O> hipError_t forward_of(const sig_linear_args& a, void
 {
     const Out o{a.bias, a.residual, a.residual_stride, a.x_scale, a.weight_scale, y, pre, (int)a.act, false};
     const Ahead k = ahead_of(a);
+    if (!k.tiles.launchable()) return kTooManyThreads;
     ws += -(uintptr_t)ws & 15;
     T *x = (T*)(ws + k.x), *w = (T*)(ws + k.w);
     hipError_t err = hipSuccess;
     if (k.pad_x) err = pad((const T*)a.x, a.x_stride, a.M, a.K, x, stream);
     if (err == hipSuccess && k.pad_w) err = pad((const T*)a.weight, a.K, a.N, a.K, w, stream);
     if (err != hipSuccess) return err;
-    return product<T, O>(a.M, a.N, k.padK, k.pad_x ? x : (const T*)a.x, k.pad_x ? k.padK : a.x_stride, k.pad_w ? w : (const T*)a.weight, k.pad_w ? k.padK : a.K, o, (float*)(ws + k.parts), stream);
+    return product<T, O>(k.tiles, k.aligned, k.pad_x ? x : (const T*)a.x, k.pad_x ? k.padK : a.x_stride, k.pad_w ? w : (const T*)a.weight, k.pad_w ? k.padK : a.K, o, (float*)(ws + k.parts), stream);
 }
 
 }  // namespace

@@ -6,15 +6,15 @@
 #include <cstdint>
 
 #include "../../include/sig.h"
+#include "launch.hpp"
 
 namespace sig {
 
 int record_hip_error(hipError_t e);     // keeps it for sig_last_hip_error and returns SIG_EHIP (api.cpp)
 
-// The hardware numbers the threads of a launch in 32 bits.  Where a call would need more in one of its launches, the functions below return
-// kTooManyThreads and enqueue nothing; the calls then return SIG_ETOOLARGE.
+// Where a call would need more threads in one of its launches than a launch numbers, the functions below return kTooManyThreads and enqueue nothing;
+// the calls then return SIG_ETOOLARGE.
 constexpr hipError_t kTooManyThreads = hipErrorInvalidConfiguration;
-inline bool launchable(int64_t workgroups, int64_t threads) { return workgroups <= 0xffffffffll / threads; }
 
 // ---- convolution (kernels_conv.hip)
 struct ConvGrads {

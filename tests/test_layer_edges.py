@@ -428,3 +428,15 @@ def test_gradient_of_rows_beyond_32_bit_offsets():
     for change in ({"N": 1 << 22}, {"K": 1 << 22, "xs": 1 << 22}):
         a = pack({**LINEAR_OK, **change}, LINEAR_ORDER)
         assert S.load_library().sig_linear_backward(a, 4096, 1 << 22, 0, 4096, 4096, 4096, 4096, BIG, 0) == -7
+
+
+@gpu
+def test_narrow_products_of_more_rows_than_small_tiles_number():
+    """Half a thousand million rows of eight values: tiles of 64 rows would be more than a launch numbers."""
+    M = (1 << 29) + 77
+    x, w = torch.empty(M, 8, dtype=B16, device="cuda").random_(-3, 4), up(whole(3, 3)(8, 8).to(B16))
+    rows = (slice(0, 300), slice(M - 300, M), slice(M // 2, M // 2 + 100), slice((1 << 29) - 100, (1 << 29) + 60))
+    y = S.sig_linear_forward(x, w)
+    gx, _, _ = S.sig_linear_backward(x, w, x, need_weight=False)
+    for r in rows:
+        assert torch.equal(y[r], product(x[r], w).to(B16)) and torch.equal(gx[r], product(x[r], w.t().contiguous()).to(B16))
