@@ -529,7 +529,7 @@ typedef struct sig_gated_args {
     const void* x;                  /* device dtype [B, L, D] */
     const void* decay_gate;         /* device dtype [B, L, D] */
     const void* input_gate;         /* device dtype [B, L, D] */
-    const float* log_rate;          /* device [D]; beyond 64 taken as 64 (gates below -88 are shut: their sigmoid is zero) */
+    const float* log_rate;          /* device [D]; beyond 64 taken as 64, its gradient zero there (gates below -88 are shut: their sigmoid is zero) */
     const float* initial_state;     /* device [B, D] or NULL (zeros) */
     const int32_t* lengths;         /* device [B] or NULL */
 } sig_gated_args;

@@ -141,7 +141,8 @@ __device__ __forceinline__ Decay decay(float rate, float open)                 /
 }
 
 // exp(log_rate) log2(e), log_rate taken as 64 beyond that: u is finite, and a product with a shut gate's zero stays one.  A NaN stays one.
-__device__ __forceinline__ float rate_of(float log_rate) { return fast_exp(log_rate > 64.0f ? 64.0f : log_rate) * kLog2e; }
+constexpr float kMostLogRate = 64.0f;
+__device__ __forceinline__ float rate_of(float log_rate) { return fast_exp(log_rate > kMostLogRate ? kMostLogRate : log_rate) * kLog2e; }
 
 struct Where {                       // of a workgroup: stream, channels, tokens of its chunk, and how many of them count
     int64_t b;
@@ -502,11 +503,12 @@ __global__ __launch_bounds__(kWaves * 64) void gated_backward_kernel(sig_gated_a
     }
 }
 
-__global__ __launch_bounds__(1024) void gated_rates_kernel(const float* rates, int64_t rows, int64_t D, float* grad_log_rate)
+// The sums of U over streams and chunks; zero where log_rate is beyond what it counts as
+__global__ __launch_bounds__(1024) void gated_rates_kernel(const float* rates, int64_t rows, int64_t D, const float* log_rate, float* grad_log_rate)
 {
     const int64_t c = (int64_t)blockIdx.x * 64 + (threadIdx.x & 63);
     const float s = sum_rows(rates + min(c, D - 1), rows, D);
-    if (threadIdx.x < 64 && c < D) grad_log_rate[c] = s;
+    if (threadIdx.x < 64 && c < D) grad_log_rate[c] = log_rate[c] > kMostLogRate ? 0.0f : s;
 }
 
 // One token: bound by latency and the call (64 x 2048 in bfloat16: 3.0 us)
@@ -585,7 +587,7 @@ template <class T> hipError_t backward_of(const sig_gated_args& a, const sig_gat
         hipError_t err = hipGetLastError();
         if (err != hipSuccess) return err;
     }
-    gated_rates_kernel<<<(uint32_t)p.groups, 1024, 0, stream>>>(rates, parts, a.D, g.grad_log_rate);
+    gated_rates_kernel<<<(uint32_t)p.groups, 1024, 0, stream>>>(rates, parts, a.D, a.log_rate, g.grad_log_rate);
     return hipGetLastError();
 }
 

@@ -440,3 +440,25 @@ def test_narrow_products_of_more_rows_than_small_tiles_number():
     gx, _, _ = S.sig_linear_backward(x, w, x, need_weight=False)
     for r in rows:
         assert torch.equal(y[r], product(x[r], w).to(B16)) and torch.equal(gx[r], product(x[r], w.t().contiguous()).to(B16))
+
+
+@gpu
+@pytest.mark.parametrize("t", [F32, B16])
+def test_rates_beyond_their_limit_have_no_gradient(t):
+    """log_rate counts as min(log_rate, 64), so its gradient is zero beyond; that of gates so far shut that u is of the size of one is what it is at 64.
+    Tolerance: exp(log_rate) and the gate are off by up to 64 times 1.5 * 2^-24 each, u by 1.2e-5 of itself; gradients of tokens by that times a few."""
+    rates = torch.tensor([60.0, 63.5, 64.0, 64.001, 65.0, 90.0, math.inf])
+    D, L = rates.numel(), 40
+    n = normal(8)
+    v = dict(x=n(2, L, D).to(t), decay_gate=(-63 + n(2, L, D)).to(t), input_gate=n(2, L, D).to(t), log_rate=rates, initial_state=n(2, D))
+    gy = n(2, L, D).to(t)
+    d = {k: up(w) for k, w in v.items()}
+    y, _, ck = S.sig_gated_scan_forward(**d, checkpoint=True)
+    got = S.sig_gated_scan_backward(d["x"], d["decay_gate"], d["input_gate"], d["log_rate"], up(gy), ck, d["initial_state"])
+    leaves = {k: w.double().requires_grad_() for k, w in v.items()}
+    want, _ = R.gated(**{**leaves, "log_rate": leaves["log_rate"].clamp(max=64.0)})
+    grads = dict(zip(leaves, torch.autograd.grad((want * gy.double()).sum(), list(leaves.values()))))
+    assert not got["log_rate"][rates > 64].any() and grads["log_rate"][:3].abs().min() > 0.01
+    for k in ("x", "decay_gate", "input_gate", "log_rate", "initial_state"):
+        slack = 1e-3 if t is F32 or k in ("log_rate", "initial_state") else 2.0 ** -7
+        within(got[k], grads[k], slack * (grads[k].abs() + grads[k].square().mean().sqrt()), k)
