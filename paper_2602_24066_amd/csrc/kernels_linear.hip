@@ -37,8 +37,9 @@ struct Out {                            // what becomes of a sum
 };
 
 // The normal distribution's Phi and its density.  exp(x^2) erfc(x) = t P(t) with t = 1 / (1 + c x), P fitted to the smallest relative error over x in
-// [0, 14], so both tails keep their relative precision, and the exponential is the density's.  For float32 of degree 8, c = 0.3 (4e-8; with float32's
-// roundings 5e-7); for values rounded to bfloat16, whose half step is 4e-3, of degree 5, c = 0.45 (1e-5): the epilogue of a product is bound by this.
+// [0, 14], and the exponential is the density's.  For float32 of degree 8, c = 0.3 (5e-8; with float32's roundings 5e-7 next to zero); for values
+// rounded to bfloat16, whose half step is 4e-3, of degree 5, c = 0.45 (1e-5): the epilogue of a product is bound by this.  The tails keep their relative
+// precision but for the exponential's, whose rounded exponent adds up to 1.13 z^2 2^-24 (in all 9e-7 down to -4, 2e-6 to -6, 7.5e-6 to -12.5).
 struct Normal { float below, density; };
 template <class O> __device__ __forceinline__ Normal normal_of(float z)
 {

@@ -462,3 +462,30 @@ def test_rates_beyond_their_limit_have_no_gradient(t):
     for k in ("x", "decay_gate", "input_gate", "log_rate", "initial_state"):
         slack = 1e-3 if t is F32 or k in ("log_rate", "initial_state") else 2.0 ** -7
         within(got[k], grads[k], slack * (grads[k].abs() + grads[k].square().mean().sqrt()), k)
+
+
+@gpu
+@pytest.mark.parametrize("name", ["silu", "gelu"])
+@pytest.mark.parametrize("t", [F32, B16])
+def test_activations_keep_their_relative_precision_far_below_zero(t, name):
+    """Values and slopes down to 1e-31, relative to what they are; a weight of one leaves the products exact.  In half steps of float32 (u = 2^-24):
+    SiLU   the exponent -z log2(e) is rounded (constant included) by 1.25 |z|, the exponential 2, the sum 1, the quotient 2, the product 1; slope: two more.
+    GELU   exp(-z^2 / 2) by 1.125 z^2 and 2; t P(t) by 25 in the worst case that its roundings and the fit's 5e-8 allow (degree 5: 178, the fit's 1e-5),
+           summed by running error analysis over [-13, 0]; the slope z phi + Phi by as much of both its terms, and two roundings.
+    bfloat16 adds half a step of its own."""
+    u, h = 2.0 ** -24, 0.0 if t is F32 else H[B16] * 1.001
+    z = (-torch.linspace(0.001, 12.0 if name == "gelu" else 70.0, 4001)).to(t)
+    one, w = torch.ones(z.numel(), 1, dtype=t, device="cuda"), torch.ones(1, 1, dtype=t, device="cuda")
+    y, pre = S.sig_linear_forward(up(z)[:, None], w, activation=name, keep=True)
+    assert torch.equal(pre.cpu()[:, 0], z)
+    gx, _, _ = S.sig_linear_backward(up(z)[:, None], w, one, name, pre)
+    v = z.double()
+    want, slope = R.act(v, name), R.slope(v, name)
+    if name == "silu":
+        off, s = (6 + 1.25 * v.abs()) * u, 1 / (1 + torch.exp(-v))
+        size, of_slope = s * (1 + v.abs() * (1 - s)), off + 2 * u
+    else:
+        off = ((25 if t is F32 else 178) + 1.2 * v * v) * u
+        size, of_slope = v.abs() * torch.exp(-v * v / 2) / math.sqrt(2 * math.pi) + 0.5 * torch.special.erfc(-v / math.sqrt(2.0)), off + 2 * u
+    within(y[:, 0], want, (off + h) * want.abs(), "value")
+    within(gx[:, 0], slope, of_slope * size + h * (slope.abs() + of_slope * size), "slope")
