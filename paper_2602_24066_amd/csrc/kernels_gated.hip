@@ -124,7 +124,7 @@ __device__ __forceinline__ Gate gate(float v)
 }
 
 // u log2(e) = x, a = 2^-x and w = 1 - a^2 for x >= 0.  Small x: the power series of 1 - exp(-v), v = 2 u < 1/2, up to v^7, whose first omitted term is
-// v^7 / 8! < 2e-7 of the value; from there on 1 - a^2 >= 0.39 loses a bit and a half at most.
+// v^8 / 8! < 2.5e-7 of the value; from there on 1 - a^2 >= 0.39 loses a bit and a half at most.
 struct Decay { float x, a, w; };
 __device__ __forceinline__ Decay decay(float rate, float open)                 // rate: exp(log_rate) log2(e)
 {
