@@ -462,7 +462,7 @@ int    sig_grad_clip(int64_t n_tensors, const void* const* in, void* const* out,
  * What a layer of a model over signature tokens has besides: the norm of the stream with the residual's addition, projections (matrix products
  * with bias, activation and residual), a gated linear recurrence as the cheaper sibling of the selective scan, their gradients and 8-bit forms.
  *
- * The conventions of the sequence operators hold: arithmetic, sums, states and statistics in float32, calls only enqueue kernels on `stream`, the
+ * The conventions of the sequence operators hold: arithmetic, sums, states and statistics in float32 (but see the product's gradient), calls only enqueue kernels on `stream`, the
  * same inputs give the same bits, no output overlaps an input unless stated, nothing has to be aligned beyond its type.  Tokens are rows here:
  * strides count elements from one row to the next (0: a broadcast input); a row is contiguous.  SIG_E4M3 is the 8-bit float of 4 exponent and 3
  * fraction bits without infinities (largest value 448).  SIG_ETOOLARGE: sizes whose product passes 2^38, strides beyond it,
@@ -482,8 +482,9 @@ typedef struct sig_norm_args {
     const float* weight;            /* device [C] */
 } sig_norm_args;
 /* total: dtype [rows, C] or NULL.  scale NULL: y is dtype [rows, C].  Else y is SIG_E4M3 [rows, C] and scale [rows]: y * scale is the norm, scale =
- * max |row| / 448, its values taken before any rounding to dtype.  Squares are summed in float32: rows with values beyond 1e19 give zeros.  Rows of zeros have scale 0; a row with an infinity or NaN has a
- * scale that is not finite, and its y is of no use but defined. */
+ * max |row| / 448, its values taken before any rounding to dtype.  Squares are summed in float32: rows with values beyond 1e19 give zeros, and with an
+ * eps below 1e-38 rows of values below 1e-19 infinities or NaN.  Rows of zeros have scale 0; a row with an infinity or NaN has a scale that is not finite,
+ * and its y is of no use but defined. */
 int    sig_norm_forward(const sig_norm_args* args, void* y, float* scale, void* total, void* stream);
 /* args->x: the total that the forward call gave (residual is not looked at).  grad_y and grad_total (or NULL) dtype [rows, C] with strides of their own ->
  * grad_x dtype [rows, C], the gradient of x and of residual alike; grad_weight [C].  Both overwritten. */
@@ -515,7 +516,10 @@ size_t sig_linear_forward_workspace_bytes(const sig_linear_args* args);
 int    sig_linear_forward(const sig_linear_args* args, void* y, void* pre, void* workspace, size_t workspace_bytes, void* stream);
 /* Gradient (SIG_F32 and SIG_BF16): grad_y dtype [M, N] with a stride of its own; pre as kept (NULL where act is SIG_ACT_NONE) -> grad_x dtype [M, K],
  * grad_weight dtype [N, K], grad_bias dtype [N]; each may be NULL, and is not computed then.  The gradient of the residual is grad_y.
- * bias, residual and scales of args are not looked at, x only for grad_weight, weight only for grad_x.  Rows of N or K elements are shorter than 4 MB. */
+ * bias, residual and scales of args are not looked at, x only for grad_weight, weight only for grad_x.  Rows of N or K elements are shorter than 4 MB.
+ * With an activation grad_y times its slope at pre, as pre was rounded, is rounded to dtype before the products that give grad_x and grad_weight: matrix
+ * instructions take operands of one type.  In SIG_BF16 that leaves 2.4e-3 of grad_x's and grad_weight's norms, where rounding the outputs alone leaves 1.7e-3;
+ * grad_bias sums the products before that rounding.  The workspace always has room for these products and the bias's sums. */
 size_t sig_linear_backward_workspace_bytes(const sig_linear_args* args);
 int    sig_linear_backward(const sig_linear_args* args, const void* grad_y, int64_t gy_stride, const void* pre, void* grad_x,
                            void* grad_weight, void* grad_bias, void* workspace, size_t workspace_bytes, void* stream);

@@ -182,7 +182,8 @@ def sig_linear_forward(x, weight, bias=None, residual=None, activation=None, kee
 def sig_linear_backward(x, weight, grad_out, activation=None, pre=None, bias=False, need_x=True, need_weight=True):
     """Gradient of sig_linear_forward: (grad_x, grad_weight, grad_bias) of x's type, None for those not asked for (need_x, need_weight, bias).
     grad_out [.., N] of x's type; pre: what the forward call with keep=True returned, needed with an activation.  The residual's gradient is
-    grad_out itself."""
+    grad_out itself.  grad_out times the activation's slope at pre is rounded to x's type before the products for grad_x and grad_weight (not for
+    grad_bias): in bfloat16 their norms are 2.4e-3 off, with outputs rounded alone 1.7e-3."""
     make, kind = _start(x)
     act = _act(activation)
     shape, index, t = x.shape, x.get_device(), x.dtype
