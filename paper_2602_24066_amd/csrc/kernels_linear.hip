@@ -10,9 +10,9 @@
 // (see Side).  Operands whose rows are not whole chunks are copied first where that pays, for the gradient always.
 //
 // Bound by the matrix units where the contraction is long: bfloat16 8192^3 in 840 us (1,308 TFLOP/s), e4m3 in 476 (2,310), float32 4096^3 in 1,000 (137).
-// Where it is short, by the outputs: 16384 x 1024 to 4096 in bfloat16 with SiLU 158 us, of which the product alone takes 127 at the rate above's; a
+// Where it is short, by the outputs: 16384 x 1024 to 4096 in bfloat16 with SiLU 158 us, of which the product alone takes 105 at the rate above; a
 // tile of 256 ends with 10 us of sums through LDS, activations and stores that the next one's loads do not overlap.  Few tokens are bound by
-// the weight's way from memory and by latency (64 x 2048 to 1024: 7.0 us).
+// the weight's way from memory and by latency (64 x 2048 to 1024 in bfloat16 7.0 us, float32 11.5, e4m3 5.3; 64 x 8192 to 8192 36, 90 and 27).
 #include <algorithm>
 #include <type_traits>
 
@@ -158,7 +158,8 @@ template <class O, int V> __device__ __forceinline__ void finish(const Out& o, c
 }
 
 // The sums of a wavefront's tile, 16 FM tokens by 16 FN outputs, to where they belong.  A lane holds four outputs of sixteen tokens' rows; 16 rows at a
-// time go through LDS (4 KB and a little a wavefront, its own), after which neighbouring lanes hold neighbouring outputs and a row is whole lines.
+// time go through LDS (kPutFloats<FN> of a wavefront's own), after which neighbouring lanes hold neighbouring outputs and a row is whole lines.
+template <int FN> constexpr int kPutFloats = 16 * (FN * 16 + 4);
 template <class O, int FM, int FN> __device__ __forceinline__ void put(const Tiles& t, const Out& o, float* parts, int split, int64_t m0, int64_t n0, Acc (&acc)[FN][FM], float* lds)
 {
     constexpr int V = 16 / sizeof(O), kWide = FN * 16, kPitch = kWide + 4, kLanes = kWide / V, kRows = 64 / kLanes;
@@ -313,7 +314,8 @@ template <class T, class O> __global__ __launch_bounds__(256) void product_kerne
         if (more) keep(buf ^ 1);
         __syncthreads();
     }
-    put<O, 4, 4>(t, o, parts, p.split, m0 + wm * 64, n0 + wn * 64, acc, (float*)lds + wave * 16 * 68);
+    static_assert(4 * kPutFloats<4> * sizeof(float) <= sizeof(lds));
+    put<O, 4, 4>(t, o, parts, p.split, m0 + wm * 64, n0 + wn * 64, acc, (float*)lds + wave * kPutFloats<4>);
 }
 
 // ---- the same for operands whose rows are multiples of 16 bytes, 16-byte aligned: chunks go from memory to LDS without passing registers, a wavefront's
@@ -476,7 +478,8 @@ __global__ __launch_bounds__(WM * WN * 64) void aligned_kernel(Tiles t, const T*
         }
     }
     asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
-    put<O, FM, FN>(t, o, parts, p.split, m0 + wm * (B / WM), n0 + wn * (B / WN), acc, (float*)lds + wave * 16 * (FN * 16 + 4));
+    static_assert(WM * WN * kPutFloats<FN> * sizeof(float) <= 2 * kStage * sizeof(Chunk));
+    put<O, FM, FN>(t, o, parts, p.split, m0 + wm * (B / WM), n0 + wn * (B / WN), acc, (float*)lds + wave * kPutFloats<FN>);
 #endif
 }
 
@@ -536,7 +539,7 @@ template <class T, class O, int FM, int FN, int kW> __global__ __launch_bounds__
     }
 }
 
-// The splits' sums, added up in order, and what becomes of them.  Bound by memory (2107 x 1024, three splits of float32 sums: 9.3 us with a launch of its own)
+// The splits' sums, added up in order, and what becomes of them.  Bound by memory (2107 x 1024, four splits of float32 sums: 9.3 us with a launch of its own)
 template <class O> __global__ __launch_bounds__(256) void join_kernel(Tiles t, Out o, const float* parts)
 {
     const int64_t quads = (t.N + 3) / 4, id = (int64_t)blockIdx.x * 256 + threadIdx.x;
@@ -557,9 +560,9 @@ template <class T> __global__ __launch_bounds__(256) void pad_kernel(const T* in
     if (row < R) out[id] = take_chunk(in + row * ld, c * (kChunk / (int)sizeof(T)), C);
 }
 
-// The gradient's pass over what comes in: times the activation's slope (pre), rounded to T as the products' other operands are of that type, into rows
-// of whole chunks (flat, `padded` elements apart), and its sums over 64 rows, unrounded, for the bias's gradient.  64 rows by 128 bfloat16 or 64 float32 values
-// a workgroup.  Bound by memory: 16384 x 4096 in bfloat16 with GELU's slope 85 us, 4.75 TB/s (by tiles through LDS 109).
+// The gradient's pass over what comes in: times the activation's slope (pre), rounded to T as the products' other operands are of that type (bfloat16:
+// gradients 2.4e-3 off by norm, 1.7e-3 with outputs rounded alone), into rows of whole chunks (flat, `padded` elements apart), and its sums over 64 rows,
+// unrounded, for the bias's gradient.  64 rows by 128 bfloat16 or 64 float32 values a workgroup.  Bound by memory: 16384 x 4096 in bfloat16 with GELU's slope 85 us, 4.75 TB/s (by tiles through LDS 109).
 template <class T> __global__ __launch_bounds__(256) void slope_kernel(const T* in, int64_t ld, int64_t R, int64_t C, const T* pre, int act, T* flat, int64_t padded, float* sums, int64_t groups, bool vec)
 {
     constexpr int V = 16 / sizeof(T), kRows = 4, kWide = 16 * V;

@@ -39,8 +39,8 @@ constexpr Cost kCosts[3][3] = {
 };
 constexpr int kUnits = 256;                                                            // compute units
 
-// Up to 64 tokens: what few_kernel takes, in us, by the rate at which a compute unit's wavefronts get its operands (measured 40 GB/s, 64 tokens bfloat16:
-// 2048 to 1024 5.9 us with tiles of 16 x 16, 1024 to 4096 6.4 with 32 x 32, 8192 to 8192 45 with 64 x 32).
+// Up to 64 tokens: what few_kernel takes, in us, by the rate at which a compute unit's wavefronts get its operands (40 GB/s; 64 tokens bfloat16, the
+// weight from the cache: 2048 to 1024 5.9 us with tiles of 16 x 16, 1024 to 4096 6.4 with 32 x 32; from memory 7.0 and 7.6, 8192 to 8192 36 with 64 x 32).
 constexpr int kFew = 64, kFewThreads = 512;
 struct FewPlan { int fm, fn; int64_t m, n; double us; };                                // fm 0: none
 inline FewPlan few_plan(int64_t M, int64_t N, int64_t bytes)
